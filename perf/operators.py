@@ -1,0 +1,445 @@
+"""The operators of an attention layer on stacked tokens, case by case: rotary positions with several axes, the cache of
+keys and values held in 4 bits (store, load and the attention that reads it), low-rank adapters beside a projection.
+
+With ``own`` false, ``run`` computes them in their plain form with elementary torch operations in 32 bits; with ``own``
+true it makes the calls a program makes of the library.  Everything is drawn on the GPU from the case's seed.
+
+The formats that the calls share with a program (include/sige.h):
+
+rotary table   int32 [pairs][4]: the bits of two floats (the frequency in turns, its rest), the axis, 0
+cache          uint8, heads x (keys, values) x a section: planes of 32 channels [tokens][16 bytes], a plane of 16
+               channels [tokens][8 bytes] if the last group has at most 16, scales [tokens][1, 2, 4 or 8 bytes];
+               byte b of a group holds channels 2b (low four bits) and 2b + 1 in e2m1, a scale byte s is 2^(s - 127);
+               tokens = the capacity rounded up to a multiple of 32
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda"
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+E2M1 = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+# smallest and largest scale exponent by the rows' type (include/sige.h)
+EXPONENTS = {"f32": (-125, 126), "bf16": (-125, 126), "f16": (-23, 13)}
+THETA = 10000.0
+
+
+def listed():
+    return [
+        # queries and keys (16 = 2 x 8 heads of 40) of one 4x4 block of a 64x64 map: nothing but latency
+        dict(name="rope_block", kind="rope", dtype="bf16", rows=16, heads=16, d=40, axes=2, layout="adjacent", blocks=4, side=64, used=40),
+        # a video's tokens, positions (t, y, x), halves of a head rotated against each other
+        dict(name="rope_video", kind="rope", dtype="bf16", rows=8192, heads=16, d=128, axes=3, layout="halves", blocks=0, side=0, used=128),
+        # K and V of an edit in the first self-attention of a latent-diffusion model (40 blocks of 4x4): stored and read back
+        dict(name="cache_edit", kind="cache", dtype="bf16", tokens=640, heads=8, d=40),
+        # the whole of a long cache, when an image is opened: bound by memory
+        dict(name="cache_fill", kind="cache", dtype="f16", tokens=16384, heads=8, d=128),
+        # one token against a long cache
+        dict(name="attend_one", kind="attend", dtype="bf16", nq=1, T=65536, heads=8, d=64, ranges=False),
+        # one 4x4 block of a 64x64 map
+        dict(name="attend_block", kind="attend", dtype="bf16", nq=16, T=4096, heads=8, d=40, ranges=False),
+        # a 15 % edit of a 64x64 map, heads of 80
+        dict(name="attend_edit", kind="attend", dtype="f16", nq=614, T=4096, heads=8, d=80, ranges=False),
+        # single precision; queries of several requests, each with its own range of the cache (some have none)
+        dict(name="attend_requests", kind="attend", dtype="f32", nq=333, T=2500, heads=3, d=72, ranges=True),
+        # the largest: a quarter of a 128x128 map edited
+        dict(name="attend_large", kind="attend", dtype="bf16", nq=4096, T=16384, heads=8, d=128, ranges=False),
+        # four requests of one 4x4 block each beside the projection to Q, K and V
+        dict(name="adapt_few", kind="adapt", dtype="bf16", rows=64, per=16, cin=320, cout=960, rank=8, adapters=4),
+        # sixteen requests' tokens in single precision, an odd number of rows, some without an adapter
+        dict(name="adapt_f32", kind="adapt", dtype="f32", rows=1011, per=37, cin=640, cout=648, rank=12, adapters=5),
+        # many tokens of wide layers
+        dict(name="adapt_large", kind="adapt", dtype="f16", rows=8192, per=64, cin=1280, cout=1280, rank=32, adapters=8),
+    ]
+
+
+def _log(rng, lo, hi):
+    return min(hi, max(lo, round(math.exp(rng.uniform(math.log(lo), math.log(hi))))))
+
+
+def draw(rng):
+    kind = rng.choice(("rope", "cache", "attend", "attend", "adapt"))
+    dtype = rng.choice(("bf16", "f16", "f32"))
+    if kind == "rope":
+        heads, d = _log(rng, 1, 32), 8 * _log(rng, 2, 32)
+        axes = rng.choice((1, 2, 3))
+        used = rng.choice((d, 2 * axes * max(1, d // (4 * axes))))
+        blocks = rng.choice((0, 3, 4, 8)) if axes > 1 else 0
+        rows = _log(rng, 1, max(1, 8192 * 16 * 128 // (heads * d * (2 if dtype == "f32" else 1))))
+        side = 0
+        if blocks:
+            side = rng.choice((30, 64, 96))
+            grid = (-(-side // blocks)) ** 2
+            rows = blocks * blocks * max(1, min(rows // (blocks * blocks), grid))
+        return dict(kind="rope", dtype=dtype, rows=rows, heads=heads, d=d, axes=axes, layout=rng.choice(("adjacent", "halves")), blocks=blocks, side=side, used=used)
+    if kind == "cache":
+        heads, d = _log(rng, 1, 16), 8 * _log(rng, 1, 32)
+        return dict(kind="cache", dtype=dtype, tokens=_log(rng, 1, max(1, 16384 * 8 * 128 // (heads * d * (2 if dtype == "f32" else 1)))), heads=heads, d=d)
+    if kind == "attend":
+        heads, d, nq = _log(rng, 1, 16), 8 * _log(rng, 1, 32), _log(rng, 1, 4096)
+        most = 4096 * 16384 * 8 * 128 // (nq * heads * d * (4 if dtype == "f32" else 1))
+        return dict(kind="attend", dtype=dtype, nq=nq, T=_log(rng, 1, max(1, min(65536, most, (1 << 26) // (heads * d)))), heads=heads, d=d, ranges=rng.random() < 0.4)
+    w = 4 if dtype == "f32" else 8
+    cin, cout, rank = w * _log(rng, 4, 1920 // w), w * _log(rng, 4, 1920 // w), w * _log(rng, 1, 96 // w)
+    rows = _log(rng, 1, max(1, 8192 * 2560 // ((cin + 2 * cout) * (2 if dtype == "f32" else 1))))
+    return dict(kind="adapt", dtype=dtype, rows=rows, per=_log(rng, 1, 64), cin=cin, cout=cout, rank=rank, adapters=_log(rng, 1, 16))
+
+
+# ---- inputs ------------------------------------------------------------------------------------------
+
+def _rotary_table(used, axes):
+    """Pairs split evenly over the axes (the first ones get the rest), theta^(-i / pairs of the axis) in turns."""
+    n = used // 2
+    per = [n // axes + (a < n % axes) for a in range(axes)]
+    f = torch.cat([THETA ** (-torch.arange(p, dtype=torch.float64) / max(p, 1)) / (2 * math.pi) for p in per])
+    axis = torch.cat([torch.full((p,), a, dtype=torch.int32) for a, p in enumerate(per)])
+    hi = f.float()
+    lo = (f - hi.double()).float()
+    return torch.stack([hi.view(torch.int32), lo.view(torch.int32), axis, torch.zeros_like(axis)], 1).contiguous().to(DEV)
+
+
+def _sections(d):
+    """Full groups of 32 channels, whether a group of 16 follows, scale bytes per token."""
+    rest = d % 32
+    tail = 0 < rest <= 16
+    groups = -(-d // 32)
+    return groups - tail, tail, 1 << (groups - 1).bit_length()
+
+
+def _quantise(x, dtype):
+    """[..., d] floats -> (codes 0..15 [..., groups * 32], exponents [..., groups]), to the nearest value, ties to the even one."""
+    lo, hi = EXPONENTS[dtype]
+    d = x.shape[-1]
+    g = torch.nn.functional.pad(x.float(), (0, -d % 32)).unflatten(-1, (-1, 32))
+    m, e = torch.frexp(g.abs().amax(-1))                       # max = m 2^e, m in [0.5, 1)
+    e = torch.where(m == 0, lo, torch.where(m > 0.75, e - 2, e - 3)).clamp(lo, hi)
+    a = torch.ldexp(g.abs(), -e.unsqueeze(-1))
+    code = (a > 0.25).int() + (a >= 0.75).int() + (a > 1.25).int() + (a >= 1.75).int() + (a > 2.5).int() + (a >= 3.5).int() + (a > 5.0).int()
+    return (code + 8 * (g < 0).int()).flatten(-2), e
+
+
+def _values(codes, e):
+    t = torch.tensor(E2M1 + tuple(-v for v in E2M1), device=codes.device)
+    return torch.ldexp(t[codes.long()].unflatten(-1, (-1, 32)), e.unsqueeze(-1)).flatten(-2)
+
+
+def _pack(k, v, dtype, capacity):
+    """The cache's bytes for k, v [tokens, heads, d]."""
+    tokens, heads, d = k.shape
+    full, tail, gs = _sections(d)
+    cap = -(-capacity // 32) * 32
+    parts = []
+    for x in (k, v):
+        codes, e = _quantise(x.transpose(0, 1), dtype)         # [heads, tokens, ...]
+        pairs = (codes[..., 0::2] | codes[..., 1::2] << 4).to(torch.uint8)
+        planes = pairs.unflatten(-1, (-1, 16)).transpose(1, 2)  # [heads, groups, tokens, 16]
+        room = torch.randint(0, 256, (heads, full, cap, 16), dtype=torch.uint8, device=DEV)    # (what lies behind the tokens is anything)
+        room[:, :, :tokens] = planes[:, :full]
+        sec = [room.flatten(1)]
+        if tail:
+            room = torch.randint(0, 256, (heads, cap, 8), dtype=torch.uint8, device=DEV)
+            room[:, :tokens] = planes[:, full, :, :8]
+            sec.append(room.flatten(1))
+        room = torch.randint(0, 256, (heads, cap, gs), dtype=torch.uint8, device=DEV)
+        room[:, :tokens, :e.shape[-1]] = (e + 127).to(torch.uint8)
+        sec.append(room.flatten(1))
+        parts.append(torch.cat(sec, 1))
+    return torch.stack(parts, 1).contiguous().flatten()
+
+
+def _ranges(nq, T, per=40):
+    """[begin, end) of each query: runs of about `per` queries are one request; every seventh has nothing."""
+    req = torch.arange(nq, device=DEV) // per
+    n = int(req[-1]) + 1
+    cut = torch.randint(0, T + 1, (n, 2), device=DEV).sort(dim=1).values
+    cut[3::7] = 0
+    return cut[req].int().contiguous()
+
+
+def prepare(case, seed):
+    torch.manual_seed(seed)
+    torch.cuda.manual_seed(seed)
+    s = dict(case)
+    td = DT[case["dtype"]]
+    randn = lambda *shape: torch.randn(*shape, device=DEV)  # noqa: E731
+    if case["kind"] == "rope":
+        s["x"] = randn(case["rows"], case["heads"] * case["d"]).to(td)
+        s["table"] = _rotary_table(case["used"], case["axes"])
+        if case["blocks"]:
+            b, side = case["blocks"], case["side"]
+            grid = -(-side // b)
+            pick = torch.randperm(grid * grid, device=DEV)[:case["rows"] // (b * b)].sort().values
+            s["indices"] = torch.stack([pick // grid * b, pick % grid * b], 1).int().contiguous()
+            s["frame"] = float(seed % 50)
+        else:
+            s["pos"] = torch.randint(0, 100000, (case["rows"], case["axes"]), device=DEV).float()
+    elif case["kind"] == "cache":
+        n = case["tokens"]
+        # channels of unlike size, as keys have them
+        size = torch.exp(0.7 * randn(case["heads"] * case["d"]))
+        s["k"], s["v"] = ((randn(n, case["heads"] * case["d"]) * size).to(td) for _ in range(2))
+        s["slots"] = torch.randperm(n, device=DEV).int()
+        s["room"] = torch.zeros(_cache_bytes(case["heads"], case["d"], n), dtype=torch.uint8, device=DEV)
+    elif case["kind"] == "attend":
+        T, heads, d = case["T"], case["heads"], case["d"]
+        s["q"] = randn(case["nq"], heads * d).to(td)
+        s["capacity"] = T + 7
+        k = randn(T, heads, d) * torch.exp(0.5 * randn(heads, d))
+        s["cache"] = _pack(k, randn(T, heads, d), case["dtype"], s["capacity"])
+        s["scale"] = 1.0 / math.sqrt(d)
+        s["ranges_"] = _ranges(case["nq"], T) if case["ranges"] else None
+    else:
+        r, cin, cout, rank, n = (case[k] for k in ("rows", "cin", "cout", "rank", "adapters"))
+        s["x"], s["base"] = randn(r, cin).to(td), randn(r, cout).to(td)
+        s["down"] = (randn(n, rank, cin) / math.sqrt(cin)).to(td)
+        s["up"] = (randn(n, cout, rank) / math.sqrt(rank)).to(td)
+        s["alpha"] = torch.rand(n, device=DEV) + 0.5
+        runs = -(-r // case["per"])
+        s["ids"] = torch.randint(-1 if runs > 4 else 0, n, (runs,), device=DEV).int()
+    return s
+
+
+def _cache_bytes(heads, d, capacity):
+    full, tail, gs = _sections(d)
+    return heads * 2 * (-(-capacity // 32) * 32) * (16 * full + 8 * tail + gs)
+
+
+# ---- one pass ----------------------------------------------------------------------------------------
+
+def run(s):
+    return {"rope": _rope, "cache": _cache, "attend": _attend, "adapt": _adapt}[s["kind"]](s)
+
+
+def _positions(s):
+    """[rows, axes] floats."""
+    if not s["blocks"]:
+        return s["pos"]
+    b = s["blocks"]
+    px = torch.arange(b * b, device=DEV)
+    yx = s["indices"].unsqueeze(1) + torch.stack([px // b, px % b], 1)
+    yx = yx.reshape(-1, 2).float()
+    return yx if s["axes"] == 2 else torch.cat([torch.full_like(yx[:, :1], s["frame"]), yx], 1)
+
+
+def _rope(s):
+    x, heads, d = s["x"], s["heads"], s["d"]
+    if own:
+        from paper_2211_02048_amd import api
+        y = torch.empty_like(x)
+        layout = api.ROPE_HALVES if s["layout"] == "halves" else api.ROPE_ADJACENT
+        if s["blocks"]:
+            g = api.geom(s["side"], s["side"], s["blocks"], 1, 1, 0)
+            api.sige_token_rope_blocks(x, y, heads, d, s["table"], g, s["indices"], None, n_blocks=s["indices"].shape[0], layout=layout,
+                                       n_axes=s["axes"], frame=s["frame"])
+        else:
+            api.sige_token_rope(x, y, heads, d, s["table"], s["pos"], n_rows=s["rows"], layout=layout)
+        return y
+    t = s["table"]
+    turns = t[:, 0].view(torch.float32).double() + t[:, 1].view(torch.float32).double()
+    angle = _positions(s)[:, t[:, 2].long()].double() * (turns * (2 * math.pi))
+    cos, sin = angle.cos().float().unsqueeze(1), angle.sin().float().unsqueeze(1)
+    h, n = x.float().view(-1, heads, d), t.shape[0]
+    if s["layout"] == "halves":
+        a, b = h[..., :n], h[..., n:2 * n]
+        out = torch.cat([a * cos - b * sin, a * sin + b * cos, h[..., 2 * n:]], -1)
+    else:
+        a, b = h[..., 0:2 * n:2], h[..., 1:2 * n:2]
+        out = torch.cat([torch.stack([a * cos - b * sin, a * sin + b * cos], -1).flatten(-2), h[..., 2 * n:]], -1)
+    return out.to(x.dtype).view_as(x)
+
+
+def _cache(s):
+    k, v, heads, d, n = s["k"], s["v"], s["heads"], s["d"], s["tokens"]
+    if own:
+        from paper_2211_02048_amd import api
+        ko, vo = torch.empty_like(k), torch.empty_like(v)
+        api.sige_cache4_store(k, v, s["room"], n, heads, d, slots=s["slots"], n_rows=n)
+        api.sige_cache4_load(s["room"], n, heads, d, ko, vo, first=0, n_tokens=n)
+        return ko, vo
+    out = []
+    for x in (k, v):
+        codes, e = _quantise(x.view(n, heads, d), s["dtype"])
+        y = torch.empty_like(x)
+        y[s["slots"].long()] = _values(codes, e)[..., :d].reshape(n, heads * d).to(x.dtype)
+        out.append(y)
+    return tuple(out)
+
+
+def _read_cache(cache, capacity, T, heads, d):
+    """k, v [heads, T, d] of the cache's bytes."""
+    full, tail, gs = _sections(d)
+    cap = -(-capacity // 32) * 32
+    sec = cache.view(heads, 2, cap * (16 * full + 8 * tail + gs))
+    at = cap * 16 * full
+    codes = sec[..., :at].view(heads, 2, full, cap, 16)[..., :T, :].transpose(2, 3).flatten(-2)
+    if tail:
+        codes = torch.cat([codes, sec[..., at:at + cap * 8].view(heads, 2, cap, 8)[:, :, :T]], -1)
+        at += cap * 8
+    codes = torch.stack([codes & 15, codes >> 4], -1).flatten(-2)
+    e = sec[..., at:].view(heads, 2, cap, gs)[:, :, :T, :full + tail].int() - 127
+    codes = torch.nn.functional.pad(codes, (0, -codes.shape[-1] % 32))
+    kv = _values(codes, e)[..., :d]
+    return kv[:, 0], kv[:, 1]
+
+
+def _attend(s):
+    q, heads, d, T = s["q"], s["heads"], s["d"], s["T"]
+    if own:
+        from paper_2211_02048_amd import api
+        if "work" not in s:                 # a program keeps it beside the cache
+            nb = api.sige_cache4_attn_workspace_bytes(s["nq"], T, heads, d)
+            s["work"] = torch.empty(nb // 4, dtype=torch.float32, device=DEV) if nb else None
+        o = torch.empty_like(q)
+        api.sige_cache4_attn(q, s["cache"], s["capacity"], o, s["scale"], T=T, heads=heads, d=d, ranges=s["ranges_"], workspace=s["work"])
+        return o
+    k, v = _read_cache(s["cache"], s["capacity"], T, heads, d)
+    logits = (q.float().view(-1, heads, d).transpose(0, 1) @ k.transpose(1, 2)) * s["scale"]
+    if s["ranges_"] is not None:
+        t = torch.arange(T, device=DEV)
+        seen = (t >= s["ranges_"][:, :1]) & (t < s["ranges_"][:, 1:])
+        logits = logits.masked_fill(~seen, float("-inf"))
+    top = logits.amax(-1, keepdim=True)
+    p = torch.exp(logits - torch.where(top == float("-inf"), 0.0, top))
+    total = p.sum(-1, keepdim=True)
+    o = (p @ v) / torch.where(total == 0, 1.0, total)
+    return o.transpose(0, 1).reshape(q.shape).to(q.dtype)
+
+
+def _adapt(s):
+    x, base, per = s["x"], s["base"], s["per"]
+    if own:
+        from paper_2211_02048_amd import api
+        y = torch.empty_like(base)
+        api.sige_token_lora(x, y, s["cin"], s["cout"], s["down"], s["up"], s["ids"], per, alpha=s["alpha"], base=base, n_rows=s["rows"])
+        return y
+    ids = s["ids"].long().repeat_interleave(per)[:s["rows"]]
+    n, rank = s["down"].shape[:2]
+    # all adapters at once, the row's own kept: n ranks per row
+    keep = (torch.arange(n, device=DEV) == ids.unsqueeze(1)).float() * s["alpha"]
+    h = (x.float() @ s["down"].float().flatten(0, 1).t()).view(-1, n, rank) * keep.unsqueeze(-1)
+    return (base.float() + h.flatten(1) @ s["up"].float().transpose(1, 2).flatten(0, 1)).to(base.dtype)
+
+
+# ---- what a pass cannot do without -------------------------------------------------------------------
+
+def work(case):
+    size = 4 if case["dtype"] == "f32" else 2
+    if case["kind"] == "rope":
+        n = case["rows"] * case["heads"] * case["d"]
+        return {"bytes": 2 * n * size + case["rows"] * (0 if case["blocks"] else 4 * case["axes"]) + 8 * case["used"], "flops": 3 * n}
+    if case["kind"] == "cache":
+        n = case["tokens"] * case["heads"]
+        held = -(-case["d"] // 8) * 4 + -(-case["d"] // 32)
+        return {"bytes": 2 * n * (2 * case["d"] * size + 2 * held) + 4 * case["tokens"], "flops": 4 * n * case["d"]}
+    if case["kind"] == "attend":
+        nq, T, heads, d = (case[k] for k in ("nq", "T", "heads", "d"))
+        held = -(-d // 8) * 4 + -(-d // 32)
+        seen = 0.4 if case["ranges"] else 1.0                  # the share of the map that ranges of two random ends leave
+        return {"bytes": 2 * nq * heads * d * size + 2 * T * heads * held, "flops": 4.0 * nq * T * heads * d * seen}
+    r, cin, cout, rank, n = (case[k] for k in ("rows", "cin", "cout", "rank", "adapters"))
+    n = min(n, -(-r // case["per"]))
+    return {"bytes": size * (r * (cin + 2 * cout) + n * rank * (cin + cout)), "flops": 2.0 * r * rank * (cin + cout)}
+
+
+# ---- the definition in 64 bits -----------------------------------------------------------------------
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return {"rope": _exact_rope, "cache": _exact_cache, "attend": _exact_attend, "adapt": _exact_adapt}[case["kind"]](s)
+
+
+def _exact_rope(s):
+    rows, heads, d, n = s["rows"], s["heads"], s["d"], s["used"] // 2
+    if s["blocks"]:
+        b = s["blocks"]
+        r = torch.arange(rows, device=DEV)
+        first = s["indices"].double()[r // (b * b)]
+        p = [first[:, 0] + r % (b * b) // b, first[:, 1] + r % b]
+        p = p if s["axes"] == 2 else [torch.full((rows,), s["frame"], dtype=torch.float64, device=DEV)] + p
+    else:
+        p = list(s["pos"].double().unbind(1))
+    x = s["x"].double().view(rows, heads, d)
+    y = x.clone()
+    at = 0
+    for axis in range(s["axes"]):
+        pairs = n // s["axes"] + (axis < n % s["axes"])
+        for i in range(pairs):
+            # (the table holds the frequency to 48 bits: 4e-15 of a far position's 2e4 turns)
+            t = p[axis] * THETA ** (-i / pairs)
+            z = torch.polar(torch.ones_like(t), t).unsqueeze(1)
+            a, b = (at, at + n) if s["layout"] == "halves" else (2 * at, 2 * at + 1)
+            w = torch.complex(x[:, :, a], x[:, :, b]) * z
+            y[:, :, a], y[:, :, b] = w.real, w.imag
+            at += 1
+    return y.view(rows, heads * d)
+
+
+def _exact_cache(s):
+    lo, hi = EXPONENTS[s["dtype"]]
+    grid = torch.tensor(E2M1, dtype=torch.float64, device=DEV)
+    out = []
+    for x in (s["k"], s["v"]):
+        x = x.double().view(s["tokens"], s["heads"], s["d"])
+        y = torch.empty_like(x)
+        for c in range(0, s["d"], 32):
+            g = x[..., c:c + 32]
+            top = g.abs().amax(-1, keepdim=True)
+            e = torch.ceil(torch.log2(top / 6))
+            e = torch.where(6 * torch.exp2(e) < top, e + 1, torch.where(6 * torch.exp2(e - 1) >= top, e - 1, e))
+            step = torch.exp2(e.clamp(lo, hi))
+            a = g.abs() / step
+            # from the largest value down: the first whose lower border is passed (a tie goes to the neighbour with an even code)
+            near = torch.zeros_like(a)
+            for i in range(1, 8):
+                border = (grid[i - 1] + grid[i]) / 2
+                near = torch.where((a > border) | ((a == border) & (i % 2 == 0)), grid[i], near)
+            y[..., c:c + 32] = torch.sign(g) * near * step
+        z = torch.empty_like(y)
+        z[s["slots"].long()] = y
+        out.append(z.view(s["tokens"], -1))
+    return tuple(out)
+
+
+def _exact_attend(s):
+    heads, d, T, nq = s["heads"], s["d"], s["T"], s["nq"]
+    full, tail, gs = _sections(d)
+    cap = -(-s["capacity"] // 32) * 32
+    size = cap * (16 * full + 8 * tail + gs)
+    out = torch.zeros(nq, heads, d, dtype=torch.float64, device=DEV)
+    q = s["q"].double().view(nq, heads, d)
+    ch = torch.arange(d, device=DEV)
+    tok = torch.arange(T, device=DEV).unsqueeze(1)
+    group = ch // 32
+    wide = torch.where(group < full, 16, 8)
+    where = cap * 16 * group + tok * wide + ch % 32 // 2
+    scale_at = cap * (16 * full + 8 * tail) + tok * gs + group
+    seen = torch.ones(nq, T, dtype=torch.bool, device=DEV)
+    if s["ranges_"] is not None:
+        seen = (tok.t() >= s["ranges_"][:, :1]) & (tok.t() < s["ranges_"][:, 1:])
+    some = seen.any(1)
+    for h in range(heads):
+        kv = []
+        for part in range(2):
+            sec = s["cache"][(2 * h + part) * size:(2 * h + part + 1) * size]
+            c = sec[where].int() >> (4 * (ch % 2)) & 15
+            e, m = c >> 1 & 3, c & 1
+            mag = torch.where(e == 0, 0.5 * m, torch.exp2(e.double() - 1) * (1 + 0.5 * m))
+            kv.append(torch.where(c > 7, -mag, mag) * torch.exp2(sec[scale_at].double() - 127))
+        for i in range(0, nq, 1024):
+            a = torch.where(seen[i:i + 1024], q[i:i + 1024, h] @ kv[0].t() * s["scale"], -math.inf)
+            ok = some[i:i + 1024]
+            out[i:i + 1024, h][ok] = torch.softmax(a[ok], -1) @ kv[1]
+    return out.view(nq, heads * d)
+
+
+def _exact_adapt(s):
+    y = s["base"].double()
+    for i, a in enumerate(s["ids"].tolist()):
+        if a >= 0:
+            r = slice(i * s["per"], (i + 1) * s["per"])
+            y[r] += float(s["alpha"][a]) * (s["x"][r].double() @ s["down"][a].double().t() @ s["up"][a].double().t())
+    return y
