@@ -24,7 +24,7 @@ DEV = "cuda"
 DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
 E2M1 = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
 # smallest and largest scale exponent by the rows' type (include/sige.h)
-EXPONENTS = {"f32": (-125, 126), "bf16": (-125, 126), "f16": (-23, 13)}
+EXPONENTS = {"f32": (-125, 125), "bf16": (-125, 125), "f16": (-23, 13)}
 THETA = 10000.0
 
 
