@@ -430,6 +430,97 @@ int sige_geglu(const void* x, sige_dtype dt, int32_t C, int32_t x_ld, const int3
                int32_t rows_per_count, int32_t max_rows, int32_t n_rows,
                void* y, int32_t y_ld, void* stream);
 
+/* ---- attention layers on stacked tokens: positions, a cache in 4 bits, adapters -------------- */
+
+/* Rotary positions with several axes, for queries and keys between their projection and the attention
+ * (Sec. 3.2 "Extension to attention layers": the token-wise operators of the stacked tokens).  A head's
+ * channels are rotated in n_pairs pairs,
+ *   (a, b) -> (a cos t - b sin t, a sin t + b cos t),  t = 2 pi * positions[row][axis_j] * f_j,
+ * pair j being channels (2j, 2j + 1) or (j, j + n_pairs); channels from 2 * n_pairs on keep their bits.  f_j, in turns
+ * per unit of position, and axis_j are the caller's table, a DEVICE array of n_pairs entries (16-byte aligned): f_j = turns + rest,
+ * two floats, so that far positions (up to 2^24) lose nothing.  sige_rope_pairs fills a HOST array for the common law: the
+ * axes' pairs follow each other, axis_pairs[a] of them each, pair i of an axis with p pairs has f = theta^(-i / p) / (2 pi).   */
+typedef struct { float turns, rest; int32_t axis, unused; } sige_rope_pair;
+typedef enum { SIGE_ROPE_ADJACENT = 0, SIGE_ROPE_HALVES = 1 } sige_rope_layout;
+int sige_rope_pairs(const int32_t* axis_pairs, int32_t n_axes, double theta, sige_rope_pair* pairs);
+
+/* x and y are rows of [heads][d] with row strides x_ld / y_ld (queries and keys side by side are 2 * heads of them); rows as in
+ * sige_token_norm (n_rows, or count * rows_per_count on the device).  positions: fp32 [rows][n_axes]; a pair whose axis is not in
+ * 0..n_axes-1 is not turned.  x == y is allowed.  d * size and the strides must be multiples of 16 bytes; in the layout of halves
+ * accesses are as wide as n_pairs allows.  Rounded once.                                    */
+int sige_token_rope(const void* x, sige_dtype dt, int32_t heads, int32_t d, int32_t x_ld, const int32_t* count,
+                    int32_t rows_per_count, int32_t max_rows, int32_t n_rows, const sige_rope_pair* pairs,
+                    int32_t n_pairs, sige_rope_layout layout, const float* positions, int32_t n_axes, void* y,
+                    int32_t y_ld, void* stream);
+/* The same with the positions taken from the block list: row i is pixel i % (block_h * block_w) of block i / (block_h * block_w), its
+ * position (y, x) for n_axes == 2 and (frame, y, x) for n_axes == 3.  g must be the geometry of a 1x1, stride-1, unpadded layer.
+ * (Pixels of a block that stick out of the map have the position they would have there.)  */
+int sige_token_rope_blocks(const void* x, sige_dtype dt, int32_t heads, int32_t d, int32_t x_ld, const sige_geom* g,
+                           const int32_t* indices, const int32_t* count, int32_t max_blocks, int32_t n_blocks,
+                           const sige_rope_pair* pairs, int32_t n_pairs, sige_rope_layout layout, int32_t n_axes,
+                           float frame, void* y, int32_t y_ld, void* stream);
+
+/* Keys and values held in 4 bits: the cache that sparse-query attention reads (Fig. "sige-attention") in about a quarter of
+ * its half-precision size.  32 channels of a head of a token (the last group may have fewer) share a scale 2^e, a byte s = e + 127;
+ * a value is 2^e times a float of four bits (sign, then 0, 0.5, 1, 1.5, 2, 3, 4, 6).  The caller owns the memory,
+ * sige_cache4_bytes(heads, d, capacity) of it, 16-byte aligned; no call needs it to be initialised.  Layout, for programs that fill or
+ * move it themselves, with cap = the capacity rounded up to a multiple of 32, G = ceil(d / 32) groups, the last of them short if it
+ * has at most 16 channels, F = the others, gs = 1, 2, 4 or 8 bytes, the first that holds G:
+ *   [heads][2: keys, values] { [F][cap][16 bytes]; if there is a short group [cap][8 bytes]; scales [cap][gs] }
+ * byte b of a group holds channel 2b in its low and 2b + 1 in its high four bits; codes behind d are 0.  A scale byte above 252 (fp16
+ * calls: above 140) marks a group that is not finite: it is read as NaN.  d must be a multiple of 8, <= 256.   */
+size_t sige_cache4_bytes(int32_t heads, int32_t d, int32_t capacity);
+
+/* Stores rows of keys and values, k and v of [heads][d] with row strides k_ld / v_ld, in any dt:
+ *   e = the smallest exponent with max|x| <= 6 * 2^e over the group, held within -125..125 (fp16: -23..13, so that what is stored
+ *   is an fp16 number); value = x / 2^e rounded to the nearest of the eight, ties to the one with an even code, at most 6.
+ * A group with an infinity or NaN gets the scale byte 255.  Row r goes to token slots[r] (DEVICE array; a slot outside 0..capacity-1:
+ * the row is not stored), or to token first + r (slots NULL; first must be 0 beside slots).  The tokens of a call must be
+ * distinct: of two rows in one slot, any mixture may remain.  Rows as in sige_token_norm.  Other tokens keep their bits.  */
+int sige_cache4_store(const void* k, int32_t k_ld, const void* v, int32_t v_ld, sige_dtype dt, int32_t heads, int32_t d,
+                      const int32_t* slots, int32_t first, const int32_t* count, int32_t rows_per_count,
+                      int32_t max_rows, int32_t n_rows, void* cache, int32_t capacity, void* stream);
+/* The same for the stacked tokens of a block list, as an edit stores them: pixel (y, x) of a block goes to token first + y * W_in + x;
+ * pixels outside the map are not stored.  g must be the geometry of a 1x1, stride-1, unpadded layer; first + H_in * W_in <= capacity. */
+int sige_cache4_store_blocks(const void* k, int32_t k_ld, const void* v, int32_t v_ld, sige_dtype dt, int32_t heads,
+                             int32_t d, const sige_geom* g, const int32_t* indices, const int32_t* count,
+                             int32_t max_blocks, int32_t n_blocks, int32_t first, void* cache, int32_t capacity,
+                             void* stream);
+/* Reads tokens first..first+n_tokens-1 back as rows of dt (k or v may be NULL: not read).  Values a store of the same dt left are exact;
+ * others are rounded to dt.                                                             */
+int sige_cache4_load(const void* cache, int32_t capacity, sige_dtype dt, int32_t heads, int32_t d, int32_t first,
+                     int32_t n_tokens, void* k, int32_t k_ld, void* v, int32_t v_ld, void* stream);
+
+/* sige_sparse_attn on such a cache: q, o rows of [heads][d] of any dt, softmax over the tokens that a row sees, fp32 sums.
+ * ranges: DEVICE int32 [Nq][2], row i sees tokens max(begin, 0)..min(end, T)-1 (the queries of several requests, each with its own
+ * part of the cache, or tokens that see only those before them); NULL: all T.  A row that sees no token is written as zeros, and
+ * what a row does not see - NaN, infinities - does not reach it.  0 <= T <= capacity.
+ * The cached values enter the products exactly (they are bf16 numbers; for fp16 queries, fp16 numbers wherever an fp16 row was stored).
+ * fp16 and bf16 round a probability to their type once; single precision loses nothing (operands in three parts).
+ * scale >= 0.  workspace: as for sige_sparse_attn, sige_cache4_attn_workspace_bytes of it.  */
+int sige_cache4_attn(const void* q, int32_t q_ld, const void* cache, int32_t capacity, sige_dtype dt, int32_t Nq,
+                     int32_t T, int32_t heads, int32_t d, float scale, const int32_t* ranges, void* o, int32_t o_ld,
+                     void* workspace, size_t workspace_bytes, void* stream);
+size_t sige_cache4_attn_workspace_bytes(int32_t Nq, int32_t T, int32_t heads, int32_t d);
+/* The same with the queries read from a full tensor by block list, as in sige_sparse_attn_blocks (ranges and o by stacked row).  */
+int sige_cache4_attn_blocks(const void* q, int32_t q_ld, const sige_geom* g, const int32_t* indices, int32_t n_blocks,
+                            const void* cache, int32_t capacity, sige_dtype dt, int32_t T, int32_t heads, int32_t d,
+                            float scale, const int32_t* ranges, void* o, int32_t o_ld, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* Low-rank adapters of many requests (or regions) beside a shared projection, on stacked tokens:
+ *   y_r = base_r + alpha_i * up_i (down_i x_r),  i = ids[r / rows_per_id],
+ * down [n_adapters][rank][Cin] and up [n_adapters][Cout][rank] of dtype dt, contiguous; alpha fp32 [n_adapters] or NULL (1).
+ * ids: DEVICE int32, one per run of rows_per_id rows (a block's tokens), any order; an id outside 0..n_adapters-1 is a run
+ * without adapter.  base [rows][Cout] is the projection's output, or NULL: y is the adapters' share alone, which sige_conv_scatter
+ * adds to its fp32 sums as residual_tiles.  y == base is allowed.  Sums in fp32, the middle vector in fp32 (half types multiply it as
+ * the sum of two halves), rounded once.  Rows: n_rows >= 0 from the host, or -1 = min(*count * rows_per_id, max_rows).
+ * Cin, Cout, rank and strides must be multiples of 16 bytes, rank <= 128.               */
+int sige_token_lora(const void* x, sige_dtype dt, int32_t Cin, int32_t x_ld, const int32_t* count, int32_t rows_per_id,
+                    int32_t max_rows, int32_t n_rows, const void* down, const void* up, int32_t rank,
+                    int32_t n_adapters, const float* alpha, const int32_t* ids, const void* base, int32_t base_ld,
+                    int32_t Cout, void* y, int32_t y_ld, void* stream);
+
 /* ---- helpers beside the path --------------------------------------------------- */
 
 /* Re-lays an OIHW weight tensor (device, dtype dt, [Cout][Cin][k][k]) into the
@@ -475,7 +566,7 @@ int sige_version(void);
  *   CONV_POINTWISE     the few-row 1x1 kernel: 0 = never, 1 = 64x32, 2 = 64x64, 3 = 32x32 patches
  *   CONV_POINTWISE_W4  its four-wave variant for 64x64 patches: 0 = never, 1 = always
  *   CONV_PAIR_WGS      most workgroups up to which sige_fused_conv_pair shares one launch
- *   ATTN_WGS           workgroups the cut of sige_sparse_attn aims for
+ *   ATTN_WGS           workgroups the cuts of sige_sparse_attn and sige_cache4_attn aim for
  *   DIFF_LOADS         16-byte loads per lane and tensor in flight in the difference kernel (1, 2, 4)
  *   DIFF_WGS           accepted and ignored (the difference kernel runs one step per wave)
  *   CONV_DIRECT        0: the shapes whose waves do not split K send their accumulators through LDS

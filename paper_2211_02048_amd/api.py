@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libsige_hip.so")
 
 SIGE_F32, SIGE_F16, SIGE_BF16 = 0, 1, 2
 ACT_NONE, ACT_SILU, ACT_RELU, ACT_LEAKY_RELU = 0, 1, 2, 3
+ROPE_ADJACENT, ROPE_HALVES = 0, 1
 _DT = {torch.float32: SIGE_F32, torch.float16: SIGE_F16, torch.bfloat16: SIGE_BF16}
 STATUS = {0: "SIGE_OK", 1: "SIGE_ERR_INVALID_ARG", 2: "SIGE_ERR_UNSUPPORTED", 3: "SIGE_ERR_CAPACITY",
           4: "SIGE_ERR_HIP"}
@@ -25,7 +26,9 @@ STATUS = {0: "SIGE_OK", 1: "SIGE_ERR_INVALID_ARG", 2: "SIGE_ERR_UNSUPPORTED", 3:
 EXPORTS = ["sige_reduce_mask", "sige_reduce_mask_workspace_bytes", "sige_reduce_mask_lists", "sige_gather", "sige_gather_modulated", "sige_conv", "sige_conv_workspace_bytes", "sige_conv_geglu", "sige_conv_scatter", "sige_scatter", "sige_fused_conv", "sige_fused_conv_pair", "sige_sparse_attn", "sige_sparse_attn_blocks",
            "sige_sparse_attn_workspace_bytes", "sige_token_norm", "sige_gather_token_norm", "sige_geglu", "sige_packed_weight_bytes", "sige_pack_weight",
            "sige_gn_stats", "sige_gn_stats_act", "sige_last_error", "sige_version", "sige_set_knob", "sige_get_knob", "sige_conv_plan", "sige_reduce_mask_noalloc", "sige_mark_blocks",
-           "sige_fused_conv_pair_marked"]
+           "sige_fused_conv_pair_marked", "sige_rope_pairs", "sige_token_rope", "sige_token_rope_blocks", "sige_cache4_bytes",
+           "sige_cache4_store", "sige_cache4_store_blocks", "sige_cache4_load", "sige_cache4_attn", "sige_cache4_attn_blocks",
+           "sige_cache4_attn_workspace_bytes", "sige_token_lora"]
 
 # sige_knob of the header
 KNOBS = {"CONV_CFG": 0, "CONV_KC": 1, "CONV_SPLIT": 2, "CONV_HALF": 3, "CONV_SPLIT_WGS": 4, "CONV_POINTWISE": 5,
@@ -132,6 +135,19 @@ def lib() -> ctypes.CDLL:
         L.sige_gn_stats.argtypes = [vp, i32, i32, i32, i32, i32, i32, vp, vp, f32, vp, vp, vp, vp, vp]
         L.sige_gn_stats_act.argtypes = [vp, i32, i32, i32, i32, i32, i32, vp, vp, f32, vp, vp, vp, vp, i32, vp, i32, vp]
         L.sige_conv_plan.argtypes = [i32, gp, i32, i32, i32, i32, i32, sz, ctypes.POINTER(ConvPlanInfo)]
+        f64 = ctypes.c_double
+        L.sige_rope_pairs.argtypes = [vp, i32, f64, vp]
+        L.sige_token_rope.argtypes = [vp, i32, i32, i32, i32, vp, i32, i32, i32, vp, i32, i32, vp, i32, vp, i32, vp]
+        L.sige_token_rope_blocks.argtypes = [vp, i32, i32, i32, i32, gp, vp, vp, i32, i32, vp, i32, i32, i32, f32, vp, i32, vp]
+        L.sige_cache4_bytes.restype = L.sige_cache4_attn_workspace_bytes.restype = ctypes.c_size_t
+        L.sige_cache4_bytes.argtypes = [i32, i32, i32]
+        L.sige_cache4_store.argtypes = [vp, i32, vp, i32, i32, i32, i32, vp, i32, vp, i32, i32, i32, vp, i32, vp]
+        L.sige_cache4_store_blocks.argtypes = [vp, i32, vp, i32, i32, i32, i32, gp, vp, vp, i32, i32, i32, vp, i32, vp]
+        L.sige_cache4_load.argtypes = [vp, i32, i32, i32, i32, i32, i32, vp, i32, vp, i32, vp]
+        L.sige_cache4_attn.argtypes = [vp, i32, vp, i32, i32, i32, i32, i32, i32, f32, vp, vp, i32, vp, sz, vp]
+        L.sige_cache4_attn_blocks.argtypes = [vp, i32, gp, vp, i32, vp, i32, i32, i32, i32, i32, f32, vp, vp, i32, vp, sz, vp]
+        L.sige_cache4_attn_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.sige_token_lora.argtypes = [vp, i32, i32, i32, vp, i32, i32, i32, vp, vp, i32, i32, vp, vp, vp, i32, i32, vp, i32, vp]
         L.sige_set_knob.argtypes = [i32, i32]
         L.sige_get_knob.argtypes = [i32]
         L.sige_get_knob.restype = i32
@@ -147,7 +163,7 @@ def lib() -> ctypes.CDLL:
 # points, which validate, plan and launch as always.
 _QUERIES = ("sige_last_error", "sige_packed_weight_bytes", "sige_sparse_attn_workspace_bytes",
             "sige_reduce_mask_workspace_bytes", "sige_conv_workspace_bytes", "sige_conv_plan", "sige_set_knob",
-            "sige_get_knob")
+            "sige_get_knob", "sige_rope_pairs", "sige_cache4_bytes", "sige_cache4_attn_workspace_bytes")
 
 
 class CallList:
@@ -516,6 +532,132 @@ def sige_sparse_attn_blocks(q_full, g: Geom, indices, n_blocks, k, v, o, scale, 
     _check(lib().sige_sparse_attn_blocks(_ptr(q_full), q_ld, ctypes.byref(g), _ptr(indices), n_blocks, _ptr(k),
                                          _ptr(v), kv_ld, _DT[q_full.dtype], T, heads, d, scale, _ptr(o), o_ld,
                                          _ptr(workspace), wsb, _stream()))
+
+
+def sige_rope_pairs(axis_pairs, theta=10000.0, device="cuda") -> torch.Tensor:
+    """The table of sige_token_rope, int32 [pairs][4] on `device`: the axes' pairs one after the other, axis_pairs[a] each,
+    pair i of an axis with p pairs turning by theta^(-i / p) / (2 pi) turns per unit of position."""
+    n = (ctypes.c_int32 * len(axis_pairs))(*axis_pairs)
+    table = torch.zeros((max(sum(axis_pairs), 0), 4), dtype=torch.int32)
+    _check(lib().sige_rope_pairs(n, len(axis_pairs), theta, _ptr(table)))
+    return table.to(device)
+
+
+def _stream_of(*tensors):
+    """The current stream, on which the call will run; refuses tensors of another device than the current one (a CPU tensor's address
+    is nothing a kernel may read)."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise SigeError(1, f"a tensor on {t.device} in a call on cuda:{dev}")
+    return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(dev))
+
+
+def sige_token_rope(x, y, heads, d, pairs, positions, *, layout=ROPE_ADJACENT, n_rows=-1, count=None, rows_per_count=0,
+                    max_rows=None, x_ld=None, y_ld=None):
+    """Rotates the `heads` heads of every row by the row's positions (fp32 [rows, axes]); y may be x."""
+    x2, y2 = x.reshape(-1, x.shape[-1]), y.reshape(-1, y.shape[-1])
+    mr = x2.shape[0] if max_rows is None else max_rows
+    _check(lib().sige_token_rope(_ptr(x), _DT[x.dtype], heads, d, x2.stride(0) if x_ld is None else x_ld, _ptr(count),
+                                 rows_per_count, mr, n_rows, _ptr(pairs), pairs.shape[0], layout, _ptr(positions),
+                                 positions.shape[-1], _ptr(y), y2.stride(0) if y_ld is None else y_ld, _stream_of(x, y, pairs, positions, count)))
+
+
+def sige_token_rope_blocks(x, y, heads, d, pairs, g: Geom, indices, count, *, n_axes=2, frame=0.0, layout=ROPE_ADJACENT,
+                           n_blocks=-1, max_blocks=None, x_ld=None, y_ld=None):
+    """The same with the positions (y, x) or (frame, y, x) of the listed blocks' pixels."""
+    x2, y2 = x.reshape(-1, x.shape[-1]), y.reshape(-1, y.shape[-1])
+    mb = indices.shape[0] if max_blocks is None else max_blocks
+    _check(lib().sige_token_rope_blocks(_ptr(x), _DT[x.dtype], heads, d, x2.stride(0) if x_ld is None else x_ld,
+                                        ctypes.byref(g), _ptr(indices), _ptr(count), mb, n_blocks, _ptr(pairs), pairs.shape[0],
+                                        layout, n_axes, frame, _ptr(y), y2.stride(0) if y_ld is None else y_ld, _stream_of(x, y, pairs, indices, count)))
+
+
+def sige_cache4_bytes(heads, d, capacity) -> int:
+    """Bytes of a cache of `capacity` tokens' keys and values in 4 bits (0: not a head size the cache has)."""
+    return int(lib().sige_cache4_bytes(heads, d, capacity))
+
+
+def _rows_ld(t, heads, d):
+    """Stride of the [heads * d] (or [heads, d]) rows of t."""
+    if t is None:
+        return 0
+    return t.stride(-3) if t.dim() == 3 and t.shape[-1] == d and t.shape[-2] == heads and t.stride(-2) == d else t.stride(-2)
+
+
+def _check_cache(cache, heads, d, capacity):
+    need = sige_cache4_bytes(heads, d, capacity)
+    if _nbytes(cache) < need:
+        raise SigeError(3, f"a cache of {capacity} tokens takes {need} bytes, the tensor has {_nbytes(cache)}")
+
+
+def sige_cache4_store(k, v, cache, capacity, heads, d, *, slots=None, first=0, n_rows=-1, count=None, rows_per_count=0,
+                      max_rows=None, k_ld=None, v_ld=None):
+    """Rows of keys and values into the cache: row r to token slots[r], or to first + r."""
+    _check_cache(cache, heads, d, capacity)
+    mr = k.shape[0] if max_rows is None else max_rows
+    _check(lib().sige_cache4_store(_ptr(k), _rows_ld(k, heads, d) if k_ld is None else k_ld, _ptr(v),
+                                   _rows_ld(v, heads, d) if v_ld is None else v_ld, _DT[k.dtype], heads, d, _ptr(slots), first,
+                                   _ptr(count), rows_per_count, mr, n_rows, _ptr(cache), capacity, _stream_of(k, v, cache, slots, count)))
+
+
+def sige_cache4_store_blocks(k, v, cache, capacity, heads, d, g: Geom, indices, count, *, n_blocks=-1, max_blocks=None, first=0,
+                             k_ld=None, v_ld=None):
+    """The stacked tokens of the listed blocks into the cache: pixel (y, x) to token first + y * W + x."""
+    _check_cache(cache, heads, d, capacity)
+    mb = indices.shape[0] if max_blocks is None else max_blocks
+    _check(lib().sige_cache4_store_blocks(_ptr(k), _rows_ld(k, heads, d) if k_ld is None else k_ld, _ptr(v),
+                                          _rows_ld(v, heads, d) if v_ld is None else v_ld, _DT[k.dtype], heads, d,
+                                          ctypes.byref(g), _ptr(indices), _ptr(count), mb, n_blocks, first, _ptr(cache),
+                                          capacity, _stream_of(k, v, cache, indices, count)))
+
+
+def sige_cache4_load(cache, capacity, heads, d, k, v, *, first=0, n_tokens=None, k_ld=None, v_ld=None):
+    """Tokens first, first + 1, ... of the cache as rows of k's and v's type (either may be None)."""
+    _check_cache(cache, heads, d, capacity)
+    t = k if k is not None else v
+    n = t.shape[0] if n_tokens is None else n_tokens
+    _check(lib().sige_cache4_load(_ptr(cache), capacity, _DT[t.dtype], heads, d, first, n, _ptr(k),
+                                  _rows_ld(k, heads, d) if k_ld is None else k_ld, _ptr(v),
+                                  _rows_ld(v, heads, d) if v_ld is None else v_ld, _stream_of(cache, k, v)))
+
+
+def sige_cache4_attn_workspace_bytes(Nq, T, heads, d) -> int:
+    return int(lib().sige_cache4_attn_workspace_bytes(Nq, T, heads, d))
+
+
+def sige_cache4_attn(q, cache, capacity, o, scale, *, T, heads, d, Nq=None, ranges=None, workspace=None, q_ld=None, o_ld=None):
+    """sige_sparse_attn on a cache in 4 bits; ranges (int32 [Nq, 2]): the tokens [begin, end) that each row sees."""
+    _check_cache(cache, heads, d, capacity)
+    Nq = q.shape[0] if Nq is None else Nq
+    _check(lib().sige_cache4_attn(_ptr(q), _rows_ld(q, heads, d) if q_ld is None else q_ld, _ptr(cache), capacity, _DT[q.dtype], Nq,
+                                  T, heads, d, scale, _ptr(ranges), _ptr(o), _rows_ld(o, heads, d) if o_ld is None else o_ld,
+                                  _ptr(workspace), _nbytes(workspace), _stream_of(q, cache, o, ranges, workspace)))
+
+
+def sige_cache4_attn_blocks(q_full, g: Geom, indices, n_blocks, cache, capacity, o, scale, *, T, heads, d, ranges=None,
+                            workspace=None, q_ld=None, o_ld=None):
+    """The same with the queries read from a full tensor by block list (sige_sparse_attn_blocks)."""
+    _check_cache(cache, heads, d, capacity)
+    _check(lib().sige_cache4_attn_blocks(_ptr(q_full), q_full.stride(-2) if q_ld is None else q_ld, ctypes.byref(g), _ptr(indices),
+                                         n_blocks, _ptr(cache), capacity, _DT[q_full.dtype], T, heads, d, scale, _ptr(ranges),
+                                         _ptr(o), _rows_ld(o, heads, d) if o_ld is None else o_ld, _ptr(workspace),
+                                         _nbytes(workspace), _stream_of(q_full, cache, o, indices, ranges, workspace)))
+
+
+def sige_token_lora(x, y, Cin, Cout, down, up, ids, rows_per_id, *, alpha=None, base=None, n_rows=-1, count=None, max_rows=None,
+                    x_ld=None, base_ld=None, y_ld=None):
+    """y[r] = base[r] + alpha[i] * up[i] (down[i] x[r]) with i = ids[r // rows_per_id]; y may be base."""
+    n, rank = down.shape[0], down.shape[1]
+    if tuple(down.shape) != (n, rank, Cin) or tuple(up.shape) != (n, Cout, rank) or not (down.is_contiguous() and up.is_contiguous()):
+        raise SigeError(1, "sige_token_lora: down is [adapters, rank, Cin] and up [adapters, Cout, rank], contiguous")
+    x2, y2 = x.reshape(-1, x.shape[-1]), y.reshape(-1, y.shape[-1])
+    b2 = None if base is None else base.reshape(-1, base.shape[-1])
+    mr = x2.shape[0] if max_rows is None else max_rows
+    _check(lib().sige_token_lora(_ptr(x), _DT[x.dtype], Cin, x2.stride(0) if x_ld is None else x_ld, _ptr(count), rows_per_id, mr,
+                                 n_rows, _ptr(down), _ptr(up), rank, n, _ptr(alpha), _ptr(ids), _ptr(base),
+                                 0 if b2 is None else b2.stride(0) if base_ld is None else base_ld, Cout, _ptr(y),
+                                 y2.stride(0) if y_ld is None else y_ld, _stream_of(x, y, down, up, ids, alpha, base, count)))
 
 
 def sige_packed_weight_bytes(dtype, Cout, Cin, k) -> int:

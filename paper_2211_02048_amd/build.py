@@ -11,7 +11,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(CSRC, "_build")
 LIB = os.path.join(HERE, "libsige_hip.so")
-SOURCES = ["conv_f16.hip", "conv_bf16.hip", "conv_f32.hip", "conv.hip", "attn.hip", "api.hip", "reduce_mask.hip", "gather_scatter.hip", "gn.hip", "token_ops.hip"]
+SOURCES = ["cache4_attn_f32.hip", "cache4_attn_bf16.hip", "cache4_attn_f16.hip", "conv_f16.hip", "conv_bf16.hip", "conv_f32.hip", "conv.hip", "attn.hip", "api.hip", "reduce_mask.hip", "gather_scatter.hip", "gn.hip", "token_ops.hip",
+           "token_rope.hip", "token_lora.hip", "cache4.hip", "cache4_attn.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I" + os.path.join(ROOT, "include"),
          "-I" + CSRC, "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-fno-gpu-rdc", "-Wall", "-Wno-unused-function"]

@@ -1,0 +1,237 @@
+// sige_token_lora: low-rank adapters of many requests (or regions of an image) beside a shared projection, on the stacked tokens of
+// the active blocks:   y_r = base_r + alpha_i * up_i (down_i x_r),   i = the adapter of the row's block.
+//
+// Bound by memory: per row and adapter 2 rank (Cin + Cout) operations against (Cin + 2 Cout) values.  One kernel, no workspace: a
+// workgroup takes 16 rows, its four waves share the contraction over Cin (the partial products meet in LDS), then each takes
+// stretches of the output channels.  Few rows alone would leave most compute units without work, so the output channels are cut
+// over workgroups too, each of which repeats the small first product.  Where the 16 rows have several adapters there is one pass
+// for each, of which its own rows keep the result: no sorting, no second launch, and nothing lost where requests are whole blocks.
+// The middle vector down_i x_r stays in 32 bits; the half types' second product takes it as the sum of two halves (the rounded
+// value and the rounded remainder: 16 bits of bf16, 22 of fp16).
+#include "common.h"
+
+#include <type_traits>
+
+namespace sige {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+struct LoraArgs {
+    const void* x;
+    const void* down;
+    const void* up;
+    const void* base;
+    void* y;
+    const float* alpha;
+    const int32_t* ids;
+    const int32_t* count;
+    int Cin, Cout, rank, adapters, x_ld, base_ld, y_ld;
+    int rows_per_id, max_rows, n_host;
+    FastDiv d_per;
+};
+
+template <typename T> struct LoraStep;            // one 16-byte vector per lane and operand: 32 (half types) or 16 channels
+template <> struct LoraStep<f16> {
+    static __device__ __forceinline__ void run(const uint4& a, const uint4& b, f32x4& c)
+    {
+        typedef _Float16 v8 __attribute__((ext_vector_type(8)));
+        c = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+    }
+};
+template <> struct LoraStep<bf16> {
+    static __device__ __forceinline__ void run(const uint4& a, const uint4& b, f32x4& c)
+    {
+        typedef __bf16 v8 __attribute__((ext_vector_type(8)));
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, a), __builtin_bit_cast(v8, b), c, 0, 0, 0);
+    }
+};
+template <> struct LoraStep<float> {
+    // (lane quarter k of instruction i: channel 4 k + i of the step, in both operands)
+    static __device__ __forceinline__ void run(const uint4& a, const uint4& b, f32x4& c)
+    {
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.x), __uint_as_float(b.x), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.y), __uint_as_float(b.y), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.z), __uint_as_float(b.z), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.w), __uint_as_float(b.w), c, 0, 0, 0);
+    }
+};
+
+constexpr int LORA_WAVES = 4;
+
+// RT = 16-wide tiles over the rank
+template <typename T, int RT>
+__global__ __launch_bounds__(64 * LORA_WAVES) void token_lora_kernel(LoraArgs a)
+{
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int VW = Vec16<T>::N, KS = 4 * VW;                  // channels per lane and per step
+    constexpr int KR = (RT * 16 + KS - 1) / KS;                   // steps over the rank
+    constexpr int RED = RT * 16 + 4;                              // floats per row of the partial products
+    constexpr int HROW = KR * KS + VW;                            // values per row of the middle vectors
+    __shared__ float red[LORA_WAVES][16][RED];
+    __shared__ uint4 hbuf[(F32 ? 1 : 2) * 16 * HROW / VW];
+    T* const hs = reinterpret_cast<T*>(hbuf);                     // [value, remainder][16][HROW]
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l16 = lane & 15, quarter = lane >> 4;
+    long rows = a.n_host;
+    if (a.n_host < 0) {
+        rows = (long)(*a.count) * a.rows_per_id;
+        if (rows > a.max_rows) rows = a.max_rows;
+    }
+    const long row0 = (long)blockIdx.x * 16;
+    if (row0 >= rows) return;
+    const long row = row0 + l16;
+    const bool live = row < rows;
+    int id = -1;                                                  // adapter of row l16, in every lane
+    if (live) {
+        int i, rest;
+        divmod((int)row, a.d_per, i, rest);
+        id = a.ids[i];
+        if ((unsigned)id >= (unsigned)a.adapters) id = -1;
+    }
+    const T* const xr = (const T*)a.x + (live ? row : row0) * a.x_ld;
+    for (int j = tid; j < (F32 ? 1 : 2) * 16 * HROW / VW; j += 64 * LORA_WAVES) hbuf[j] = make_uint4(0, 0, 0, 0);
+
+    for (unsigned long todo = __builtin_amdgcn_ballot_w64(id >= 0); todo != 0;) {
+        const int cur = __builtin_amdgcn_readlane(id, __builtin_ctzl(todo));
+        todo &= ~__builtin_amdgcn_ballot_w64(id == cur);
+        const T* const down = (const T*)a.down + (long)cur * a.rank * a.Cin;
+        f32x4 acc[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) acc[rt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s = wave; s * KS < a.Cin; s += LORA_WAVES) {
+            const int ch = s * KS + VW * quarter;
+            const bool in = ch < a.Cin;
+            const uint4 xv = in && live ? *(const uint4*)(xr + ch) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const int r = rt * 16 + l16;
+                const uint4 dv = in && r < a.rank ? *(const uint4*)(down + (long)r * a.Cin + ch) : make_uint4(0, 0, 0, 0);
+                LoraStep<T>::run(dv, xv, acc[rt]);                // rows: ranks, columns: tokens
+            }
+        }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) *(f32x4*)&red[wave][l16][rt * 16 + 4 * quarter] = acc[rt];
+        __syncthreads();
+        const float alpha = a.alpha != nullptr ? a.alpha[cur] : 1.0f;
+        for (int j = tid; j < 16 * 4 * RT; j += 64 * LORA_WAVES) {       // (whole waves: 64 RT of them)
+            const int t = j / (4 * RT), q = j % (4 * RT);
+            f32x4 s = *(const f32x4*)&red[0][t][4 * q];
+#pragma unroll
+            for (int w = 1; w < LORA_WAVES; ++w) s += *(const f32x4*)&red[w][t][4 * q];
+            if (__shfl(id, t) != cur) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float v = alpha * s[i];
+                const T h = from_f32<T>(v);
+                hs[t * HROW + 4 * q + i] = h;
+                if constexpr (!F32) hs[(16 + t) * HROW + 4 * q + i] = from_f32<T>(v - to_f32(h));
+            }
+        }
+        __syncthreads();
+    }
+
+    // y^T = up h^T: rows are output channels, so that a lane holds consecutive ones of one token.  Half types: two products of 16
+    // whose rows are dealt out in fours, eight consecutive channels per lane.
+    constexpr int TU = F32 ? 1 : 2, CU = 16 * TU;
+    const int units = (a.Cout + CU - 1) / CU, stride = gridDim.y * LORA_WAVES;
+    for (int u = blockIdx.y * LORA_WAVES + wave; u < units; u += stride) {
+        f32x4 sum[TU];
+#pragma unroll
+        for (int t = 0; t < TU; ++t) sum[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (unsigned long todo = __builtin_amdgcn_ballot_w64(id >= 0); todo != 0;) {
+            const int cur = __builtin_amdgcn_readlane(id, __builtin_ctzl(todo));
+            todo &= ~__builtin_amdgcn_ballot_w64(id == cur);
+            const T* const up = (const T*)a.up + (long)cur * a.Cout * a.rank;
+            f32x4 acc[TU];
+#pragma unroll
+            for (int t = 0; t < TU; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int s = 0; s < KR; ++s) {
+                const int k = s * KS + VW * quarter;
+                const uint4 hv = *(const uint4*)(hs + l16 * HROW + k);
+                uint4 hl;
+                if constexpr (!F32) hl = *(const uint4*)(hs + (16 + l16) * HROW + k);
+#pragma unroll
+                for (int t = 0; t < TU; ++t) {
+                    const int c = u * CU + (F32 ? l16 : (l16 >> 2) * 8 + t * 4 + (l16 & 3));
+                    const uint4 uv = c < a.Cout && k < a.rank ? *(const uint4*)(up + (long)c * a.rank + k) : make_uint4(0, 0, 0, 0);
+                    LoraStep<T>::run(uv, hv, acc[t]);
+                    if constexpr (!F32) LoraStep<T>::run(uv, hl, acc[t]);
+                }
+            }
+            // (taken over by the adapter's own rows, not added as zeros: what another adapter holds may be no number)
+#pragma unroll
+            for (int t = 0; t < TU; ++t)
+                if (id == cur) sum[t] = acc[t];
+        }
+        const int c = u * CU + 4 * TU * quarter;
+        if (!live || c >= a.Cout) continue;
+        float f[VW];
+#pragma unroll
+        for (int t = 0; t < TU; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[4 * t + i] = sum[t][i];
+        if (a.base != nullptr) {
+            float b[VW];
+            unpack<T>(*(const uint4*)((const T*)a.base + row * a.base_ld + c), b);
+#pragma unroll
+            for (int i = 0; i < VW; ++i) f[i] += b[i];
+        }
+        *(uint4*)((T*)a.y + row * a.y_ld + c) = pack<T>(f);
+    }
+}
+
+template <typename T>
+static int launch_lora(const LoraArgs& a, int rows, hipStream_t st)
+{
+    const int tiles = (rows + 15) / 16, units = (a.Cout * (int)sizeof(T) + 63) / 64;
+    // workgroups per 16 rows: two per compute unit where the rows alone are fewer, a stretch of channels per wave at least
+    int cut = (512 + tiles - 1) / tiles;
+    const int most = (units + LORA_WAVES - 1) / LORA_WAVES;
+    if (cut > most) cut = most;
+    const dim3 grid(tiles, cut);
+    auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(64 * LORA_WAVES), 0, st, a); };
+    const int rt = (a.rank + 15) / 16;
+    if (rt == 1) go(token_lora_kernel<T, 1>);
+    else if (rt == 2) go(token_lora_kernel<T, 2>);
+    else if (rt <= 4) go(token_lora_kernel<T, 4>);
+    else go(token_lora_kernel<T, 8>);
+    SIGE_LAUNCH_CHECK("sige_token_lora");
+    return SIGE_OK;
+}
+
+}  // namespace sige
+
+using namespace sige;
+
+extern "C" int sige_token_lora(const void* x, sige_dtype dt, int32_t Cin, int32_t x_ld, const int32_t* count, int32_t rows_per_id,
+                               int32_t max_rows, int32_t n_rows, const void* down, const void* up, int32_t rank,
+                               int32_t n_adapters, const float* alpha, const int32_t* ids, const void* base, int32_t base_ld,
+                               int32_t Cout, void* y, int32_t y_ld, void* stream)
+{
+    clear_error();
+    const char* who = "sige_token_lora";
+    SIGE_REQUIRE(dtype_ok(dt), SIGE_ERR_INVALID_ARG, "%s: unknown dtype %d", who, (int)dt);
+    SIGE_REQUIRE(Cin > 0 && Cout > 0 && rank > 0 && n_adapters > 0 && rows_per_id > 0, SIGE_ERR_INVALID_ARG,
+                 "%s: need Cin, Cout, rank, n_adapters and rows_per_id > 0", who);
+    SIGE_REQUIRE(max_rows >= 0 && n_rows >= -1 && n_rows <= max_rows, n_rows > max_rows ? SIGE_ERR_CAPACITY : SIGE_ERR_INVALID_ARG,
+                 "%s: need 0 <= n_rows <= max_rows (or n_rows = -1)", who);
+    SIGE_REQUIRE(n_rows >= 0 || count != nullptr, SIGE_ERR_INVALID_ARG, "%s: count is required when n_rows is -1", who);
+    SIGE_REQUIRE(x_ld >= Cin && y_ld >= Cout && (base == nullptr || base_ld >= Cout), SIGE_ERR_INVALID_ARG,
+                 "%s: row strides must be >= the channel counts", who);
+    const int vw = (int)(16 / dtype_size(dt));
+    SIGE_REQUIRE(rank <= 128, SIGE_ERR_UNSUPPORTED, "%s: the rank must be <= 128", who);
+    SIGE_REQUIRE(Cin % vw == 0 && Cout % vw == 0 && rank % vw == 0 && x_ld % vw == 0 && y_ld % vw == 0 && (base == nullptr || base_ld % vw == 0),
+                 SIGE_ERR_UNSUPPORTED, "%s: channel counts, rank and row strides must be multiples of %d elements", who, vw);
+    const int rows = n_rows >= 0 ? n_rows : max_rows;
+    if (rows == 0) return SIGE_OK;
+    SIGE_REQUIRE(x && down && up && ids && y, SIGE_ERR_INVALID_ARG, "%s: x, down, up, ids and y are required", who);
+    SIGE_REQUIRE(aligned16(x) && aligned16(down) && aligned16(up) && aligned16(base) && aligned16(y), SIGE_ERR_UNSUPPORTED,
+                 "%s: pointers must be 16-byte aligned", who);
+    LoraArgs a;
+    a.x = x; a.down = down; a.up = up; a.base = base; a.y = y; a.alpha = alpha; a.ids = ids; a.count = count;
+    a.Cin = Cin; a.Cout = Cout; a.rank = rank; a.adapters = n_adapters; a.x_ld = x_ld; a.base_ld = base_ld; a.y_ld = y_ld;
+    a.rows_per_id = rows_per_id; a.max_rows = max_rows; a.n_host = n_rows; a.d_per = fast_div(rows_per_id);
+    hipStream_t st = (hipStream_t)stream;
+    return dt == SIGE_F32 ? launch_lora<float>(a, rows, st) : dt == SIGE_F16 ? launch_lora<f16>(a, rows, st) : launch_lora<bf16>(a, rows, st);
+}

@@ -1,0 +1,150 @@
+"""What the rotary, 4-bit cache and adapter calls refuse, and what they compute on the host (no GPU: nothing below is enqueued)."""
+import ctypes
+import os
+
+import numpy as np
+import pytest
+import torch
+
+import cache4_oracle as ref
+from paper_2211_02048_amd import api
+
+FAKE = ctypes.c_void_p(0x10000)  # never dereferenced: every call below fails validation first
+ODD = ctypes.c_void_p(0x10008)
+F = ctypes.c_float(0.1)
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(api.LIB_PATH):
+        from paper_2211_02048_amd import build
+        build.build()
+    return api.lib()
+
+
+def err(L):
+    return L.sige_last_error().decode()
+
+
+def good():
+    return api.geom(16, 16, 4, 1, 1, 0)
+
+
+def test_rope_pairs(L):
+    t = api.sige_rope_pairs((3, 0, 5), 10000.0, device="cpu")
+    f = t[:, 0].view(torch.float32).double() + t[:, 1].view(torch.float32).double()
+    want = np.concatenate([10000.0 ** (-np.arange(3) / 3), 10000.0 ** (-np.arange(5) / 5)]) / (2 * np.pi)
+    np.testing.assert_allclose(f.numpy(), want, rtol=2.0 ** -46)
+    assert t[:, 2].tolist() == [0] * 3 + [2] * 5 and (t[:, 3] == 0).all()
+    n = (ctypes.c_int32 * 2)(2, -1)
+    assert L.sige_rope_pairs(n, 2, 10.0, FAKE) == 1 and "negative" in err(L)
+    for theta in (0.0, -1.0, float("inf"), float("nan")):
+        assert L.sige_rope_pairs((ctypes.c_int32 * 1)(2), 1, theta, FAKE) == 1
+    assert L.sige_rope_pairs(None, 1, 10.0, FAKE) == 1
+    assert L.sige_rope_pairs((ctypes.c_int32 * 1)(2), 0, 10.0, FAKE) == 1
+
+
+def rope(L, x=FAKE, dt=1, heads=4, d=40, x_ld=160, count=None, per=0, mr=8, n=8, pairs=FAKE, n_pairs=20, layout=0, pos=FAKE, axes=2, y=FAKE, y_ld=160):
+    return L.sige_token_rope(x, dt, heads, d, x_ld, count, per, mr, n, pairs, n_pairs, layout, pos, axes, y, y_ld, None)
+
+
+def test_rope_refusals(L):
+    assert rope(L, n=0) == 0 and err(L) == ""
+    assert rope(L, x=None, n=0) == 0
+    for kw in (dict(x=None), dict(y=None), dict(pairs=None), dict(pos=None), dict(dt=3), dict(heads=0), dict(d=0), dict(n_pairs=0), dict(n_pairs=21),
+               dict(layout=2), dict(x_ld=152), dict(y_ld=152), dict(n=-1), dict(n=-1, count=FAKE), dict(n=-2), dict(mr=-1, n=-1, count=FAKE, per=1), dict(axes=0)):
+        assert rope(L, **kw) == 1, kw
+    for kw in (dict(d=36, x_ld=160, n_pairs=4), dict(x_ld=164), dict(y_ld=164), dict(x=ODD), dict(y=ODD), dict(pairs=ODD), dict(dt=0, x_ld=162)):
+        assert rope(L, **kw) == 2, kw
+    assert rope(L, n=9) == 3
+    g = good()
+    call = lambda g=g, idx=FAKE, count=FAKE, mb=4, n=2, axes=2: L.sige_token_rope_blocks(  # noqa: E731
+        FAKE, 1, 4, 40, 160, ctypes.byref(g), idx, count, mb, n, FAKE, 20, 0, axes, F, FAKE, 160, None)
+    assert call(n=0) == 0
+    assert call(n=5) == 3 and call(idx=None) == 1 and call(count=None, n=-1) == 1 and call(axes=1) == 1 and call(axes=4) == 1
+    assert call(g=api.geom(16, 16, 4, 3, 1, 1)) == 2
+
+
+@pytest.mark.parametrize("d", [8, 16, 24, 32, 40, 64, 72, 80, 136, 160, 248, 256])
+def test_cache_bytes(L, d):
+    for heads, capacity in ((1, 1), (3, 32), (8, 33), (2, 100)):
+        full, tail, gs = ref.sections(d)
+        assert api.sige_cache4_bytes(heads, d, capacity) == heads * 2 * (-(-capacity // 32) * 32) * (16 * full + 8 * tail + gs)
+    assert api.sige_cache4_bytes(8, d, 2 ** 31 - 1) == 16 * 2 ** 31 * sum(np.array(ref.sections(d)) * (16, 8, 1))
+
+
+def test_cache_bytes_of_what_there_is_not(L):
+    for heads, d, capacity in ((0, 64, 8), (1, 0, 8), (1, 64, 0), (1, 4, 8), (1, 12, 8), (1, 264, 8), (-1, 64, 8), (65536, 64, 8), (1, 64, -5)):
+        assert api.sige_cache4_bytes(heads, d, capacity) == 0
+
+
+def test_store_and_load_refusals(L):
+    def store(k=FAKE, k_ld=320, v=FAKE, v_ld=320, dt=2, heads=8, d=40, slots=None, first=0, count=None, per=0, mr=8, n=8, cache=FAKE, cap=64):
+        return L.sige_cache4_store(k, k_ld, v, v_ld, dt, heads, d, slots, first, count, per, mr, n, cache, cap, None)
+    assert store(n=0) == 0
+    for kw in (dict(k=None), dict(v=None), dict(cache=None), dict(dt=9), dict(heads=0), dict(d=0), dict(cap=0), dict(k_ld=312), dict(v_ld=312), dict(n=-1),
+               dict(n=-1, count=FAKE), dict(first=-1), dict(slots=FAKE, first=1), dict(n=-2)):
+        assert store(**kw) == 1, kw
+    for kw in (dict(d=36), dict(d=264, heads=1), dict(k_ld=324), dict(v_ld=324), dict(k=ODD), dict(v=ODD), dict(cache=ODD), dict(dt=0, k_ld=322), dict(heads=70000)):
+        assert store(**kw) == 2, kw
+    assert store(n=9) == 3 and store(first=57) == 3 and "capacity" in err(L)
+
+    def blocks(g=good(), idx=FAKE, count=FAKE, mb=4, n=2, first=0, cap=256):
+        return L.sige_cache4_store_blocks(FAKE, 320, FAKE, 320, 2, 8, 40, ctypes.byref(g), idx, count, mb, n, first, FAKE, cap, None)
+    assert blocks(n=0) == 0
+    assert blocks(idx=None) == 1 and blocks(n=-1, count=None) == 1
+    assert blocks(n=5) == 3 and blocks(cap=255) == 3 and blocks(first=1) == 3 and blocks(first=-1) == 3
+    assert blocks(g=api.geom(16, 16, 4, 3, 1, 1)) == 2
+
+    def load(cache=FAKE, cap=64, dt=1, heads=8, d=40, first=0, n=8, k=FAKE, k_ld=320, v=FAKE, v_ld=320):
+        return L.sige_cache4_load(cache, cap, dt, heads, d, first, n, k, k_ld, v, v_ld, None)
+    assert load(n=0) == 0
+    for kw in (dict(cache=None), dict(k=None, v=None), dict(k_ld=312), dict(v_ld=312), dict(first=-1), dict(n=-1), dict(dt=-1)):
+        assert load(**kw) == 1, kw
+    assert load(k_ld=324) == 2 and load(v=ODD) == 2 and load(d=44) == 2
+    assert load(n=65) == 3 and load(first=60) == 3 and load(first=2 ** 31 - 1, n=2 ** 31 - 1) == 3
+
+
+def test_attention_refusals(L):
+    def attn(q=FAKE, q_ld=320, cache=FAKE, cap=64, dt=2, nq=8, T=64, heads=8, d=40, scale=F, ranges=None, o=FAKE, o_ld=320):
+        return L.sige_cache4_attn(q, q_ld, cache, cap, dt, nq, T, heads, d, scale, ranges, o, o_ld, None, 0, None)
+    assert attn(nq=0, q=None, o=None) == 0
+    for kw in (dict(q=None), dict(cache=None), dict(o=None), dict(dt=3), dict(nq=-1), dict(T=-1), dict(heads=0), dict(d=-8), dict(cap=0, T=0), dict(q_ld=312), dict(o_ld=312)):
+        assert attn(**kw) == 1, kw
+    for kw in (dict(d=36), dict(d=264, heads=1), dict(q_ld=324), dict(o_ld=324), dict(q=ODD), dict(o=ODD), dict(cache=ODD), dict(scale=ctypes.c_float(-1)),
+               dict(scale=ctypes.c_float(float("nan"))), dict(heads=70000), dict(dt=0, q_ld=322)):
+        assert attn(**kw) == 2, kw
+    assert attn(T=65) == 3
+    g = good()
+    call = lambda g=g, idx=FAKE, n=2: L.sige_cache4_attn_blocks(FAKE, 320, ctypes.byref(g), idx, n, FAKE, 64, 2, 65 if n == 7 else 64, 8, 40, F, None, FAKE, 320, None, 0, None)  # noqa: E731
+    assert call(n=0) == 0 and call(n=-1) == 1 and call(idx=None) == 1 and call(n=7) == 3 and call(g=api.geom(16, 16, 4, 3, 1, 1)) == 2
+    for bad in ((0, 64, 8, 40), (8, 0, 8, 40), (8, 64, 0, 40), (8, 64, 8, 0), (8, 64, 8, 264)):
+        assert api.sige_cache4_attn_workspace_bytes(*bad) == 0
+    assert api.sige_cache4_attn_workspace_bytes(4, 65536, 1, 64) > 0
+
+
+def test_lora_refusals(L):
+    def lora(x=FAKE, dt=1, cin=320, x_ld=320, count=None, per=4, mr=8, n=8, down=FAKE, up=FAKE, rank=8, ad=2, alpha=None, ids=FAKE, base=FAKE, base_ld=64,
+             cout=64, y=FAKE, y_ld=64):
+        return L.sige_token_lora(x, dt, cin, x_ld, count, per, mr, n, down, up, rank, ad, alpha, ids, base, base_ld, cout, y, y_ld, None)
+    assert lora(n=0) == 0
+    for kw in (dict(x=None), dict(down=None), dict(up=None), dict(ids=None), dict(y=None), dict(dt=5), dict(cin=0), dict(cout=0), dict(rank=0), dict(ad=0), dict(per=0),
+               dict(x_ld=312), dict(y_ld=56), dict(base_ld=56), dict(n=-1), dict(n=-2), dict(mr=-1, n=-1, count=FAKE)):
+        assert lora(**kw) == 1, kw
+    for kw in (dict(rank=136), dict(rank=12), dict(cin=324, x_ld=328), dict(cout=60), dict(x_ld=324), dict(y_ld=68), dict(base_ld=68), dict(x=ODD), dict(down=ODD),
+               dict(up=ODD), dict(base=ODD), dict(y=ODD)):
+        assert lora(**kw) == 2, kw
+    assert lora(n=9) == 3
+    assert lora(n=0, base=None, base_ld=0) == 0
+
+
+def test_the_binding_refuses_what_it_can_see():
+    """A cache tensor that is too small for the call, adapters of another shape, tensors that are not on the GPU."""
+    q = torch.zeros(4, 128)
+    small = torch.zeros(api.sige_cache4_bytes(2, 64, 32) - 1, dtype=torch.uint8)
+    with pytest.raises(api.SigeError, match="takes"):
+        api.sige_cache4_attn(q, small, 32, q, 1.0, T=4, heads=2, d=64)
+    with pytest.raises(api.SigeError, match="takes"):
+        api.sige_cache4_store(q, q, small, 32, 2, 64, n_rows=4)
+    with pytest.raises(api.SigeError, match="contiguous"):
+        api.sige_token_lora(q, q, 128, 128, torch.zeros(2, 8, 128), torch.zeros(2, 8, 128), None, 4, n_rows=4)

@@ -1,0 +1,171 @@
+"""Low-rank adapters beside a projection on the GPU against their definition in float64, and in the layer they belong to."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2211_02048_amd import api
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+def make(seed, rows, per, cin, cout, rank, n, dtype, ld=0):
+    g = torch.Generator().manual_seed(seed)
+    r = lambda *s: torch.randn(*s, generator=g, dtype=torch.float64)   # noqa: E731
+    x = torch.zeros(rows, cin + ld, dtype=DT[dtype])
+    x[:, :cin] = r(rows, cin)
+    down, up = (r(n, rank, cin) / cin ** 0.5).to(DT[dtype]), (r(n, cout, rank) / rank ** 0.5).to(DT[dtype])
+    ids = torch.randint(-1, n, (-(-rows // per),), generator=g, dtype=torch.int32)
+    alpha = torch.rand(n, generator=g) + 0.5
+    return x.cuda()[:, :cin], down.cuda(), up.cuda(), ids.cuda(), alpha.cuda(), r(rows, cout).to(DT[dtype]).cuda()
+
+
+def expected(x, down, up, ids, per, alpha, base, cout):
+    """The result and what bounds its error: |base| + alpha |up| |down| |x|."""
+    x, down, up, ids = f64(x), f64(down), f64(up), ids.cpu().numpy()
+    y = np.zeros((x.shape[0], cout)) if base is None else f64(base)
+    mag = np.abs(y)
+    for i, a in enumerate(ids):
+        r = slice(i * per, (i + 1) * per)
+        if 0 <= a < down.shape[0]:
+            s = 1.0 if alpha is None else float(alpha[a])
+            y[r] += s * (x[r] @ down[a].T @ up[a].T)
+            mag[r] += s * (np.abs(x[r]) @ np.abs(down[a]).T @ np.abs(up[a]).T)
+    return y, mag
+
+
+def close(y, want, mag, cin, rank, dtype, what=""):
+    # fp32 sums of cin and of rank terms, the middle vector as two halves (bf16: 2^-17 of it), the rounding of the result
+    bound = ((cin + rank + 4) * 2.0 ** -24 + (0 if dtype == "f32" else 2.0 ** -16)) * mag + torch.finfo(DT[dtype]).eps / 2 * np.abs(want)
+    err = np.abs(f64(y) - want)
+    assert (err <= bound + 1e-30).all(), f"{what}: {np.max(err / (bound + 1e-30)):.2f} of the bound"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,per,cin,cout,rank,n", [
+    (1, 1, 8, 8, 8, 1), (16, 16, 320, 960, 8, 4), (17, 1, 40, 24, 16, 5), (64, 16, 320, 320, 24, 3), (100, 37, 640, 72, 40, 6),
+    (257, 4, 64, 1000, 64, 2), (50, 3, 1288, 136, 128, 9), (33, 7, 48, 16, 96, 2), (1500, 25, 96, 104, 32, 7),
+])
+def test_adapters(rows, per, cin, cout, rank, n, dtype):
+    x, down, up, ids, alpha, base = make(rows + rank, rows, per, cin, cout, rank, n, dtype, ld=8)
+    for b, a in ((base, alpha), (None, alpha), (base, None)):
+        want, mag = expected(x, down, up, ids, per, a, b, cout)
+        y = torch.full((rows + 1, cout + 8), 7.0, dtype=DT[dtype], device="cuda")
+        api.sige_token_lora(x, y[:rows, :cout], cin, cout, down, up, ids, per, alpha=a, base=b, n_rows=rows)
+        torch.cuda.synchronize()
+        close(y[:rows, :cout], want, mag, cin, rank, dtype, "adapters")
+        assert (y[rows] == 7.0).all() and (y[:, cout:] == 7.0).all()
+    y = base.clone()                              # in place: the projection's output becomes the sum
+    api.sige_token_lora(x, y, cin, cout, down, up, ids, per, alpha=alpha, base=y, n_rows=rows)
+    torch.cuda.synchronize()
+    want, mag = expected(x, down, up, ids, per, alpha, base, cout)
+    close(y, want, mag, cin, rank, dtype, "in place")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_ids_counts_and_neighbours(dtype):
+    """Every row its own adapter, ids that name none, the same adapter twice; rows by a device count; rows and adapters of NaN reach
+    no one else."""
+    rows, cin, cout, rank, n = 45, 72, 40, 8, 20
+    x, down, up, _, alpha, base = make(3, rows, 1, cin, cout, rank, n, dtype)
+    ids = torch.from_numpy(np.random.default_rng(1).permutation(np.r_[np.arange(n), np.arange(n), [-1, n, 10 ** 6, -7, 3]])).int().cuda()
+    want, mag = expected(x, down, up, ids, 1, alpha, base, cout)
+    y = torch.full_like(base, 7.0)
+    api.sige_token_lora(x, y, cin, cout, down, up, ids, 1, alpha=alpha, base=base, count=torch.tensor([31], dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    close(y[:31], want[:31], mag[:31], cin, rank, dtype, "a device count")
+    assert (y[31:] == 7.0).all()
+    bad = ids.cpu().numpy() == 4
+    x2, down2, up2 = x.clone(), down.clone(), up.clone()
+    down2[4] = float("nan")
+    up2[4] = float("inf")
+    x2[7] = float("nan")
+    bad[7] = True
+    api.sige_token_lora(x2, y, cin, cout, down2, up2, ids, 1, alpha=alpha, base=base, n_rows=rows)
+    torch.cuda.synchronize()
+    close(y[torch.from_numpy(~bad).cuda()], want[~bad], mag[~bad], cin, rank, dtype, "beside NaN")
+    none = torch.full_like(ids, -1)               # nobody has one
+    api.sige_token_lora(x2, y, cin, cout, down2, up2, none, 1, alpha=alpha, base=base, n_rows=rows)
+    torch.cuda.synchronize()
+    assert torch.equal(y, base)
+    api.sige_token_lora(x2, y, cin, cout, down2, up2, none, 1, alpha=alpha, n_rows=rows)
+    torch.cuda.synchronize()
+    assert (y == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_attention_layer_of_an_edit(dtype):
+    """One attention layer of an edited image as it is used, captured into a graph: block list -> tokens normalised -> adapters per
+    block -> projection to Q, K, V that adds them -> rotary (y, x) -> K and V into the cache -> attention on it.  Every tensor
+    against float64 on the stored tensors before it, after each of several replays on a new image."""
+    import cache4_oracle as ref
+    from test_gpu_cache4 import close as attn_close
+    td = DT[dtype]
+    heads, d, res, b = 4, 40, 16, 4
+    C, T, rank, n_ad = heads * d, res * res, 8, 3
+    torch.manual_seed(0)
+    g = api.geom(res, res, b, 1, 1, 0)
+    pick = [1, 4, 6, 15]
+    n, n_tok = len(pick), len(pick) * b * b
+    idx = torch.tensor([[p // 4 * b, p % 4 * b] for p in pick], dtype=torch.int32, device="cuda")
+    cnt = torch.tensor([n], dtype=torch.int32, device="cuda")
+    x = torch.randn(res, res, C).to(td).cuda()
+    w = (torch.randn(3 * C, C, 1, 1) / C ** 0.5).to(td).cuda()
+    packed, bias = api.sige_pack_weight(w), torch.randn(3 * C).cuda()
+    down, up = (torch.randn(n_ad, rank, C) / C ** 0.5).to(td).cuda(), (torch.randn(n_ad, 3 * C, rank) / rank ** 0.5).to(td).cuda()
+    ids = torch.tensor([0, 2, -1, 1], dtype=torch.int32, device="cuda")
+    table = api.sige_rope_pairs((10, 10), 100.0)
+    cache = torch.empty(api.sige_cache4_bytes(heads, d, T), dtype=torch.uint8, device="cuda")
+    k0, v0 = torch.randn(T, C).to(td).cuda(), torch.randn(T, C).to(td).cuda()
+    api.sige_cache4_store(k0, v0, cache, T, heads, d, n_rows=T)
+    tn, delta = torch.empty(n_tok, C, dtype=td, device="cuda"), torch.empty(n_tok, 3 * C, dtype=td, device="cuda")
+    full = torch.zeros(res, res, 3 * C, dtype=td, device="cuda")       # the layer's Q | K | V, by pixel
+    qkv = torch.empty(n_tok, 3 * C, dtype=td, device="cuda")
+    rot = torch.empty(n_tok, 2 * C, dtype=td, device="cuda")
+    o = torch.empty(n_tok, C, dtype=td, device="cuda")
+    ws = torch.empty(max(api.sige_cache4_attn_workspace_bytes(n_tok, T, heads, d) // 4, 1), dtype=torch.float32, device="cuda")
+    scale = d ** -0.5
+
+    def layer():
+        api.sige_gather_token_norm(x, g, idx, cnt, tn.view(n, b, b, C), C, n_blocks=n)
+        api.sige_token_lora(tn, delta, C, 3 * C, down, up, ids, b * b, n_rows=n_tok)
+        api.sige_conv_scatter(tn.view(n, b, b, C), g, idx, cnt, C, 3 * C, packed, bias, full, n_blocks=n, residual_tiles=delta)
+        api.sige_gather(full, g, idx, cnt, qkv.view(n, b, b, 3 * C), n_blocks=n)
+        api.sige_token_rope_blocks(qkv[:, :2 * C], rot, 2 * heads, d, table, g, idx, cnt, n_blocks=n, x_ld=3 * C)
+        api.sige_cache4_store_blocks(rot[:, C:], qkv[:, 2 * C:], cache, T, heads, d, g, idx, cnt, n_blocks=n)
+        api.sige_cache4_attn(rot[:, :C], cache, T, o, scale, T=T, heads=heads, d=d, workspace=ws)
+
+    layer()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        layer()
+    tok = np.array([(p // 4 * b + i // b) * res + p % 4 * b + i % b for p in pick for i in range(b * b)])
+    pos = np.stack([tok // res, tok % res], 1).astype(float)
+    from test_gpu_token_rope import check as rope_check
+    for replay in range(3):
+        x.copy_(torch.randn(res, res, C).to(td))
+        o.fill_(7.0)
+        before = cache.cpu().numpy().copy()
+        graph.replay()
+        torch.cuda.synchronize()
+        want, mag = expected(tn, down, up, ids, b * b, None, None, 3 * C)
+        close(delta, want, mag, C, rank, dtype, "the adapters' share")
+        t64, w64 = f64(tn), f64(w).reshape(3 * C, C)
+        want = t64 @ w64.T + f64(bias) + f64(delta)
+        mag = np.abs(t64) @ np.abs(w64).T + np.abs(f64(bias)) + np.abs(f64(delta))
+        close(qkv, want, mag, C, 2, dtype, "projection and adapters")
+        rope_check(rot, qkv[:, :2 * C].contiguous(), pos, (10, 10), 100.0, 0, 2 * heads, d, dtype)
+        for which, t in enumerate((rot[:, C:], qkv[:, 2 * C:])):
+            code, byte = ref.quantise(f64(t).reshape(n_tok, heads, d), td)
+            for r, p in enumerate(tok):
+                ref.put(before, heads, d, T, p, code[r], byte[r], which)
+        k, v = ref.read(before, heads, d, T, T, 0), ref.read(before, heads, d, T, T, 1)
+        after = cache.cpu().numpy()
+        assert np.array_equal(ref.read(after, heads, d, T, T, 0), k) and np.array_equal(ref.read(after, heads, d, T, T, 1), v)
+        q64 = f64(rot[:, :C]).reshape(n_tok, heads, d)
+        want, mag = ref.attention(q64, k, v, scale)
+        attn_close(o, want, mag, q64, k, scale, dtype, T, "attention")
