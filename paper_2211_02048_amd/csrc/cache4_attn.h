@@ -111,6 +111,9 @@ __device__ __forceinline__ int wave_min(int v)
     return v;
 }
 
+// waves per SIMD that the registers are shared among, four waves on common chunks, half types: told so, the compiler keeps the sums of
+// heads up to 128 in half of what it takes otherwise (4096 queries of 16384 x 8 of 128 580 -> 367 us, 2048 of 4096 x 160 146 -> 85)
+constexpr int cache4_side_by_side(int NQ, size_t size) { return NQ > 1 && size == 2 ? 2 : 1; }
 constexpr int cache4_keys(int DT, int NQ) { return NQ > 1 && DT <= 4 ? 64 : 32; }       // per chunk
 // bytes between V rows in LDS: an odd multiple of 64, so that the keys of a transposed read fall on different banks; between K rows:
 // 16 bytes more than the channels
@@ -123,7 +126,7 @@ constexpr int cache4_chunk_bytes(int DT, int ODD, int NQ) { return cache4_keys(D
 // other is multiplied, one barrier per chunk).  NQ = 1: NK waves have the same 32 queries and take every NK-th chunk each; their (maximum,
 // denominator, sums) meet in LDS at the end.
 template <typename T, int DT, bool ODD, int NQ, int NK>
-__global__ __launch_bounds__(64 * NQ * NK, 1) void cache4_attend_kernel(Cache4AttnArgs a)
+__global__ __launch_bounds__(64 * NQ * NK, cache4_side_by_side(NQ, sizeof(T))) void cache4_attend_kernel(Cache4AttnArgs a)
 {
     static_assert(NQ == 1 || NK == 1, "queries or keys over the waves");
     using C = typename Cache4Compute<T>::type;
@@ -223,23 +226,32 @@ __global__ __launch_bounds__(64 * NQ * NK, 1) void cache4_attend_kernel(Cache4At
             const int key = KCH == 64 ? lane : l32;
             char* const dst = kv + buf * CHUNK + (which ? KCH * KROW + key * VROW : key * KROW) + g * 64;
             const float scale = cache4_scale(sbyte[i]);
+            // V rows lie an odd multiple of 64 bytes apart, four lanes on the banks of one: every four lanes start with another of their
+            // group's four vectors (else the writes took 60 of the 110 cycles that LDS was busy per chunk, 4096 queries of 16384 x 128)
+            u32x4 w = code[i];
+            int turn = 0;
+            if (which && !(ODD && g == DT - 1)) {
+                turn = (key >> 2) & 3;
+                if (turn & 1) w = u32x4{w.y, w.z, w.w, w.x};
+                if (turn & 2) w = u32x4{w.z, w.w, w.x, w.y};
+            }
             uint4 x[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = cache4_eight<C>(code[i][j], scale);
+            for (int j = 0; j < 4; ++j) x[j] = cache4_eight<C>(w[j], scale);
             const bool bad = sbyte[i] > LAST;
             if (__builtin_amdgcn_ballot_w64(bad) != 0ull) {
                 // a group that is no number: NaN for all who see it.  In a chunk of which some row does not see everything its
                 // values are left out instead (0 * NaN is NaN), and the rows that see them are marked below.
                 const uint32_t nan = __is_same(C, f16) ? 0x7e007e00u : 0x7fc07fc0u;
-                const uint32_t w = which && partial ? 0u : nan;
+                const uint32_t v = which && partial ? 0u : nan;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    if (bad) x[j] = make_uint4(w, w, w, w);
+                    if (bad) x[j] = make_uint4(v, v, v, v);
                 if (bad && which && partial) bad_chunk[NQ > 1 ? buf : wk] = c + 1;
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (!(ODD && g == DT - 1 && j >= 2)) *(uint4*)(dst + 16 * j) = x[j];
+                if (!(ODD && g == DT - 1 && j >= 2)) *(uint4*)(dst + 16 * ((j + turn) & 3)) = x[j];
         }
     };
     int c = c_begin + wk;
@@ -302,13 +314,20 @@ __global__ __launch_bounds__(64 * NQ * NK, 1) void cache4_attend_kernel(Cache4At
         for (int kt = 0; kt < KT; ++kt) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) sacc[kt][r] = 0.0f;
-            u32x4 kf[DK];
+            constexpr int AT_ONCE = DK > 14 ? 8 : DK;       // (K fragments on their way: heads of 256 have no registers for all)
 #pragma unroll
-            for (int s = 0; s < DK; ++s) kf[s] = *(const u32x4*)(ks + (kt * 32 + l32) * KROW + (16 * s + 8 * half) * 2);
+            for (int s0 = 0; s0 < DK; s0 += AT_ONCE) {
+                u32x4 kf[AT_ONCE];
 #pragma unroll
-            for (int p = NP - 1; p >= 0; --p)      // (the small parts first)
+                for (int s = 0; s < AT_ONCE; ++s)
+                    if (s0 + s < DK) kf[s] = *(const u32x4*)(ks + (kt * 32 + l32) * KROW + (16 * (s0 + s) + 8 * half) * 2);
 #pragma unroll
-                for (int s = 0; s < DK; ++s) mma32<C>(kf[s], qf[p][s], sacc[kt]);
+                for (int p = NP - 1; p >= 0; --p)  // (the small parts first)
+#pragma unroll
+                    for (int s = 0; s < AT_ONCE; ++s)
+                        if (s0 + s < DK) mma32<C>(kf[s], qf[p][s0 + s], sacc[kt]);
+                if (AT_ONCE < DK) __builtin_amdgcn_sched_barrier(0);
+            }
         }
         // of tile kt this lane holds keys 8 * (r / 4) + 4 * half + r % 4 of its query
         if (t0 < lo_most || t0 + KCH > hi_least) { // a chunk of which some row does not see everything
@@ -376,20 +395,27 @@ __global__ __launch_bounds__(64 * NQ * NK, 1) void cache4_attend_kernel(Cache4At
                     for (int p = 0; p < NP; ++p) pf[p][j] = w[p];
                     if constexpr (!ODD) lsum += p0 + p1;
                 }
-                s16x4 vlo[DT], vhi[DT];
+                constexpr int TILES = DT > 6 ? 4 : DT;
 #pragma unroll
-                for (int nt = 0; nt < DT; ++nt) {
-                    char* const at = (char*)ks + tr + (kt * 32 + 16 * s) * VROW + nt * 64;
-                    vlo[nt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(__attribute__((address_space(3))) char*)at);
-                    vhi[nt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(__attribute__((address_space(3))) char*)(at + 8 * VROW));
-                }
+                for (int n0 = 0; n0 < DT; n0 += TILES) {
+                    s16x4 vlo[TILES], vhi[TILES];
 #pragma unroll
-                for (int nt = 0; nt < DT; ++nt) {
-                    union { s16x4 h[2]; u32x4 u; } vf;
-                    vf.h[0] = vlo[nt];
-                    vf.h[1] = vhi[nt];
+                    for (int nt = 0; nt < TILES; ++nt) {
+                        if (n0 + nt >= DT) break;
+                        char* const at = (char*)ks + tr + (kt * 32 + 16 * s) * VROW + (n0 + nt) * 64;
+                        vlo[nt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(__attribute__((address_space(3))) char*)at);
+                        vhi[nt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(__attribute__((address_space(3))) char*)(at + 8 * VROW));
+                    }
 #pragma unroll
-                    for (int p = NP - 1; p >= 0; --p) mma32<C>(vf.u, pf[p], oacc[nt]);
+                    for (int nt = 0; nt < TILES; ++nt) {
+                        if (n0 + nt >= DT) break;
+                        union { s16x4 h[2]; u32x4 u; } vf;
+                        vf.h[0] = vlo[nt];
+                        vf.h[1] = vhi[nt];
+#pragma unroll
+                        for (int p = NP - 1; p >= 0; --p) mma32<C>(vf.u, pf[p], oacc[n0 + nt]);
+                    }
+                    if (TILES < DT) __builtin_amdgcn_sched_barrier(0);
                 }
             }
         l_run += lsum;
