@@ -8,6 +8,7 @@ is no fallback: if the library has not been built, or a call is refused, a
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from dataclasses import dataclass
 
@@ -543,36 +544,50 @@ def sige_rope_pairs(axis_pairs, theta=10000.0, device="cuda") -> torch.Tensor:
     return table.to(device)
 
 
-def _stream_of(*tensors):
+# The wrappers below are called per layer and step, where the host's time is what a small call costs: pointers are passed as plain
+# integers (the argtypes convert them), strides are read without making views.
+
+def _stream_of(x, *tensors):
     """The current stream, on which the call will run; refuses tensors of another device than the current one (a CPU tensor's address
     is nothing a kernel may read)."""
-    dev = torch.cuda.current_device()
+    dev = x.get_device()
     for t in tensors:
         if t is not None and t.get_device() != dev:
-            raise SigeError(1, f"a tensor on {t.device} in a call on cuda:{dev}")
-    return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(dev))
+            raise SigeError(1, f"tensors on {x.device} and on {t.device} in one call")
+    if dev < 0 or dev != torch._C._cuda_getDevice():
+        raise SigeError(1, f"a tensor on {x.device} in a call on another device")
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
 
 
 def sige_token_rope(x, y, heads, d, pairs, positions, *, layout=ROPE_ADJACENT, n_rows=-1, count=None, rows_per_count=0,
                     max_rows=None, x_ld=None, y_ld=None):
     """Rotates the `heads` heads of every row by the row's positions (fp32 [rows, axes]); y may be x."""
-    x2, y2 = x.reshape(-1, x.shape[-1]), y.reshape(-1, y.shape[-1])
-    mr = x2.shape[0] if max_rows is None else max_rows
-    _check(lib().sige_token_rope(_ptr(x), _DT[x.dtype], heads, d, x2.stride(0) if x_ld is None else x_ld, _ptr(count),
-                                 rows_per_count, mr, n_rows, _ptr(pairs), pairs.shape[0], layout, _ptr(positions),
-                                 positions.shape[-1], _ptr(y), y2.stride(0) if y_ld is None else y_ld, _stream_of(x, y, pairs, positions, count)))
+    stream = _stream_of(x, y, pairs, positions, count)
+    mr = x.numel() // x.shape[-1] if max_rows is None else max_rows
+    rc = lib().sige_token_rope(x.data_ptr(), _DT[x.dtype], heads, d, x.stride(-2) if x_ld is None else x_ld, _at(count),
+                               rows_per_count, mr, n_rows, pairs.data_ptr(), pairs.shape[0], layout, positions.data_ptr(),
+                               positions.shape[-1], y.data_ptr(), y.stride(-2) if y_ld is None else y_ld, stream)
+    if rc:
+        _check(rc)
 
 
 def sige_token_rope_blocks(x, y, heads, d, pairs, g: Geom, indices, count, *, n_axes=2, frame=0.0, layout=ROPE_ADJACENT,
                            n_blocks=-1, max_blocks=None, x_ld=None, y_ld=None):
     """The same with the positions (y, x) or (frame, y, x) of the listed blocks' pixels."""
-    x2, y2 = x.reshape(-1, x.shape[-1]), y.reshape(-1, y.shape[-1])
-    mb = indices.shape[0] if max_blocks is None else max_blocks
-    _check(lib().sige_token_rope_blocks(_ptr(x), _DT[x.dtype], heads, d, x2.stride(0) if x_ld is None else x_ld,
-                                        ctypes.byref(g), _ptr(indices), _ptr(count), mb, n_blocks, _ptr(pairs), pairs.shape[0],
-                                        layout, n_axes, frame, _ptr(y), y2.stride(0) if y_ld is None else y_ld, _stream_of(x, y, pairs, indices, count)))
+    stream = _stream_of(x, y, pairs, indices, count)
+    rc = lib().sige_token_rope_blocks(x.data_ptr(), _DT[x.dtype], heads, d, x.stride(-2) if x_ld is None else x_ld, ctypes.byref(g),
+                                      indices.data_ptr(), _at(count), indices.shape[0] if max_blocks is None else max_blocks,
+                                      n_blocks, pairs.data_ptr(), pairs.shape[0], layout, n_axes, frame, y.data_ptr(),
+                                      y.stride(-2) if y_ld is None else y_ld, stream)
+    if rc:
+        _check(rc)
 
 
+@functools.lru_cache(maxsize=None)
 def sige_cache4_bytes(heads, d, capacity) -> int:
     """Bytes of a cache of `capacity` tokens' keys and values in 4 bits (0: not a head size the cache has)."""
     return int(lib().sige_cache4_bytes(heads, d, capacity))
@@ -582,7 +597,9 @@ def _rows_ld(t, heads, d):
     """Stride of the [heads * d] (or [heads, d]) rows of t."""
     if t is None:
         return 0
-    return t.stride(-3) if t.dim() == 3 and t.shape[-1] == d and t.shape[-2] == heads and t.stride(-2) == d else t.stride(-2)
+    if t.dim() == 3 and t.shape[-1] == d and t.shape[-2] == heads and t.stride(-2) == d:
+        return t.stride(0)
+    return t.stride(-2)
 
 
 def _check_cache(cache, heads, d, capacity):
@@ -595,31 +612,38 @@ def sige_cache4_store(k, v, cache, capacity, heads, d, *, slots=None, first=0, n
                       max_rows=None, k_ld=None, v_ld=None):
     """Rows of keys and values into the cache: row r to token slots[r], or to first + r."""
     _check_cache(cache, heads, d, capacity)
-    mr = k.shape[0] if max_rows is None else max_rows
-    _check(lib().sige_cache4_store(_ptr(k), _rows_ld(k, heads, d) if k_ld is None else k_ld, _ptr(v),
-                                   _rows_ld(v, heads, d) if v_ld is None else v_ld, _DT[k.dtype], heads, d, _ptr(slots), first,
-                                   _ptr(count), rows_per_count, mr, n_rows, _ptr(cache), capacity, _stream_of(k, v, cache, slots, count)))
+    stream = _stream_of(k, v, cache, slots, count)
+    rc = lib().sige_cache4_store(k.data_ptr(), _rows_ld(k, heads, d) if k_ld is None else k_ld, v.data_ptr(),
+                                 _rows_ld(v, heads, d) if v_ld is None else v_ld, _DT[k.dtype], heads, d, _at(slots), first,
+                                 _at(count), rows_per_count, k.shape[0] if max_rows is None else max_rows, n_rows,
+                                 cache.data_ptr(), capacity, stream)
+    if rc:
+        _check(rc)
 
 
 def sige_cache4_store_blocks(k, v, cache, capacity, heads, d, g: Geom, indices, count, *, n_blocks=-1, max_blocks=None, first=0,
                              k_ld=None, v_ld=None):
     """The stacked tokens of the listed blocks into the cache: pixel (y, x) to token first + y * W + x."""
     _check_cache(cache, heads, d, capacity)
-    mb = indices.shape[0] if max_blocks is None else max_blocks
-    _check(lib().sige_cache4_store_blocks(_ptr(k), _rows_ld(k, heads, d) if k_ld is None else k_ld, _ptr(v),
-                                          _rows_ld(v, heads, d) if v_ld is None else v_ld, _DT[k.dtype], heads, d,
-                                          ctypes.byref(g), _ptr(indices), _ptr(count), mb, n_blocks, first, _ptr(cache),
-                                          capacity, _stream_of(k, v, cache, indices, count)))
+    stream = _stream_of(k, v, cache, indices, count)
+    rc = lib().sige_cache4_store_blocks(k.data_ptr(), _rows_ld(k, heads, d) if k_ld is None else k_ld, v.data_ptr(),
+                                        _rows_ld(v, heads, d) if v_ld is None else v_ld, _DT[k.dtype], heads, d, ctypes.byref(g),
+                                        indices.data_ptr(), _at(count), indices.shape[0] if max_blocks is None else max_blocks,
+                                        n_blocks, first, cache.data_ptr(), capacity, stream)
+    if rc:
+        _check(rc)
 
 
 def sige_cache4_load(cache, capacity, heads, d, k, v, *, first=0, n_tokens=None, k_ld=None, v_ld=None):
     """Tokens first, first + 1, ... of the cache as rows of k's and v's type (either may be None)."""
     _check_cache(cache, heads, d, capacity)
     t = k if k is not None else v
-    n = t.shape[0] if n_tokens is None else n_tokens
-    _check(lib().sige_cache4_load(_ptr(cache), capacity, _DT[t.dtype], heads, d, first, n, _ptr(k),
-                                  _rows_ld(k, heads, d) if k_ld is None else k_ld, _ptr(v),
-                                  _rows_ld(v, heads, d) if v_ld is None else v_ld, _stream_of(cache, k, v)))
+    stream = _stream_of(cache, k, v)
+    rc = lib().sige_cache4_load(cache.data_ptr(), capacity, _DT[t.dtype], heads, d, first, t.shape[0] if n_tokens is None else n_tokens,
+                                _at(k), _rows_ld(k, heads, d) if k_ld is None else k_ld, _at(v),
+                                _rows_ld(v, heads, d) if v_ld is None else v_ld, stream)
+    if rc:
+        _check(rc)
 
 
 def sige_cache4_attn_workspace_bytes(Nq, T, heads, d) -> int:
@@ -629,35 +653,40 @@ def sige_cache4_attn_workspace_bytes(Nq, T, heads, d) -> int:
 def sige_cache4_attn(q, cache, capacity, o, scale, *, T, heads, d, Nq=None, ranges=None, workspace=None, q_ld=None, o_ld=None):
     """sige_sparse_attn on a cache in 4 bits; ranges (int32 [Nq, 2]): the tokens [begin, end) that each row sees."""
     _check_cache(cache, heads, d, capacity)
-    Nq = q.shape[0] if Nq is None else Nq
-    _check(lib().sige_cache4_attn(_ptr(q), _rows_ld(q, heads, d) if q_ld is None else q_ld, _ptr(cache), capacity, _DT[q.dtype], Nq,
-                                  T, heads, d, scale, _ptr(ranges), _ptr(o), _rows_ld(o, heads, d) if o_ld is None else o_ld,
-                                  _ptr(workspace), _nbytes(workspace), _stream_of(q, cache, o, ranges, workspace)))
+    stream = _stream_of(q, cache, o, ranges, workspace)
+    rc = lib().sige_cache4_attn(q.data_ptr(), _rows_ld(q, heads, d) if q_ld is None else q_ld, cache.data_ptr(), capacity, _DT[q.dtype],
+                                q.shape[0] if Nq is None else Nq, T, heads, d, scale, _at(ranges), o.data_ptr(),
+                                _rows_ld(o, heads, d) if o_ld is None else o_ld, _at(workspace), _nbytes(workspace), stream)
+    if rc:
+        _check(rc)
 
 
 def sige_cache4_attn_blocks(q_full, g: Geom, indices, n_blocks, cache, capacity, o, scale, *, T, heads, d, ranges=None,
                             workspace=None, q_ld=None, o_ld=None):
     """The same with the queries read from a full tensor by block list (sige_sparse_attn_blocks)."""
     _check_cache(cache, heads, d, capacity)
-    _check(lib().sige_cache4_attn_blocks(_ptr(q_full), q_full.stride(-2) if q_ld is None else q_ld, ctypes.byref(g), _ptr(indices),
-                                         n_blocks, _ptr(cache), capacity, _DT[q_full.dtype], T, heads, d, scale, _ptr(ranges),
-                                         _ptr(o), _rows_ld(o, heads, d) if o_ld is None else o_ld, _ptr(workspace),
-                                         _nbytes(workspace), _stream_of(q_full, cache, o, indices, ranges, workspace)))
+    stream = _stream_of(q_full, cache, o, indices, ranges, workspace)
+    rc = lib().sige_cache4_attn_blocks(q_full.data_ptr(), q_full.stride(-2) if q_ld is None else q_ld, ctypes.byref(g),
+                                       indices.data_ptr(), n_blocks, cache.data_ptr(), capacity, _DT[q_full.dtype], T, heads, d, scale,
+                                       _at(ranges), o.data_ptr(), _rows_ld(o, heads, d) if o_ld is None else o_ld, _at(workspace),
+                                       _nbytes(workspace), stream)
+    if rc:
+        _check(rc)
 
 
 def sige_token_lora(x, y, Cin, Cout, down, up, ids, rows_per_id, *, alpha=None, base=None, n_rows=-1, count=None, max_rows=None,
                     x_ld=None, base_ld=None, y_ld=None):
     """y[r] = base[r] + alpha[i] * up[i] (down[i] x[r]) with i = ids[r // rows_per_id]; y may be base."""
-    n, rank = down.shape[0], down.shape[1]
-    if tuple(down.shape) != (n, rank, Cin) or tuple(up.shape) != (n, Cout, rank) or not (down.is_contiguous() and up.is_contiguous()):
+    n, rank, _ = down.shape
+    if down.shape != (n, rank, Cin) or up.shape != (n, Cout, rank) or not (down.is_contiguous() and up.is_contiguous()):
         raise SigeError(1, "sige_token_lora: down is [adapters, rank, Cin] and up [adapters, Cout, rank], contiguous")
-    x2, y2 = x.reshape(-1, x.shape[-1]), y.reshape(-1, y.shape[-1])
-    b2 = None if base is None else base.reshape(-1, base.shape[-1])
-    mr = x2.shape[0] if max_rows is None else max_rows
-    _check(lib().sige_token_lora(_ptr(x), _DT[x.dtype], Cin, x2.stride(0) if x_ld is None else x_ld, _ptr(count), rows_per_id, mr,
-                                 n_rows, _ptr(down), _ptr(up), rank, n, _ptr(alpha), _ptr(ids), _ptr(base),
-                                 0 if b2 is None else b2.stride(0) if base_ld is None else base_ld, Cout, _ptr(y),
-                                 y2.stride(0) if y_ld is None else y_ld, _stream_of(x, y, down, up, ids, alpha, base, count)))
+    stream = _stream_of(x, y, down, up, ids, alpha, base, count)
+    rc = lib().sige_token_lora(x.data_ptr(), _DT[x.dtype], Cin, x.stride(-2) if x_ld is None else x_ld, _at(count), rows_per_id,
+                               x.numel() // x.shape[-1] if max_rows is None else max_rows, n_rows, down.data_ptr(), up.data_ptr(), rank,
+                               n, _at(alpha), ids.data_ptr(), _at(base), 0 if base is None else base.stride(-2) if base_ld is None else base_ld,
+                               Cout, y.data_ptr(), y.stride(-2) if y_ld is None else y_ld, stream)
+    if rc:
+        _check(rc)
 
 
 def sige_packed_weight_bytes(dtype, Cout, Cin, k) -> int:

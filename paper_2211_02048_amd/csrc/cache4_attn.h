@@ -251,7 +251,7 @@ __global__ __launch_bounds__(64 * NQ * NK, cache4_side_by_side(NQ, sizeof(T))) v
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (!(ODD && g == DT - 1 && j >= 2)) *(uint4*)(dst + 16 * ((j + turn) & 3)) = x[j];
+                if (!(ODD && g == DT - 1 && j >= 2)) *(u32x4*)(dst + 16 * ((j + turn) & 3)) = u32x4{x[j].x, x[j].y, x[j].z, x[j].w};
         }
     };
     int c = c_begin + wk;
