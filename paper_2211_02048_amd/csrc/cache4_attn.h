@@ -20,6 +20,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace sige {
 
@@ -111,36 +112,41 @@ __device__ __forceinline__ int wave_min(int v)
     return v;
 }
 
-// waves per SIMD that the registers are shared among, four waves on common chunks, half types: told so, the compiler keeps the sums of
-// heads up to 128 in half of what it takes otherwise (4096 queries of 16384 x 8 of 128 580 -> 367 us, 2048 of 4096 x 160 146 -> 85)
-constexpr int cache4_side_by_side(int NQ, size_t size) { return NQ > 1 && size == 2 ? 2 : 1; }
-constexpr int cache4_keys(int DT, int NQ) { return NQ > 1 && DT <= 4 ? 64 : 32; }       // per chunk
-// bytes between V rows in LDS: an odd multiple of 64, so that the keys of a transposed read fall on different banks; between K rows:
-// 16 bytes more than the channels
-constexpr int cache4_v_row(int DT) { return 64 * (DT | 1); }
-constexpr int cache4_k_row(int DT, int ODD) { return 32 * (2 * DT - ODD) + 16; }
-constexpr int cache4_chunk_bytes(int DT, int ODD, int NQ) { return cache4_keys(DT, NQ) * (cache4_v_row(DT) + cache4_k_row(DT, ODD)); }
+#ifndef KTH
+#define KTH 3
+#define KTF 2
+#endif
+// 32-key tiles per chunk, by what their logits take in registers
+constexpr int cache4_tiles(int DT, int parts) { return DT <= (parts > 1 ? KTF : KTH) ? 2 : 1; }
+constexpr int cache4_v_bytes(int DT, int parts) { return 32 * cache4_tiles(DT, parts) * 64 * DT; }      // a chunk's V rows in LDS
+// The 64 bytes of group g of a V row: which of the row's groups of 64 bytes holds it.  Four neighbouring keys keep a group on
+// different banks, in the writes (a lane per key) and in the transposed reads (four keys per 16 lanes).
+template <int DT> __device__ __forceinline__ int cache4_v_group(int key, int g)
+{
+    return DT % 2 ? g : DT % 4 ? g ^ ((key >> 1) & 1) : g ^ (key & 3);
+}
 
+#ifndef WPS
+#define WPS(DT, NP) ((NP) > 1 ? 1 : (DT) <= 7 ? 2 : 1)
+#endif
 // DT = 32-wide tiles over d; ODD: the last one has 16 channels (d % 32 is 8 or 16), and its row 16 is the row of ones.
-// NQ = 4: four waves, 32 queries each, share their chunks (two buffers in LDS: the next chunk is expanded into one while the
-// other is multiplied, one barrier per chunk).  NQ = 1: NK waves have the same 32 queries and take every NK-th chunk each; their (maximum,
-// denominator, sums) meet in LDS at the end.
+// Every wave works by itself: 32 queries, K from memory straight into the first product's operands (8 bytes of a key and group per
+// lane: the order of the channels is the queries' too), V through the wave's own rows in LDS, which it is transposed out of.  NQ
+// waves of a workgroup take different queries, NK the same ones and every NK-th chunk of the tokens; these meet in LDS at the end.
 template <typename T, int DT, bool ODD, int NQ, int NK>
-__global__ __launch_bounds__(64 * NQ * NK, cache4_side_by_side(NQ, sizeof(T))) void cache4_attend_kernel(Cache4AttnArgs a)
+__global__ __launch_bounds__(64 * NQ * NK, WPS(DT, Cache4Compute<T>::parts)) void cache4_attend_kernel(Cache4AttnArgs a)
 {
     static_assert(NQ == 1 || NK == 1, "queries or keys over the waves");
     using C = typename Cache4Compute<T>::type;
     constexpr int NP = Cache4Compute<T>::parts;
     constexpr unsigned LAST = Cache4Compute<T>::last;
-    constexpr int KCH = cache4_keys(DT, NQ), KT = KCH / 32;
-    constexpr int VROW = cache4_v_row(DT), KROW = cache4_k_row(DT, ODD), CHUNK = cache4_chunk_bytes(DT, ODD, NQ);
+    constexpr int KT = cache4_tiles(DT, NP), KCH = 32 * KT;
+    constexpr int VROW = 64 * DT;
     constexpr int DK = 2 * DT - ODD;               // 16-wide steps over d for S^T
-    constexpr int UNITS = KCH == 64 ? 2 * DT : DT; // what a wave expands at a time: 64 groups of 32 channels
-    constexpr int NU = (UNITS + NQ - 1) / NQ;
-    constexpr int NBUF = NQ > 1 ? 2 : 1;
+    constexpr int VU = KT == 2 ? DT : (DT + 1) / 2;        // groups a lane expands per chunk: of one of 64 keys, or every other one of 32
+    constexpr int SW = (DT + 3) / 4;               // words of a token's scales
+    constexpr int GS = DT == 1 ? 1 : DT == 2 ? 2 : DT <= 4 ? 4 : 8;
     extern __shared__ uint4 lds4[];
-    __shared__ int bad_chunk[NQ > 1 ? 2 : NK];     // the chunk (+ 1) that left a value that is no number out of a buffer
-    __shared__ int ends[NQ][4];
     char* const lds = reinterpret_cast<char*>(lds4);
     const int d = a.d;
     const int tid = threadIdx.x, lane = tid & 63;
@@ -150,121 +156,81 @@ __global__ __launch_bounds__(64 * NQ * NK, cache4_side_by_side(NQ, sizeof(T))) v
     int qt, head;                                  // (the heads side by side: with eight of them each XCD keeps one in its L2)
     divmod((int)blockIdx.x, a.d_heads, qt, head);
     const int q0 = (qt * NQ + wq) * 32, qi = q0 + l32;
+    if (NQ > 1 && q0 >= a.Nq) return;
     const bool q_ok = qi < a.Nq;
 
     // what the rows see: a row that sees nothing is left out of the bounds and written as zeros
     int begin = 0, end = a.T;
-    if (q_ok) cache4_range(a.ranges, a.T, qi, begin, end);
-    const bool none = !q_ok || begin >= end;
-    int lo = none ? a.T : begin, hi = none ? 0 : end, lo_most = none ? 0 : begin, hi_least = none ? a.T : end;
-    if (a.ranges != nullptr || a.T == 0) {
-        lo = wave_min(lo);
-        hi = -wave_min(-hi);
-        lo_most = -wave_min(-lo_most);
-        hi_least = wave_min(hi_least);
-    } else {                                       // (all rows see all tokens; rows past Nq compute what no one reads)
-        lo = 0; hi = a.T; lo_most = 0; hi_least = a.T;
+    int lo = 0, hi = a.T, lo_most = 0, hi_least = a.T;
+    bool none = a.T == 0;
+    if (a.ranges != nullptr) {
+        if (q_ok) cache4_range(a.ranges, a.T, qi, begin, end);
+        none = !q_ok || begin >= end;
+        lo = __builtin_amdgcn_readfirstlane(wave_min(none ? a.T : begin));
+        hi = __builtin_amdgcn_readfirstlane(-wave_min(none ? 0 : -end));
+        lo_most = __builtin_amdgcn_readfirstlane(-wave_min(none ? 0 : -begin));
+        hi_least = __builtin_amdgcn_readfirstlane(wave_min(none ? a.T : end));
     }
-    if (tid < (NQ > 1 ? 2 : NK)) bad_chunk[tid] = 0;
-    if constexpr (NQ > 1) {
-        if (lane == 0) { ends[wq][0] = lo; ends[wq][1] = hi; ends[wq][2] = lo_most; ends[wq][3] = hi_least; }
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < NQ; ++w) {
-            lo = min(lo, ends[w][0]);
-            hi = max(hi, ends[w][1]);
-            lo_most = max(lo_most, ends[w][2]);
-            hi_least = min(hi_least, ends[w][3]);
-        }
-    } else {
-        __syncthreads();
-    }
-    lo = __builtin_amdgcn_readfirstlane(lo);
-    hi = __builtin_amdgcn_readfirstlane(hi);
-    lo_most = __builtin_amdgcn_readfirstlane(lo_most);
-    hi_least = __builtin_amdgcn_readfirstlane(hi_least);
-    int c_begin = blockIdx.z * a.chunks_per_split, c_end = c_begin + a.chunks_per_split;
-    c_begin = max(c_begin, lo / KCH);
-    c_end = min(c_end, (hi + KCH - 1) / KCH);
+    int c = max((int)blockIdx.z * a.chunks_per_split, lo / KCH) + wk;
+    const int c_end = min(((int)blockIdx.z + 1) * a.chunks_per_split, (int)(((long)hi + KCH - 1) / KCH));
 
-    char* const kv = lds + (NQ > 1 ? 0 : wk * CHUNK);        // a buffer: the K rows, then the V rows
-    const uint8_t* const sec = a.cache + 2L * head * a.section;
+    char* const vs = lds + wave * cache4_v_bytes(DT, NP);
+    const uint8_t* const ksec = a.cache + 2L * head * a.section;
+    const uint8_t* const vsec = ksec + a.section;
 
-    // a unit's 64 groups: of 64 keys (KCH 64; K's units, then V's), or of the keys and the values of 32
-    u32x4 code[NU];
-    unsigned sbyte[NU];
+    // a chunk on its way: of K, this lane's half of the groups of keys l32 (and l32 + 32); of V, the groups of a key
+    u32x2 kc[KT][DT];
+    u32x4 vc[VU];
+    uint32_t ksc[KT][SW], vsc[SW];
+    const int vkey = KT == 2 ? lane : l32;
+    auto scales = [&](const uint8_t* p, uint32_t (&w)[SW]) {
+        if constexpr (DT == 1) w[0] = *p;
+        else if constexpr (DT == 2) w[0] = *(const uint16_t*)p;
+        else if constexpr (DT <= 4) w[0] = *(const uint32_t*)p;
+        else { const u32x2 v = *(const u32x2*)p; w[0] = v.x; w[SW - 1] = v.y; }
+    };
     auto fetch = [&](int c) {
         const long t0 = (long)c * KCH;
-        const int last = (int)min((long)KCH, (long)a.T - t0) - 1;   // keys past the end read the last key's
+        const int last = (int)min((long)KCH, (long)a.T - t0) - 1;   // (tokens past the end: the last one again)
 #pragma unroll
-        for (int i = 0; i < NU; ++i) {
-            const int u = wq + NQ * i;
-            if (UNITS % NQ != 0 && u >= UNITS) break;
-            const int g = KCH == 64 ? (u >= DT ? u - DT : u) : u;
-            const int which = KCH == 64 ? (u >= DT) : half;
-            const int key = min(KCH == 64 ? lane : l32, last);
-            const uint8_t* const base = sec + (which ? a.section : 0);
-            if (ODD && g == DT - 1) {
-                const u32x2 w = *(const u32x2*)(base + a.full * a.cap * 16 + t0 * 8 + key * 8);
-                code[i] = u32x4{w.x, w.y, 0u, 0u};
+        for (int kt = 0; kt < KT; ++kt) {
+            const int key = min(kt * 32 + l32, last);
+#pragma unroll
+            for (int g = 0; g < DT; ++g) {
+                if (ODD && g == DT - 1) kc[kt][g] = u32x2{*(const uint32_t*)(ksec + a.full * a.cap * 16 + t0 * 8 + (key * 8 + half * 4)), 0u};
+                else kc[kt][g] = *(const u32x2*)(ksec + g * a.cap * 16 + t0 * 16 + (key * 16 + half * 8));
+            }
+            scales(ksec + a.scales + t0 * GS + key * GS, ksc[kt]);
+        }
+        const int key = min(vkey, last);
+#pragma unroll
+        for (int u = 0; u < VU; ++u) {
+            const int g = KT == 2 ? u : 2 * u + half;
+            if (KT == 1 && 2 * u + 1 >= DT && half) break;          // (an odd number of groups: the last one is the lower half's)
+            if (ODD && (KT == 2 ? u == DT - 1 : 2 * u + 1 >= DT - 1 && g == DT - 1)) {
+                const u32x2 w = *(const u32x2*)(vsec + a.full * a.cap * 16 + t0 * 8 + key * 8);
+                vc[u] = u32x4{w.x, w.y, 0u, 0u};
             } else {
-                code[i] = *(const u32x4*)(base + g * a.cap * 16 + t0 * 16 + key * 16);
+                vc[u] = *(const u32x4*)(vsec + g * a.cap * 16 + t0 * 16 + key * 16);
             }
-            sbyte[i] = base[a.scales + (t0 << a.gs_log2) + ((long)key << a.gs_log2) + g];
         }
+        scales(vsec + a.scales + t0 * GS + key * GS, vsc);
     };
-    // the expanded unit's row in LDS
-    auto stage = [&](int c, int buf) {
-        const int t0 = c * KCH;
-        const bool partial = t0 < lo_most || t0 + KCH > hi_least;
-#pragma unroll
-        for (int i = 0; i < NU; ++i) {
-            const int u = wq + NQ * i;
-            if (UNITS % NQ != 0 && u >= UNITS) break;
-            const int g = KCH == 64 ? (u >= DT ? u - DT : u) : u;
-            const int which = KCH == 64 ? (u >= DT) : half;
-            const int key = KCH == 64 ? lane : l32;
-            char* const dst = kv + buf * CHUNK + (which ? KCH * KROW + key * VROW : key * KROW) + g * 64;
-            const float scale = cache4_scale(sbyte[i]);
-            // V rows lie an odd multiple of 64 bytes apart, four lanes on the banks of one: every four lanes start with another of their
-            // group's four vectors (else the writes took 60 of the 110 cycles that LDS was busy per chunk, 4096 queries of 16384 x 128)
-            u32x4 w = code[i];
-            int turn = 0;
-            if (which && !(ODD && g == DT - 1)) {
-                turn = (key >> 2) & 3;
-                if (turn & 1) w = u32x4{w.y, w.z, w.w, w.x};
-                if (turn & 2) w = u32x4{w.z, w.w, w.x, w.y};
-            }
-            uint4 x[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = cache4_eight<C>(w[j], scale);
-            const bool bad = sbyte[i] > LAST;
-            if (__builtin_amdgcn_ballot_w64(bad) != 0ull) {
-                // a group that is no number: NaN for all who see it.  In a chunk of which some row does not see everything its
-                // values are left out instead (0 * NaN is NaN), and the rows that see them are marked below.
-                const uint32_t nan = __is_same(C, f16) ? 0x7e007e00u : 0x7fc07fc0u;
-                const uint32_t v = which && partial ? 0u : nan;
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (bad) x[j] = make_uint4(v, v, v, v);
-                if (bad && which && partial) bad_chunk[NQ > 1 ? buf : wk] = c + 1;
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (!(ODD && g == DT - 1 && j >= 2)) *(u32x4*)(dst + 16 * ((j + turn) & 3)) = u32x4{x[j].x, x[j].y, x[j].z, x[j].w};
-        }
+    // a group's scale; one that is no number is the power of two that the conversion makes NaN of
+    auto scale_of = [&](uint32_t word, int shift) {
+        const unsigned byte = (word >> shift) & 255u;
+        return cache4_scale(byte > LAST ? 255u : byte);
     };
-    int c = c_begin + wk;
     if (c < c_end) fetch(c);
 
-    // Q fragments (B operand of S^T = K Q^T): 8 consecutive channels of this lane's query
+    // Q fragments (B operand of S^T = K Q^T): the channels that the lane's half of a group of K holds
     u32x4 qf[NP][DK];
     {
         const long qrow = cache4_query_row(a, min(qi, a.Nq - 1));
         const char* const qp = (const char*)a.q + (qrow * a.q_ld + (long)head * d) * (long)sizeof(T);
 #pragma unroll
         for (int s = 0; s < DK; ++s) {
-            const int dd = 16 * s + 8 * half;
+            const int dd = ODD && s == DK - 1 ? 16 * s + 8 * half : 32 * (s >> 1) + 16 * half + 8 * (s & 1);
 #pragma unroll
             for (int p = 0; p < NP; ++p) qf[p][s] = u32x4{0u, 0u, 0u, 0u};
             if (q_ok && dd < d) {
@@ -285,19 +251,22 @@ __global__ __launch_bounds__(64 * NQ * NK, cache4_side_by_side(NQ, sizeof(T))) v
             }
         }
     }
-    // the columns of the V rows that no group fills (row 16 of the last tile: ones)
-    if constexpr (ODD) {
+    // V rows: the 16-byte vectors of a group lie in the order of their number ^ ((key >> 2) & 3), for the banks of the writes
+    auto v_at = [&](int key, int g, int j) { return key * VROW + cache4_v_group<DT>(key, g) * 64 + ((j ^ ((key >> 2) & 3)) * 16); };
+    if constexpr (ODD) {                           // the columns that no group fills (row 16 of the last tile: ones)
         constexpr uint32_t ONE = __is_same(C, f16) ? 0x3c00u : 0x3f80u;
-        for (int j = NQ > 1 ? tid : lane; j < NBUF * KCH * 2; j += 64 * NQ) {
-            const int buf = j / (KCH * 2), key = (j >> 1) % KCH;
-            *(uint4*)(kv + buf * CHUNK + KCH * KROW + key * VROW + (DT - 1) * 64 + 32 + (j & 1) * 16) = make_uint4(j & 1 ? 0u : ONE, 0, 0, 0);
-        }
+        for (int j = lane; j < KCH * 2; j += 64) *(u32x4*)(vs + v_at(j >> 1, DT - 1, 2 + (j & 1))) = u32x4{j & 1 ? 0u : ONE, 0u, 0u, 0u};
     }
     // where this lane's share of a transposed read starts: four lanes take the 16 columns of one key, four keys per 16 lanes,
-    // lane i of the 16 receives column i of the four keys
+    // lane i of the 16 receives column i of the four keys.  (The keys of one lane differ by multiples of 8: one more turn of 2
+    // in the order of the vectors for every 8.)
     typedef short s16x4 __attribute__((ext_vector_type(4)));
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-    const int tr = KCH * KROW + (4 * half + ((lane & 15) >> 2)) * VROW + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+    const int rkey = 4 * half + ((lane & 15) >> 2), rvec = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    int r_lo[DT % 2 ? 1 : DT];                     // by tile (an odd number of them: the tiles follow each other)
+#pragma unroll
+    for (int nt = 0; nt < (DT % 2 ? 1 : DT); ++nt) r_lo[nt] = v_at(rkey, nt, rvec) + (lane & 1) * 8;
+    const int r_up = ((rvec ^ half ^ 2) - (rvec ^ half)) * 16;      // what the vector's place differs by 8 keys on
 
     f32x16 oacc[DT];
 #pragma unroll
@@ -306,44 +275,69 @@ __global__ __launch_bounds__(64 * NQ * NK, cache4_side_by_side(NQ, sizeof(T))) v
         for (int r = 0; r < 16; ++r) oacc[nt][r] = 0.0f;
     float m_run = -INFINITY, l_run = 0.0f;
 
-    auto multiply = [&](int c, int buf) {
+    for (; c < c_end; c += NK) {
         const int t0 = c * KCH;
-        const char* const ks = kv + buf * CHUNK;
+        // a chunk of which some row does not see everything
+        const bool partial = t0 < lo_most || (long)t0 + KCH > hi_least;
+        bool lost_v = false;                       // some token's value in it is no number
+        if (partial) {
+#pragma unroll
+            for (int g = 0; g < DT; ++g) lost_v |= ((vsc[g >> 2] >> (8 * (g & 3))) & 255u) > LAST;
+            lost_v = __builtin_amdgcn_ballot_w64(lost_v) != 0ull;
+        }
+        // V rows (LDS operations of a wave stay in order: the last chunk's reads are behind it)
+#pragma unroll
+        for (int u = 0; u < VU; ++u) {
+            const int g = KT == 2 ? u : 2 * u + half;
+            const float scale = scale_of(vsc[(KT == 2 ? u : 2 * u) >> 2], KT == 2 ? 8 * (u & 3) : 16 * (u & 1) + 8 * half);
+            const bool tail = ODD && (KT == 2 ? u == DT - 1 : 2 * u + 1 >= DT - 1 && g == DT - 1);
+            u32x4 x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint4 e = cache4_eight<C>(vc[u][j], scale);
+                x[j] = u32x4{e.x, e.y, e.z, e.w};
+            }
+            // (a value that is no number is left out of a chunk that some row sees only a part of - 0 * NaN is NaN -, and the rows
+            // that see it are marked below)
+            if (lost_v && __float_as_uint(scale) == 0x7f800000u) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[j] = u32x4{0u, 0u, 0u, 0u};
+            }
+            if (KT == 1 && 2 * u + 1 >= DT && half) continue;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (!(tail && j >= 2)) *(u32x4*)(vs + v_at(vkey, g, j)) = x[j];
+        }
+        // S^T: rows = keys, columns = queries
         f32x16 sacc[KT];
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
+        for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) sacc[kt][r] = 0.0f;
-            constexpr int AT_ONCE = DK > 14 ? 8 : DK;       // (K fragments on their way: heads of 256 have no registers for all)
 #pragma unroll
-            for (int s0 = 0; s0 < DK; s0 += AT_ONCE) {
-                u32x4 kf[AT_ONCE];
+        for (int s = 0; s < DK; ++s)
 #pragma unroll
-                for (int s = 0; s < AT_ONCE; ++s)
-                    if (s0 + s < DK) kf[s] = *(const u32x4*)(ks + (kt * 32 + l32) * KROW + (16 * (s0 + s) + 8 * half) * 2);
+            for (int kt = 0; kt < KT; ++kt) {
+                const int g = s >> 1;
+                const uint4 e = cache4_eight<C>(kc[kt][g][s & 1], scale_of(ksc[kt][g >> 2], 8 * (g & 3)));
 #pragma unroll
-                for (int p = NP - 1; p >= 0; --p)  // (the small parts first)
-#pragma unroll
-                    for (int s = 0; s < AT_ONCE; ++s)
-                        if (s0 + s < DK) mma32<C>(kf[s], qf[p][s0 + s], sacc[kt]);
-                if (AT_ONCE < DK) __builtin_amdgcn_sched_barrier(0);
+                for (int p = NP - 1; p >= 0; --p) mma32<C>(u32x4{e.x, e.y, e.z, e.w}, qf[p][s], sacc[kt]);      // (the small parts first)
             }
-        }
+        if (c + NK < c_end) fetch(c + NK);         // in flight during the softmax and the second product
         // of tile kt this lane holds keys 8 * (r / 4) + 4 * half + r % 4 of its query
-        if (t0 < lo_most || t0 + KCH > hi_least) { // a chunk of which some row does not see everything
+        if (partial) {
             unsigned lost = 0;
-            const bool look = __builtin_amdgcn_readfirstlane(bad_chunk[NQ > 1 ? buf : wk]) == c + 1;
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int t = t0 + kt * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
                     if (t < begin || t >= end) sacc[kt][r] = -INFINITY;
-                    else if (look)
+                    else if (lost_v)
                         for (int g = 0; g < DT; ++g)
-                            if (sec[a.section + a.scales + ((long)t << a.gs_log2) + g] > LAST) lost |= 1u << g;
+                            if (vsec[a.scales + (long)t * GS + g] > LAST) lost |= 1u << g;
                 }
-            if (look) {
+            if (lost_v) {
                 lost |= (unsigned)__shfl_xor((int)lost, 32);
 #pragma unroll
                 for (int nt = 0; nt < DT; ++nt)
@@ -359,8 +353,8 @@ __global__ __launch_bounds__(64 * NQ * NK, cache4_side_by_side(NQ, sizeof(T))) v
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) mr = fmaxf(mr, sacc[kt][r]);
-        mr = fmaxf(mr, __shfl_xor(mr, 32));
-        const float mx = fmaxf(m_run, mr * a.scale_log2e);
+        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mr), __float_as_uint(mr), false, false);
+        const float mx = fmaxf(m_run, fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * a.scale_log2e);
         const float m_at = mx == -INFINITY ? 0.0f : mx;             // (only tokens out of sight so far: nothing is subtracted)
         if (__builtin_amdgcn_ballot_w64(mx != m_run) != 0ull) {     // some query's maximum moved
             const float alpha = __builtin_amdgcn_exp2f(m_run - m_at);
@@ -395,51 +389,17 @@ __global__ __launch_bounds__(64 * NQ * NK, cache4_side_by_side(NQ, sizeof(T))) v
                     for (int p = 0; p < NP; ++p) pf[p][j] = w[p];
                     if constexpr (!ODD) lsum += p0 + p1;
                 }
-                constexpr int TILES = DT > 6 ? 4 : DT;
 #pragma unroll
-                for (int n0 = 0; n0 < DT; n0 += TILES) {
-                    s16x4 vlo[TILES], vhi[TILES];
+                for (int nt = 0; nt < DT; ++nt) {
+                    char* const at = vs + (kt * 32 + 16 * s) * VROW + (DT % 2 ? r_lo[0] + nt * 64 : r_lo[nt]);
+                    union { s16x4 h[2]; u32x4 u; } vf;
+                    vf.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(__attribute__((address_space(3))) char*)at);
+                    vf.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(__attribute__((address_space(3))) char*)(at + 8 * VROW + r_up));
 #pragma unroll
-                    for (int nt = 0; nt < TILES; ++nt) {
-                        if (n0 + nt >= DT) break;
-                        char* const at = (char*)ks + tr + (kt * 32 + 16 * s) * VROW + (n0 + nt) * 64;
-                        vlo[nt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(__attribute__((address_space(3))) char*)at);
-                        vhi[nt] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(__attribute__((address_space(3))) char*)(at + 8 * VROW));
-                    }
-#pragma unroll
-                    for (int nt = 0; nt < TILES; ++nt) {
-                        if (n0 + nt >= DT) break;
-                        union { s16x4 h[2]; u32x4 u; } vf;
-                        vf.h[0] = vlo[nt];
-                        vf.h[1] = vhi[nt];
-#pragma unroll
-                        for (int p = NP - 1; p >= 0; --p) mma32<C>(vf.u, pf[p], oacc[n0 + nt]);
-                    }
-                    if (TILES < DT) __builtin_amdgcn_sched_barrier(0);
+                    for (int p = NP - 1; p >= 0; --p) mma32<C>(vf.u, pf[p], oacc[nt]);
                 }
             }
         l_run += lsum;
-    };
-
-    if constexpr (NQ > 1) {
-        if (c < c_end) {
-            stage(c, 0);
-            if (c + 1 < c_end) fetch(c + 1);
-        }
-        for (int buf = 0; c < c_end; ++c, buf ^= 1) {
-            __syncthreads();                       // this chunk's rows are there, the other buffer's have been read
-            if (c + 1 < c_end) {
-                stage(c + 1, buf ^ 1);
-                if (c + 2 < c_end) fetch(c + 2);
-            }
-            multiply(c, buf);
-        }
-    } else {
-        for (; c < c_end; c += NK) {
-            stage(c, 0);                           // (LDS operations of a wave stay in order: the last chunk's reads are behind it)
-            if (c + NK < c_end) fetch(c + NK);
-            multiply(c, 0);
-        }
     }
 
     float l_tot;
@@ -592,8 +552,8 @@ template <typename T> constexpr int cache4_nk(int DT) { return DT <= (sizeof(T) 
 template <typename T, int DT, bool ODD, int NQ, int NK>
 static int launch_cache4_as(const Cache4AttnArgs& a, hipStream_t st)
 {
-    const size_t lds = NQ > 1 ? 2 * (size_t)cache4_chunk_bytes(DT, ODD, NQ)
-                              : std::max((size_t)NK * cache4_chunk_bytes(DT, ODD, NQ), (size_t)NK * 32 * (a.d + 4) * sizeof(float));
+    const size_t rows = (size_t)NQ * NK * cache4_v_bytes(DT, Cache4Compute<T>::parts);
+    const size_t lds = NQ > 1 ? rows : std::max(rows, (size_t)NK * 32 * (a.d + 4) * sizeof(float));
     const long tiles = (a.Nq + 32L * NQ - 1) / (32 * NQ) * a.heads;
     SIGE_REQUIRE(tiles < (1L << 31), SIGE_ERR_UNSUPPORTED, "sige_cache4_attn: too many queries");
     auto kern = cache4_attend_kernel<T, DT, ODD, NQ, NK>;

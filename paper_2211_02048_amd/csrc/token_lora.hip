@@ -10,6 +10,7 @@
 // value and the rounded remainder: 16 bits of bf16, 22 of fp16).
 #include "common.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace sige {
@@ -27,6 +28,7 @@ struct LoraArgs {
     const int32_t* count;
     int Cin, Cout, rank, adapters, x_ld, base_ld, y_ld;
     int rows_per_id, max_rows, n_host;
+    int span;                  // stretches of output channels per wave
     FastDiv d_per;
 };
 
@@ -58,7 +60,8 @@ template <> struct LoraStep<float> {
 
 constexpr int LORA_WAVES = 4;
 
-// RT = 16-wide tiles over the rank
+// RT = 16-wide tiles over the rank.  No load is guarded (a guard is a branch of its own): lanes past the end read the last vector or
+// row again, and what they make of it is either multiplied by the zeros behind the rank, or not stored.
 template <typename T, int RT>
 __global__ __launch_bounds__(64 * LORA_WAVES) void token_lora_kernel(LoraArgs a)
 {
@@ -67,6 +70,9 @@ __global__ __launch_bounds__(64 * LORA_WAVES) void token_lora_kernel(LoraArgs a)
     constexpr int KR = (RT * 16 + KS - 1) / KS;                   // steps over the rank
     constexpr int RED = RT * 16 + 4;                              // floats per row of the partial products
     constexpr int HROW = KR * KS + VW;                            // values per row of the middle vectors
+    constexpr int AHEAD = RT <= 2 ? 5 : RT <= 4 ? 3 : 2;          // steps over Cin whose operands are on their way together
+    constexpr int TU = F32 ? 1 : 2, CU = 16 * TU;                 // products per stretch of output channels, its channels
+    constexpr int BATCH = KR <= 1 ? 5 : KR <= 2 ? 2 : 1;          // stretches whose operands are on their way together
     __shared__ float red[LORA_WAVES][16][RED];
     __shared__ uint4 hbuf[(F32 ? 1 : 2) * 16 * HROW / VW];
     T* const hs = reinterpret_cast<T*>(hbuf);                     // [value, remainder][16][HROW]
@@ -79,49 +85,86 @@ __global__ __launch_bounds__(64 * LORA_WAVES) void token_lora_kernel(LoraArgs a)
     }
     const long row0 = (long)blockIdx.x * 16;
     if (row0 >= rows) return;
-    const long row = row0 + l16;
-    const bool live = row < rows;
-    int id = -1;                                                  // adapter of row l16, in every lane
-    if (live) {
-        int i, rest;
-        divmod((int)row, a.d_per, i, rest);
-        id = a.ids[i];
-        if ((unsigned)id >= (unsigned)a.adapters) id = -1;
-    }
-    const T* const xr = (const T*)a.x + (live ? row : row0) * a.x_ld;
-    for (int j = tid; j < (F32 ? 1 : 2) * 16 * HROW / VW; j += 64 * LORA_WAVES) hbuf[j] = make_uint4(0, 0, 0, 0);
+    const bool live = row0 + l16 < rows;
+    const long row = live ? row0 + l16 : row0;
+    int run, rest;
+    divmod((int)row, a.d_per, run, rest);
+    int id = a.ids[run];                                          // adapter of row l16, in every lane
+    if (!live || (unsigned)id >= (unsigned)a.adapters) id = -1;
+    const T* const xr = (const T*)a.x + row * a.x_ld + VW * quarter;
+    if (KR * KS > RT * 16)                                        // (the half types' step of 32 over a rank of 16)
+        for (int j = tid; j < 2 * 16 * HROW / VW; j += 64 * LORA_WAVES) hbuf[j] = make_uint4(0, 0, 0, 0);
 
-    for (unsigned long todo = __builtin_amdgcn_ballot_w64(id >= 0); todo != 0;) {
+    const unsigned long all = __builtin_amdgcn_ballot_w64(id >= 0);
+    unsigned long todo = all;
+    auto next = [&]() {                                           // the next adapter of the 16 rows
         const int cur = __builtin_amdgcn_readlane(id, __builtin_ctzl(todo));
         todo &= ~__builtin_amdgcn_ballot_w64(id == cur);
-        const T* const down = (const T*)a.down + (long)cur * a.rank * a.Cin;
-        f32x4 acc[RT];
+        return cur;
+    };
+    const int full = a.Cin / KS, tail = a.Cin - full * KS;        // steps, channels of the last one
+    const int share = (full + LORA_WAVES - 1) / LORA_WAVES;       // of a wave, one after the other: whole lines of memory
+    while (todo != 0) {
+        // two adapters per pass, where there are two: of their products a lane keeps its own token's
+        const int cur0 = next(), cur1 = todo != 0 ? next() : -1;
+        f32x4 own[RT];
+        for (int n = 0; n < (cur1 >= 0 ? 2 : 1); ++n) {
+            const int cur = n == 0 ? cur0 : cur1;
+            const T* dr[RT];
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) acc[rt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        for (int s = wave; s * KS < a.Cin; s += LORA_WAVES) {
-            const int ch = s * KS + VW * quarter;
-            const bool in = ch < a.Cin;
-            const uint4 xv = in && live ? *(const uint4*)(xr + ch) : make_uint4(0, 0, 0, 0);
+            for (int rt = 0; rt < RT; ++rt)
+                dr[rt] = (const T*)a.down + ((long)cur * a.rank + min(rt * 16 + l16, a.rank - 1)) * a.Cin + VW * quarter;
+            f32x4 acc[RT];
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                const int r = rt * 16 + l16;
-                const uint4 dv = in && r < a.rank ? *(const uint4*)(down + (long)r * a.Cin + ch) : make_uint4(0, 0, 0, 0);
-                LoraStep<T>::run(dv, xv, acc[rt]);                // rows: ranks, columns: tokens
+            for (int rt = 0; rt < RT; ++rt) acc[rt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            auto steps = [&](auto count, int s0) {                // that many of the wave's steps, from s0 on
+                constexpr int N = decltype(count)::value;
+                uint4 xv[N], dv[N][RT];
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    xv[i] = *(const uint4*)(xr + (s0 + i) * KS);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) dv[i][rt] = *(const uint4*)(dr[rt] + (s0 + i) * KS);
+                }
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) LoraStep<T>::run(dv[i][rt], xv[i], acc[rt]);      // rows: ranks, columns: tokens
+            };
+            int s = wave * share;
+            const int end = min(s + share, full);
+            for (; s + AHEAD <= end; s += AHEAD) steps(std::integral_constant<int, AHEAD>(), s);
+            for (; s < end; ++s) steps(std::integral_constant<int, 1>(), s);
+            if (tail != 0 && wave == LORA_WAVES - 1) {            // the last channels
+                const bool in = VW * quarter < tail;
+                const int at = full * KS - (in ? 0 : VW * quarter);
+                uint4 xv = *(const uint4*)(xr + at);
+                if (!in) xv = make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    uint4 dv = *(const uint4*)(dr[rt] + at);
+                    if (!in) dv = make_uint4(0, 0, 0, 0);
+                    LoraStep<T>::run(dv, xv, acc[rt]);
+                }
             }
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+                if (n == 0 || id == cur) own[rt] = acc[rt];
         }
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) *(f32x4*)&red[wave][l16][rt * 16 + 4 * quarter] = acc[rt];
+        for (int rt = 0; rt < RT; ++rt) *(f32x4*)&red[wave][l16][rt * 16 + 4 * quarter] = own[rt];
         __syncthreads();
-        const float alpha = a.alpha != nullptr ? a.alpha[cur] : 1.0f;
         for (int j = tid; j < 16 * 4 * RT; j += 64 * LORA_WAVES) {       // (whole waves: 64 RT of them)
             const int t = j / (4 * RT), q = j % (4 * RT);
             f32x4 s = *(const f32x4*)&red[0][t][4 * q];
 #pragma unroll
             for (int w = 1; w < LORA_WAVES; ++w) s += *(const f32x4*)&red[w][t][4 * q];
-            if (__shfl(id, t) != cur) continue;
+            const int mine = __shfl(id, t);
+            if (mine < 0 || (mine != cur0 && mine != cur1)) continue;
+            const float alpha = a.alpha != nullptr ? a.alpha[mine] : 1.0f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float v = alpha * s[i];
+                const float v = 4 * q + i < a.rank ? alpha * s[i] : 0.0f;
                 const T h = from_f32<T>(v);
                 hs[t * HROW + 4 * q + i] = h;
                 if constexpr (!F32) hs[(16 + t) * HROW + 4 * q + i] = from_f32<T>(v - to_f32(h));
@@ -132,63 +175,80 @@ __global__ __launch_bounds__(64 * LORA_WAVES) void token_lora_kernel(LoraArgs a)
 
     // y^T = up h^T: rows are output channels, so that a lane holds consecutive ones of one token.  Half types: two products of 16
     // whose rows are dealt out in fours, eight consecutive channels per lane.
-    constexpr int TU = F32 ? 1 : 2, CU = 16 * TU;
-    const int units = (a.Cout + CU - 1) / CU, stride = gridDim.y * LORA_WAVES;
-    for (int u = blockIdx.y * LORA_WAVES + wave; u < units; u += stride) {
-        f32x4 sum[TU];
+    uint4 hv[KR], hl[KR];
 #pragma unroll
-        for (int t = 0; t < TU; ++t) sum[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        for (unsigned long todo = __builtin_amdgcn_ballot_w64(id >= 0); todo != 0;) {
-            const int cur = __builtin_amdgcn_readlane(id, __builtin_ctzl(todo));
-            todo &= ~__builtin_amdgcn_ballot_w64(id == cur);
+    for (int s = 0; s < KR; ++s) {
+        hv[s] = *(const uint4*)(hs + l16 * HROW + s * KS + VW * quarter);
+        if constexpr (!F32) hl[s] = *(const uint4*)(hs + (16 + l16) * HROW + s * KS + VW * quarter);
+    }
+    int u0 = (blockIdx.y * LORA_WAVES + wave) * a.span;
+    const int u_end = min(u0 + a.span, (a.Cout + CU - 1) / CU);
+    for (; u0 < u_end; u0 += BATCH) {
+        uint4 bv[BATCH];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            bv[i] = make_uint4(0, 0, 0, 0);
+            if (a.base != nullptr) bv[i] = *(const uint4*)((const T*)a.base + row * a.base_ld + min((u0 + i) * CU + 4 * TU * quarter, a.Cout - VW));
+        }
+        f32x4 sum[BATCH][TU];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i)
+#pragma unroll
+            for (int t = 0; t < TU; ++t) sum[i][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        todo = all;
+        while (todo != 0) {
+            const int cur = next();
             const T* const up = (const T*)a.up + (long)cur * a.Cout * a.rank;
-            f32x4 acc[TU];
+            uint4 uv[BATCH][KR][TU];
 #pragma unroll
-            for (int t = 0; t < TU; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int s = 0; s < KR; ++s) {
-                const int k = s * KS + VW * quarter;
-                const uint4 hv = *(const uint4*)(hs + l16 * HROW + k);
-                uint4 hl;
-                if constexpr (!F32) hl = *(const uint4*)(hs + (16 + l16) * HROW + k);
+            for (int i = 0; i < BATCH; ++i)
 #pragma unroll
                 for (int t = 0; t < TU; ++t) {
-                    const int c = u * CU + (F32 ? l16 : (l16 >> 2) * 8 + t * 4 + (l16 & 3));
-                    const uint4 uv = c < a.Cout && k < a.rank ? *(const uint4*)(up + (long)c * a.rank + k) : make_uint4(0, 0, 0, 0);
-                    LoraStep<T>::run(uv, hv, acc[t]);
-                    if constexpr (!F32) LoraStep<T>::run(uv, hl, acc[t]);
+                    const T* const ur = up + (long)min((u0 + i) * CU + (F32 ? l16 : (l16 >> 2) * 8 + t * 4 + (l16 & 3)), a.Cout - 1) * a.rank;
+#pragma unroll
+                    for (int s = 0; s < KR; ++s) uv[i][s][t] = *(const uint4*)(ur + min(s * KS + VW * quarter, a.rank - VW));
                 }
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                f32x4 acc[TU];
+#pragma unroll
+                for (int t = 0; t < TU; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int s = 0; s < KR; ++s)
+#pragma unroll
+                    for (int t = 0; t < TU; ++t) {
+                        LoraStep<T>::run(uv[i][s][t], hv[s], acc[t]);
+                        if constexpr (!F32) LoraStep<T>::run(uv[i][s][t], hl[s], acc[t]);
+                    }
+                // (taken over by the adapter's own rows, not added as zeros: what another adapter holds may be no number)
+#pragma unroll
+                for (int t = 0; t < TU; ++t)
+                    if (id == cur) sum[i][t] = acc[t];
             }
-            // (taken over by the adapter's own rows, not added as zeros: what another adapter holds may be no number)
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int c = (u0 + i) * CU + 4 * TU * quarter;
+            if (!live || u0 + i >= u_end || c >= a.Cout) continue;
+            float f[VW], b[VW];
+            unpack<T>(bv[i], b);
 #pragma unroll
             for (int t = 0; t < TU; ++t)
-                if (id == cur) sum[t] = acc[t];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f[4 * t + e] = sum[i][t][e] + b[4 * t + e];
+            *(uint4*)((T*)a.y + row * a.y_ld + c) = pack<T>(f);
         }
-        const int c = u * CU + 4 * TU * quarter;
-        if (!live || c >= a.Cout) continue;
-        float f[VW];
-#pragma unroll
-        for (int t = 0; t < TU; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) f[4 * t + i] = sum[t][i];
-        if (a.base != nullptr) {
-            float b[VW];
-            unpack<T>(*(const uint4*)((const T*)a.base + row * a.base_ld + c), b);
-#pragma unroll
-            for (int i = 0; i < VW; ++i) f[i] += b[i];
-        }
-        *(uint4*)((T*)a.y + row * a.y_ld + c) = pack<T>(f);
     }
 }
 
 template <typename T>
-static int launch_lora(const LoraArgs& a, int rows, hipStream_t st)
+static int launch_lora(LoraArgs& a, int rows, hipStream_t st)
 {
     const int tiles = (rows + 15) / 16, units = (a.Cout * (int)sizeof(T) + 63) / 64;
-    // workgroups per 16 rows: two per compute unit where the rows alone are fewer, a stretch of channels per wave at least
-    int cut = (512 + tiles - 1) / tiles;
-    const int most = (units + LORA_WAVES - 1) / LORA_WAVES;
-    if (cut > most) cut = most;
+    // workgroups per 16 rows: one per compute unit where the rows alone are fewer (two take 8.6 instead of 6.8 us for 1011 rows of
+    // 640 -> 648 in single precision, half of one 7.8), a stretch of channels per wave at least
+    const int cut = std::max(std::min((256 + tiles - 1) / tiles, (units + LORA_WAVES - 1) / LORA_WAVES), 1);
+    a.span = (units + cut * LORA_WAVES - 1) / (cut * LORA_WAVES);
     const dim3 grid(tiles, cut);
     auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(64 * LORA_WAVES), 0, st, a); };
     const int rt = (a.rank + 15) / 16;
