@@ -55,9 +55,10 @@ template <typename C, int SEL> __device__ __forceinline__ uint32_t cache4_pair(u
 }
 
 // Eight values (four bytes) as a 16-byte vector of the compute type.
-template <typename C> __device__ __forceinline__ uint4 cache4_eight(uint32_t w, float scale)
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <typename C> __device__ __forceinline__ u32x4 cache4_eight(uint32_t w, float scale)
 {
-    return make_uint4(cache4_pair<C, 0>(w, scale), cache4_pair<C, 1>(w, scale), cache4_pair<C, 2>(w, scale), cache4_pair<C, 3>(w, scale));
+    return u32x4{cache4_pair<C, 0>(w, scale), cache4_pair<C, 1>(w, scale), cache4_pair<C, 2>(w, scale), cache4_pair<C, 3>(w, scale)};
 }
 
 }  // namespace sige

@@ -6,14 +6,18 @@
 // registers of lanes l and l + 32, and the probabilities feed O^T += V^T P^T straight from there, because the order of the contraction
 // is free as long as V^T is read in the same one.
 //
-// A cached value is exact in bf16 (fp16 queries: in fp16), so a chunk is expanded once per workgroup, on its way from registers
-// to LDS: sixteen conversions per 32 channels, the scale folded in by the instruction, against the 32 x 32 logits that every wave
-// makes of them.  What differs by type is the other operand: bf16 and fp16 queries enter as they are; a single-precision
+// A cached value is exact in bf16 (fp16 queries: in fp16): sixteen conversions per 32 channels, the scale folded in by the
+// instruction.  What differs by type is the other operand: bf16 and fp16 queries enter as they are; a single-precision
 // query, and the probabilities beside it, as the sum of three bf16 numbers (24 bits), so that single precision runs on the bf16 matrix
 // instructions at a third of their rate (the fp32 ones have a sixteenth) with exact products.
 // A probability is rounded to the compute type once (bf16: 2^-9 of each at most, without bias; the values behind it were
-// rounded to 2 bits of significand); the denominator adds what was multiplied (a column of ones beside V) where the
-// head size leaves a column free, the unrounded values otherwise.
+// rounded to 2 bits of significand), and the denominator adds what was multiplied: through a column of ones beside V where the
+// head size leaves one free, else as dot products of the rounded pairs with ones (single precision: the values themselves).
+//
+// Two forms.  cache4_apart_kernel: every wave by itself, the waves of a workgroup share the keys out among them; no barrier until
+// they meet.  cache4_common_kernel: four waves on 128 queries that expand every chunk once for all.  The vector instructions bound
+// the first (per 64 keys x 32 queries x 64: about 90 for the expansion, 110 for the softmax), LDS and the order of the
+// two kinds of instructions the second.
 #pragma once
 
 #include "cache4.h"
@@ -25,8 +29,7 @@
 namespace sige {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 struct Cache4AttnArgs {
     const void* q;
@@ -112,35 +115,225 @@ __device__ __forceinline__ int wave_min(int v)
     return v;
 }
 
-#ifndef KTH
-#define KTH 3
-#define KTF 2
-#endif
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+__device__ __forceinline__ s16x4 read_transposed(char* lds)
+{
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(__attribute__((address_space(3))) char*)lds);
+}
+
+// What the 32 rows of a wave see (one row per lane pair).  A row that sees nothing is left out of the bounds and written as zeros.
+struct Cache4Seen {
+    int begin, end;                // this lane's row
+    bool none;
+    int lo, hi;                    // the wave: the first token that some row sees, the end of the last one
+    int lo_most, hi_least;         // the tokens between are seen by all rows
+    __device__ __forceinline__ bool partial(int t0, int n) const { return t0 < lo_most || (long)t0 + n > hi_least; }
+};
+__device__ __forceinline__ Cache4Seen cache4_seen(const Cache4AttnArgs& a, int qi)
+{
+    Cache4Seen s = {0, a.T, a.T == 0, 0, a.T, 0, a.T};
+    if (a.ranges != nullptr) {
+        if (qi < a.Nq) cache4_range(a.ranges, a.T, qi, s.begin, s.end);
+        s.none = qi >= a.Nq || s.begin >= s.end;
+        s.lo = __builtin_amdgcn_readfirstlane(wave_min(s.none ? a.T : s.begin));
+        s.hi = __builtin_amdgcn_readfirstlane(-wave_min(s.none ? 0 : -s.end));
+        s.lo_most = __builtin_amdgcn_readfirstlane(-wave_min(s.none ? 0 : -s.begin));
+        s.hi_least = __builtin_amdgcn_readfirstlane(wave_min(s.none ? a.T : s.end));
+    }
+    return s;
+}
+
+// Q fragments (B operand of S^T = K Q^T) of row qi: step s holds 8 channels per lane.  HALVES: the lower lanes have the first 16
+// channels of a group of 32 and the upper ones the others (a group takes two steps); else a step is 16 channels in their order.
+template <typename T, int DT, bool ODD, bool HALVES, int NP>
+__device__ __forceinline__ void cache4_queries(const Cache4AttnArgs& a, int qi, int head, int half, u32x4 (&qf)[NP][2 * DT - ODD])
+{
+    constexpr int DK = 2 * DT - ODD;
+    using C = typename Cache4Compute<T>::type;
+    const long qrow = cache4_query_row(a, min(qi, a.Nq - 1));
+    const char* const qp = (const char*)a.q + (qrow * a.q_ld + (long)head * a.d) * (long)sizeof(T);
+#pragma unroll
+    for (int s = 0; s < DK; ++s) {
+        const int dd = HALVES && !(ODD && s == DK - 1) ? 32 * (s >> 1) + 16 * half + 8 * (s & 1) : 16 * s + 8 * half;
+#pragma unroll
+        for (int p = 0; p < NP; ++p) qf[p][s] = u32x4{0u, 0u, 0u, 0u};
+        if (qi < a.Nq && dd < a.d) {
+            if constexpr (sizeof(T) == 4) {
+                float f[8];
+                unpack<float>(*(const uint4*)(qp + dd * 4), f);
+                unpack<float>(*(const uint4*)(qp + dd * 4 + 16), f + 4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t w[NP];
+                    split2<C, NP>(f[2 * j], f[2 * j + 1], w);
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) qf[p][s][j] = w[p];
+                }
+            } else {
+                qf[0][s] = *(const u32x4*)(qp + dd * 2);
+            }
+        }
+    }
+}
+
+// The sums of a wave's 32 rows.  Of a 32-key tile of logits a lane holds keys 8 * (r / 4) + 4 * half + r % 4 of its row.
+template <typename T, int DT, bool ODD, int KT> struct Cache4Sums {
+    using C = typename Cache4Compute<T>::type;
+    static constexpr int NP = Cache4Compute<T>::parts;
+    f32x16 o[DT];
+    float m, l;
+
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int nt = 0; nt < DT; ++nt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[nt][r] = 0.0f;
+        m = -INFINITY;
+        l = 0.0f;
+    }
+    // A chunk of which some row does not see everything: those logits are out.  marked: some value in it is no number (and counts 0 in
+    // the products); the rows that see it have NaN in the channels of its group.  vscales: the scale bytes of the chunk's first value
+    __device__ __forceinline__ void hide(const Cache4AttnArgs& a, const Cache4Seen& seen, int t0, int half, bool marked,
+                                         const uint8_t* vscales, f32x16 (&sacc)[KT])
+    {
+        unsigned lost = 0;
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int at = kt * 32 + 8 * (r >> 2) + 4 * half + (r & 3), t = t0 + at;
+                if (t < seen.begin || t >= seen.end) sacc[kt][r] = -INFINITY;
+                else if (marked)
+                    for (int g = 0; g < DT; ++g)
+                        if (vscales[(at << a.gs_log2) + g] > Cache4Compute<T>::last) lost |= 1u << g;
+            }
+        if (!marked) return;
+        lost |= (unsigned)__shfl_xor((int)lost, 32);
+#pragma unroll
+        for (int nt = 0; nt < DT; ++nt)
+            if (lost >> nt & 1u) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (!(ODD && nt == DT - 1 && r >= 8)) o[nt][r] = NAN;
+            }
+    }
+    // The running maximum, and the sums brought to it; returns what the exponents subtract.  Logits are compared raw: the scale
+    // (> 0) goes into the exponent.
+    __device__ __forceinline__ float settle(float scale_log2e, const f32x16 (&sacc)[KT])
+    {
+        float mr = sacc[0][0];
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) mr = fmaxf(mr, sacc[kt][r]);
+        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mr), __float_as_uint(mr), false, false);
+        const float mx = fmaxf(m, fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * scale_log2e);
+        const float m_at = mx == -INFINITY ? 0.0f : mx;            // (only tokens out of sight so far: nothing is subtracted)
+        if (__builtin_amdgcn_ballot_w64(mx != m) != 0ull) {        // some row's maximum moved
+            const float alpha = __builtin_amdgcn_exp2f(m - m_at);
+            m = mx;
+            l *= alpha;
+#pragma unroll
+            for (int nt = 0; nt < DT; ++nt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[nt][r] *= alpha;
+        }
+        // (fp16: probabilities times 2^15, numerator and denominator alike, so that those down to 2^-29 keep their 11 bits and
+        // only what is below 2^-40 is lost)
+        return m_at - (__is_same(C, f16) ? 15.0f : 0.0f);
+    }
+    // The probabilities, and O^T += V^T P^T in steps of 16 keys; v(kt, s, nt): the V^T fragment
+    template <typename V> __device__ __forceinline__ void add(float scale_log2e, float m_sub, f32x16 (&sacc)[KT], V v)
+    {
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                sacc[kt][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[kt][r], scale_log2e, -m_sub));
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                u32x4 pf[NP];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float p0 = sacc[kt][8 * s + 2 * j], p1 = sacc[kt][8 * s + 2 * j + 1];
+                    uint32_t w[NP];
+                    split2<C, NP>(p0, p1, w);
+#pragma unroll
+                    for (int p = 0; p < NP; ++p) pf[p][j] = w[p];
+                    if constexpr (!ODD) {
+                        typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+                        typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+                        if constexpr (NP > 1) l += p0 + p1;
+                        else if constexpr (__is_same(C, f16)) l = __builtin_amdgcn_fdot2(__builtin_bit_cast(h2, w[0]), __builtin_bit_cast(h2, 0x3c003c00u), l, false);
+                        else l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, w[0]), __builtin_bit_cast(b2, 0x3f803f80u), l, false);
+                    }
+                }
+                constexpr int TILES = DT > 6 ? 4 : DT;       // (fragments on their way: heads beyond 192 have no registers for all)
+#pragma unroll
+                for (int n0 = 0; n0 < DT; n0 += TILES) {
+                    u32x4 vf[TILES];
+#pragma unroll
+                    for (int nt = 0; nt < TILES; ++nt)
+                        if (n0 + nt < DT) vf[nt] = v(kt, s, n0 + nt);
+#pragma unroll
+                    for (int nt = 0; nt < TILES; ++nt)
+                        if (n0 + nt < DT) {
+#pragma unroll
+                            for (int p = NP - 1; p >= 0; --p) mma32<C>(vf[nt], pf[p], o[n0 + nt]);       // (the small parts first)
+                        }
+                    if (TILES < DT) __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+    }
+    // The denominator, in both lanes of a row
+    __device__ __forceinline__ float total(int l32) const
+    {
+        if constexpr (ODD) return __shfl(o[DT - 1][8], l32);       // row 16 of the last tile: register 8 of the lower half
+        else return l + __shfl_xor(l, 32);
+    }
+    // Four consecutive channels from dd on
+    __device__ __forceinline__ float4 four(int nt, int rq) const
+    {
+        return make_float4(o[nt][4 * rq], o[nt][4 * rq + 1], o[nt][4 * rq + 2], o[nt][4 * rq + 3]);
+    }
+};
+
+template <typename T> __device__ __forceinline__ void cache4_write(T* out, float4 v)
+{
+    if constexpr (sizeof(T) == 4) *(float4*)out = v;
+    else *(uint2*)out = make_uint2(round2<T>(v.x, v.y), round2<T>(v.z, v.w));
+}
+
+// ---- every wave by itself ----------------------------------------------------------------------------------------------------
+
 // 32-key tiles per chunk, by what their logits take in registers
-constexpr int cache4_tiles(int DT, int parts) { return DT <= (parts > 1 ? KTF : KTH) ? 2 : 1; }
-constexpr int cache4_v_bytes(int DT, int parts) { return 32 * cache4_tiles(DT, parts) * 64 * DT; }      // a chunk's V rows in LDS
+constexpr int cache4_apart_tiles(int DT, int parts) { return DT <= (parts > 1 ? 2 : 3) ? 2 : 1; }
+constexpr int cache4_apart_bytes(int DT, int parts) { return 32 * cache4_apart_tiles(DT, parts) * 64 * DT; }     // a chunk's V rows in LDS
+// waves of a workgroup: what their sums take in LDS when they meet
+constexpr int cache4_apart_waves(int DT, int parts) { return DT <= (parts > 1 ? 2 : 4) ? 8 : 4; }
 // The 64 bytes of group g of a V row: which of the row's groups of 64 bytes holds it.  Four neighbouring keys keep a group on
 // different banks, in the writes (a lane per key) and in the transposed reads (four keys per 16 lanes).
-template <int DT> __device__ __forceinline__ int cache4_v_group(int key, int g)
+template <int DT> __device__ __forceinline__ int cache4_apart_group(int key, int g)
 {
     return DT % 2 ? g : DT % 4 ? g ^ ((key >> 1) & 1) : g ^ (key & 3);
 }
 
-#ifndef WPS
-#define WPS(DT, NP) ((NP) > 1 ? 1 : (DT) <= 7 ? 2 : 1)
-#endif
 // DT = 32-wide tiles over d; ODD: the last one has 16 channels (d % 32 is 8 or 16), and its row 16 is the row of ones.
-// Every wave works by itself: 32 queries, K from memory straight into the first product's operands (8 bytes of a key and group per
-// lane: the order of the channels is the queries' too), V through the wave's own rows in LDS, which it is transposed out of.  NQ
-// waves of a workgroup take different queries, NK the same ones and every NK-th chunk of the tokens; these meet in LDS at the end.
-template <typename T, int DT, bool ODD, int NQ, int NK>
-__global__ __launch_bounds__(64 * NQ * NK, WPS(DT, Cache4Compute<T>::parts)) void cache4_attend_kernel(Cache4AttnArgs a)
+// The NK waves of a workgroup have the same 32 queries and take every NK-th chunk of the tokens.  K goes from memory straight into the
+// first product's operands (8 bytes of a key and group per lane: the order of the channels is the queries' too), V through the
+// wave's own rows in LDS, which it is transposed out of.  Two waves per SIMD, whose registers hold the next chunk beside everything:
+// with four of half the registers they spill (1 query of 65536 x 8 of 64 18.5 us against 15.5).
+template <typename T, int DT, bool ODD, int NK>
+__global__ __launch_bounds__(64 * NK, sizeof(T) == 4 || DT > 5 ? 1 : 2) void cache4_apart_kernel(Cache4AttnArgs a)
 {
-    static_assert(NQ == 1 || NK == 1, "queries or keys over the waves");
     using C = typename Cache4Compute<T>::type;
     constexpr int NP = Cache4Compute<T>::parts;
     constexpr unsigned LAST = Cache4Compute<T>::last;
-    constexpr int KT = cache4_tiles(DT, NP), KCH = 32 * KT;
+    constexpr int KT = cache4_apart_tiles(DT, NP), KCH = 32 * KT;
     constexpr int VROW = 64 * DT;
     constexpr int DK = 2 * DT - ODD;               // 16-wide steps over d for S^T
     constexpr int VU = KT == 2 ? DT : (DT + 1) / 2;        // groups a lane expands per chunk: of one of 64 keys, or every other one of 32
@@ -149,32 +342,16 @@ __global__ __launch_bounds__(64 * NQ * NK, WPS(DT, Cache4Compute<T>::parts)) voi
     extern __shared__ uint4 lds4[];
     char* const lds = reinterpret_cast<char*>(lds4);
     const int d = a.d;
-    const int tid = threadIdx.x, lane = tid & 63;
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wq = NQ > 1 ? wave : 0, wk = NQ > 1 ? 0 : wave;
-    const int half = lane >> 5, l32 = lane & 31;
     int qt, head;                                  // (the heads side by side: with eight of them each XCD keeps one in its L2)
     divmod((int)blockIdx.x, a.d_heads, qt, head);
-    const int q0 = (qt * NQ + wq) * 32, qi = q0 + l32;
-    if (NQ > 1 && q0 >= a.Nq) return;
-    const bool q_ok = qi < a.Nq;
+    const int qi = qt * 32 + l32;
+    const Cache4Seen seen = cache4_seen(a, qi);
+    int c = max((int)blockIdx.z * a.chunks_per_split, seen.lo / KCH) + wave;
+    const int c_end = min(((int)blockIdx.z + 1) * a.chunks_per_split, (int)(((long)seen.hi + KCH - 1) / KCH));
 
-    // what the rows see: a row that sees nothing is left out of the bounds and written as zeros
-    int begin = 0, end = a.T;
-    int lo = 0, hi = a.T, lo_most = 0, hi_least = a.T;
-    bool none = a.T == 0;
-    if (a.ranges != nullptr) {
-        if (q_ok) cache4_range(a.ranges, a.T, qi, begin, end);
-        none = !q_ok || begin >= end;
-        lo = __builtin_amdgcn_readfirstlane(wave_min(none ? a.T : begin));
-        hi = __builtin_amdgcn_readfirstlane(-wave_min(none ? 0 : -end));
-        lo_most = __builtin_amdgcn_readfirstlane(-wave_min(none ? 0 : -begin));
-        hi_least = __builtin_amdgcn_readfirstlane(wave_min(none ? a.T : end));
-    }
-    int c = max((int)blockIdx.z * a.chunks_per_split, lo / KCH) + wk;
-    const int c_end = min(((int)blockIdx.z + 1) * a.chunks_per_split, (int)(((long)hi + KCH - 1) / KCH));
-
-    char* const vs = lds + wave * cache4_v_bytes(DT, NP);
+    char* const vs = lds + wave * cache4_apart_bytes(DT, NP);
     const uint8_t* const ksec = a.cache + 2L * head * a.section;
     const uint8_t* const vsec = ksec + a.section;
 
@@ -194,65 +371,39 @@ __global__ __launch_bounds__(64 * NQ * NK, WPS(DT, Cache4Compute<T>::parts)) voi
         const int last = (int)min((long)KCH, (long)a.T - t0) - 1;   // (tokens past the end: the last one again)
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
-            const int key = min(kt * 32 + l32, last);
+            const unsigned key = (unsigned)min(kt * 32 + l32, last);
 #pragma unroll
             for (int g = 0; g < DT; ++g) {
-                if (ODD && g == DT - 1) kc[kt][g] = u32x2{*(const uint32_t*)(ksec + a.full * a.cap * 16 + t0 * 8 + (key * 8 + half * 4)), 0u};
-                else kc[kt][g] = *(const u32x2*)(ksec + g * a.cap * 16 + t0 * 16 + (key * 16 + half * 8));
+                if (ODD && g == DT - 1) kc[kt][g] = u32x2{*(const uint32_t*)(ksec + (a.full * a.cap * 16 + t0 * 8) + (key * 8u + half * 4u)), 0u};
+                else kc[kt][g] = *(const u32x2*)(ksec + (g * a.cap * 16 + t0 * 16) + (key * 16u + half * 8u));
             }
-            scales(ksec + a.scales + t0 * GS + key * GS, ksc[kt]);
+            scales(ksec + (a.scales + t0 * GS) + key * (unsigned)GS, ksc[kt]);
         }
-        const int key = min(vkey, last);
+        const unsigned key = (unsigned)min(vkey, last);
 #pragma unroll
         for (int u = 0; u < VU; ++u) {
             const int g = KT == 2 ? u : 2 * u + half;
             if (KT == 1 && 2 * u + 1 >= DT && half) break;          // (an odd number of groups: the last one is the lower half's)
             if (ODD && (KT == 2 ? u == DT - 1 : 2 * u + 1 >= DT - 1 && g == DT - 1)) {
-                const u32x2 w = *(const u32x2*)(vsec + a.full * a.cap * 16 + t0 * 8 + key * 8);
+                const u32x2 w = *(const u32x2*)(vsec + (a.full * a.cap * 16 + t0 * 8) + key * 8u);
                 vc[u] = u32x4{w.x, w.y, 0u, 0u};
             } else {
-                vc[u] = *(const u32x4*)(vsec + g * a.cap * 16 + t0 * 16 + key * 16);
+                vc[u] = *(const u32x4*)(vsec + (g * a.cap * 16 + t0 * 16) + key * 16u);
             }
         }
-        scales(vsec + a.scales + t0 * GS + key * GS, vsc);
+        scales(vsec + (a.scales + t0 * GS) + key * (unsigned)GS, vsc);
     };
-    // a group's scale; one that is no number is the power of two that the conversion makes NaN of
-    auto scale_of = [&](uint32_t word, int shift) {
+    // a group's scale; one that is no number is the power of two that the conversion makes NaN of (or 0, see below)
+    auto scale_of = [&](uint32_t word, int shift, unsigned bad) {
         const unsigned byte = (word >> shift) & 255u;
-        return cache4_scale(byte > LAST ? 255u : byte);
+        return __uint_as_float(byte > LAST ? bad : byte << 23);
     };
     if (c < c_end) fetch(c);
-
-    // Q fragments (B operand of S^T = K Q^T): the channels that the lane's half of a group of K holds
     u32x4 qf[NP][DK];
-    {
-        const long qrow = cache4_query_row(a, min(qi, a.Nq - 1));
-        const char* const qp = (const char*)a.q + (qrow * a.q_ld + (long)head * d) * (long)sizeof(T);
-#pragma unroll
-        for (int s = 0; s < DK; ++s) {
-            const int dd = ODD && s == DK - 1 ? 16 * s + 8 * half : 32 * (s >> 1) + 16 * half + 8 * (s & 1);
-#pragma unroll
-            for (int p = 0; p < NP; ++p) qf[p][s] = u32x4{0u, 0u, 0u, 0u};
-            if (q_ok && dd < d) {
-                if constexpr (sizeof(T) == 4) {
-                    float f[8];
-                    unpack<float>(*(const uint4*)(qp + dd * 4), f);
-                    unpack<float>(*(const uint4*)(qp + dd * 4 + 16), f + 4);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint32_t w[NP];
-                        split2<C, NP>(f[2 * j], f[2 * j + 1], w);
-#pragma unroll
-                        for (int p = 0; p < NP; ++p) qf[p][s][j] = w[p];
-                    }
-                } else {
-                    qf[0][s] = *(const u32x4*)(qp + dd * 2);
-                }
-            }
-        }
-    }
+    cache4_queries<T, DT, ODD, true>(a, qi, head, half, qf);
+
     // V rows: the 16-byte vectors of a group lie in the order of their number ^ ((key >> 2) & 3), for the banks of the writes
-    auto v_at = [&](int key, int g, int j) { return key * VROW + cache4_v_group<DT>(key, g) * 64 + ((j ^ ((key >> 2) & 3)) * 16); };
+    auto v_at = [&](int key, int g, int j) { return key * VROW + cache4_apart_group<DT>(key, g) * 64 + ((j ^ ((key >> 2) & 3)) * 16); };
     if constexpr (ODD) {                           // the columns that no group fills (row 16 of the last tile: ones)
         constexpr uint32_t ONE = __is_same(C, f16) ? 0x3c00u : 0x3f80u;
         for (int j = lane; j < KCH * 2; j += 64) *(u32x4*)(vs + v_at(j >> 1, DT - 1, 2 + (j & 1))) = u32x4{j & 1 ? 0u : ONE, 0u, 0u, 0u};
@@ -260,49 +411,42 @@ __global__ __launch_bounds__(64 * NQ * NK, WPS(DT, Cache4Compute<T>::parts)) voi
     // where this lane's share of a transposed read starts: four lanes take the 16 columns of one key, four keys per 16 lanes,
     // lane i of the 16 receives column i of the four keys.  (The keys of one lane differ by multiples of 8: one more turn of 2
     // in the order of the vectors for every 8.)
-    typedef short s16x4 __attribute__((ext_vector_type(4)));
-    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
     const int rkey = 4 * half + ((lane & 15) >> 2), rvec = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
     int r_lo[DT % 2 ? 1 : DT];                     // by tile (an odd number of them: the tiles follow each other)
 #pragma unroll
     for (int nt = 0; nt < (DT % 2 ? 1 : DT); ++nt) r_lo[nt] = v_at(rkey, nt, rvec) + (lane & 1) * 8;
     const int r_up = ((rvec ^ half ^ 2) - (rvec ^ half)) * 16;      // what the vector's place differs by 8 keys on
+    auto v_fragment = [&](int kt, int s, int nt) {
+        char* const at = vs + (kt * 32 + 16 * s) * VROW + (DT % 2 ? r_lo[0] + nt * 64 : r_lo[nt]);
+        union { s16x4 h[2]; u32x4 u; } vf;
+        vf.h[0] = read_transposed(at);
+        vf.h[1] = read_transposed(at + 8 * VROW + r_up);
+        return vf.u;
+    };
 
-    f32x16 oacc[DT];
-#pragma unroll
-    for (int nt = 0; nt < DT; ++nt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) oacc[nt][r] = 0.0f;
-    float m_run = -INFINITY, l_run = 0.0f;
-
+    Cache4Sums<T, DT, ODD, KT> sums;
+    sums.clear();
     for (; c < c_end; c += NK) {
         const int t0 = c * KCH;
-        // a chunk of which some row does not see everything
-        const bool partial = t0 < lo_most || (long)t0 + KCH > hi_least;
-        bool lost_v = false;                       // some token's value in it is no number
+        // In a chunk of which some row does not see everything a value that is no number counts 0 - a probability of 0 times NaN
+        // is NaN -, and the rows that see it are marked below.
+        const bool partial = seen.partial(t0, KCH);
+        const unsigned bad_v = partial ? 0u : 0x7f800000u;
+        bool marked = false;
         if (partial) {
 #pragma unroll
-            for (int g = 0; g < DT; ++g) lost_v |= ((vsc[g >> 2] >> (8 * (g & 3))) & 255u) > LAST;
-            lost_v = __builtin_amdgcn_ballot_w64(lost_v) != 0ull;
+            for (int g = 0; g < DT; ++g) marked |= ((vsc[g >> 2] >> (8 * (g & 3))) & 255u) > LAST;
+            marked = __builtin_amdgcn_ballot_w64(marked) != 0ull;
         }
         // V rows (LDS operations of a wave stay in order: the last chunk's reads are behind it)
 #pragma unroll
         for (int u = 0; u < VU; ++u) {
             const int g = KT == 2 ? u : 2 * u + half;
-            const float scale = scale_of(vsc[(KT == 2 ? u : 2 * u) >> 2], KT == 2 ? 8 * (u & 3) : 16 * (u & 1) + 8 * half);
+            const float scale = scale_of(vsc[(KT == 2 ? u : 2 * u) >> 2], KT == 2 ? 8 * (u & 3) : 16 * (u & 1) + 8 * half, bad_v);
             const bool tail = ODD && (KT == 2 ? u == DT - 1 : 2 * u + 1 >= DT - 1 && g == DT - 1);
             u32x4 x[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint4 e = cache4_eight<C>(vc[u][j], scale);
-                x[j] = u32x4{e.x, e.y, e.z, e.w};
-            }
-            // (a value that is no number is left out of a chunk that some row sees only a part of - 0 * NaN is NaN -, and the rows
-            // that see it are marked below)
-            if (lost_v && __float_as_uint(scale) == 0x7f800000u) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[j] = u32x4{0u, 0u, 0u, 0u};
-            }
+            for (int j = 0; j < 4; ++j) x[j] = cache4_eight<C>(vc[u][j], scale);
             if (KT == 1 && 2 * u + 1 >= DT && half) continue;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -319,174 +463,261 @@ __global__ __launch_bounds__(64 * NQ * NK, WPS(DT, Cache4Compute<T>::parts)) voi
 #pragma unroll
             for (int kt = 0; kt < KT; ++kt) {
                 const int g = s >> 1;
-                const uint4 e = cache4_eight<C>(kc[kt][g][s & 1], scale_of(ksc[kt][g >> 2], 8 * (g & 3)));
+                const u32x4 kf = cache4_eight<C>(kc[kt][g][s & 1], scale_of(ksc[kt][g >> 2], 8 * (g & 3), 0x7f800000u));
 #pragma unroll
-                for (int p = NP - 1; p >= 0; --p) mma32<C>(u32x4{e.x, e.y, e.z, e.w}, qf[p][s], sacc[kt]);      // (the small parts first)
+                for (int p = NP - 1; p >= 0; --p) mma32<C>(kf, qf[p][s], sacc[kt]);      // (the small parts first)
             }
         if (c + NK < c_end) fetch(c + NK);         // in flight during the softmax and the second product
-        // of tile kt this lane holds keys 8 * (r / 4) + 4 * half + r % 4 of its query
-        if (partial) {
-            unsigned lost = 0;
-#pragma unroll
-            for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int t = t0 + kt * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
-                    if (t < begin || t >= end) sacc[kt][r] = -INFINITY;
-                    else if (lost_v)
-                        for (int g = 0; g < DT; ++g)
-                            if (vsec[a.scales + (long)t * GS + g] > LAST) lost |= 1u << g;
-                }
-            if (lost_v) {
-                lost |= (unsigned)__shfl_xor((int)lost, 32);
-#pragma unroll
-                for (int nt = 0; nt < DT; ++nt)
-                    if (lost >> nt & 1u) {
-#pragma unroll
-                        for (int r = 0; r < 16; ++r)
-                            if (!(ODD && nt == DT - 1 && r >= 8)) oacc[nt][r] = NAN;
-                    }
-            }
-        }
-        float mr = sacc[0][0];                     // raw logits: the scale (>= 0) goes into the exponent
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) mr = fmaxf(mr, sacc[kt][r]);
-        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(mr), __float_as_uint(mr), false, false);
-        const float mx = fmaxf(m_run, fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * a.scale_log2e);
-        const float m_at = mx == -INFINITY ? 0.0f : mx;             // (only tokens out of sight so far: nothing is subtracted)
-        if (__builtin_amdgcn_ballot_w64(mx != m_run) != 0ull) {     // some query's maximum moved
-            const float alpha = __builtin_amdgcn_exp2f(m_run - m_at);
-            m_run = mx;
-            l_run *= alpha;
-#pragma unroll
-            for (int nt = 0; nt < DT; ++nt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) oacc[nt][r] *= alpha;
-        }
-        // (fp16: probabilities times 2^15, numerator and denominator alike, so that those down to 2^-29 keep their 11 bits and
-        // only what is below 2^-40 is lost)
-        const float m_sub = m_at - (__is_same(C, f16) ? 15.0f : 0.0f);
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                sacc[kt][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[kt][r], a.scale_log2e, -m_sub));
-        // O^T += V^T P^T, two steps of 16 keys per tile; step s uses registers 8s..8s+7
-        float lsum = 0.0f;
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                u32x4 pf[NP];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float p0 = sacc[kt][8 * s + 2 * j], p1 = sacc[kt][8 * s + 2 * j + 1];
-                    uint32_t w[NP];
-                    split2<C, NP>(p0, p1, w);
-#pragma unroll
-                    for (int p = 0; p < NP; ++p) pf[p][j] = w[p];
-                    if constexpr (!ODD) lsum += p0 + p1;
-                }
-#pragma unroll
-                for (int nt = 0; nt < DT; ++nt) {
-                    char* const at = vs + (kt * 32 + 16 * s) * VROW + (DT % 2 ? r_lo[0] + nt * 64 : r_lo[nt]);
-                    union { s16x4 h[2]; u32x4 u; } vf;
-                    vf.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(__attribute__((address_space(3))) char*)at);
-                    vf.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(__attribute__((address_space(3))) char*)(at + 8 * VROW + r_up));
-#pragma unroll
-                    for (int p = NP - 1; p >= 0; --p) mma32<C>(vf.u, pf[p], oacc[nt]);
-                }
-            }
-        l_run += lsum;
+        if (partial) sums.hide(a, seen, t0, half, marked, vsec + a.scales + (long)t0 * GS, sacc);
+        const float m_sub = sums.settle(a.scale_log2e, sacc);
+        sums.add(a.scale_log2e, m_sub, sacc, v_fragment);
     }
 
-    float l_tot;
-    if constexpr (ODD) l_tot = __shfl(oacc[DT - 1][8], l32);        // row 16 of the last tile: register 8 of the lower half
-    else l_tot = l_run + __shfl_xor(l_run, 32);
-    if (none) { m_run = -INFINITY; l_tot = 0.0f; }                  // (what such a row added up is not read)
-    if constexpr (NQ > 1) {
-        if (!q_ok) return;
-        const float inv = 1.0f / l_tot;
-        float* const w = a.ws + (((long)blockIdx.z * a.heads + head) * a.Nq + qi) * (d + 4);
-        if (a.splits > 1 && half == 0) *(float2*)(w + d) = make_float2(m_run, l_tot);
+    // the waves' shares of the tokens, brought to a common maximum and added in wave order
+    float l_tot = sums.total(l32);
+    if (seen.none) { sums.m = -INFINITY; l_tot = 0.0f; }            // (what such a row added up is not read)
+    float* const comb = reinterpret_cast<float*>(lds);              // [NK][32 queries][d sums, maximum, denominator, 2 unused]
+    const int cs = d + 4;
+    __syncthreads();                                                // (chunks no longer needed)
+    {
+        float* const mine = comb + (wave * 32 + l32) * cs;
+        if (half == 0) *(float2*)(mine + d) = make_float2(sums.m, l_tot);
 #pragma unroll
         for (int nt = 0; nt < DT; ++nt)
 #pragma unroll
             for (int rq = 0; rq < 4; ++rq) {
                 const int dd = nt * 32 + 8 * rq + 4 * half;
-                if (dd >= d) continue;
-                float v[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = none ? 0.0f : oacc[nt][4 * rq + e];
-                if (a.splits == 1) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = none ? 0.0f : v[e] * inv;
-                    T* const out = (T*)a.o + (long)qi * a.o_ld + head * d + dd;
-                    if constexpr (sizeof(T) == 4) *(float4*)out = make_float4(v[0], v[1], v[2], v[3]);
-                    else *(uint2*)out = make_uint2(round2<T>(v[0], v[1]), round2<T>(v[2], v[3]));
-                } else {
-                    *(float4*)(w + dd) = make_float4(v[0], v[1], v[2], v[3]);
-                }
+                if (dd < d) *(float4*)(mine + dd) = sums.four(nt, rq);
             }
-    } else {
-        // the waves' shares of the keys, brought to a common maximum and added in wave order
-        float* const comb = reinterpret_cast<float*>(lds);          // [NK][32 queries][d sums, maximum, denominator, 2 unused]
-        const int cs = d + 4;
-        __syncthreads();                                            // (chunks no longer needed)
-        {
-            float* const mine = comb + (wk * 32 + l32) * cs;
-            if (half == 0) *(float2*)(mine + d) = make_float2(m_run, l_tot);
+    }
+    __syncthreads();
+    const int dq = d >> 2;
+    for (int e = tid; e < 32 * dq; e += 64 * NK) {
+        int q, g;
+        divmod(e, a.d_dq, q, g);
+        const int qq = qt * 32 + q;
+        if (qq >= a.Nq) break;
+        const float* const src = comb + q * cs;
+        float m = -INFINITY, den = 0.0f;
+        float4 num = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-            for (int nt = 0; nt < DT; ++nt)
+        for (int w = 0; w < NK; ++w) m = fmaxf(m, src[w * 32 * cs + d]);
 #pragma unroll
-                for (int rq = 0; rq < 4; ++rq) {
-                    const int dd = nt * 32 + 8 * rq + 4 * half;
-                    if (dd < d)
-                        *(float4*)(mine + dd) = none ? make_float4(0.0f, 0.0f, 0.0f, 0.0f)
-                                                     : make_float4(oacc[nt][4 * rq], oacc[nt][4 * rq + 1], oacc[nt][4 * rq + 2], oacc[nt][4 * rq + 3]);
-                }
+        for (int w = 0; w < NK; ++w) {
+            const float2 ml = *(const float2*)(src + w * 32 * cs + d);
+            const float4 v = *(const float4*)(src + w * 32 * cs + 4 * g);
+            // (a wave without keys carries -inf, 0 and zeros; one whose values hold a NaN keeps it whatever its weight)
+            const float f = ml.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - m);
+            den += ml.y * f;
+            num.x += v.x * f; num.y += v.y * f; num.z += v.z * f; num.w += v.w * f;
         }
-        __syncthreads();
-        const int dq = d >> 2;
-        for (int e = tid; e < 32 * dq; e += 64 * NK) {
-            int q, g;
-            divmod(e, a.d_dq, q, g);
-            const int qq = qt * 32 + q;
-            if (qq >= a.Nq) break;
-            const float* const src = comb + q * cs;
-            float m = -INFINITY, den = 0.0f, num[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int w = 0; w < NK; ++w) m = fmaxf(m, src[w * 32 * cs + d]);
-#pragma unroll
-            for (int w = 0; w < NK; ++w) {
-                const float mw = src[w * 32 * cs + d], lw = src[w * 32 * cs + d + 1];
-                const float4 v = *(const float4*)(src + w * 32 * cs + 4 * g);
-                // (a wave without keys carries -inf, 0 and zeros; one whose values hold a NaN keeps it whatever its weight)
-                const float f = mw == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(mw - m);
-                den += lw * f;
-                num[0] += v.x * f; num[1] += v.y * f; num[2] += v.z * f; num[3] += v.w * f;
-            }
-            if (a.splits == 1) {
-                int b, en;
-                cache4_range(a.ranges, a.T, qq, b, en);
-                const float inv = 1.0f / den;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) num[i] = b >= en ? 0.0f : num[i] * inv;
-                T* const out = (T*)a.o + (long)qq * a.o_ld + head * d + 4 * g;
-                if constexpr (sizeof(T) == 4) *(float4*)out = make_float4(num[0], num[1], num[2], num[3]);
-                else *(uint2*)out = make_uint2(round2<T>(num[0], num[1]), round2<T>(num[2], num[3]));
-            } else {
-                float* const w = a.ws + (((long)blockIdx.z * a.heads + head) * a.Nq + qq) * (d + 4);
-                *(float4*)(w + 4 * g) = make_float4(num[0], num[1], num[2], num[3]);
-                if (g == 0) *(float2*)(w + d) = make_float2(m, den);
-            }
+        int b, en;
+        cache4_range(a.ranges, a.T, qq, b, en);
+        if (b >= en) num = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (a.splits == 1) {
+            const float inv = b >= en ? 0.0f : 1.0f / den;
+            cache4_write((T*)a.o + (long)qq * a.o_ld + head * d + 4 * g, make_float4(num.x * inv, num.y * inv, num.z * inv, num.w * inv));
+        } else {
+            float* const w = a.ws + (((long)blockIdx.z * a.heads + head) * a.Nq + qq) * (d + 4);
+            *(float4*)(w + 4 * g) = num;
+            if (g == 0) *(float2*)(w + d) = make_float2(m, den);
         }
     }
 }
 
-// The splits' partial results, added in their order: four consecutive channels of a (query, head) per P neighbouring lanes.
+// ---- four waves on the same chunks (half types) ------------------------------------------------------------------------------
+
+constexpr int CACHE4_COMMON_WAVES = 4;
+constexpr int cache4_common_tiles(int DT) { return DT <= 4 ? 2 : 1; }                    // 32-key tiles per chunk
+// bytes between V rows in LDS: an odd multiple of 64, so that the keys of a transposed read fall on different banks; between K rows:
+// 16 bytes more than the channels
+constexpr int cache4_common_v_row(int DT) { return 64 * (DT | 1); }
+constexpr int cache4_common_k_row(int DT, bool ODD) { return 32 * (2 * DT - ODD) + 16; }
+constexpr int cache4_common_bytes(int DT, bool ODD) { return 32 * cache4_common_tiles(DT) * (cache4_common_v_row(DT) + cache4_common_k_row(DT, ODD)); }
+
+// The waves have 32 queries each and expand every chunk once for all, K and V rows of the compute type in LDS: the next chunk into one
+// buffer while the other is multiplied, one barrier per chunk.  The registers are bounded for two waves per SIMD: told so, the
+// compiler keeps heads up to 128 in half of what it takes otherwise (4096 queries of 16384 x 8 of 128 580 -> 367 us, 2048 of 4096 x 160
+// 146 -> 85).  Heads of 225 to 256 leave a few registers in memory then, and gain all the same (1024 of 4096 x 256 125 -> 77 us).
+template <typename T, int DT, bool ODD>
+__global__ __launch_bounds__(64 * CACHE4_COMMON_WAVES, DT <= 3 ? 3 : 2) void cache4_common_kernel(Cache4AttnArgs a)
+{
+    using C = typename Cache4Compute<T>::type;
+    constexpr int NW = CACHE4_COMMON_WAVES;
+    constexpr unsigned LAST = Cache4Compute<T>::last;
+    constexpr int KT = cache4_common_tiles(DT), KCH = 32 * KT;
+    constexpr int VROW = cache4_common_v_row(DT), KROW = cache4_common_k_row(DT, ODD), CHUNK = cache4_common_bytes(DT, ODD);
+    constexpr int DK = 2 * DT - ODD;               // 16-wide steps over d for S^T
+    constexpr int UNITS = KT == 2 ? 2 * DT : DT;   // what a wave expands at a time: 64 groups of 32 channels
+    constexpr int NU = (UNITS + NW - 1) / NW;
+    extern __shared__ uint4 lds4[];
+    __shared__ int marked_chunk[2];                // the chunk (+ 1) that left a value that is no number out of a buffer
+    __shared__ int ends[NW][4];
+    char* const lds = reinterpret_cast<char*>(lds4);
+    const int d = a.d;
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, l32 = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int qt, head;                                  // (the heads side by side: with eight of them each XCD keeps one in its L2)
+    divmod((int)blockIdx.x, a.d_heads, qt, head);
+    const int qi = (qt * NW + wave) * 32 + l32;
+    const bool q_ok = qi < a.Nq;
+    Cache4Seen seen = cache4_seen(a, qi);
+    if (tid < 2) marked_chunk[tid] = 0;
+    if (a.ranges != nullptr) {                     // what the workgroup's rows see
+        if (lane == 0) { ends[wave][0] = seen.lo; ends[wave][1] = seen.hi; ends[wave][2] = seen.lo_most; ends[wave][3] = seen.hi_least; }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            seen.lo = min(seen.lo, ends[w][0]);
+            seen.hi = max(seen.hi, ends[w][1]);
+            seen.lo_most = max(seen.lo_most, ends[w][2]);
+            seen.hi_least = min(seen.hi_least, ends[w][3]);
+        }
+        seen.lo = __builtin_amdgcn_readfirstlane(seen.lo);
+        seen.hi = __builtin_amdgcn_readfirstlane(seen.hi);
+        seen.lo_most = __builtin_amdgcn_readfirstlane(seen.lo_most);
+        seen.hi_least = __builtin_amdgcn_readfirstlane(seen.hi_least);
+    } else {
+        __syncthreads();
+    }
+    int c = max((int)blockIdx.z * a.chunks_per_split, seen.lo / KCH);
+    const int c_end = min(((int)blockIdx.z + 1) * a.chunks_per_split, (int)(((long)seen.hi + KCH - 1) / KCH));
+    const uint8_t* const sec = a.cache + 2L * head * a.section;
+
+    // a unit's 64 groups: of 64 keys (K's units, then V's), or of the keys and the values of 32
+    u32x4 code[NU];
+    unsigned sbyte[NU];
+    auto fetch = [&](int c) {
+        const long t0 = (long)c * KCH;
+        const int last = (int)min((long)KCH, (long)a.T - t0) - 1;   // (tokens past the end: the last one again)
+        const unsigned key = (unsigned)min(KT == 2 ? lane : l32, last);
+#pragma unroll
+        for (int i = 0; i < NU; ++i) {
+            const int u = wave + NW * i;
+            if (UNITS % NW != 0 && u >= UNITS) break;
+            const int g = KT == 2 && u >= DT ? u - DT : u;
+            const uint8_t* const base = sec + ((KT == 2 ? u >= DT : half) ? a.section : 0);
+            if (ODD && g == DT - 1) {
+                const u32x2 w = *(const u32x2*)(base + (a.full * a.cap * 16 + t0 * 8) + key * 8u);
+                code[i] = u32x4{w.x, w.y, 0u, 0u};
+            } else {
+                code[i] = *(const u32x4*)(base + (g * a.cap * 16 + t0 * 16) + key * 16u);
+            }
+            sbyte[i] = (base + (a.scales + (t0 << a.gs_log2)) + g)[key << a.gs_log2];
+        }
+    };
+    // the expanded units' rows in a buffer (K rows, then V rows)
+    auto stage = [&](int c, int buf) {
+        const bool partial = seen.partial(c * KCH, KCH);
+#pragma unroll
+        for (int i = 0; i < NU; ++i) {
+            const int u = wave + NW * i;
+            if (UNITS % NW != 0 && u >= UNITS) break;
+            const int g = KT == 2 && u >= DT ? u - DT : u;
+            const int which = KT == 2 ? u >= DT : half;
+            const int key = KT == 2 ? lane : l32;
+            const bool tail = ODD && g == DT - 1;
+            char* const dst = lds + buf * CHUNK + (which ? KCH * KROW + key * VROW : key * KROW) + g * 64;
+            // a group that is no number: NaN for all who see it; a value in a chunk of which some row does not see everything: 0 - a
+            // probability of 0 times NaN is NaN -, and the rows that see it are marked below
+            const bool bad = sbyte[i] > LAST;
+            const float scale = __uint_as_float(bad ? (which && partial ? 0u : 0x7f800000u) : sbyte[i] << 23);
+            if (partial && bad && which) marked_chunk[buf] = c + 1;
+            // V rows lie an odd multiple of 64 bytes apart, four lanes on the banks of one: every four lanes start with another of their
+            // group's four vectors (else the writes took 60 of the 110 cycles that LDS was busy per chunk, 4096 queries of 16384 x 128)
+            u32x4 w = code[i];
+            int turn = 0;
+            if (which && !tail) {
+                turn = (key >> 2) & 3;
+                if (turn & 1) w = u32x4{w.y, w.z, w.w, w.x};
+                if (turn & 2) w = u32x4{w.z, w.w, w.x, w.y};
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (!(tail && j >= 2)) *(u32x4*)(dst + 16 * ((j + turn) & 3)) = cache4_eight<C>(w[j], scale);
+        }
+    };
+    if (c < c_end) fetch(c);
+    u32x4 qf[1][DK];
+    cache4_queries<T, DT, ODD, false>(a, qi, head, half, qf);
+    if constexpr (ODD) {                           // the columns of the V rows that no group fills (row 16 of the last tile: ones)
+        constexpr uint32_t ONE = __is_same(C, f16) ? 0x3c00u : 0x3f80u;
+        for (int j = tid; j < 2 * KCH * 2; j += 64 * NW) {
+            const int buf = j / (KCH * 2), key = (j >> 1) % KCH;
+            *(u32x4*)(lds + buf * CHUNK + KCH * KROW + key * VROW + (DT - 1) * 64 + 32 + (j & 1) * 16) = u32x4{j & 1 ? 0u : ONE, 0u, 0u, 0u};
+        }
+    }
+    // where this lane's share of a transposed read starts: four lanes take the 16 columns of one key, four keys per 16 lanes,
+    // lane i of the 16 receives column i of the four keys
+    const int tr = KCH * KROW + (4 * half + ((lane & 15) >> 2)) * VROW + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+
+    Cache4Sums<T, DT, ODD, KT> sums;
+    sums.clear();
+    if (c < c_end) {
+        stage(c, 0);
+        if (c + 1 < c_end) fetch(c + 1);
+    }
+    for (int buf = 0; c < c_end; ++c, buf ^= 1) {
+        __syncthreads();                           // this chunk's rows are there, the other buffer's have been read
+        if (c + 1 < c_end) {
+            stage(c + 1, buf ^ 1);
+            if (c + 2 < c_end) fetch(c + 2);
+        }
+        const int t0 = c * KCH;
+        char* const rows = lds + buf * CHUNK;
+        f32x16 sacc[KT];
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sacc[kt][r] = 0.0f;
+            constexpr int AT_ONCE = DK > 14 ? 8 : DK;       // (K fragments on their way: heads of 256 have no registers for all)
+#pragma unroll
+            for (int s0 = 0; s0 < DK; s0 += AT_ONCE) {
+                u32x4 kf[AT_ONCE];
+#pragma unroll
+                for (int s = 0; s < AT_ONCE; ++s)
+                    if (s0 + s < DK) kf[s] = *(const u32x4*)(rows + (kt * 32 + l32) * KROW + (16 * (s0 + s) + 8 * half) * 2);
+#pragma unroll
+                for (int s = 0; s < AT_ONCE; ++s)
+                    if (s0 + s < DK) mma32<C>(kf[s], qf[0][s0 + s], sacc[kt]);
+                if (AT_ONCE < DK) __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        if (seen.partial(t0, KCH))
+            sums.hide(a, seen, t0, half, __builtin_amdgcn_readfirstlane(marked_chunk[buf]) == c + 1,
+                      sec + a.section + a.scales + ((long)t0 << a.gs_log2), sacc);
+        const float m_sub = sums.settle(a.scale_log2e, sacc);
+        sums.add(a.scale_log2e, m_sub, sacc, [&](int kt, int s, int nt) {
+            char* const at = rows + tr + (kt * 32 + 16 * s) * VROW + nt * 64;
+            union { s16x4 h[2]; u32x4 u; } vf;
+            vf.h[0] = read_transposed(at);
+            vf.h[1] = read_transposed(at + 8 * VROW);
+            return vf.u;
+        });
+    }
+
+    float l_tot = sums.total(l32);
+    if (!q_ok) return;
+    if (seen.none) { sums.m = -INFINITY; l_tot = 0.0f; }
+    const float inv = seen.none ? 0.0f : 1.0f / l_tot;
+    float* const w = a.ws + (((long)blockIdx.z * a.heads + head) * a.Nq + qi) * (d + 4);
+    if (a.splits > 1 && half == 0) *(float2*)(w + d) = make_float2(sums.m, l_tot);
+#pragma unroll
+    for (int nt = 0; nt < DT; ++nt)
+#pragma unroll
+        for (int rq = 0; rq < 4; ++rq) {
+            const int dd = nt * 32 + 8 * rq + 4 * half;
+            if (dd >= d) continue;
+            float4 v = sums.four(nt, rq);
+            if (seen.none) v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);          // (what such a row added up is not read)
+            if (a.splits == 1) cache4_write((T*)a.o + (long)qi * a.o_ld + head * d + dd, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+            else *(float4*)(w + dd) = v;
+        }
+}
+
+// ---- the splits' partial results ---------------------------------------------------------------------------------------------
+
+// Added in their order: four consecutive channels of a (query, head) per P neighbouring lanes.
 template <typename T, int P>
 __global__ __launch_bounds__(256) void cache4_merge_kernel(Cache4AttnArgs a)
 {
@@ -534,66 +765,67 @@ __global__ __launch_bounds__(256) void cache4_merge_kernel(Cache4AttnArgs a)
     const float inv = 1.0f / den;
 #pragma unroll
     for (int e = 0; e < 4; ++e) num[e] = b >= en ? 0.0f : num[e] * inv;
-    T* const out = (T*)a.o + (long)qi * a.o_ld + head * d + dd;
-    if constexpr (sizeof(T) == 4) *(float4*)out = make_float4(num[0], num[1], num[2], num[3]);
-    else *(uint2*)out = make_uint2(round2<T>(num[0], num[1]), round2<T>(num[2], num[3]));
+    cache4_write((T*)a.o + (long)qi * a.o_ld + head * d + dd, make_float4(num[0], num[1], num[2], num[3]));
 }
 
-// How a call is cut (cache4.hip) and its launch, one file per type.
-struct Cache4Form { int nq, nk, splits; };
-int cache4_few_waves(int d, sige_dtype dt);                 // NK of the form whose waves split the keys
+// How a call is cut (cache4_attn.hip), and its launch, one file per type.
+struct Cache4Form { bool common; int splits; };
 int launch_cache4_f32(const Cache4AttnArgs& a, const Cache4Form& f, hipStream_t st);
 int launch_cache4_f16(const Cache4AttnArgs& a, const Cache4Form& f, hipStream_t st);
 int launch_cache4_bf16(const Cache4AttnArgs& a, const Cache4Form& f, hipStream_t st);
 
-// waves that split the keys: what their chunks and their sums take in LDS, and what a query takes in registers
-template <typename T> constexpr int cache4_nk(int DT) { return DT <= (sizeof(T) == 4 ? 2 : 4) ? 8 : 4; }
-
-template <typename T, int DT, bool ODD, int NQ, int NK>
-static int launch_cache4_as(const Cache4AttnArgs& a, hipStream_t st)
+template <typename T, int DT, bool ODD>
+static int launch_cache4_as(const Cache4AttnArgs& a, const Cache4Form& f, hipStream_t st)
 {
-    const size_t rows = (size_t)NQ * NK * cache4_v_bytes(DT, Cache4Compute<T>::parts);
-    const size_t lds = NQ > 1 ? rows : std::max(rows, (size_t)NK * 32 * (a.d + 4) * sizeof(float));
-    const long tiles = (a.Nq + 32L * NQ - 1) / (32 * NQ) * a.heads;
-    SIGE_REQUIRE(tiles < (1L << 31), SIGE_ERR_UNSUPPORTED, "sige_cache4_attn: too many queries");
-    auto kern = cache4_attend_kernel<T, DT, ODD, NQ, NK>;
+    constexpr int NP = Cache4Compute<T>::parts, NK = cache4_apart_waves(DT, NP);
+    void (*kern)(Cache4AttnArgs) = cache4_apart_kernel<T, DT, ODD, NK>;
+    int rows = 32, threads = 64 * NK;
+    size_t lds = NK * std::max((size_t)cache4_apart_bytes(DT, NP), 32 * (a.d + 4) * sizeof(float));
+    if constexpr (sizeof(T) == 2)
+        if (f.common) {
+            kern = cache4_common_kernel<T, DT, ODD>;
+            rows = 32 * CACHE4_COMMON_WAVES;
+            threads = 64 * CACHE4_COMMON_WAVES;
+            lds = 2 * (size_t)cache4_common_bytes(DT, ODD);
+        }
+    const long tiles = ((long)a.Nq + rows - 1) / rows * a.heads, groups = (long)a.Nq * a.heads * (a.d / 4);
+    const int P = a.splits <= 4 ? 1 : a.splits <= 16 ? 4 : 16;             // (at most 64 splits)
+    SIGE_REQUIRE(tiles < (1L << 31) && groups < (1L << 33), SIGE_ERR_UNSUPPORTED, "sige_cache4_attn: too many queries");
     if (lds > 48 * 1024) {
         const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         SIGE_REQUIRE(e == hipSuccess, SIGE_ERR_HIP, "sige_cache4_attn: cannot reserve %zu bytes of LDS: %s", lds, hipGetErrorString(e));
     }
-    hipLaunchKernelGGL(kern, dim3((unsigned)tiles, 1, a.splits), dim3(64 * NQ * NK), lds, st, a);
+    hipLaunchKernelGGL(kern, dim3((unsigned)tiles, 1, a.splits), dim3(threads), lds, st, a);
     SIGE_LAUNCH_CHECK("sige_cache4_attn");
     if (a.splits == 1) return SIGE_OK;
-    const long groups = (long)a.Nq * a.heads * (a.d / 4);
-    auto merge = [&](auto m, int P) { hipLaunchKernelGGL(m, dim3((unsigned)((groups * P + 255) / 256)), dim3(256), 0, st, a); };
-    if (a.splits <= 4) merge(cache4_merge_kernel<T, 1>, 1);
-    else if (a.splits <= 16) merge(cache4_merge_kernel<T, 4>, 4);
-    else merge(cache4_merge_kernel<T, 16>, 16);             // at most 64 splits
+    auto merge = [&](auto m) { hipLaunchKernelGGL(m, dim3((unsigned)((groups * P + 255) / 256)), dim3(256), 0, st, a); };
+    if (P == 1) merge(cache4_merge_kernel<T, 1>);
+    else if (P == 4) merge(cache4_merge_kernel<T, 4>);
+    else merge(cache4_merge_kernel<T, 16>);
     SIGE_LAUNCH_CHECK("sige_cache4_attn(merge)");
     return SIGE_OK;
-}
-
-template <typename T, int DT>
-static int launch_cache4_dt(const Cache4AttnArgs& a, const Cache4Form& f, hipStream_t st)
-{
-    const bool odd = ((a.d + 15) / 16) & 1;
-    if (f.nq > 1) return odd ? launch_cache4_as<T, DT, true, 4, 1>(a, st) : launch_cache4_as<T, DT, false, 4, 1>(a, st);
-    constexpr int NK = cache4_nk<T>(DT);
-    return odd ? launch_cache4_as<T, DT, true, 1, NK>(a, st) : launch_cache4_as<T, DT, false, 1, NK>(a, st);
 }
 
 template <typename T>
 static int launch_cache4(const Cache4AttnArgs& a, const Cache4Form& f, hipStream_t st)
 {
-    switch ((a.d + 31) / 32) {
-    case 1: return launch_cache4_dt<T, 1>(a, f, st);
-    case 2: return launch_cache4_dt<T, 2>(a, f, st);
-    case 3: return launch_cache4_dt<T, 3>(a, f, st);
-    case 4: return launch_cache4_dt<T, 4>(a, f, st);
-    case 5: return launch_cache4_dt<T, 5>(a, f, st);
-    case 6: return launch_cache4_dt<T, 6>(a, f, st);
-    case 7: return launch_cache4_dt<T, 7>(a, f, st);
-    default: return launch_cache4_dt<T, 8>(a, f, st);
+    switch ((a.d + 15) / 16) {                     // 16-wide steps over a head
+    case 1: return launch_cache4_as<T, 1, true>(a, f, st);
+    case 2: return launch_cache4_as<T, 1, false>(a, f, st);
+    case 3: return launch_cache4_as<T, 2, true>(a, f, st);
+    case 4: return launch_cache4_as<T, 2, false>(a, f, st);
+    case 5: return launch_cache4_as<T, 3, true>(a, f, st);
+    case 6: return launch_cache4_as<T, 3, false>(a, f, st);
+    case 7: return launch_cache4_as<T, 4, true>(a, f, st);
+    case 8: return launch_cache4_as<T, 4, false>(a, f, st);
+    case 9: return launch_cache4_as<T, 5, true>(a, f, st);
+    case 10: return launch_cache4_as<T, 5, false>(a, f, st);
+    case 11: return launch_cache4_as<T, 6, true>(a, f, st);
+    case 12: return launch_cache4_as<T, 6, false>(a, f, st);
+    case 13: return launch_cache4_as<T, 7, true>(a, f, st);
+    case 14: return launch_cache4_as<T, 7, false>(a, f, st);
+    case 15: return launch_cache4_as<T, 8, true>(a, f, st);
+    default: return launch_cache4_as<T, 8, false>(a, f, st);
     }
 }
 

@@ -4,26 +4,26 @@
 
 namespace sige {
 
-int cache4_few_waves(int d, sige_dtype dt)
+// Tokens per chunk, and waves that share the chunks of a workgroup's queries out among them.
+static int cache4_chunk(int d, sige_dtype dt, bool common)
 {
     const int DT = (d + 31) / 32;
-    return dt == SIGE_F32 ? cache4_nk<float>(DT) : cache4_nk<f16>(DT);
+    return 32 * (common ? cache4_common_tiles(DT) : cache4_apart_tiles(DT, dt == SIGE_F32 ? Cache4Compute<float>::parts : 1));
 }
-
-static int cache4_chunk(int DT, sige_dtype dt) { return 32 * cache4_tiles(DT, dt == SIGE_F32 ? Cache4Compute<float>::parts : 1); }
 
 // room: floats of workspace, what the splits' partial sums have to fit into.
 static Cache4Form plan_cache4(int Nq, int T, int heads, int d, sige_dtype dt, size_t room = ~(size_t)0)
 {
     const int DT = (d + 31) / 32;
     const int target = knob(SIGE_KNOB_ATTN_WGS);
-    Cache4Form f = {1, cache4_few_waves(d, dt), 1};
-    if (Nq > 64) f = {4, 1, 1};
-    const int KCH = cache4_chunk(DT, dt);
+    Cache4Form f = {dt != SIGE_F32 && (long)heads * ((Nq + 31) / 32) >= 512, 1};
+    const int nk = f.common ? 1 : cache4_apart_waves(DT, dt == SIGE_F32 ? Cache4Compute<float>::parts : 1);
+    const long rows = f.common ? 32 * CACHE4_COMMON_WAVES : 32;
+    const int KCH = cache4_chunk(d, dt, f.common);
     const long chunks = ((long)T + KCH - 1) / KCH;
-    const long base = (long)heads * ((Nq + 32 * f.nq - 1) / (32 * f.nq));
-    long want = ((target >= 0 ? target : 512) + base - 1) / base;
-    const long cap = chunks / (2 * f.nk);
+    const long base = (long)heads * ((Nq + rows - 1) / rows);
+    long want = ((target >= 0 ? target : f.common ? 512 : 256) + base - 1) / base;
+    const long cap = chunks / (2 * nk);
     if (want > cap) want = cap;
     if (want > 64) want = 64;
     if (want < 1) want = 1;
@@ -62,7 +62,7 @@ static int cache4_attn_entry(const char* who, Cache4AttnArgs& a, const void* q, 
     a.d_heads = fast_div(heads); a.d_tpb = fast_div(a.q_tpb); a.d_qbw = fast_div(a.q_bw); a.d_dq = fast_div(d / 4);
     const bool room = workspace != nullptr && aligned16(workspace);
     const Cache4Form f = plan_cache4(Nq, T, heads, d, dt, room ? workspace_bytes / sizeof(float) : 0);
-    const int KCH = cache4_chunk((d + 31) / 32, dt);
+    const int KCH = cache4_chunk(d, dt, f.common);
     const int chunks = (int)(((long)T + KCH - 1) / KCH);
     a.splits = f.splits;
     a.chunks_per_split = (chunks + f.splits - 1) / f.splits;

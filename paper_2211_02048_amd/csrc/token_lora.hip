@@ -72,7 +72,7 @@ __global__ __launch_bounds__(64 * LORA_WAVES) void token_lora_kernel(LoraArgs a)
     constexpr int HROW = KR * KS + VW;                            // values per row of the middle vectors
     constexpr int AHEAD = RT <= 2 ? 5 : RT <= 4 ? 3 : 2;          // steps over Cin whose operands are on their way together
     constexpr int TU = F32 ? 1 : 2, CU = 16 * TU;                 // products per stretch of output channels, its channels
-    constexpr int BATCH = KR <= 1 ? 5 : KR <= 2 ? 2 : 1;          // stretches whose operands are on their way together
+    constexpr int BATCH = KR <= 1 ? (F32 ? 4 : 5) : KR <= 2 ? 2 : 1;          // stretches whose operands are on their way together
     __shared__ float red[LORA_WAVES][16][RED];
     __shared__ uint4 hbuf[(F32 ? 1 : 2) * 16 * HROW / VW];
     T* const hs = reinterpret_cast<T*>(hbuf);                     // [value, remainder][16][HROW]
