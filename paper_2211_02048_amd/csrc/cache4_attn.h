@@ -198,18 +198,23 @@ template <typename T, int DT, bool ODD, int KT> struct Cache4Sums {
     __device__ __forceinline__ void hide(const Cache4AttnArgs& a, const Cache4Seen& seen, int t0, int half, bool marked,
                                          const uint8_t* vscales, f32x16 (&sacc)[KT])
     {
-        unsigned lost = 0;
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const int at = kt * 32 + 8 * (r >> 2) + 4 * half + (r & 3), t = t0 + at;
+                const int t = t0 + kt * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
                 if (t < seen.begin || t >= seen.end) sacc[kt][r] = -INFINITY;
-                else if (marked)
-                    for (int g = 0; g < DT; ++g)
-                        if (vscales[(at << a.gs_log2) + g] > Cache4Compute<T>::last) lost |= 1u << g;
             }
         if (!marked) return;
+        unsigned lost = 0;
+#pragma unroll 1
+        for (int i = 0; i < 16 * KT; ++i) {                        // (rolled: unrolled, its addresses took 60 registers)
+            const int at = 8 * (i >> 2) + 4 * half + (i & 3);
+            if (t0 + at < seen.begin || t0 + at >= seen.end) continue;
+#pragma unroll 1
+            for (int g = 0; g < DT; ++g)
+                if (vscales[(at << a.gs_log2) + g] > Cache4Compute<T>::last) lost |= 1u << g;
+        }
         lost |= (unsigned)__shfl_xor((int)lost, 32);
 #pragma unroll
         for (int nt = 0; nt < DT; ++nt)
@@ -315,6 +320,12 @@ constexpr int cache4_apart_tiles(int DT, int parts) { return DT <= (parts > 1 ? 
 constexpr int cache4_apart_bytes(int DT, int parts) { return 32 * cache4_apart_tiles(DT, parts) * 64 * DT; }     // a chunk's V rows in LDS
 // waves of a workgroup: what their sums take in LDS when they meet
 constexpr int cache4_apart_waves(int DT, int parts) { return DT <= (parts > 1 ? 2 : 4) ? 8 : 4; }
+// waves per SIMD: their registers hold the next chunk beside everything, and the waves of one workgroup are two per SIMD anyway
+constexpr int cache4_apart_side(int DT, int parts) { return parts > 1 ? (DT <= 3 ? 2 : 1) : DT <= 7 ? 2 : 1; }
+// Many queries, half types.  Heads up to 64: four waves per SIMD, two workgroups side by side (4096 queries of 4096 x 8 of 64 74 -> 64 us,
+// of 40 62 -> 50; one query of 65536 keys 15.1 -> 16.1).  Larger heads have no registers for that: the common form.
+constexpr bool cache4_crowds(int DT, int parts) { return parts == 1 && DT <= 2; }
+constexpr bool cache4_has_common(int DT, int parts) { return parts == 1 && DT > 2; }
 // The 64 bytes of group g of a V row: which of the row's groups of 64 bytes holds it.  Four neighbouring keys keep a group on
 // different banks, in the writes (a lane per key) and in the transposed reads (four keys per 16 lanes).
 template <int DT> __device__ __forceinline__ int cache4_apart_group(int key, int g)
@@ -325,10 +336,9 @@ template <int DT> __device__ __forceinline__ int cache4_apart_group(int key, int
 // DT = 32-wide tiles over d; ODD: the last one has 16 channels (d % 32 is 8 or 16), and its row 16 is the row of ones.
 // The NK waves of a workgroup have the same 32 queries and take every NK-th chunk of the tokens.  K goes from memory straight into the
 // first product's operands (8 bytes of a key and group per lane: the order of the channels is the queries' too), V through the
-// wave's own rows in LDS, which it is transposed out of.  Two waves per SIMD, whose registers hold the next chunk beside everything:
-// with four of half the registers they spill (1 query of 65536 x 8 of 64 18.5 us against 15.5).
-template <typename T, int DT, bool ODD, int NK>
-__global__ __launch_bounds__(64 * NK, sizeof(T) == 4 || DT > 5 ? 1 : 2) void cache4_apart_kernel(Cache4AttnArgs a)
+// wave's own rows in LDS, which it is transposed out of.  WAVES: per SIMD, whose registers they share.
+template <typename T, int DT, bool ODD, int NK, int WAVES>
+__global__ __launch_bounds__(64 * NK, WAVES) void cache4_apart_kernel(Cache4AttnArgs a)
 {
     using C = typename Cache4Compute<T>::type;
     constexpr int NP = Cache4Compute<T>::parts;
@@ -481,22 +491,23 @@ __global__ __launch_bounds__(64 * NK, sizeof(T) == 4 || DT > 5 ? 1 : 2) void cac
     __syncthreads();                                                // (chunks no longer needed)
     {
         float* const mine = comb + (wave * 32 + l32) * cs;
-        if (half == 0) *(float2*)(mine + d) = make_float2(sums.m, l_tot);
+        if (qi < a.Nq) {                                            // (few queries: few rows to bring together)
+            if (half == 0) *(float2*)(mine + d) = make_float2(sums.m, l_tot);
 #pragma unroll
-        for (int nt = 0; nt < DT; ++nt)
+            for (int nt = 0; nt < DT; ++nt)
 #pragma unroll
-            for (int rq = 0; rq < 4; ++rq) {
-                const int dd = nt * 32 + 8 * rq + 4 * half;
-                if (dd < d) *(float4*)(mine + dd) = sums.four(nt, rq);
-            }
+                for (int rq = 0; rq < 4; ++rq) {
+                    const int dd = nt * 32 + 8 * rq + 4 * half;
+                    if (dd < d) *(float4*)(mine + dd) = sums.four(nt, rq);
+                }
+        }
     }
     __syncthreads();
-    const int dq = d >> 2;
-    for (int e = tid; e < 32 * dq; e += 64 * NK) {
+    const int dq = d >> 2, todo = min(32, a.Nq - qt * 32) * dq;
+    for (int e = tid; e < todo; e += 64 * NK) {
         int q, g;
         divmod(e, a.d_dq, q, g);
         const int qq = qt * 32 + q;
-        if (qq >= a.Nq) break;
         const float* const src = comb + q * cs;
         float m = -INFINITY, den = 0.0f;
         float4 num = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -540,7 +551,7 @@ constexpr int cache4_common_bytes(int DT, bool ODD) { return 32 * cache4_common_
 // compiler keeps heads up to 128 in half of what it takes otherwise (4096 queries of 16384 x 8 of 128 580 -> 367 us, 2048 of 4096 x 160
 // 146 -> 85).  Heads of 225 to 256 leave a few registers in memory then, and gain all the same (1024 of 4096 x 256 125 -> 77 us).
 template <typename T, int DT, bool ODD>
-__global__ __launch_bounds__(64 * CACHE4_COMMON_WAVES, DT <= 3 ? 3 : 2) void cache4_common_kernel(Cache4AttnArgs a)
+__global__ __launch_bounds__(64 * CACHE4_COMMON_WAVES, 2) void cache4_common_kernel(Cache4AttnArgs a)
 {
     using C = typename Cache4Compute<T>::type;
     constexpr int NW = CACHE4_COMMON_WAVES;
@@ -769,7 +780,7 @@ __global__ __launch_bounds__(256) void cache4_merge_kernel(Cache4AttnArgs a)
 }
 
 // How a call is cut (cache4_attn.hip), and its launch, one file per type.
-struct Cache4Form { bool common; int splits; };
+struct Cache4Form { bool many; int splits; };                // many: enough queries for the form that takes them
 int launch_cache4_f32(const Cache4AttnArgs& a, const Cache4Form& f, hipStream_t st);
 int launch_cache4_f16(const Cache4AttnArgs& a, const Cache4Form& f, hipStream_t st);
 int launch_cache4_bf16(const Cache4AttnArgs& a, const Cache4Form& f, hipStream_t st);
@@ -778,11 +789,13 @@ template <typename T, int DT, bool ODD>
 static int launch_cache4_as(const Cache4AttnArgs& a, const Cache4Form& f, hipStream_t st)
 {
     constexpr int NP = Cache4Compute<T>::parts, NK = cache4_apart_waves(DT, NP);
-    void (*kern)(Cache4AttnArgs) = cache4_apart_kernel<T, DT, ODD, NK>;
+    void (*kern)(Cache4AttnArgs) = cache4_apart_kernel<T, DT, ODD, NK, cache4_apart_side(DT, NP)>;
     int rows = 32, threads = 64 * NK;
     size_t lds = NK * std::max((size_t)cache4_apart_bytes(DT, NP), 32 * (a.d + 4) * sizeof(float));
-    if constexpr (sizeof(T) == 2)
-        if (f.common) {
+    if constexpr (cache4_crowds(DT, NP))
+        if (f.many) kern = cache4_apart_kernel<T, DT, ODD, NK, 4>;
+    if constexpr (cache4_has_common(DT, NP))
+        if (f.many) {
             kern = cache4_common_kernel<T, DT, ODD>;
             rows = 32 * CACHE4_COMMON_WAVES;
             threads = 64 * CACHE4_COMMON_WAVES;

@@ -4,29 +4,37 @@
 
 namespace sige {
 
-// Tokens per chunk, and waves that share the chunks of a workgroup's queries out among them.
-static int cache4_chunk(int d, sige_dtype dt, bool common)
+// How the queries and tokens of a call are dealt out, by its form: queries per workgroup, waves that share its tokens, tokens per chunk.
+struct Cache4Cut { int rows, waves, chunk; };
+static Cache4Cut cache4_cut(int d, sige_dtype dt, bool many)
 {
-    const int DT = (d + 31) / 32;
-    return 32 * (common ? cache4_common_tiles(DT) : cache4_apart_tiles(DT, dt == SIGE_F32 ? Cache4Compute<float>::parts : 1));
+    const int DT = (d + 31) / 32, parts = dt == SIGE_F32 ? Cache4Compute<float>::parts : 1;
+    if (many && cache4_has_common(DT, parts)) return {32 * CACHE4_COMMON_WAVES, 1, 32 * cache4_common_tiles(DT)};
+    return {32, cache4_apart_waves(DT, parts), 32 * cache4_apart_tiles(DT, parts)};
 }
 
 // room: floats of workspace, what the splits' partial sums have to fit into.
+//
+// Half types, from where on a call counts as one of many queries (heads x tiles of 32, "tiles"):
+//   heads up to 64    more tiles than compute units: workgroups side by side (512 tiles of 1024 tokens x 40 13.5 against 15.9 us; 256 of
+//                     3000 x 64 17.4 against 16.7)
+//   larger heads      tiles x tokens from 2^21 on: four waves on common chunks (1024 x 16384 x 128 320 against 433 us, 512 x 4096 x 160
+//                     84 against 94; 512 x 2048 x 128 44 against 36, 256 x 3000 x 128 38 against 25)
+// Splits over workgroups: as many as fill the chip once (common chunks: with the two, three workgroups that a compute unit holds), since
+// a wave works as fast beside others; none for fewer than four chunks per wave, which end before the merge kernel (3 us) would have
+// (16 queries of 4096 x 8 of 40, eight chunks per wave: 16.2 us alone, 12.9, 10.0 and 9.0 in 2, 4 and 8 splits; 160 tiles of 4096 x 80
+// 22.6 alone, 29.6 in two).
 static Cache4Form plan_cache4(int Nq, int T, int heads, int d, sige_dtype dt, size_t room = ~(size_t)0)
 {
-    const int DT = (d + 31) / 32;
     const int target = knob(SIGE_KNOB_ATTN_WGS);
-    Cache4Form f = {dt != SIGE_F32 && (long)heads * ((Nq + 31) / 32) >= 512, 1};
-    const int nk = f.common ? 1 : cache4_apart_waves(DT, dt == SIGE_F32 ? Cache4Compute<float>::parts : 1);
-    const long rows = f.common ? 32 * CACHE4_COMMON_WAVES : 32;
-    const int KCH = cache4_chunk(d, dt, f.common);
-    const long chunks = ((long)T + KCH - 1) / KCH;
-    const long base = (long)heads * ((Nq + rows - 1) / rows);
-    long want = ((target >= 0 ? target : f.common ? 512 : 256) + base - 1) / base;
-    const long cap = chunks / (2 * nk);
-    if (want > cap) want = cap;
-    if (want > 64) want = 64;
-    if (want < 1) want = 1;
+    const long tiles = (long)heads * (((long)Nq + 31) / 32);
+    Cache4Form f = {dt != SIGE_F32 && (d <= 64 ? tiles > 256 : tiles * T >= (1L << 21)), 1};
+    const Cache4Cut cut = cache4_cut(d, dt, f.many);
+    const long chunks = ((long)T + cut.chunk - 1) / cut.chunk;
+    const long base = (long)heads * (((long)Nq + cut.rows - 1) / cut.rows);
+    const long fill = cut.waves > 1 ? 256 : d <= 96 ? 768 : 512;
+    long want = target >= 0 ? (target + base - 1) / base : chunks < 4 * cut.waves ? 1 : fill / base;
+    want = std::max(std::min(std::min(want, chunks / cut.waves), 64L), 1L);
     const long per = std::max((chunks + want - 1) / want, 1L);
     f.splits = (int)std::max((chunks + per - 1) / per, 1L);
     while (f.splits > 1 && (size_t)f.splits * heads * Nq * (d + 4) > room) {
@@ -62,7 +70,7 @@ static int cache4_attn_entry(const char* who, Cache4AttnArgs& a, const void* q, 
     a.d_heads = fast_div(heads); a.d_tpb = fast_div(a.q_tpb); a.d_qbw = fast_div(a.q_bw); a.d_dq = fast_div(d / 4);
     const bool room = workspace != nullptr && aligned16(workspace);
     const Cache4Form f = plan_cache4(Nq, T, heads, d, dt, room ? workspace_bytes / sizeof(float) : 0);
-    const int KCH = cache4_chunk(d, dt, f.common);
+    const int KCH = cache4_cut(d, dt, f.many).chunk;
     const int chunks = (int)(((long)T + KCH - 1) / KCH);
     a.splits = f.splits;
     a.chunks_per_split = (chunks + f.splits - 1) / f.splits;
