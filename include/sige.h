@@ -574,13 +574,14 @@ int sige_version(void);
  *   CONV_LDS_PAD       bytes between the staged pixels' channel runs in LDS (a multiple of 16)
  *   CONV_AHEAD         requests ahead in the shapes whose waves split K (the next chunk, or the only one at once): 0 = never,
  *                      1 = a tiled call that cannot request its next chunk ahead ends in SIGE_ERR_UNSUPPORTED,
- *                      2 = one that cannot request its only chunk at once does                                */
+ *                      2 = one that cannot request its only chunk at once does
+ *   CACHE4_MANY        sige_cache4_attn, half types: 0 = the form for few queries, 1 = the one for many           */
 typedef enum {
     SIGE_KNOB_CONV_CFG = 0, SIGE_KNOB_CONV_KC = 1, SIGE_KNOB_CONV_SPLIT = 2, SIGE_KNOB_CONV_HALF = 3,
     SIGE_KNOB_CONV_SPLIT_WGS = 4, SIGE_KNOB_CONV_POINTWISE = 5, SIGE_KNOB_CONV_POINTWISE_W4 = 6,
     SIGE_KNOB_CONV_PAIR_WGS = 7, SIGE_KNOB_ATTN_WGS = 8, SIGE_KNOB_DIFF_LOADS = 9, SIGE_KNOB_DIFF_WGS = 10,
     SIGE_KNOB_CONV_DIRECT = 11, SIGE_KNOB_CONV_LDS_PAD = 12, SIGE_KNOB_CONV_AHEAD = 13,
-    SIGE_KNOB_COUNT = 14
+    SIGE_KNOB_CACHE4_MANY = 14, SIGE_KNOB_COUNT = 15
 } sige_knob;
 int sige_set_knob(sige_knob knob, int32_t value);
 int32_t sige_get_knob(sige_knob knob);

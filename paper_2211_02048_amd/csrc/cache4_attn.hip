@@ -28,7 +28,8 @@ static Cache4Form plan_cache4(int Nq, int T, int heads, int d, sige_dtype dt, si
 {
     const int target = knob(SIGE_KNOB_ATTN_WGS);
     const long tiles = (long)heads * (((long)Nq + 31) / 32);
-    Cache4Form f = {dt != SIGE_F32 && (d <= 64 ? tiles > 256 : tiles * T >= (1L << 21)), 1};
+    const int many = knob(SIGE_KNOB_CACHE4_MANY);
+    Cache4Form f = {dt != SIGE_F32 && (many >= 0 ? many != 0 : d <= 64 ? tiles > 256 : tiles * T >= (1L << 21)), 1};
     const Cache4Cut cut = cache4_cut(d, dt, f.many);
     const long chunks = ((long)T + cut.chunk - 1) / cut.chunk;
     const long base = (long)heads * (((long)Nq + cut.rows - 1) / cut.rows);

@@ -201,6 +201,11 @@ def attend(q, cache, capacity, T, heads, d, scale, ranges=None, ws=True):
 SIZES = [(1, 1), (1, 700), (5, 33), (16, 320), (33, 64), (70, 65), (130, 257)]
 
 
+def forms(dtype):
+    """The forms of a call: by its own rule, that for few queries, that for many (half types)."""
+    return (None,) if dtype == "f32" else (None, 0, 1)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("d", HEADS_OF)
 def test_attention(d, dtype):
@@ -209,9 +214,11 @@ def test_attention(d, dtype):
         q, cache, cap, k, v = case(d + nq, nq, T, heads, d, dtype)
         scale = 1 / math.sqrt(d)
         want, mag = ref.attention(f64(q).reshape(nq, heads, d), k, v, scale)
-        for ws in (True, False):
-            o = attend(q, cache, cap, T, heads, d, scale, ws=ws)
-            close(o, want, mag, f64(q).reshape(nq, heads, d), k, scale, dtype, T, f"{nq} of {T} x {d}, workspace {ws}")
+        for many in forms(dtype):
+            for ws in (True, False):
+                with api.knobs(CACHE4_MANY=many):
+                    o = attend(q, cache, cap, T, heads, d, scale, ws=ws)
+                close(o, want, mag, f64(q).reshape(nq, heads, d), k, scale, dtype, T, f"{nq} of {T} x {d}, form {many}, workspace {ws}")
 
 
 def some_ranges(nq, T, seed):
@@ -233,18 +240,20 @@ def test_attention_ranges(nq, T, heads, d, dtype):
     scale = 1 / math.sqrt(d)
     q64 = f64(q).reshape(nq, heads, d)
     want, mag = ref.attention(q64, k, v, scale, ranges)
-    for ws in (True, False):
-        o = attend(q, cache, cap, T, heads, d, scale, ranges, ws)
-        close(o, want, mag, q64, k, scale, dtype, T, f"ranges, workspace {ws}")
-        empty = np.array([max(b, 0) >= min(e, T) for b, e in ranges])
-        assert empty.any() and (o[torch.from_numpy(empty).cuda()] == 0).all()
-    # no row sees anything
-    o = attend(q, cache, cap, T, heads, d, scale, np.zeros((nq, 2)))
-    assert (o == 0).all()
     # every row sees the tokens up to its own (a row per token of the last ones)
-    ranges = np.stack([np.zeros(nq), np.minimum(np.arange(nq) + max(T - nq, 0) + 1, T)], 1).astype(int)
-    want, mag = ref.attention(q64, k, v, scale, ranges)
-    close(attend(q, cache, cap, T, heads, d, scale, ranges), want, mag, q64, k, scale, dtype, T, "up to its own token")
+    own = np.stack([np.zeros(nq), np.minimum(np.arange(nq) + max(T - nq, 0) + 1, T)], 1).astype(int)
+    want_own, mag_own = ref.attention(q64, k, v, scale, own)
+    for many in forms(dtype):
+        with api.knobs(CACHE4_MANY=many):
+            for ws in (True, False):
+                o = attend(q, cache, cap, T, heads, d, scale, ranges, ws)
+                close(o, want, mag, q64, k, scale, dtype, T, f"ranges, form {many}, workspace {ws}")
+                empty = np.array([max(b, 0) >= min(e, T) for b, e in ranges])
+                assert empty.any() and (o[torch.from_numpy(empty).cuda()] == 0).all()
+            # no row sees anything
+            o = attend(q, cache, cap, T, heads, d, scale, np.zeros((nq, 2)))
+            assert (o == 0).all()
+            close(attend(q, cache, cap, T, heads, d, scale, own), want_own, mag_own, q64, k, scale, dtype, T, "up to its own token")
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
@@ -269,9 +278,11 @@ def test_attention_of_tokens_that_are_no_numbers(nq, d, dtype):
         want, mag = ref.attention(q64, k, v, scale, r)
         if r is not None and r is not ranges:
             assert np.isfinite(want).all()
-        for ws in (True, False):
-            o = attend(q, cache, cap, T, heads, d, scale, r, ws)
-            close(o, want, mag, q64, k, scale, dtype, T, "tokens that are no numbers")
+        for many in forms(dtype):
+            for ws in (True, False):
+                with api.knobs(CACHE4_MANY=many):
+                    o = attend(q, cache, cap, T, heads, d, scale, r, ws)
+                close(o, want, mag, q64, k, scale, dtype, T, f"tokens that are no numbers, form {many}")
 
 
 def test_attention_edges():
@@ -359,16 +370,19 @@ def test_attention_far_into_a_long_cache():
 
 def test_attention_splits():
     """The keys cut over workgroups, as often as a workspace holds them (the knob aims for more and more workgroups)."""
-    for dtype, nq, T, heads, d in (("bf16", 100, 3000, 1, 64), ("f16", 20, 5000, 2, 40), ("f32", 70, 2500, 1, 128)):
+    for dtype, nq, T, heads, d in (("bf16", 100, 3000, 1, 64), ("f16", 20, 5000, 2, 40), ("f32", 70, 2500, 1, 128), ("bf16", 150, 2000, 2, 96),
+                                   ("f16", 40, 1500, 1, 200)):
         q, cache, cap, k, v = case(9, nq, T, heads, d, dtype)
         q64 = f64(q).reshape(nq, heads, d)
         scale = 1 / math.sqrt(d)
         ranges = some_ranges(nq, T, 8)
         for r in (None, ranges):
             want, mag = ref.attention(q64, k, v, scale, r)
-            for wgs in (1, 3, 9, 40, 200):
-                with api.knobs(ATTN_WGS=wgs):
-                    close(attend(q, cache, cap, T, heads, d, scale, r), want, mag, q64, k, scale, dtype, T, f"{wgs} workgroups")
+            for many in forms(dtype):
+                for wgs in (1, 3, 9, 40, 200):
+                    with api.knobs(ATTN_WGS=wgs, CACHE4_MANY=many):
+                        o = attend(q, cache, cap, T, heads, d, scale, r)
+                    close(o, want, mag, q64, k, scale, dtype, T, f"form {many}, {wgs} workgroups")
         ws = torch.empty(3 * heads * nq * (d + 4), dtype=torch.float32, device="cuda")      # room for three
         o = torch.empty_like(q)
         api.sige_cache4_attn(q, cache, cap, o, scale, T=T, heads=heads, d=d, workspace=ws)
@@ -413,3 +427,19 @@ def test_captured_and_on_another_stream():
         step()
     side.synchronize()
     assert torch.equal(o, want)
+
+
+def test_attention_takes_the_form_for_many_queries():
+    """Calls that the rule gives to the forms for many queries (heads up to 64: more tiles of 32 queries than compute units; larger
+    ones: tiles x tokens from 2^21 on), every row against float64 on the GPU."""
+    for dtype, nq, T, heads, d in (("bf16", 2100, 300, 5, 64), ("f16", 1500, 700, 6, 40), ("bf16", 4200, 8200, 2, 96), ("f16", 4100, 16400, 1, 128)):
+        q, cache, cap, k, v = case(7, nq, T, heads, d, dtype)
+        k, v = torch.from_numpy(k).cuda(), torch.from_numpy(v).cuda()
+        scale = 1 / math.sqrt(d)
+        o = attend(q, cache, cap, T, heads, d, scale)
+        q64 = q.double().view(nq, heads, d)
+        for h in range(heads):
+            s = q64[:, h] @ k[:, h].t() * scale
+            p = torch.softmax(s, -1)
+            want, mag = (p @ v[:, h]).cpu().numpy()[:, None], ((p + 2.0 ** -30) @ v[:, h].abs()).cpu().numpy()[:, None]
+            close(o[:, h * d:(h + 1) * d], want, mag, q64[:, h:h + 1].cpu().numpy(), k[:, h:h + 1].cpu().numpy(), scale, dtype, T, f"{nq} of {T} x {d}")
