@@ -183,6 +183,7 @@ template <typename T, int DT, bool ODD, int KT> struct Cache4Sums {
     static constexpr int NP = Cache4Compute<T>::parts;
     f32x16 o[DT];
     float m, l;
+    unsigned lost;                 // groups of 32 channels in which the row sees a value that is no number
 
     __device__ __forceinline__ void clear()
     {
@@ -192,33 +193,38 @@ template <typename T, int DT, bool ODD, int KT> struct Cache4Sums {
             for (int r = 0; r < 16; ++r) o[nt][r] = 0.0f;
         m = -INFINITY;
         l = 0.0f;
+        lost = 0u;
     }
     // A chunk of which some row does not see everything: those logits are out.  marked: some value in it is no number (and counts 0 in
-    // the products); the rows that see it have NaN in the channels of its group.  vscales: the scale bytes of the chunk's first value
+    // the products); the groups of those that the row sees are noted.  vscales: the scale bytes of the chunk's first value
     __device__ __forceinline__ void hide(const Cache4AttnArgs& a, const Cache4Seen& seen, int t0, int half, bool marked,
                                          const uint8_t* vscales, f32x16 (&sacc)[KT])
     {
+        if (marked) {
+#pragma unroll 1
+            for (int i = 0; i < 16 * KT; ++i) {                    // (rolled: unrolled, its addresses took 60 registers)
+                const int at = 8 * (i >> 2) + 4 * half + (i & 3);
+                if (t0 + at < seen.begin || t0 + at >= seen.end) continue;
+#pragma unroll 1
+                for (int g = 0; g < DT; ++g)
+                    if (vscales[(at << a.gs_log2) + g] > Cache4Compute<T>::last) lost |= 1u << g;
+            }
+        }
+        const unsigned width = (unsigned)max(seen.end - seen.begin, 0), off = (unsigned)(t0 + 4 * half - seen.begin);
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int t = t0 + kt * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
-                if (t < seen.begin || t >= seen.end) sacc[kt][r] = -INFINITY;
-            }
-        if (!marked) return;
-        unsigned lost = 0;
-#pragma unroll 1
-        for (int i = 0; i < 16 * KT; ++i) {                        // (rolled: unrolled, its addresses took 60 registers)
-            const int at = 8 * (i >> 2) + 4 * half + (i & 3);
-            if (t0 + at < seen.begin || t0 + at >= seen.end) continue;
-#pragma unroll 1
-            for (int g = 0; g < DT; ++g)
-                if (vscales[(at << a.gs_log2) + g] > Cache4Compute<T>::last) lost |= 1u << g;
-        }
-        lost |= (unsigned)__shfl_xor((int)lost, 32);
+            for (int r = 0; r < 16; ++r)
+                if (off + (kt * 32 + 8 * (r >> 2) + (r & 3)) >= width) sacc[kt][r] = -INFINITY;
+    }
+    // After the last chunk: the noted groups of a row are NaN
+    __device__ __forceinline__ void finish()
+    {
+        if (__builtin_amdgcn_ballot_w64(lost != 0u) == 0ull) return;
+        const unsigned both = lost | (unsigned)__shfl_xor((int)lost, 32);
 #pragma unroll
         for (int nt = 0; nt < DT; ++nt)
-            if (lost >> nt & 1u) {
+            if (both >> nt & 1u) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     if (!(ODD && nt == DT - 1 && r >= 8)) o[nt][r] = NAN;
@@ -484,6 +490,7 @@ __global__ __launch_bounds__(64 * NK, WAVES) void cache4_apart_kernel(Cache4Attn
     }
 
     // the waves' shares of the tokens, brought to a common maximum and added in wave order
+    sums.finish();
     float l_tot = sums.total(l32);
     if (seen.none) { sums.m = -INFINITY; l_tot = 0.0f; }            // (what such a row added up is not read)
     float* const comb = reinterpret_cast<float*>(lds);              // [NK][32 queries][d sums, maximum, denominator, 2 unused]
@@ -707,6 +714,7 @@ __global__ __launch_bounds__(64 * CACHE4_COMMON_WAVES, 2) void cache4_common_ker
         });
     }
 
+    sums.finish();
     float l_tot = sums.total(l32);
     if (!q_ok) return;
     if (seen.none) { sums.m = -INFINITY; l_tot = 0.0f; }
