@@ -255,8 +255,9 @@ template <typename T, int DT, bool ODD, int KT> struct Cache4Sums {
         // only what is below 2^-40 is lost)
         return m_at - (__is_same(C, f16) ? 15.0f : 0.0f);
     }
-    // The probabilities, and O^T += V^T P^T in steps of 16 keys; v(kt, s, nt): the V^T fragment
-    template <typename V> __device__ __forceinline__ void add(float scale_log2e, float m_sub, f32x16 (&sacc)[KT], V v)
+    // The probabilities, and O^T += V^T P^T in steps of 16 keys; v(kt, s, nt): the V^T fragment.  URGENT: from the product on the wave
+    // goes before the others of its SIMD
+    template <bool URGENT, typename V> __device__ __forceinline__ void add(float scale_log2e, float m_sub, f32x16 (&sacc)[KT], V v)
     {
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt)
@@ -283,6 +284,7 @@ template <typename T, int DT, bool ODD, int KT> struct Cache4Sums {
                         else l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(b2, w[0]), __builtin_bit_cast(b2, 0x3f803f80u), l, false);
                     }
                 }
+                if (URGENT && kt == 0 && s == 0) __builtin_amdgcn_s_setprio(1);
                 constexpr int TILES = DT > 6 ? 4 : DT;       // (fragments on their way: heads beyond 192 have no registers for all)
 #pragma unroll
                 for (int n0 = 0; n0 < DT; n0 += TILES) {
@@ -486,7 +488,7 @@ __global__ __launch_bounds__(64 * NK, WAVES) void cache4_apart_kernel(Cache4Attn
         if (c + NK < c_end) fetch(c + NK);         // in flight during the softmax and the second product
         if (partial) sums.hide(a, seen, t0, half, marked, vsec + a.scales + (long)t0 * GS, sacc);
         const float m_sub = sums.settle(a.scale_log2e, sacc);
-        sums.add(a.scale_log2e, m_sub, sacc, v_fragment);
+        sums.template add<false>(a.scale_log2e, m_sub, sacc, v_fragment);
     }
 
     // the waves' shares of the tokens, brought to a common maximum and added in wave order
@@ -681,8 +683,12 @@ __global__ __launch_bounds__(64 * CACHE4_COMMON_WAVES, 2) void cache4_common_ker
             stage(c + 1, buf ^ 1);
             if (c + 2 < c_end) fetch(c + 2);
         }
+        __builtin_amdgcn_s_setprio(0);
         const int t0 = c * KCH;
         char* const rows = lds + buf * CHUNK;
+        // Of the two waves on a SIMD the one in a product goes first: its matrix instructions fill while the other expands or
+        // does its softmax (4096 queries of 16384 x 8 of 128 299.5 -> 293 us, 2048 of 4096 x 160 78.8 -> 75.7; the reverse 299)
+        __builtin_amdgcn_s_setprio(1);
         f32x16 sacc[KT];
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
@@ -701,11 +707,12 @@ __global__ __launch_bounds__(64 * CACHE4_COMMON_WAVES, 2) void cache4_common_ker
                 if (AT_ONCE < DK) __builtin_amdgcn_sched_barrier(0);
             }
         }
+        __builtin_amdgcn_s_setprio(0);
         if (seen.partial(t0, KCH))
             sums.hide(a, seen, t0, half, __builtin_amdgcn_readfirstlane(marked_chunk[buf]) == c + 1,
                       sec + a.section + a.scales + ((long)t0 << a.gs_log2), sacc);
         const float m_sub = sums.settle(a.scale_log2e, sacc);
-        sums.add(a.scale_log2e, m_sub, sacc, [&](int kt, int s, int nt) {
+        sums.template add<true>(a.scale_log2e, m_sub, sacc, [&](int kt, int s, int nt) {
             char* const at = rows + tr + (kt * 32 + 16 * s) * VROW + nt * 64;
             union { s16x4 h[2]; u32x4 u; } vf;
             vf.h[0] = read_transposed(at);
