@@ -447,7 +447,7 @@ int sige_rope_pairs(const int32_t* axis_pairs, int32_t n_axes, double theta, sig
 /* x and y are rows of [heads][d] with row strides x_ld / y_ld (queries and keys side by side are 2 * heads of them); rows as in
  * sige_token_norm (n_rows, or count * rows_per_count on the device).  positions: fp32 [rows][n_axes]; a pair whose axis is not in
  * 0..n_axes-1 is not turned.  x == y is allowed.  d * size and the strides must be multiples of 16 bytes; in the layout of halves
- * accesses are as wide as n_pairs allows.  Rounded once.                                    */
+ * accesses are as wide as n_pairs allows.  x == y needs x_ld == y_ld.  Rounded once.                */
 int sige_token_rope(const void* x, sige_dtype dt, int32_t heads, int32_t d, int32_t x_ld, const int32_t* count,
                     int32_t rows_per_count, int32_t max_rows, int32_t n_rows, const sige_rope_pair* pairs,
                     int32_t n_pairs, sige_rope_layout layout, const float* positions, int32_t n_axes, void* y,
@@ -468,7 +468,8 @@ int sige_token_rope_blocks(const void* x, sige_dtype dt, int32_t heads, int32_t 
  * has at most 16 channels, F = the others, gs = 1, 2, 4 or 8 bytes, the first that holds G:
  *   [heads][2: keys, values] { [F][cap][16 bytes]; if there is a short group [cap][8 bytes]; scales [cap][gs] }
  * byte b of a group holds channel 2b in its low and 2b + 1 in its high four bits; codes behind d are 0.  A scale byte above 252 (fp16
- * calls: above 140) marks a group that is not finite: it is read as NaN.  d must be a multiple of 8, <= 256.   */
+ * calls: above 140) marks a group that is not finite: it is read as NaN.  (The byte 0, which no store writes, may be read as the scale 0.)
+ * d must be a multiple of 8, <= 256.                                                     */
 size_t sige_cache4_bytes(int32_t heads, int32_t d, int32_t capacity);
 
 /* Stores rows of keys and values, k and v of [heads][d] with row strides k_ld / v_ld, in any dt:
@@ -497,7 +498,8 @@ int sige_cache4_load(const void* cache, int32_t capacity, sige_dtype dt, int32_t
  * what a row does not see - NaN, infinities - does not reach it.  0 <= T <= capacity.
  * The cached values enter the products exactly (they are bf16 numbers; for fp16 queries, fp16 numbers wherever an fp16 row was stored).
  * fp16 and bf16 round a probability to their type once; single precision loses nothing (operands in three parts).
- * scale >= 0.  workspace: as for sige_sparse_attn, sige_cache4_attn_workspace_bytes of it.  */
+ * scale >= 0.  workspace: as for sige_sparse_attn, sige_cache4_attn_workspace_bytes of it; two calls that may run at the same time (on
+ * two streams, in two graphs) need one each.  T < 2^31 - 128.                              */
 int sige_cache4_attn(const void* q, int32_t q_ld, const void* cache, int32_t capacity, sige_dtype dt, int32_t Nq,
                      int32_t T, int32_t heads, int32_t d, float scale, const int32_t* ranges, void* o, int32_t o_ld,
                      void* workspace, size_t workspace_bytes, void* stream);
@@ -515,7 +517,7 @@ int sige_cache4_attn_blocks(const void* q, int32_t q_ld, const sige_geom* g, con
  * without adapter.  base [rows][Cout] is the projection's output, or NULL: y is the adapters' share alone, which sige_conv_scatter
  * adds to its fp32 sums as residual_tiles.  y == base is allowed.  Sums in fp32, the middle vector in fp32 (half types multiply it as
  * the sum of two halves), rounded once.  Rows: n_rows >= 0 from the host, or -1 = min(*count * rows_per_id, max_rows).
- * Cin, Cout, rank and strides must be multiples of 16 bytes, rank <= 128.               */
+ * Cin, Cout, rank and strides must be multiples of 16 bytes, rank <= 128.  y may not be x; y == base needs y_ld == base_ld.  */
 int sige_token_lora(const void* x, sige_dtype dt, int32_t Cin, int32_t x_ld, const int32_t* count, int32_t rows_per_id,
                     int32_t max_rows, int32_t n_rows, const void* down, const void* up, int32_t rank,
                     int32_t n_adapters, const float* alpha, const int32_t* ids, const void* base, int32_t base_ld,

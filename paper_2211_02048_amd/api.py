@@ -563,14 +563,50 @@ def _at(t):
     return None if t is None else t.data_ptr()
 
 
+def _like(x, *tensors):
+    """The tensors a kernel takes for the type of x."""
+    for t in tensors:
+        if t is not None and t.dtype is not x.dtype:
+            raise SigeError(1, f"{t.dtype} beside {x.dtype} in one call")
+
+
+def _table(what, t, dtype, n):
+    """A table the kernels read entry by entry: at least n of them, one after the other."""
+    if t is not None and (t.dtype is not dtype or t.numel() < n or not t.is_contiguous()):
+        raise SigeError(1, f"{what}: {n} entries of {dtype}, contiguous, not {tuple(t.shape)} of {t.dtype}")
+
+
+def _lines(t):
+    """Stride of the rows of t, [..., channels] with rows that follow each other at one distance."""
+    st = t.stride()
+    if len(st) == 2 and st[1] == 1:
+        return st[0]
+    sh = t.shape
+    if len(st) < 2 or st[-1] != 1 or any(sh[i] > 1 and st[i] != sh[i + 1] * st[i + 1] for i in range(len(sh) - 2)):
+        raise SigeError(1, f"rows of channels at one distance, not {tuple(sh)} with strides {st}")
+    return st[-2]
+
+
+def _block_list(indices, count, n_blocks, max_blocks=None):
+    """The most blocks of a list that a call may read."""
+    mb = indices.shape[0] if max_blocks is None else max_blocks
+    _table("indices", indices, torch.int32, 2 * (mb if n_blocks < 0 else n_blocks))
+    _table("count", count, torch.int32, 1)
+    return mb
+
+
 def sige_token_rope(x, y, heads, d, pairs, positions, *, layout=ROPE_ADJACENT, n_rows=-1, count=None, rows_per_count=0,
                     max_rows=None, x_ld=None, y_ld=None):
     """Rotates the `heads` heads of every row by the row's positions (fp32 [rows, axes]); y may be x."""
-    stream = _stream_of(x, y, pairs, positions, count)
+    _like(x, y)
     mr = x.numel() // x.shape[-1] if max_rows is None else max_rows
-    rc = lib().sige_token_rope(x.data_ptr(), _DT[x.dtype], heads, d, x.stride(-2) if x_ld is None else x_ld, _at(count),
+    _table("pairs", pairs, torch.int32, 4 * pairs.shape[0])
+    _table("positions", positions, torch.float32, (mr if n_rows < 0 else n_rows) * positions.shape[-1])
+    _table("count", count, torch.int32, 1)
+    stream = _stream_of(x, y, pairs, positions, count)
+    rc = lib().sige_token_rope(x.data_ptr(), _DT[x.dtype], heads, d, _lines(x) if x_ld is None else x_ld, _at(count),
                                rows_per_count, mr, n_rows, pairs.data_ptr(), pairs.shape[0], layout, positions.data_ptr(),
-                               positions.shape[-1], y.data_ptr(), y.stride(-2) if y_ld is None else y_ld, stream)
+                               positions.shape[-1], y.data_ptr(), _lines(y) if y_ld is None else y_ld, stream)
     if rc:
         _check(rc)
 
@@ -578,28 +614,31 @@ def sige_token_rope(x, y, heads, d, pairs, positions, *, layout=ROPE_ADJACENT, n
 def sige_token_rope_blocks(x, y, heads, d, pairs, g: Geom, indices, count, *, n_axes=2, frame=0.0, layout=ROPE_ADJACENT,
                            n_blocks=-1, max_blocks=None, x_ld=None, y_ld=None):
     """The same with the positions (y, x) or (frame, y, x) of the listed blocks' pixels."""
+    _like(x, y)
+    _table("pairs", pairs, torch.int32, 4 * pairs.shape[0])
+    mb = _block_list(indices, count, n_blocks, max_blocks)
     stream = _stream_of(x, y, pairs, indices, count)
-    rc = lib().sige_token_rope_blocks(x.data_ptr(), _DT[x.dtype], heads, d, x.stride(-2) if x_ld is None else x_ld, ctypes.byref(g),
-                                      indices.data_ptr(), _at(count), indices.shape[0] if max_blocks is None else max_blocks,
-                                      n_blocks, pairs.data_ptr(), pairs.shape[0], layout, n_axes, frame, y.data_ptr(),
-                                      y.stride(-2) if y_ld is None else y_ld, stream)
+    rc = lib().sige_token_rope_blocks(x.data_ptr(), _DT[x.dtype], heads, d, _lines(x) if x_ld is None else x_ld, ctypes.byref(g),
+                                      indices.data_ptr(), _at(count), mb, n_blocks, pairs.data_ptr(), pairs.shape[0], layout, n_axes,
+                                      frame, y.data_ptr(), _lines(y) if y_ld is None else y_ld, stream)
     if rc:
         _check(rc)
 
 
-@functools.lru_cache(maxsize=None)
+@functools.lru_cache(maxsize=4096)
 def sige_cache4_bytes(heads, d, capacity) -> int:
     """Bytes of a cache of `capacity` tokens' keys and values in 4 bits (0: not a head size the cache has)."""
     return int(lib().sige_cache4_bytes(heads, d, capacity))
 
 
 def _rows_ld(t, heads, d):
-    """Stride of the [heads * d] (or [heads, d]) rows of t."""
+    """Stride of the rows of t, [rows, heads * d or more] or [rows, heads, d]."""
     if t is None:
         return 0
-    if t.dim() == 3 and t.shape[-1] == d and t.shape[-2] == heads and t.stride(-2) == d:
-        return t.stride(0)
-    return t.stride(-2)
+    st = t.stride()
+    if st[-1] == 1 and (len(st) == 2 or len(st) == 3 and st[1] == d and t.shape[1:] == (heads, d)):
+        return st[0]
+    raise SigeError(1, f"rows of {heads} heads of {d} channels, not {tuple(t.shape)} with strides {st}")
 
 
 def _check_cache(cache, heads, d, capacity):
@@ -612,11 +651,14 @@ def sige_cache4_store(k, v, cache, capacity, heads, d, *, slots=None, first=0, n
                       max_rows=None, k_ld=None, v_ld=None):
     """Rows of keys and values into the cache: row r to token slots[r], or to first + r."""
     _check_cache(cache, heads, d, capacity)
+    _like(k, v)
+    mr = k.shape[0] if max_rows is None else max_rows
+    _table("slots", slots, torch.int32, mr if n_rows < 0 else n_rows)
+    _table("count", count, torch.int32, 1)
     stream = _stream_of(k, v, cache, slots, count)
     rc = lib().sige_cache4_store(k.data_ptr(), _rows_ld(k, heads, d) if k_ld is None else k_ld, v.data_ptr(),
                                  _rows_ld(v, heads, d) if v_ld is None else v_ld, _DT[k.dtype], heads, d, _at(slots), first,
-                                 _at(count), rows_per_count, k.shape[0] if max_rows is None else max_rows, n_rows,
-                                 cache.data_ptr(), capacity, stream)
+                                 _at(count), rows_per_count, mr, n_rows, cache.data_ptr(), capacity, stream)
     if rc:
         _check(rc)
 
@@ -625,11 +667,12 @@ def sige_cache4_store_blocks(k, v, cache, capacity, heads, d, g: Geom, indices, 
                              k_ld=None, v_ld=None):
     """The stacked tokens of the listed blocks into the cache: pixel (y, x) to token first + y * W + x."""
     _check_cache(cache, heads, d, capacity)
+    _like(k, v)
+    mb = _block_list(indices, count, n_blocks, max_blocks)
     stream = _stream_of(k, v, cache, indices, count)
     rc = lib().sige_cache4_store_blocks(k.data_ptr(), _rows_ld(k, heads, d) if k_ld is None else k_ld, v.data_ptr(),
                                         _rows_ld(v, heads, d) if v_ld is None else v_ld, _DT[k.dtype], heads, d, ctypes.byref(g),
-                                        indices.data_ptr(), _at(count), indices.shape[0] if max_blocks is None else max_blocks,
-                                        n_blocks, first, cache.data_ptr(), capacity, stream)
+                                        indices.data_ptr(), _at(count), mb, n_blocks, first, cache.data_ptr(), capacity, stream)
     if rc:
         _check(rc)
 
@@ -638,6 +681,7 @@ def sige_cache4_load(cache, capacity, heads, d, k, v, *, first=0, n_tokens=None,
     """Tokens first, first + 1, ... of the cache as rows of k's and v's type (either may be None)."""
     _check_cache(cache, heads, d, capacity)
     t = k if k is not None else v
+    _like(t, v)
     stream = _stream_of(cache, k, v)
     rc = lib().sige_cache4_load(cache.data_ptr(), capacity, _DT[t.dtype], heads, d, first, t.shape[0] if n_tokens is None else n_tokens,
                                 _at(k), _rows_ld(k, heads, d) if k_ld is None else k_ld, _at(v),
@@ -653,9 +697,12 @@ def sige_cache4_attn_workspace_bytes(Nq, T, heads, d) -> int:
 def sige_cache4_attn(q, cache, capacity, o, scale, *, T, heads, d, Nq=None, ranges=None, workspace=None, q_ld=None, o_ld=None):
     """sige_sparse_attn on a cache in 4 bits; ranges (int32 [Nq, 2]): the tokens [begin, end) that each row sees."""
     _check_cache(cache, heads, d, capacity)
+    _like(q, o)
+    nq = q.shape[0] if Nq is None else Nq
+    _table("ranges", ranges, torch.int32, 2 * nq)
     stream = _stream_of(q, cache, o, ranges, workspace)
     rc = lib().sige_cache4_attn(q.data_ptr(), _rows_ld(q, heads, d) if q_ld is None else q_ld, cache.data_ptr(), capacity, _DT[q.dtype],
-                                q.shape[0] if Nq is None else Nq, T, heads, d, scale, _at(ranges), o.data_ptr(),
+                                nq, T, heads, d, scale, _at(ranges), o.data_ptr(),
                                 _rows_ld(o, heads, d) if o_ld is None else o_ld, _at(workspace), _nbytes(workspace), stream)
     if rc:
         _check(rc)
@@ -665,8 +712,11 @@ def sige_cache4_attn_blocks(q_full, g: Geom, indices, n_blocks, cache, capacity,
                             workspace=None, q_ld=None, o_ld=None):
     """The same with the queries read from a full tensor by block list (sige_sparse_attn_blocks)."""
     _check_cache(cache, heads, d, capacity)
+    _like(q_full, o)
+    _block_list(indices, None, n_blocks)
+    _table("ranges", ranges, torch.int32, 2 * n_blocks * g.block_h * g.block_w)
     stream = _stream_of(q_full, cache, o, indices, ranges, workspace)
-    rc = lib().sige_cache4_attn_blocks(q_full.data_ptr(), q_full.stride(-2) if q_ld is None else q_ld, ctypes.byref(g),
+    rc = lib().sige_cache4_attn_blocks(q_full.data_ptr(), _lines(q_full) if q_ld is None else q_ld, ctypes.byref(g),
                                        indices.data_ptr(), n_blocks, cache.data_ptr(), capacity, _DT[q_full.dtype], T, heads, d, scale,
                                        _at(ranges), o.data_ptr(), _rows_ld(o, heads, d) if o_ld is None else o_ld, _at(workspace),
                                        _nbytes(workspace), stream)
@@ -680,11 +730,16 @@ def sige_token_lora(x, y, Cin, Cout, down, up, ids, rows_per_id, *, alpha=None, 
     n, rank, _ = down.shape
     if down.shape != (n, rank, Cin) or up.shape != (n, Cout, rank) or not (down.is_contiguous() and up.is_contiguous()):
         raise SigeError(1, "sige_token_lora: down is [adapters, rank, Cin] and up [adapters, Cout, rank], contiguous")
+    _like(x, y, down, up, base)
+    mr = x.numel() // x.shape[-1] if max_rows is None else max_rows
+    _table("ids", ids, torch.int32, -(-(mr if n_rows < 0 else n_rows) // max(rows_per_id, 1)))
+    _table("alpha", alpha, torch.float32, n)
+    _table("count", count, torch.int32, 1)
     stream = _stream_of(x, y, down, up, ids, alpha, base, count)
-    rc = lib().sige_token_lora(x.data_ptr(), _DT[x.dtype], Cin, x.stride(-2) if x_ld is None else x_ld, _at(count), rows_per_id,
-                               x.numel() // x.shape[-1] if max_rows is None else max_rows, n_rows, down.data_ptr(), up.data_ptr(), rank,
-                               n, _at(alpha), ids.data_ptr(), _at(base), 0 if base is None else base.stride(-2) if base_ld is None else base_ld,
-                               Cout, y.data_ptr(), y.stride(-2) if y_ld is None else y_ld, stream)
+    rc = lib().sige_token_lora(x.data_ptr(), _DT[x.dtype], Cin, _lines(x) if x_ld is None else x_ld, _at(count), rows_per_id, mr,
+                               n_rows, down.data_ptr(), up.data_ptr(), rank, n, _at(alpha), ids.data_ptr(), _at(base),
+                               0 if base is None else _lines(base) if base_ld is None else base_ld, Cout, y.data_ptr(),
+                               _lines(y) if y_ld is None else y_ld, stream)
     if rc:
         _check(rc)
 

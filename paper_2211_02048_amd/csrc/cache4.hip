@@ -175,7 +175,7 @@ static void fill_rows(Cache4Rows& a, const void* cache, int capacity, int heads,
 static int launch_rows(const char* who, const Cache4Rows& a, sige_dtype dt, int rows, bool store, hipStream_t st)
 {
     const long waves = ((long)rows + 15) / 16 * (2L * a.heads * a.groups);
-    SIGE_REQUIRE(waves < (1L << 31) - 4, SIGE_ERR_UNSUPPORTED, "%s: too many rows", who);
+    SIGE_REQUIRE(waves < (1L << 26) - 4, SIGE_ERR_UNSUPPORTED, "%s: too many rows", who);     // (a launch has 2^32 threads)
     const dim3 grid((unsigned)((waves + 3) / 4));
     auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, a); };
     if (store) {

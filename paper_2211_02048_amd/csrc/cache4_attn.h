@@ -818,7 +818,8 @@ static int launch_cache4_as(const Cache4AttnArgs& a, const Cache4Form& f, hipStr
         }
     const long tiles = ((long)a.Nq + rows - 1) / rows * a.heads, groups = (long)a.Nq * a.heads * (a.d / 4);
     const int P = a.splits <= 4 ? 1 : a.splits <= 16 ? 4 : 16;             // (at most 64 splits)
-    SIGE_REQUIRE(tiles < (1L << 31) && groups < (1L << 33), SIGE_ERR_UNSUPPORTED, "sige_cache4_attn: too many queries");
+    SIGE_REQUIRE(tiles * a.splits * threads < (1L << 32) && (a.splits == 1 || groups * P < (1L << 32) - 256), SIGE_ERR_UNSUPPORTED,
+                 "sige_cache4_attn: too many queries");                       // (what a launch can have of threads)
     if (lds > 48 * 1024) {
         const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         SIGE_REQUIRE(e == hipSuccess, SIGE_ERR_HIP, "sige_cache4_attn: cannot reserve %zu bytes of LDS: %s", lds, hipGetErrorString(e));

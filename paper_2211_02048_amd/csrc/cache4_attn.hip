@@ -56,6 +56,7 @@ static int cache4_attn_entry(const char* who, Cache4AttnArgs& a, const void* q, 
     const int vw = dt == SIGE_F32 ? 4 : 8;
     SIGE_REQUIRE(d % 8 == 0 && d <= 256, SIGE_ERR_UNSUPPORTED, "%s: d must be a multiple of 8 and <= 256", who);
     SIGE_REQUIRE(heads <= 65535, SIGE_ERR_UNSUPPORTED, "%s: too many heads", who);
+    SIGE_REQUIRE(T <= 0x7fffffff - 128, SIGE_ERR_UNSUPPORTED, "%s: too many tokens", who);       // (a chunk's end is an int)
     if (Nq == 0) return SIGE_OK;
     SIGE_REQUIRE(q && cache && o, SIGE_ERR_INVALID_ARG, "%s: q, cache and o are required", who);
     SIGE_REQUIRE(q_ld >= (long)heads * d && o_ld >= (long)heads * d, SIGE_ERR_INVALID_ARG, "%s: row strides must be >= heads*d", who);

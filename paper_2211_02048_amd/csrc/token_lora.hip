@@ -7,7 +7,8 @@
 // over workgroups too, each of which repeats the small first product.  Where the 16 rows have several adapters there is one pass
 // for each, of which its own rows keep the result: no sorting, no second launch, and nothing lost where requests are whole blocks.
 // The middle vector down_i x_r stays in 32 bits; the half types' second product takes it as the sum of two halves (the rounded
-// value and the rounded remainder: 16 bits of bf16, 22 of fp16).
+// value and the rounded remainder: 16 bits of bf16, 22 of fp16).  fp16 has a power of two per row taken off before and put back on the
+// sums, so that neither end of its range is in the way.
 #include "common.h"
 
 #include <algorithm>
@@ -75,6 +76,7 @@ __global__ __launch_bounds__(64 * LORA_WAVES) void token_lora_kernel(LoraArgs a)
     constexpr int BATCH = KR <= 1 ? (F32 ? 4 : 5) : KR <= 2 ? 2 : 1;          // stretches whose operands are on their way together
     __shared__ float red[LORA_WAVES][16][RED];
     __shared__ uint4 hbuf[(F32 ? 1 : 2) * 16 * HROW / VW];
+    __shared__ float hscale[16];                                  // fp16: what the rows' sums are multiplied by at the end
     T* const hs = reinterpret_cast<T*>(hbuf);                     // [value, remainder][16][HROW]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, quarter = lane >> 4;
@@ -162,12 +164,27 @@ __global__ __launch_bounds__(64 * LORA_WAVES) void token_lora_kernel(LoraArgs a)
             const int mine = __shfl(id, t);
             if (mine < 0 || (mine != cur0 && mine != cur1)) continue;
             const float alpha = a.alpha != nullptr ? a.alpha[mine] : 1.0f;
+            float v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = 4 * q + i < a.rank ? alpha * s[i] : 0.0f;
+            if constexpr (__is_same(T, f16)) {                    // the row's largest value to 2^14..2^15 (4 RT lanes hold the row)
+                unsigned top = 0u;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+#pragma unroll
+                for (int x = 1; x < 4 * RT; x <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, x));
+                const int e = min(max((int)(top >> 23), 27), 254);         // (a row of zeros, of infinities)
+                const float down = __uint_as_float((unsigned)(127 + 127 + 14 - e) << 23);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] *= down;
+                if (q == 0) hscale[t] = __uint_as_float((unsigned)(e - 14) << 23);
+            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float v = 4 * q + i < a.rank ? alpha * s[i] : 0.0f;
-                const T h = from_f32<T>(v);
+                const T h = from_f32<T>(v[i]);
                 hs[t * HROW + 4 * q + i] = h;
-                if constexpr (!F32) hs[(16 + t) * HROW + 4 * q + i] = from_f32<T>(v - to_f32(h));
+                // (an infinity has no remainder: its difference to itself would be NaN)
+                if constexpr (!F32) hs[(16 + t) * HROW + 4 * q + i] = from_f32<T>(fabsf(to_f32(h)) == INFINITY ? 0.0f : v[i] - to_f32(h));
             }
         }
         __syncthreads();
@@ -181,6 +198,8 @@ __global__ __launch_bounds__(64 * LORA_WAVES) void token_lora_kernel(LoraArgs a)
         hv[s] = *(const uint4*)(hs + l16 * HROW + s * KS + VW * quarter);
         if constexpr (!F32) hl[s] = *(const uint4*)(hs + (16 + l16) * HROW + s * KS + VW * quarter);
     }
+    float back = 1.0f;
+    if constexpr (__is_same(T, f16)) back = hscale[l16];
     int u0 = (blockIdx.y * LORA_WAVES + wave) * a.span;
     const int u_end = min(u0 + a.span, (a.Cout + CU - 1) / CU);
     for (; u0 < u_end; u0 += BATCH) {
@@ -223,7 +242,7 @@ __global__ __launch_bounds__(64 * LORA_WAVES) void token_lora_kernel(LoraArgs a)
                 // (taken over by the adapter's own rows, not added as zeros: what another adapter holds may be no number)
 #pragma unroll
                 for (int t = 0; t < TU; ++t)
-                    if (id == cur) sum[i][t] = acc[t];
+                    if (id == cur) sum[i][t] = __is_same(T, f16) ? acc[t] * back : acc[t];
             }
         }
 #pragma unroll
@@ -288,6 +307,9 @@ extern "C" int sige_token_lora(const void* x, sige_dtype dt, int32_t Cin, int32_
     SIGE_REQUIRE(x && down && up && ids && y, SIGE_ERR_INVALID_ARG, "%s: x, down, up, ids and y are required", who);
     SIGE_REQUIRE(aligned16(x) && aligned16(down) && aligned16(up) && aligned16(base) && aligned16(y), SIGE_ERR_UNSUPPORTED,
                  "%s: pointers must be 16-byte aligned", who);
+    SIGE_REQUIRE(x != y, SIGE_ERR_UNSUPPORTED, "%s: y cannot be x", who);
+    SIGE_REQUIRE(y != base || y_ld == base_ld, SIGE_ERR_UNSUPPORTED, "%s: y == base needs the same row stride", who);
+    SIGE_REQUIRE(rows <= (1 << 28) - 16, SIGE_ERR_UNSUPPORTED, "%s: too many rows", who);        // (16 per workgroup of 256, a launch has 2^32 threads)
     LoraArgs a;
     a.x = x; a.down = down; a.up = up; a.base = base; a.y = y; a.alpha = alpha; a.ids = ids; a.count = count;
     a.Cin = Cin; a.Cout = Cout; a.rank = rank; a.adapters = n_adapters; a.x_ld = x_ld; a.base_ld = base_ld; a.y_ld = y_ld;

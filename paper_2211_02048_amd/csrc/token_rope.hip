@@ -129,6 +129,7 @@ static int rope_entry(const char* who, RopeArgs& a, sige_dtype dt, int rows, sig
     if (rows == 0) return SIGE_OK;
     SIGE_REQUIRE(a.x && a.y && a.pairs && (a.positions || a.indices), SIGE_ERR_INVALID_ARG, "%s: x, y, the table and the positions are required", who);
     SIGE_REQUIRE(aligned16(a.x) && aligned16(a.y) && aligned16(a.pairs), SIGE_ERR_UNSUPPORTED, "%s: pointers must be 16-byte aligned", who);
+    SIGE_REQUIRE(a.x != a.y || a.x_ld == a.y_ld, SIGE_ERR_UNSUPPORTED, "%s: x == y needs the same row stride", who);
     int w = vw;                                    // the split layout: as wide as n_pairs allows
     if (layout == SIGE_ROPE_HALVES)
         while (a.n_pairs % w) w /= 2;

@@ -148,3 +148,60 @@ def test_the_binding_refuses_what_it_can_see():
         api.sige_cache4_store(q, q, small, 32, 2, 64, n_rows=4)
     with pytest.raises(api.SigeError, match="contiguous"):
         api.sige_token_lora(q, q, 128, 128, torch.zeros(2, 8, 128), torch.zeros(2, 8, 128), None, 4, n_rows=4)
+
+
+def test_more_than_a_launch_can_have(L):
+    """Calls of more threads than a launch has, aliases whose rows lie at other distances, tokens whose chunks would end past an int."""
+    big = 2 ** 31 - 1
+    assert rope(L, mr=big, n=big) == 2
+    assert rope(L, y=FAKE, y_ld=168) == 2 and "stride" in err(L)
+    assert L.sige_cache4_store(FAKE, 320, FAKE, 320, 2, 8, 40, None, 0, None, 0, 2 ** 27, 2 ** 27, FAKE, 2 ** 27, None) == 2 and "rows" in err(L)
+    assert L.sige_cache4_load(FAKE, 2 ** 27, 2, 8, 40, 0, 2 ** 27, FAKE, 320, FAKE, 320, None) == 2
+    assert L.sige_cache4_attn(FAKE, 320, FAKE, big, 2, 8, big, 8, 40, F, None, FAKE, 320, None, 0, None) == 2 and "tokens" in err(L)
+    for dt, d in ((2, 40), (1, 128), (0, 256)):
+        assert L.sige_cache4_attn(FAKE, 8 * d, FAKE, 64, dt, big, 64, 8, d, F, None, FAKE, 8 * d, None, 0, None) == 2 and "queries" in err(L)
+    other = ctypes.c_void_p(0x20000)
+    lora = lambda n=8, y=other, base=None, base_ld=64, y_ld=64: L.sige_token_lora(  # noqa: E731
+        FAKE, 1, 320, 320, None, 4, n, n, FAKE, FAKE, 8, 2, None, FAKE, base, base_ld, 64, y, y_ld, None)
+    assert lora(y=FAKE) == 2 and "y cannot be x" in err(L)
+    assert lora(base=other, y_ld=72) == 2 and "stride" in err(L)
+    assert lora(n=2 ** 28) == 2 and "rows" in err(L)
+
+
+def test_the_binding_refuses_tables_and_types():
+    """Tables of another type or too short (ids of 64 bits, ranges of fewer rows), operands of different types."""
+    h, i = torch.bfloat16, torch.int32
+    x = torch.zeros(8, 128, dtype=h)
+    cache = torch.zeros(api.sige_cache4_bytes(2, 64, 32), dtype=torch.uint8)
+    table = torch.zeros(32, 4, dtype=i)
+    g = good()
+    idx, cnt = torch.zeros(2, 2, dtype=i), torch.zeros(1, dtype=i)
+    down, up = torch.zeros(2, 8, 128, dtype=h), torch.zeros(2, 128, 8, dtype=h)
+    calls = {
+        "bfloat16": [lambda: api.sige_token_rope(x, x.float(), 2, 64, table, torch.zeros(8, 2), n_rows=8),
+                     lambda: api.sige_cache4_store(x, x.float(), cache, 32, 2, 64, n_rows=8),
+                     lambda: api.sige_cache4_load(cache, 32, 2, 64, x, x.half()),
+                     lambda: api.sige_cache4_attn(x, cache, 32, x.float(), 1.0, T=4, heads=2, d=64),
+                     lambda: api.sige_token_lora(x, x, 128, 128, down.float(), up, torch.zeros(2, dtype=i), 4, n_rows=8),
+                     lambda: api.sige_token_lora(x, x, 128, 128, down, up, torch.zeros(2, dtype=i), 4, base=x.float(), n_rows=8)],
+        "pairs": [lambda: api.sige_token_rope(x, x, 2, 64, table.long(), torch.zeros(8, 2), n_rows=8)],
+        "positions": [lambda: api.sige_token_rope(x, x, 2, 64, table, torch.zeros(8, 2, dtype=torch.float64), n_rows=8),
+                      lambda: api.sige_token_rope(x, x, 2, 64, table, torch.zeros(7, 2), n_rows=8),
+                      lambda: api.sige_token_rope(x, x, 2, 64, table, torch.zeros(2, 8).t(), n_rows=8)],
+        "indices": [lambda: api.sige_token_rope_blocks(x, x, 2, 64, table, g, idx.long(), cnt),
+                    lambda: api.sige_cache4_store_blocks(x, x, cache, 32, 2, 64, g, idx, cnt, n_blocks=3),
+                    lambda: api.sige_cache4_attn_blocks(x, g, idx, 3, cache, 32, x, 1.0, T=4, heads=2, d=64)],
+        "count": [lambda: api.sige_token_rope_blocks(x, x, 2, 64, table, g, idx, cnt.long())],
+        "slots": [lambda: api.sige_cache4_store(x, x, cache, 32, 2, 64, slots=torch.zeros(8, dtype=torch.int64), n_rows=8),
+                  lambda: api.sige_cache4_store(x, x, cache, 32, 2, 64, slots=torch.zeros(7, dtype=i), n_rows=8)],
+        "ranges": [lambda: api.sige_cache4_attn(x, cache, 32, x, 1.0, T=4, heads=2, d=64, ranges=torch.zeros(7, 2, dtype=i)),
+                   lambda: api.sige_cache4_attn(x, cache, 32, x, 1.0, T=4, heads=2, d=64, ranges=torch.zeros(8, 2)),
+                   lambda: api.sige_cache4_attn_blocks(x, g, idx, 2, cache, 32, x, 1.0, T=4, heads=2, d=64, ranges=torch.zeros(31, 2, dtype=i))],
+        "ids": [lambda: api.sige_token_lora(x, x, 128, 128, down, up, torch.zeros(2, dtype=torch.int64), 4, n_rows=8),
+                lambda: api.sige_token_lora(x, x, 128, 128, down, up, torch.zeros(2, dtype=i), 3, n_rows=8)],
+        "alpha": [lambda: api.sige_token_lora(x, x, 128, 128, down, up, torch.zeros(2, dtype=i), 4, alpha=torch.zeros(1), n_rows=8)],
+    }
+    for what, bad in calls.items():
+        for call in bad:
+            with pytest.raises(api.SigeError, match=what):
+                call()

@@ -97,6 +97,31 @@ def test_ids_counts_and_neighbours(dtype):
     assert (y == 0).all()
 
 
+@pytest.mark.parametrize("rank", [8, 24, 64, 128])
+def test_middle_vectors_beyond_the_range_of_fp16(rank):
+    """down x above 65504 and far below 2^-14, up the other way round: the results are ordinary numbers.  Infinite ones stay infinite."""
+    rows, per, cin, cout, n = 37, 3, 256, 72, 4
+    x, down, up, ids, alpha, base = make(rank, rows, per, cin, cout, rank, n, "f16")
+    size = torch.tensor([2.0 ** 14, 1.0, 2.0 ** -13, 0.0], device="cuda").half().view(n, 1, 1)
+    alpha = torch.tensor([512.0, 1.0, 2.0 ** -8, 3.0], device="cuda")
+    down = down * size
+    up = up * torch.tensor([2.0 ** -13, 1.0, 2.0 ** 8, 1.0], device="cuda").half().view(n, 1, 1)
+    x = x / 64
+    for b in (base, None):
+        want, mag = expected(x, down, up, ids, per, alpha, b, cout)
+        y = torch.empty(rows, cout, dtype=torch.float16, device="cuda")
+        api.sige_token_lora(x, y, cin, cout, down, up, ids, per, alpha=alpha, base=b, n_rows=rows)
+        torch.cuda.synchronize()
+        # as in close(), and half a step of fp16's subnormal results
+        bound = ((cin + rank + 4) * 2.0 ** -24 + 2.0 ** -16) * mag + 2.0 ** -11 * np.abs(want) + 2.0 ** -25
+        assert (np.abs(f64(y) - want) <= bound).all(), np.max(np.abs(f64(y) - want) / bound)
+    x[5, 3] = float("inf")
+    want, _ = expected(x, down, up, ids, per, alpha, base, cout)
+    api.sige_token_lora(x, y, cin, cout, down, up, ids, per, alpha=alpha, base=base, n_rows=rows)
+    torch.cuda.synchronize()
+    assert np.array_equal(np.isfinite(f64(y)), np.isfinite(want))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 def test_attention_layer_of_an_edit(dtype):
     """One attention layer of an edited image as it is used, captured into a graph: block list -> tokens normalised -> adapters per
@@ -169,3 +194,45 @@ def test_attention_layer_of_an_edit(dtype):
         q64 = f64(rot[:, :C]).reshape(n_tok, heads, d)
         want, mag = ref.attention(q64, k, v, scale)
         attn_close(o, want, mag, q64, k, scale, dtype, T, "attention")
+
+
+def test_calls_kept_and_made_again_and_what_the_binding_refuses():
+    """The new calls in a recorded list; rows that do not lie at one distance."""
+    heads, d, rows = 2, 64, 24
+    C = heads * d
+    x = torch.randn(rows, 3 * C, device="cuda").bfloat16()
+    base = torch.randn(rows, C, device="cuda").bfloat16()
+    down, up = torch.randn(2, 8, C, device="cuda").bfloat16(), torch.randn(2, C, 8, device="cuda").bfloat16()
+    ids = torch.tensor([0, 1, 1], dtype=torch.int32, device="cuda")
+    table, pos = api.sige_rope_pairs((16, 16)), torch.rand(rows, 2, device="cuda") * 50
+    cache = torch.zeros(api.sige_cache4_bytes(heads, d, rows), dtype=torch.uint8, device="cuda")
+    y, z, o = (torch.empty_like(base) for _ in range(3))
+
+    def step():
+        api.sige_token_lora(x[:, :C], y, C, C, down, up, ids, 8, base=base, n_rows=rows)
+        api.sige_token_rope(y, z, heads, d, table, pos, n_rows=rows)
+        api.sige_cache4_store(z, x[:, 2 * C:], cache, rows, heads, d, n_rows=rows)
+        api.sige_cache4_attn(z, cache, rows, o, 0.1, T=rows, heads=heads, d=d)
+    with api.record() as calls:
+        step()
+    assert len(calls) == 4
+    x.copy_(torch.randn(rows, 3 * C, device="cuda"))
+    calls.run()
+    torch.cuda.synchronize()
+    got = o.clone()
+    o.fill_(7.0)
+    step()
+    torch.cuda.synchronize()
+    assert torch.equal(got, o)
+    three = x.view(2, 12, 3 * C)
+    for call in (lambda: api.sige_token_rope(x.t(), z, heads, d, table, pos, n_rows=rows),
+                 lambda: api.sige_token_rope(x.view(3, 8, 3 * C)[:, :4, :C], z, heads, d, table, pos, n_rows=12),
+                 lambda: api.sige_cache4_store(three, three, cache, rows, heads, d, n_rows=2),
+                 lambda: api.sige_cache4_attn(three, cache, rows, o, 0.1, T=rows, heads=heads, d=d),
+                 lambda: api.sige_token_lora(x[:, ::3], y, C, C, down, up, ids, 8, n_rows=rows)):
+        with pytest.raises(api.SigeError, match="rows of"):
+            call()
+    tiles = x.view(6, 2, 2, 3 * C)[..., :C]       # stacked tiles, a channel range of each: rows at one distance
+    api.sige_token_lora(tiles, z, C, C, down, up, ids, 8, base=base, n_rows=rows)
+    torch.cuda.synchronize()
+    assert torch.equal(z, y)
