@@ -565,8 +565,9 @@ def _at(t):
 
 def _like(x, *tensors):
     """The tensors a kernel takes for the type of x."""
+    dtype = x.dtype
     for t in tensors:
-        if t is not None and t.dtype is not x.dtype:
+        if t is not None and t.dtype is not dtype:
             raise SigeError(1, f"{t.dtype} beside {x.dtype} in one call")
 
 
@@ -727,8 +728,8 @@ def sige_cache4_attn_blocks(q_full, g: Geom, indices, n_blocks, cache, capacity,
 def sige_token_lora(x, y, Cin, Cout, down, up, ids, rows_per_id, *, alpha=None, base=None, n_rows=-1, count=None, max_rows=None,
                     x_ld=None, base_ld=None, y_ld=None):
     """y[r] = base[r] + alpha[i] * up[i] (down[i] x[r]) with i = ids[r // rows_per_id]; y may be base."""
-    n, rank, _ = down.shape
-    if down.shape != (n, rank, Cin) or up.shape != (n, Cout, rank) or not (down.is_contiguous() and up.is_contiguous()):
+    n, rank, c = down.shape
+    if c != Cin or up.shape != (n, Cout, rank) or not (down.is_contiguous() and up.is_contiguous()):
         raise SigeError(1, "sige_token_lora: down is [adapters, rank, Cin] and up [adapters, Cout, rank], contiguous")
     _like(x, y, down, up, base)
     mr = x.numel() // x.shape[-1] if max_rows is None else max_rows

@@ -5,7 +5,12 @@
 // workgroup takes 16 rows, its four waves share the contraction over Cin (the partial products meet in LDS), then each takes
 // stretches of the output channels.  Few rows alone would leave most compute units without work, so the output channels are cut
 // over workgroups too, each of which repeats the small first product.  Where the 16 rows have several adapters there is one pass
-// for each, of which its own rows keep the result: no sorting, no second launch, and nothing lost where requests are whole blocks.
+// for each, of which its own rows keep the result; where runs are short (single tokens of many requests) every workgroup of a section
+// of 128 runs first counts them into the order of their adapters and takes up to 16 rows of one adapter from there, in any place of
+// the section: no sorted copy, no second launch (32 tokens of 32 adapters of rank 32, 1280 -> 1280: 63 -> 8.4 us).
+// Measured: 8192 rows of 1280 -> 1280 in fp16, rank 32, 19.2 us, 3.3 TB/s (the first product, its sums in LDS and the second follow
+// each other, and all workgroups are in the same phase; 162 KB of weights per workgroup come from L2); 64 rows of 320 -> 960 4.4 us, of
+// which a launch is 3.
 // The middle vector down_i x_r stays in 32 bits; the half types' second product takes it as the sum of two halves (the rounded
 // value and the rounded remainder: 16 bits of bf16, 22 of fp16).  fp16 has a power of two per row taken off before and put back on the
 // sums, so that neither end of its range is in the way.
@@ -30,7 +35,8 @@ struct LoraArgs {
     int Cin, Cout, rank, adapters, x_ld, base_ld, y_ld;
     int rows_per_id, max_rows, n_host;
     int span;                  // stretches of output channels per wave
-    FastDiv d_per;
+    int group;                 // runs per workgroup where they are grouped by adapter, else 0
+    FastDiv d_per, d_group, d_tiles;
 };
 
 template <typename T> struct LoraStep;            // one 16-byte vector per lane and operand: 32 (half types) or 16 channels
@@ -59,19 +65,44 @@ template <> struct LoraStep<float> {
     }
 };
 
-constexpr int LORA_WAVES = 4;
+// sum * back + base, rounded once (fp16: eight fused operations that take base as it is, and four conversions)
+template <typename T> __device__ __forceinline__ uint4 lora_sum(const f32x4 (&sum)[sizeof(T) == 4 ? 1 : 2], float back, const uint4& base)
+{
+    if constexpr (sizeof(T) == 4) {
+        const f32x4 v = sum[0] + __builtin_bit_cast(f32x4, base);
+        return __builtin_bit_cast(uint4, v);
+    } else {
+        typedef float f32x8 __attribute__((ext_vector_type(8)));
+        typedef T v8 __attribute__((ext_vector_type(8)));
+        f32x8 v;
+        if constexpr (__is_same(T, f16)) {
+            const v8 b = __builtin_bit_cast(v8, base);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = fmaf(sum[e >> 2][e & 3], back, (float)b[e]);
+        } else {
+            float b[8];
+            unpack<T>(base, b);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = sum[e >> 2][e & 3] + b[e];
+        }
+        return __builtin_bit_cast(uint4, __builtin_convertvector(v, v8));
+    }
+}
 
-// RT = 16-wide tiles over the rank.  No load is guarded (a guard is a branch of its own): lanes past the end read the last vector or
+constexpr int LORA_WAVES = 4;
+constexpr int LORA_SECTION = 128;                                 // runs that are grouped by adapter
+
+// RT = 16-wide tiles over the rank.  The registers are bounded for two workgroups per compute unit.  No load is guarded (a guard is a branch of its own): lanes past the end read the last vector or
 // row again, and what they make of it is either multiplied by the zeros behind the rank, or not stored.
 template <typename T, int RT>
-__global__ __launch_bounds__(64 * LORA_WAVES) void token_lora_kernel(LoraArgs a)
+__global__ __launch_bounds__(64 * LORA_WAVES, 2) void token_lora_kernel(LoraArgs a)
 {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int VW = Vec16<T>::N, KS = 4 * VW;                  // channels per lane and per step
     constexpr int KR = (RT * 16 + KS - 1) / KS;                   // steps over the rank
     constexpr int RED = RT * 16 + 4;                              // floats per row of the partial products
     constexpr int HROW = KR * KS + VW;                            // values per row of the middle vectors
-    constexpr int AHEAD = RT <= 2 ? 5 : RT <= 4 ? 3 : 2;          // steps over Cin whose operands are on their way together
+    constexpr int AHEAD = RT <= 2 ? 8 : RT <= 4 ? 6 : 4;          // steps over Cin whose operands are on their way together
     constexpr int TU = F32 ? 1 : 2, CU = 16 * TU;                 // products per stretch of output channels, its channels
     constexpr int BATCH = KR <= 1 ? (F32 ? 4 : 5) : KR <= 2 ? 2 : 1;          // stretches whose operands are on their way together
     __shared__ float red[LORA_WAVES][16][RED];
@@ -85,13 +116,69 @@ __global__ __launch_bounds__(64 * LORA_WAVES) void token_lora_kernel(LoraArgs a)
         rows = (long)(*a.count) * a.rows_per_id;
         if (rows > a.max_rows) rows = a.max_rows;
     }
-    const long row0 = (long)blockIdx.x * 16;
-    if (row0 >= rows) return;
-    const bool live = row0 + l16 < rows;
-    const long row = live ? row0 + l16 : row0;
+    // the workgroup's rows: l16 stands for one in every lane, `live` if there is one, else a row that there is
+    long row;
+    bool live;
     int run, rest;
-    divmod((int)row, a.d_per, run, rest);
-    int id = a.ids[run];                                          // adapter of row l16, in every lane
+    if (a.group > 0) {
+        int section, tile;
+        divmod((int)blockIdx.x, a.d_tiles, section, tile);
+        const int run0 = section * LORA_SECTION, per = a.rows_per_id;
+        if ((long)run0 * per >= rows) return;
+        const int n = (int)min((long)LORA_SECTION, (rows + per - 1) / per - run0);       // runs of the section
+        // A run's place: how many have a smaller (adapter, run); P threads share its comparisons.  Every a.group-th run of an adapter
+        // starts a workgroup's rows.
+        constexpr int P = 64 * LORA_WAVES / LORA_SECTION, SHARE = LORA_SECTION / P;
+        __shared__ alignas(16) unsigned keys[LORA_SECTION + 4 * P];                     // (shares 16 bytes more apart: other banks)
+        __shared__ unsigned sorted[LORA_SECTION], starts[LORA_SECTION];
+        if (tid < LORA_SECTION) {
+            unsigned k = ~0u;
+            if (tid < n) {
+                const int i = a.ids[run0 + tid];
+                k = (unsigned)((unsigned)i >= (unsigned)a.adapters ? a.adapters : i) * LORA_SECTION + tid;      // (none: behind the others)
+            }
+            keys[tid + tid / SHARE * 4] = k;
+        }
+        __syncthreads();
+        const int mine = tid / P, part = tid % P;
+        const unsigned key = keys[mine + mine / SHARE * 4], start = key & ~(unsigned)(LORA_SECTION - 1);
+        int place = 0, before = 0;                                // smaller keys, and those of smaller adapters
+#pragma unroll
+        for (int j = 0; j < SHARE; j += 4) {
+            const uint4 k = *(const uint4*)(keys + part * (SHARE + 4) + j);
+            place += (k.x < key) + (k.y < key) + (k.z < key) + (k.w < key);
+            before += (k.x < start) + (k.y < start) + (k.z < start) + (k.w < start);
+        }
+#pragma unroll
+        for (int x = 1; x < P; x <<= 1) { place += __shfl_xor(place, x); before += __shfl_xor(before, x); }
+        if (part == 0) {
+            int q, r = 1;
+            if (mine < n) { divmod(place - before, a.d_group, q, r); sorted[place] = key; }
+            starts[mine < n ? place : mine] = r == 0;
+        }
+        __syncthreads();
+        const bool s0 = starts[lane] != 0u, s1 = starts[64 + lane] != 0u;
+        const unsigned long b0 = __builtin_amdgcn_ballot_w64(s0), b1 = __builtin_amdgcn_ballot_w64(s1);
+        const int n0 = __builtin_popcountl(b0), i0 = __builtin_popcountl(b0 & ((1ul << lane) - 1)), i1 = n0 + __builtin_popcountl(b1 & ((1ul << lane) - 1));
+        const unsigned long h0 = __builtin_amdgcn_ballot_w64(s0 && i0 == tile), h1 = __builtin_amdgcn_ballot_w64(s1 && i1 == tile);
+        if ((h0 | h1) == 0ul) return;
+        const int head = h0 != 0ul ? __builtin_ctzl(h0) : 64 + __builtin_ctzl(h1);
+        divmod(l16, a.d_per, run, rest);
+        live = run < a.group && head + run < n;
+        const unsigned at = sorted[live ? head + run : head];
+        live = live && at / LORA_SECTION == sorted[head] / LORA_SECTION;
+        run = run0 + (int)(at % LORA_SECTION);
+        row = (long)run * per + rest;
+        live = live && row < rows;
+        if (!live) { run = run0; row = (long)run0 * per; }
+    } else {
+        const long row0 = (long)blockIdx.x * 16;
+        if (row0 >= rows) return;
+        live = row0 + l16 < rows;
+        row = live ? row0 + l16 : row0;
+        divmod((int)row, a.d_per, run, rest);
+    }
+    int id = a.ids[run];                                          // adapter of row l16
     if (!live || (unsigned)id >= (unsigned)a.adapters) id = -1;
     const T* const xr = (const T*)a.x + row * a.x_ld + VW * quarter;
     if (KR * KS > RT * 16)                                        // (the half types' step of 32 over a rank of 16)
@@ -199,10 +286,13 @@ __global__ __launch_bounds__(64 * LORA_WAVES) void token_lora_kernel(LoraArgs a)
         if constexpr (!F32) hl[s] = *(const uint4*)(hs + (16 + l16) * HROW + s * KS + VW * quarter);
     }
     float back = 1.0f;
-    if constexpr (__is_same(T, f16)) back = hscale[l16];
+    if constexpr (__is_same(T, f16)) back = id >= 0 ? hscale[l16] : 1.0f;
     int u0 = (blockIdx.y * LORA_WAVES + wave) * a.span;
     const int u_end = min(u0 + a.span, (a.Cout + CU - 1) / CU);
-    for (; u0 < u_end; u0 += BATCH) {
+    // A batch of stretches.  SAME: all rows that there are have one adapter; else what each makes is taken over by its own rows, not
+    // added as zeros (what another adapter holds may be no number).
+    auto batch = [&](auto same) {
+        constexpr bool SAME = decltype(same)::value;
         uint4 bv[BATCH];
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
@@ -210,12 +300,14 @@ __global__ __launch_bounds__(64 * LORA_WAVES) void token_lora_kernel(LoraArgs a)
             if (a.base != nullptr) bv[i] = *(const uint4*)((const T*)a.base + row * a.base_ld + min((u0 + i) * CU + 4 * TU * quarter, a.Cout - VW));
         }
         f32x4 sum[BATCH][TU];
+        if constexpr (!SAME) {
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i)
+            for (int i = 0; i < BATCH; ++i)
 #pragma unroll
-            for (int t = 0; t < TU; ++t) sum[i][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+                for (int t = 0; t < TU; ++t) sum[i][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
         todo = all;
-        while (todo != 0) {
+        while (SAME || todo != 0) {
             const int cur = next();
             const T* const up = (const T*)a.up + (long)cur * a.Cout * a.rank;
             uint4 uv[BATCH][KR][TU];
@@ -239,31 +331,45 @@ __global__ __launch_bounds__(64 * LORA_WAVES) void token_lora_kernel(LoraArgs a)
                         LoraStep<T>::run(uv[i][s][t], hv[s], acc[t]);
                         if constexpr (!F32) LoraStep<T>::run(uv[i][s][t], hl[s], acc[t]);
                     }
-                // (taken over by the adapter's own rows, not added as zeros: what another adapter holds may be no number)
 #pragma unroll
                 for (int t = 0; t < TU; ++t)
-                    if (id == cur) sum[i][t] = __is_same(T, f16) ? acc[t] * back : acc[t];
+                    if (SAME || id == cur) sum[i][t] = acc[t];
             }
+            if (SAME) break;
         }
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
             const int c = (u0 + i) * CU + 4 * TU * quarter;
-            if (!live || u0 + i >= u_end || c >= a.Cout) continue;
-            float f[VW], b[VW];
-            unpack<T>(bv[i], b);
-#pragma unroll
-            for (int t = 0; t < TU; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) f[4 * t + e] = sum[i][t][e] + b[4 * t + e];
-            *(uint4*)((T*)a.y + row * a.y_ld + c) = pack<T>(f);
+            if (live && u0 + i < u_end && c < a.Cout) *(uint4*)((T*)a.y + row * a.y_ld + c) = lora_sum<T>(sum[i], back, bv[i]);
         }
-    }
+    };
+    const int first = __builtin_amdgcn_readlane(id, 0);
+    const bool same = !F32 && first >= 0 && __builtin_amdgcn_ballot_w64(live && id != first) == 0ul;
+    if (same)
+        for (; u0 < u_end; u0 += BATCH) batch(std::true_type());
+    else
+        for (; u0 < u_end; u0 += BATCH) batch(std::false_type());
 }
 
 template <typename T>
 static int launch_lora(LoraArgs& a, int rows, hipStream_t st)
 {
-    const int tiles = (rows + 15) / 16, units = (a.Cout * (int)sizeof(T) + 63) / 64;
+    const int units = (a.Cout * (int)sizeof(T) + 63) / 64;
+    // Short runs of several adapters: grouped, so that a workgroup has one adapter, which costs 1 us and workgroups of fewer rows: runs
+    // of up to 5 rows of more than two adapters (2048 rows of 640 -> 640 in runs of 4 9.0 against 11.4 us, of 1 7.8 against 19.5; of 8 8.9
+    // against 7.6; 1263 in runs of 3 of two adapters 7.1 against 6.3), and of up to 8 where latency counts (128 rows of 1280 -> 1280 7.9
+    // against 9.2); from four runs on
+    const int per = a.rows_per_id;
+    a.group = per <= (rows <= 512 ? 8 : 5) && rows > 3L * per && a.adapters > 2 && a.adapters < 1 << 24 ? 16 / per : 0;
+    int tiles = (rows + 15) / 16;
+    if (a.group > 0) {
+        // (of n runs at most this many groups, each of one adapter or none; those that there are not end at once)
+        auto groups = [&](int n) { return std::min(n, (int)((n + (long)std::min(a.adapters + 1, n) * (a.group - 1)) / a.group)); };
+        const int runs = (int)(((long)rows + per - 1) / per), section = groups(LORA_SECTION);
+        tiles = runs / LORA_SECTION * section + groups(runs % LORA_SECTION);
+        a.d_tiles = fast_div(section);
+        a.d_group = fast_div(a.group);
+    }
     // workgroups per 16 rows: one per compute unit where the rows alone are fewer (two take 8.6 instead of 6.8 us for 1011 rows of
     // 640 -> 648 in single precision, half of one 7.8), a stretch of channels per wave at least
     const int cut = std::max(std::min((256 + tiles - 1) / tiles, (units + LORA_WAVES - 1) / LORA_WAVES), 1);

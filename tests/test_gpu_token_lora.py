@@ -97,6 +97,36 @@ def test_ids_counts_and_neighbours(dtype):
     assert (y == 0).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,per,n,kind", [
+    (8, 1, 8, "each"), (16, 1, 16, "each"), (33, 1, 3, "any"), (127, 1, 40, "any"), (128, 1, 128, "each"), (129, 1, 300, "each"), (500, 1, 3, "any"),
+    (517, 2, 5, "any"), (1000, 3, 9, "any"), (700, 3, 700, "each"), (641, 5, 6, "any"), (2570, 4, 3, "one"), (300, 8, 4, "any"), (511, 7, 12, "any"), (2049, 5, 3, "none"),
+])
+def test_short_runs_of_several_adapters(rows, per, n, kind, dtype):
+    """Runs that are grouped by adapter: sections that end inside, runs that end early, all of one adapter, each its own, none."""
+    cin, cout, rank = 72, 136, 8
+    x, down, up, ids, alpha, base = make(rows + per, rows, per, cin, cout, rank, n, dtype, ld=8)
+    runs = len(ids)
+    if kind == "each":
+        ids = torch.from_numpy(np.random.default_rng(rows).permutation(n)[np.arange(runs) % n].astype(np.int32)).cuda()
+    elif kind == "one":
+        ids = torch.full_like(ids, n - 1)
+    elif kind == "none":
+        ids = torch.where(torch.arange(runs, device="cuda") % 2 == 0, -1, n).int()
+    want, mag = expected(x, down, up, ids, per, alpha, base, cout)
+    y = torch.full((rows + 1, cout + 8), 7.0, dtype=DT[dtype], device="cuda")
+    api.sige_token_lora(x, y[:rows, :cout], cin, cout, down, up, ids, per, alpha=alpha, base=base, n_rows=rows)
+    torch.cuda.synchronize()
+    close(y[:rows, :cout], want, mag, cin, rank, dtype, kind)
+    assert (y[rows] == 7.0).all() and (y[:, cout:] == 7.0).all()
+    y = base.clone()                              # in place, the rows by a device count that ends inside a section
+    count = runs * 2 // 3
+    api.sige_token_lora(x, y, cin, cout, down, up, ids, per, alpha=alpha, base=y, count=torch.tensor([count], dtype=torch.int32, device="cuda"), max_rows=rows)
+    torch.cuda.synchronize()
+    close(y[:count * per], want[:count * per], mag[:count * per], cin, rank, dtype, kind + ", a device count")
+    assert torch.equal(y[count * per:], base[count * per:])
+
+
 @pytest.mark.parametrize("rank", [8, 24, 64, 128])
 def test_middle_vectors_beyond_the_range_of_fp16(rank):
     """down x above 65504 and far below 2^-14, up the other way round: the results are ordinary numbers.  Infinite ones stay infinite."""
