@@ -40,11 +40,12 @@ struct Cache4AttnArgs {
     const int32_t* q_blocks;   // queries by block list, as sige_sparse_attn_blocks
     long section, cap, scales; // of Cache4Layout
     int q_ld, o_ld, Nq, T, heads, d;
-    int splits, chunks_per_split;
+    int splits, share;         // workgroups that share the tokens of a query out, and their chunks of all T
+    int waves;                 // of a workgroup, where they share its tokens out: 1, 2, 4 or 8
     int full, gs_log2;
     float scale_log2e;
     int q_tpb, q_bw, q_H, q_W;
-    FastDiv d_heads, d_tpb, d_qbw, d_dq;
+    FastDiv d_heads, d_tpb, d_qbw, d_dq, d_splits;
 };
 
 template <typename T> struct Cache4Compute { typedef bf16 type; static constexpr int parts = 1; static constexpr unsigned last = CACHE4_LAST; };
@@ -129,6 +130,21 @@ struct Cache4Seen {
     int lo, hi;                    // the wave: the first token that some row sees, the end of the last one
     int lo_most, hi_least;         // the tokens between are seen by all rows
     __device__ __forceinline__ bool partial(int t0, int n) const { return t0 < lo_most || (long)t0 + n > hi_least; }
+    // whether some row of this wave sees some of n tokens
+    __device__ __forceinline__ bool any(long t0, int n) const { return __builtin_amdgcn_ballot_w64(!none && begin < t0 + n && end > t0) != 0ull; }
+    // The chunks of n tokens of split z: an equal share of those between lo and hi, whatever part of the cache they are
+    __device__ __forceinline__ void chunks(const Cache4AttnArgs& a, int n, int z, int& first, int& last) const
+    {
+        int c0 = 0, c1 = (int)(((long)hi + n - 1) / n), per = a.share;
+        if (a.ranges != nullptr) {
+            int rest;
+            c0 = lo / n;
+            c1 = max(c1, c0);
+            divmod(c1 - c0 + a.splits - 1, a.d_splits, per, rest);
+        }
+        first = c0 + z * per;
+        last = min(first + per, c1);
+    }
 };
 __device__ __forceinline__ Cache4Seen cache4_seen(const Cache4AttnArgs& a, int qi)
 {
@@ -333,6 +349,7 @@ constexpr int cache4_apart_side(int DT, int parts) { return parts > 1 ? (DT <= 3
 // Many queries, half types.  Heads up to 64: four waves per SIMD, two workgroups side by side (4096 queries of 4096 x 8 of 64 74 -> 64 us,
 // of 40 62 -> 50; one query of 65536 keys 15.1 -> 16.1).  Larger heads have no registers for that: the common form.
 constexpr bool cache4_crowds(int DT, int parts) { return parts == 1 && DT <= 2; }
+constexpr int CACHE4_CROWD_WAVES = 4;              // of a workgroup (eight: 1500 queries of 1500 x 8 of 64 18.4 -> 19.2 us)
 constexpr bool cache4_has_common(int DT, int parts) { return parts == 1 && DT > 2; }
 // The 64 bytes of group g of a V row: which of the row's groups of 64 bytes holds it.  Four neighbouring keys keep a group on
 // different banks, in the writes (a lane per key) and in the transposed reads (four keys per 16 lanes).
@@ -342,7 +359,7 @@ template <int DT> __device__ __forceinline__ int cache4_apart_group(int key, int
 }
 
 // DT = 32-wide tiles over d; ODD: the last one has 16 channels (d % 32 is 8 or 16), and its row 16 is the row of ones.
-// The NK waves of a workgroup have the same 32 queries and take every NK-th chunk of the tokens.  K goes from memory straight into the
+// The waves of a workgroup (up to NK) have the same 32 queries and take every waves-th chunk of the tokens.  K goes from memory straight into the
 // first product's operands (8 bytes of a key and group per lane: the order of the channels is the queries' too), V through the
 // wave's own rows in LDS, which it is transposed out of.  WAVES: per SIMD, whose registers they share.
 template <typename T, int DT, bool ODD, int NK, int WAVES>
@@ -366,8 +383,12 @@ __global__ __launch_bounds__(64 * NK, WAVES) void cache4_apart_kernel(Cache4Attn
     divmod((int)blockIdx.x, a.d_heads, qt, head);
     const int qi = qt * 32 + l32;
     const Cache4Seen seen = cache4_seen(a, qi);
-    int c = max((int)blockIdx.z * a.chunks_per_split, seen.lo / KCH) + wave;
-    const int c_end = min(((int)blockIdx.z + 1) * a.chunks_per_split, (int)(((long)seen.hi + KCH - 1) / KCH));
+    const int waves = a.waves;
+    int c, c_end;
+    seen.chunks(a, KCH, blockIdx.z, c, c_end);
+    c += wave;
+    if (a.ranges != nullptr)                       // (between the parts that the rows see there may be chunks that none does)
+        while (c < c_end && !seen.any((long)c * KCH, KCH)) c += waves;
 
     char* const vs = lds + wave * cache4_apart_bytes(DT, NP);
     const uint8_t* const ksec = a.cache + 2L * head * a.section;
@@ -444,8 +465,11 @@ __global__ __launch_bounds__(64 * NK, WAVES) void cache4_apart_kernel(Cache4Attn
 
     Cache4Sums<T, DT, ODD, KT> sums;
     sums.clear();
-    for (; c < c_end; c += NK) {
+    while (c < c_end) {
         const int t0 = c * KCH;
+        int next = c + waves;
+        if (a.ranges != nullptr)
+            while (next < c_end && !seen.any((long)next * KCH, KCH)) next += waves;
         // In a chunk of which some row does not see everything a value that is no number counts 0 - a probability of 0 times NaN
         // is NaN -, and the rows that see it are marked below.
         const bool partial = seen.partial(t0, KCH);
@@ -485,10 +509,11 @@ __global__ __launch_bounds__(64 * NK, WAVES) void cache4_apart_kernel(Cache4Attn
 #pragma unroll
                 for (int p = NP - 1; p >= 0; --p) mma32<C>(kf, qf[p][s], sacc[kt]);      // (the small parts first)
             }
-        if (c + NK < c_end) fetch(c + NK);         // in flight during the softmax and the second product
+        if (next < c_end) fetch(next);             // in flight during the softmax and the second product
         if (partial) sums.hide(a, seen, t0, half, marked, vsec + a.scales + (long)t0 * GS, sacc);
         const float m_sub = sums.settle(a.scale_log2e, sacc);
         sums.template add<false>(a.scale_log2e, m_sub, sacc, v_fragment);
+        c = next;
     }
 
     // the waves' shares of the tokens, brought to a common maximum and added in wave order
@@ -513,36 +538,43 @@ __global__ __launch_bounds__(64 * NK, WAVES) void cache4_apart_kernel(Cache4Attn
     }
     __syncthreads();
     const int dq = d >> 2, todo = min(32, a.Nq - qt * 32) * dq;
-    for (int e = tid; e < todo; e += 64 * NK) {
-        int q, g;
-        divmod(e, a.d_dq, q, g);
-        const int qq = qt * 32 + q;
-        const float* const src = comb + q * cs;
-        float m = -INFINITY, den = 0.0f;
-        float4 num = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    auto meet = [&](auto count) {
+        constexpr int N = decltype(count)::value;
+        for (int e = tid; e < todo; e += 64 * N) {
+            int q, g;
+            divmod(e, a.d_dq, q, g);
+            const int qq = qt * 32 + q;
+            const float* const src = comb + q * cs;
+            float m = -INFINITY, den = 0.0f;
+            float4 num = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-        for (int w = 0; w < NK; ++w) m = fmaxf(m, src[w * 32 * cs + d]);
+            for (int w = 0; w < N; ++w) m = fmaxf(m, src[w * 32 * cs + d]);
 #pragma unroll
-        for (int w = 0; w < NK; ++w) {
-            const float2 ml = *(const float2*)(src + w * 32 * cs + d);
-            const float4 v = *(const float4*)(src + w * 32 * cs + 4 * g);
-            // (a wave without keys carries -inf, 0 and zeros; one whose values hold a NaN keeps it whatever its weight)
-            const float f = ml.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - m);
-            den += ml.y * f;
-            num.x += v.x * f; num.y += v.y * f; num.z += v.z * f; num.w += v.w * f;
+            for (int w = 0; w < N; ++w) {
+                const float2 ml = *(const float2*)(src + w * 32 * cs + d);
+                const float4 v = *(const float4*)(src + w * 32 * cs + 4 * g);
+                // (a wave without keys carries -inf, 0 and zeros; one whose values hold a NaN keeps it whatever its weight)
+                const float f = ml.x == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ml.x - m);
+                den += ml.y * f;
+                num.x += v.x * f; num.y += v.y * f; num.z += v.z * f; num.w += v.w * f;
+            }
+            int b, en;
+            cache4_range(a.ranges, a.T, qq, b, en);
+            if (b >= en) num = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (a.splits == 1) {
+                const float inv = b >= en ? 0.0f : 1.0f / den;
+                cache4_write((T*)a.o + (long)qq * a.o_ld + head * d + 4 * g, make_float4(num.x * inv, num.y * inv, num.z * inv, num.w * inv));
+            } else {
+                float* const w = a.ws + (((long)blockIdx.z * a.heads + head) * a.Nq + qq) * (d + 4);
+                *(float4*)(w + 4 * g) = num;
+                if (g == 0) *(float2*)(w + d) = make_float2(m, den);
+            }
         }
-        int b, en;
-        cache4_range(a.ranges, a.T, qq, b, en);
-        if (b >= en) num = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (a.splits == 1) {
-            const float inv = b >= en ? 0.0f : 1.0f / den;
-            cache4_write((T*)a.o + (long)qq * a.o_ld + head * d + 4 * g, make_float4(num.x * inv, num.y * inv, num.z * inv, num.w * inv));
-        } else {
-            float* const w = a.ws + (((long)blockIdx.z * a.heads + head) * a.Nq + qq) * (d + 4);
-            *(float4*)(w + 4 * g) = num;
-            if (g == 0) *(float2*)(w + d) = make_float2(m, den);
-        }
-    }
+    };
+    if (waves == NK) meet(std::integral_constant<int, NK>());
+    else if (waves == 1) meet(std::integral_constant<int, 1>());
+    else if (waves == 2 || NK == 4) meet(std::integral_constant<int, 2>());
+    else meet(std::integral_constant<int, NK == 4 ? 2 : 4>());
 }
 
 // ---- four waves on the same chunks (half types) ------------------------------------------------------------------------------
@@ -600,8 +632,8 @@ __global__ __launch_bounds__(64 * CACHE4_COMMON_WAVES, 2) void cache4_common_ker
     } else {
         __syncthreads();
     }
-    int c = max((int)blockIdx.z * a.chunks_per_split, seen.lo / KCH);
-    const int c_end = min(((int)blockIdx.z + 1) * a.chunks_per_split, (int)(((long)seen.hi + KCH - 1) / KCH));
+    int c, c_end;
+    seen.chunks(a, KCH, blockIdx.z, c, c_end);
     const uint8_t* const sec = a.cache + 2L * head * a.section;
 
     // a unit's 64 groups: of 64 keys (K's units, then V's), or of the keys and the values of 32
@@ -805,10 +837,10 @@ static int launch_cache4_as(const Cache4AttnArgs& a, const Cache4Form& f, hipStr
 {
     constexpr int NP = Cache4Compute<T>::parts, NK = cache4_apart_waves(DT, NP);
     void (*kern)(Cache4AttnArgs) = cache4_apart_kernel<T, DT, ODD, NK, cache4_apart_side(DT, NP)>;
-    int rows = 32, threads = 64 * NK;
-    size_t lds = NK * std::max((size_t)cache4_apart_bytes(DT, NP), 32 * (a.d + 4) * sizeof(float));
+    int rows = 32, threads = 64 * a.waves;
+    size_t lds = a.waves * std::max((size_t)cache4_apart_bytes(DT, NP), 32 * (a.d + 4) * sizeof(float));
     if constexpr (cache4_crowds(DT, NP))
-        if (f.many) kern = cache4_apart_kernel<T, DT, ODD, NK, 4>;
+        if (f.many) kern = cache4_apart_kernel<T, DT, ODD, CACHE4_CROWD_WAVES, 4>;
     if constexpr (cache4_has_common(DT, NP))
         if (f.many) {
             kern = cache4_common_kernel<T, DT, ODD>;

@@ -10,7 +10,22 @@ static Cache4Cut cache4_cut(int d, sige_dtype dt, bool many)
 {
     const int DT = (d + 31) / 32, parts = dt == SIGE_F32 ? Cache4Compute<float>::parts : 1;
     if (many && cache4_has_common(DT, parts)) return {32 * CACHE4_COMMON_WAVES, 1, 32 * cache4_common_tiles(DT)};
-    return {32, cache4_apart_waves(DT, parts), 32 * cache4_apart_tiles(DT, parts)};
+    return {32, many ? CACHE4_CROWD_WAVES : cache4_apart_waves(DT, parts), 32 * cache4_apart_tiles(DT, parts)};
+}
+
+// Waves of a workgroup.  Of more workgroups than compute units those with all waves fill the chip in few uneven rounds, and with few
+// chunks leave most waves idle: as many waves as the chip holds at once by registers (heads from 136 on, single precision from 72 on: one
+// per SIMD runs best), a power of two, none without a chunk (4096 queries of 77 tokens x 8 of 80 22 -> 9 us, of 160 25 -> 15; of 1500
+// tokens x 80 43 -> 32, x 160 85 -> 72; the wrong way 1500 queries of 1500 x 160 42 -> 49).  Where rows have ranges workgroups differ in length,
+// and large ones end sooner (2889 rows with ranges of 12052 x 10 of 32 68 us, 88 with four waves).  Fewer workgroups than
+// compute units: idle waves cost nothing, and all of them write.
+static int cache4_waves(const Cache4Cut& cut, long workgroups, int share, bool many, bool ranges)
+{
+    if (cut.waves == 1 || workgroups <= 256) return cut.waves;
+    const long hold = ranges ? cut.waves : 256L * cut.waves * (many ? 4 : 1) / workgroups;
+    int w = cut.waves;
+    while (w > 1 && (w > hold || w / 2 >= share)) w /= 2;
+    return w;
 }
 
 // room: floats of workspace, what the splits' partial sums have to fit into.
@@ -23,8 +38,9 @@ static Cache4Cut cache4_cut(int d, sige_dtype dt, bool many)
 // Splits over workgroups: as many as fill the chip once (common chunks: with the two, three workgroups that a compute unit holds), since
 // a wave works as fast beside others; none for fewer than four chunks per wave, which end before the merge kernel (3 us) would have
 // (16 queries of 4096 x 8 of 40, eight chunks per wave: 16.2 us alone, 12.9, 10.0 and 9.0 in 2, 4 and 8 splits; 160 tiles of 4096 x 80
-// 22.6 alone, 29.6 in two).
-static Cache4Form plan_cache4(int Nq, int T, int heads, int d, sige_dtype dt, size_t room = ~(size_t)0)
+// 22.6 alone, 29.6 in two).  Rows with ranges of their own make workgroups of different lengths: up to four (side by side: eight) times as many then, of eight
+// chunks per wave at least (2379 rows with ranges of 20391 x 2 of 32 52 -> 31 us; 640 of 4096 x 8 of 64 18.3, 22.5 in two of four chunks).
+static Cache4Form plan_cache4(int Nq, int T, int heads, int d, sige_dtype dt, bool ranges, size_t room = ~(size_t)0)
 {
     const int target = knob(SIGE_KNOB_ATTN_WGS);
     const long tiles = (long)heads * (((long)Nq + 31) / 32);
@@ -35,6 +51,7 @@ static Cache4Form plan_cache4(int Nq, int T, int heads, int d, sige_dtype dt, si
     const long base = (long)heads * (((long)Nq + cut.rows - 1) / cut.rows);
     const long fill = cut.waves > 1 ? 256 : d <= 96 ? 768 : 512;
     long want = target >= 0 ? (target + base - 1) / base : chunks < 4 * cut.waves ? 1 : fill / base;
+    if (target < 0 && ranges && cut.waves > 1) want = std::max(want, std::min((f.many ? 8 : 4) * fill / base, chunks / (8 * cut.waves)));
     want = std::max(std::min(std::min(want, chunks / cut.waves), 64L), 1L);
     const long per = std::max((chunks + want - 1) / want, 1L);
     f.splits = (int)std::max((chunks + per - 1) / per, 1L);
@@ -71,11 +88,12 @@ static int cache4_attn_entry(const char* who, Cache4AttnArgs& a, const void* q, 
     a.scale_log2e = std::max(scale * 1.4426950408889634f, 1.4e-45f);
     a.d_heads = fast_div(heads); a.d_tpb = fast_div(a.q_tpb); a.d_qbw = fast_div(a.q_bw); a.d_dq = fast_div(d / 4);
     const bool room = workspace != nullptr && aligned16(workspace);
-    const Cache4Form f = plan_cache4(Nq, T, heads, d, dt, room ? workspace_bytes / sizeof(float) : 0);
-    const int KCH = cache4_cut(d, dt, f.many).chunk;
-    const int chunks = (int)(((long)T + KCH - 1) / KCH);
+    const Cache4Form f = plan_cache4(Nq, T, heads, d, dt, ranges != nullptr, room ? workspace_bytes / sizeof(float) : 0);
+    const Cache4Cut cut = cache4_cut(d, dt, f.many);
     a.splits = f.splits;
-    a.chunks_per_split = (chunks + f.splits - 1) / f.splits;
+    a.share = (int)((((long)T + cut.chunk - 1) / cut.chunk + f.splits - 1) / f.splits);
+    a.d_splits = fast_div(f.splits);
+    a.waves = cache4_waves(cut, (((long)Nq + cut.rows - 1) / cut.rows) * heads * f.splits, a.share, f.many, ranges != nullptr);
     hipStream_t st = (hipStream_t)stream;
     return dt == SIGE_F32 ? launch_cache4_f32(a, f, st) : dt == SIGE_F16 ? launch_cache4_f16(a, f, st) : launch_cache4_bf16(a, f, st);
 }
@@ -87,7 +105,9 @@ using namespace sige;
 extern "C" size_t sige_cache4_attn_workspace_bytes(int32_t Nq, int32_t T, int32_t heads, int32_t d)
 {
     if (Nq <= 0 || T <= 0 || heads <= 0 || d <= 0 || d > 256) return 0;
-    const int splits = std::max(plan_cache4(Nq, T, heads, d, SIGE_F16).splits, plan_cache4(Nq, T, heads, d, SIGE_F32).splits);
+    int splits = 1;
+    for (sige_dtype dt : {SIGE_F16, SIGE_F32})
+        for (bool ranges : {false, true}) splits = std::max(splits, plan_cache4(Nq, T, heads, d, dt, ranges).splits);
     return splits <= 1 ? 0 : (size_t)splits * heads * Nq * (d + 4) * sizeof(float);
 }
 

@@ -257,6 +257,41 @@ def test_attention_ranges(nq, T, heads, d, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("nq,heads,T,d", [(1030, 8, 3, 128), (1030, 8, 77, 40), (1030, 9, 200, 80), (830, 20, 77, 64), (830, 20, 200, 24), (820, 21, 77, 160),
+                                          (860, 40, 70, 40), (860, 40, 77, 96), (350, 97, 90, 72), (400, 24, 130, 256)])
+def test_attention_of_many_rows_and_few_tokens(nq, heads, T, d, dtype):
+    """More workgroups than compute units: fewer waves in each, down to one."""
+    q, cache, cap, k, v = case(nq, nq, T, heads, d, dtype)
+    scale = 1 / math.sqrt(d)
+    q64 = f64(q).reshape(nq, heads, d)
+    want, mag = ref.attention(q64, k, v, scale)
+    close(attend(q, cache, cap, T, heads, d, scale), want, mag, q64, k, scale, dtype, T, "all tokens")
+    ranges = some_ranges(nq, T, d)
+    want, mag = ref.attention(q64, k, v, scale, ranges)
+    close(attend(q, cache, cap, T, heads, d, scale, ranges), want, mag, q64, k, scale, dtype, T, "ranges")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("nq,heads,T,d,wgs", [(70, 1, 3000, 40, None), (70, 1, 3000, 40, 40), (300, 2, 2500, 64, 300), (140, 2, 2100, 160, 64), (40, 1, 1000, 248, 9)])
+def test_attention_of_ranges_far_apart(nq, heads, T, d, wgs, dtype):
+    """Neighbouring rows see parts of the cache with long stretches between them that nobody sees; the splits share out what a tile of
+    rows spans."""
+    q, cache, cap, k, v = case(d, nq, T, heads, d, dtype)
+    i = np.arange(nq)
+    ranges = np.stack([i % 3 * 900 + i % 7, np.minimum(i % 3 * 900 + 30 + i % 50, T)], 1)
+    ranges[32:64] = (T - 5, T)                    # (a tile of its own: the last chunk alone)
+    ranges[3] = (0, 0)
+    scale = 1 / math.sqrt(d)
+    q64 = f64(q).reshape(nq, heads, d)
+    want, mag = ref.attention(q64, k, v, scale, ranges)
+    for many in forms(dtype):
+        for ws in (True, False):
+            with api.knobs(CACHE4_MANY=many, ATTN_WGS=wgs):
+                o = attend(q, cache, cap, T, heads, d, scale, ranges, ws)
+            close(o, want, mag, q64, k, scale, dtype, T, f"far apart, form {many}, workspace {ws}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("nq,d", [(3, 64), (20, 40), (100, 64), (100, 40), (90, 160)])
 def test_attention_of_tokens_that_are_no_numbers(nq, d, dtype):
     """Tokens whose keys, or whose values in one group, are not finite: NaN for the rows that see them (values: in that group's
