@@ -243,29 +243,35 @@ __global__ __launch_bounds__(64 * LORA_WAVES, 2) void token_lora_kernel(LoraArgs
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) *(f32x4*)&red[wave][l16][rt * 16 + 4 * quarter] = own[rt];
         __syncthreads();
-        for (int j = tid; j < 16 * 4 * RT; j += 64 * LORA_WAVES) {       // (whole waves: 64 RT of them)
-            const int t = j / (4 * RT), q = j % (4 * RT);
-            f32x4 s = *(const f32x4*)&red[0][t][4 * q];
-#pragma unroll
-            for (int w = 1; w < LORA_WAVES; ++w) s += *(const f32x4*)&red[w][t][4 * q];
+        constexpr int LANES = RT <= 1 ? 4 : RT <= 2 ? 8 : RT <= 4 ? 16 : 32;     // of a row: four ranks each
+        for (int j = tid; j < 16 * LANES; j += 64 * LORA_WAVES) {        // (whole waves)
+            const int t = j / LANES, q = j % LANES;
             const int mine = __shfl(id, t);
             if (mine < 0 || (mine != cur0 && mine != cur1)) continue;
+            const bool on = LANES == 4 * RT || q < 4 * RT;
+            f32x4 s = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            if (on) {
+                s = *(const f32x4*)&red[0][t][4 * q];
+#pragma unroll
+                for (int w = 1; w < LORA_WAVES; ++w) s += *(const f32x4*)&red[w][t][4 * q];
+            }
             const float alpha = a.alpha != nullptr ? a.alpha[mine] : 1.0f;
             float v[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = 4 * q + i < a.rank ? alpha * s[i] : 0.0f;
-            if constexpr (__is_same(T, f16)) {                    // the row's largest value to 2^14..2^15 (4 RT lanes hold the row)
+            if constexpr (__is_same(T, f16)) {                    // the row's largest value to 2^14..2^15
                 unsigned top = 0u;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
 #pragma unroll
-                for (int x = 1; x < 4 * RT; x <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, x));
+                for (int x = 1; x < LANES; x <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, x));
                 const int e = min(max((int)(top >> 23), 27), 254);         // (a row of zeros, of infinities)
                 const float down = __uint_as_float((unsigned)(127 + 127 + 14 - e) << 23);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) v[i] *= down;
                 if (q == 0) hscale[t] = __uint_as_float((unsigned)(e - 14) << 23);
             }
+            if (!on) continue;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const T h = from_f32<T>(v[i]);
@@ -379,7 +385,10 @@ static int launch_lora(LoraArgs& a, int rows, hipStream_t st)
     const int rt = (a.rank + 15) / 16;
     if (rt == 1) go(token_lora_kernel<T, 1>);
     else if (rt == 2) go(token_lora_kernel<T, 2>);
-    else if (rt <= 4) go(token_lora_kernel<T, 4>);
+    else if (rt == 3) go(token_lora_kernel<T, 3>);
+    else if (rt == 4) go(token_lora_kernel<T, 4>);
+    else if (rt == 5) go(token_lora_kernel<T, 5>);
+    else if (rt == 6) go(token_lora_kernel<T, 6>);
     else go(token_lora_kernel<T, 8>);
     SIGE_LAUNCH_CHECK("sige_token_lora");
     return SIGE_OK;

@@ -66,6 +66,20 @@ def test_adapters(rows, per, cin, cout, rank, n, dtype):
     close(y, want, mag, cin, rank, dtype, "in place")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rank", [4, 12, 20, 36, 48, 68, 80, 92, 104, 120])
+def test_ranks(rank, dtype):
+    """Every number of 16-wide tiles over the rank, whole and not."""
+    if dtype != "f32":
+        rank += -rank % 8
+    x, down, up, ids, alpha, base = make(rank, 70, 9, 136, 88, rank, 4, dtype)
+    want, mag = expected(x, down, up, ids, 9, alpha, base, 88)
+    y = torch.empty_like(base)
+    api.sige_token_lora(x, y, 136, 88, down, up, ids, 9, alpha=alpha, base=base, n_rows=70)
+    torch.cuda.synchronize()
+    close(y, want, mag, 136, rank, dtype, "rank %d" % rank)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_ids_counts_and_neighbours(dtype):
     """Every row its own adapter, ids that name none, the same adapter twice; rows by a device count; rows and adapters of NaN reach
@@ -127,7 +141,7 @@ def test_short_runs_of_several_adapters(rows, per, n, kind, dtype):
     assert torch.equal(y[count * per:], base[count * per:])
 
 
-@pytest.mark.parametrize("rank", [8, 24, 64, 128])
+@pytest.mark.parametrize("rank", [8, 24, 40, 64, 72, 96, 128])
 def test_middle_vectors_beyond_the_range_of_fp16(rank):
     """down x above 65504 and far below 2^-14, up the other way round: the results are ordinary numbers.  Infinite ones stay infinite."""
     rows, per, cin, cout, n = 37, 3, 256, 72, 4
