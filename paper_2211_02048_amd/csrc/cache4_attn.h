@@ -577,9 +577,12 @@ __global__ __launch_bounds__(64 * NK, WAVES) void cache4_apart_kernel(Cache4Attn
     else meet(std::integral_constant<int, NK == 4 ? 2 : 4>());
 }
 
-// ---- four waves on the same chunks (half types) ------------------------------------------------------------------------------
+// ---- waves on the same chunks (half types) -----------------------------------------------------------------------------------
 
-constexpr int CACHE4_COMMON_WAVES = 4;
+// Waves of a workgroup.  Heads up to 96: four, three workgroups per compute unit.  Larger ones: eight, which halves what a query pays for the
+// expansion (4096 queries of 16384 x 8 of 128 327 -> 298 us, 1024 of 16384 x 128 102 -> 93, 2048 of 4096 x 160 81 -> 76, 1024 of 4096 x 256
+// 82 both; 4096 of 4096 x 80 78 against 70 with four).
+constexpr int cache4_common_waves(int DT) { return DT <= 3 ? 4 : 8; }
 constexpr int cache4_common_tiles(int DT) { return DT <= 4 ? 2 : 1; }                    // 32-key tiles per chunk
 // bytes between V rows in LDS: an odd multiple of 64, so that the keys of a transposed read fall on different banks; between K rows:
 // 16 bytes more than the channels
@@ -592,10 +595,10 @@ constexpr int cache4_common_bytes(int DT, bool ODD) { return 32 * cache4_common_
 // compiler keeps heads up to 128 in half of what it takes otherwise (4096 queries of 16384 x 8 of 128 580 -> 367 us, 2048 of 4096 x 160
 // 146 -> 85).  Heads of 225 to 256 leave a few registers in memory then, and gain all the same (1024 of 4096 x 256 125 -> 77 us).
 template <typename T, int DT, bool ODD>
-__global__ __launch_bounds__(64 * CACHE4_COMMON_WAVES, 2) void cache4_common_kernel(Cache4AttnArgs a)
+__global__ __launch_bounds__(64 * cache4_common_waves(DT), 2) void cache4_common_kernel(Cache4AttnArgs a)
 {
     using C = typename Cache4Compute<T>::type;
-    constexpr int NW = CACHE4_COMMON_WAVES;
+    constexpr int NW = cache4_common_waves(DT);
     constexpr unsigned LAST = Cache4Compute<T>::last;
     constexpr int KT = cache4_common_tiles(DT), KCH = 32 * KT;
     constexpr int VROW = cache4_common_v_row(DT), KROW = cache4_common_k_row(DT, ODD), CHUNK = cache4_common_bytes(DT, ODD);
@@ -844,8 +847,8 @@ static int launch_cache4_as(const Cache4AttnArgs& a, const Cache4Form& f, hipStr
     if constexpr (cache4_has_common(DT, NP))
         if (f.many) {
             kern = cache4_common_kernel<T, DT, ODD>;
-            rows = 32 * CACHE4_COMMON_WAVES;
-            threads = 64 * CACHE4_COMMON_WAVES;
+            rows = 32 * cache4_common_waves(DT);
+            threads = 64 * cache4_common_waves(DT);
             lds = 2 * (size_t)cache4_common_bytes(DT, ODD);
         }
     const long tiles = ((long)a.Nq + rows - 1) / rows * a.heads, groups = (long)a.Nq * a.heads * (a.d / 4);

@@ -9,7 +9,7 @@ struct Cache4Cut { int rows, waves, chunk; };
 static Cache4Cut cache4_cut(int d, sige_dtype dt, bool many)
 {
     const int DT = (d + 31) / 32, parts = dt == SIGE_F32 ? Cache4Compute<float>::parts : 1;
-    if (many && cache4_has_common(DT, parts)) return {32 * CACHE4_COMMON_WAVES, 1, 32 * cache4_common_tiles(DT)};
+    if (many && cache4_has_common(DT, parts)) return {32 * cache4_common_waves(DT), 1, 32 * cache4_common_tiles(DT)};
     return {32, many ? CACHE4_CROWD_WAVES : cache4_apart_waves(DT, parts), 32 * cache4_apart_tiles(DT, parts)};
 }
 
@@ -33,26 +33,39 @@ static int cache4_waves(const Cache4Cut& cut, long workgroups, int share, bool m
 // Half types, from where on a call counts as one of many queries (heads x tiles of 32, "tiles"):
 //   heads up to 64    more tiles than compute units: workgroups side by side (512 tiles of 1024 tokens x 40 13.5 against 15.9 us; 256 of
 //                     3000 x 64 17.4 against 16.7)
-//   larger heads      tiles x tokens from 2^21 on: four waves on common chunks (1024 x 16384 x 128 320 against 433 us, 512 x 4096 x 160
-//                     84 against 94; 512 x 2048 x 128 44 against 36, 256 x 3000 x 128 38 against 25)
-// Splits over workgroups: as many as fill the chip once (common chunks: with the two, three workgroups that a compute unit holds), since
-// a wave works as fast beside others; none for fewer than four chunks per wave, which end before the merge kernel (3 us) would have
-// (16 queries of 4096 x 8 of 40, eight chunks per wave: 16.2 us alone, 12.9, 10.0 and 9.0 in 2, 4 and 8 splits; 160 tiles of 4096 x 80
-// 22.6 alone, 29.6 in two).  Rows with ranges of their own make workgroups of different lengths: up to four (side by side: eight) times as many then, of eight
-// chunks per wave at least (2379 rows with ranges of 20391 x 2 of 32 52 -> 31 us; 640 of 4096 x 8 of 64 18.3, 22.5 in two of four chunks).
+//   larger heads      a product of tiles, tokens and d^2 beyond which common chunks win, within 10 % (d = 96: tiles x tokens 2^21 53
+//                     against 42 us, 2^22 74.5 against 73.5; 128: 2^20 45 against 32, 2^21 55 against 56, 2^22 85 against 98; 160: 2^20 52
+//                     against 50, 2^21 74 against 87; 256: 2^18 46 against 45, 2^19 55 against 47, 2^20 67 against 83)
+// Splits over workgroups: of one to six rounds of the chip (of common chunks up to d = 96 a compute unit holds three workgroups, else one)
+// the number that costs least at 2.5 us per round, 2 per chunk (measured: 1.3 - 2.2 over all forms), and 3 and the partial sums' bytes
+// for the merge (1500 queries of 16384 x 3 of 40, 141 tiles: 51 -> 39 us); none for fewer than four chunks per wave, which end before that (16 queries of 4096 x 8 of 40, eight chunks per wave:
+// 16.2 us alone, 12.9, 10.0 and 9.0 in 2, 4 and 8 splits; 160 tiles of 4096 x 80 22.6 alone, 29.6 in two), nor side by side.  Rows
+// with ranges of their own make workgroups of different lengths: up to four (side by side: eight) times as many then, of eight chunks per
+// wave at least (2379 rows with ranges of 20391 x 2 of 32 52 -> 31 us; 640 of 4096 x 8 of 64 18.3, 22.5 in two of four chunks).
 static Cache4Form plan_cache4(int Nq, int T, int heads, int d, sige_dtype dt, bool ranges, size_t room = ~(size_t)0)
 {
     const int target = knob(SIGE_KNOB_ATTN_WGS);
     const long tiles = (long)heads * (((long)Nq + 31) / 32);
     const int many = knob(SIGE_KNOB_CACHE4_MANY);
-    Cache4Form f = {dt != SIGE_F32 && (many >= 0 ? many != 0 : d <= 64 ? tiles > 256 : tiles * T >= (1L << 21)), 1};
+    Cache4Form f = {dt != SIGE_F32 && (many >= 0 ? many != 0 : d <= 64 ? tiles > 256 : (double)tiles * T * d * d >= (double)(1L << 35)), 1};
     const Cache4Cut cut = cache4_cut(d, dt, f.many);
     const long chunks = ((long)T + cut.chunk - 1) / cut.chunk;
     const long base = (long)heads * (((long)Nq + cut.rows - 1) / cut.rows);
-    const long fill = cut.waves > 1 ? 256 : d <= 96 ? 768 : 512;
-    long want = target >= 0 ? (target + base - 1) / base : chunks < 4 * cut.waves ? 1 : fill / base;
-    if (target < 0 && ranges && cut.waves > 1) want = std::max(want, std::min((f.many ? 8 : 4) * fill / base, chunks / (8 * cut.waves)));
-    want = std::max(std::min(std::min(want, chunks / cut.waves), 64L), 1L);
+    const long fill = cut.waves == 1 && d <= 96 ? 768 : 256;
+    const bool crowd = f.many && cut.waves > 1;
+    const long most = std::max(std::min(chunks / cut.waves, 64L), 1L);
+    long want = target >= 0 ? (target + base - 1) / base : 1;
+    if (target < 0 && !crowd && chunks >= 4 * cut.waves) {
+        double least = INFINITY;
+        for (int rounds = 1; rounds <= 6; ++rounds) {
+            const long z = std::max(std::min(fill * rounds / base, most), 1L);
+            const double cost = ((base * z + fill - 1) / fill) * (2.5 + 2.0 * ((chunks + z * cut.waves - 1) / (z * cut.waves))) +
+                                (z > 1 ? 3.0 + 1.6e-6 * z * heads * Nq * (d + 4) : 0.0);
+            if (cost < least) { least = cost; want = z; }
+        }
+    }
+    if (target < 0 && ranges && cut.waves > 1) want = std::max(want, std::min((crowd ? 8 : 4) * fill / base, chunks / (8 * cut.waves)));
+    want = std::max(std::min(want, most), 1L);
     const long per = std::max((chunks + want - 1) / want, 1L);
     f.splits = (int)std::max((chunks + per - 1) / per, 1L);
     while (f.splits > 1 && (size_t)f.splits * heads * Nq * (d + 4) > room) {
