@@ -15,9 +15,11 @@
 // head size leaves one free, else as dot products of the rounded pairs with ones (single precision: the values themselves).
 //
 // Two forms.  cache4_apart_kernel: every wave by itself, the waves of a workgroup share the keys out among them; no barrier until
-// they meet.  cache4_common_kernel: four waves on 128 queries that expand every chunk once for all.  The vector instructions bound
-// the first (per 64 keys x 32 queries x 64: about 90 for the expansion, 110 for the softmax), LDS and the order of the
-// two kinds of instructions the second.
+// they meet.  cache4_common_kernel: four or eight waves of 32 queries each that expand every chunk once for all.  The vector instructions
+// bound the first where there is work (per 64 keys x 32 queries x 64: about 90 for the expansion, 110 for the softmax), LDS and the order
+// of the two kinds of instructions the second.  Measured: one query of 65536 x 8 of 64 in bf16 14.7 us (with the merge; 35.7 MB, 2.4 TB/s),
+// 614 of 4096 x 8 of 80 in fp16 21 us (300 TFLOP/s: 160 workgroups of eight chunks per wave), 4096 of 16384 x 8 of 128 in bf16 291 us (945
+// TFLOP/s; a library product reaches 1167).
 #pragma once
 
 #include "cache4.h"
@@ -592,8 +594,8 @@ constexpr int cache4_common_bytes(int DT, bool ODD) { return 32 * cache4_common_
 
 // The waves have 32 queries each and expand every chunk once for all, K and V rows of the compute type in LDS: the next chunk into one
 // buffer while the other is multiplied, one barrier per chunk.  The registers are bounded for two waves per SIMD: told so, the
-// compiler keeps heads up to 128 in half of what it takes otherwise (4096 queries of 16384 x 8 of 128 580 -> 367 us, 2048 of 4096 x 160
-// 146 -> 85).  Heads of 225 to 256 leave a few registers in memory then, and gain all the same (1024 of 4096 x 256 125 -> 77 us).
+// compiler keeps heads up to 128 in half of what it takes otherwise (with four waves, 4096 queries of 16384 x 8 of 128 580 -> 367 us, 2048
+// of 4096 x 160 146 -> 85, 1024 of 4096 x 256 125 -> 77).
 template <typename T, int DT, bool ODD>
 __global__ __launch_bounds__(64 * cache4_common_waves(DT), 2) void cache4_common_kernel(Cache4AttnArgs a)
 {
