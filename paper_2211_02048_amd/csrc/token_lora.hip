@@ -92,9 +92,9 @@ template <typename T> __device__ __forceinline__ uint4 lora_sum(const f32x4 (&su
 constexpr int LORA_WAVES = 4;
 constexpr int LORA_SECTION = 128;                                 // runs that are grouped by adapter
 
-// RT = 16-wide tiles over the rank.  The registers are bounded for two workgroups per compute unit.  No load is guarded (a guard is a branch of its own): lanes past the end read the last vector or
+// ALONE: every wave has 16 rows of its own and shares nothing: no barriers, no sums in LDS.  RT = 16-wide tiles over the rank.  The registers are bounded for two workgroups per compute unit.  No load is guarded (a guard is a branch of its own): lanes past the end read the last vector or
 // row again, and what they make of it is either multiplied by the zeros behind the rank, or not stored.
-template <typename T, int RT>
+template <typename T, int RT, bool ALONE>
 __global__ __launch_bounds__(64 * LORA_WAVES, 2) void token_lora_kernel(LoraArgs a)
 {
     constexpr bool F32 = sizeof(T) == 4;
@@ -105,11 +105,13 @@ __global__ __launch_bounds__(64 * LORA_WAVES, 2) void token_lora_kernel(LoraArgs
     constexpr int AHEAD = RT <= 2 ? 8 : RT <= 4 ? 6 : 4;          // steps over Cin whose operands are on their way together
     constexpr int TU = F32 ? 1 : 2, CU = 16 * TU;                 // products per stretch of output channels, its channels
     constexpr int BATCH = KR <= 1 ? (F32 ? 4 : 5) : KR <= 2 ? 2 : 1;          // stretches whose operands are on their way together
-    __shared__ float red[LORA_WAVES][16][RED];
-    __shared__ uint4 hbuf[(F32 ? 1 : 2) * 16 * HROW / VW];
+    constexpr int HBUF = (F32 ? 1 : 2) * 16 * HROW / VW;
+    __shared__ float red[ALONE ? 1 : LORA_WAVES][16][RED];
+    __shared__ uint4 hall[ALONE ? LORA_WAVES : 1][HBUF];
     __shared__ float hscale[16];                                  // fp16: what the rows' sums are multiplied by at the end
-    T* const hs = reinterpret_cast<T*>(hbuf);                     // [value, remainder][16][HROW]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    uint4* const hbuf = hall[ALONE ? wave : 0];
+    T* const hs = reinterpret_cast<T*>(hbuf);                     // [value, remainder][16][HROW]
     const int l16 = lane & 15, quarter = lane >> 4;
     long rows = a.n_host;
     if (a.n_host < 0) {
@@ -123,6 +125,7 @@ __global__ __launch_bounds__(64 * LORA_WAVES, 2) void token_lora_kernel(LoraArgs
     if (a.group > 0) {
         int section, tile;
         divmod((int)blockIdx.x, a.d_tiles, section, tile);
+        if (ALONE) tile = tile * LORA_WAVES + wave;
         const int run0 = section * LORA_SECTION, per = a.rows_per_id;
         if ((long)run0 * per >= rows) return;
         const int n = (int)min((long)LORA_SECTION, (rows + per - 1) / per - run0);       // runs of the section
@@ -172,7 +175,7 @@ __global__ __launch_bounds__(64 * LORA_WAVES, 2) void token_lora_kernel(LoraArgs
         live = live && row < rows;
         if (!live) { run = run0; row = (long)run0 * per; }
     } else {
-        const long row0 = (long)blockIdx.x * 16;
+        const long row0 = ((long)blockIdx.x * (ALONE ? LORA_WAVES : 1) + (ALONE ? wave : 0)) * 16;
         if (row0 >= rows) return;
         live = row0 + l16 < rows;
         row = live ? row0 + l16 : row0;
@@ -182,7 +185,8 @@ __global__ __launch_bounds__(64 * LORA_WAVES, 2) void token_lora_kernel(LoraArgs
     if (!live || (unsigned)id >= (unsigned)a.adapters) id = -1;
     const T* const xr = (const T*)a.x + row * a.x_ld + VW * quarter;
     if (KR * KS > RT * 16)                                        // (the half types' step of 32 over a rank of 16)
-        for (int j = tid; j < 2 * 16 * HROW / VW; j += 64 * LORA_WAVES) hbuf[j] = make_uint4(0, 0, 0, 0);
+        for (int j = ALONE ? lane : tid; j < HBUF; j += ALONE ? 64 : 64 * LORA_WAVES) hbuf[j] = make_uint4(0, 0, 0, 0);
+    if constexpr (ALONE) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");          // (zeros first, then the values)
 
     const unsigned long all = __builtin_amdgcn_ballot_w64(id >= 0);
     unsigned long todo = all;
@@ -192,7 +196,20 @@ __global__ __launch_bounds__(64 * LORA_WAVES, 2) void token_lora_kernel(LoraArgs
         return cur;
     };
     const int full = a.Cin / KS, tail = a.Cin - full * KS;        // steps, channels of the last one
-    const int share = (full + LORA_WAVES - 1) / LORA_WAVES;       // of a wave, one after the other: whole lines of memory
+    const int share = ALONE ? full : (full + LORA_WAVES - 1) / LORA_WAVES;       // of a wave, one after the other: whole lines of memory
+    const int part = ALONE ? 0 : wave;
+    float back = 1.0f;
+    // the middle vector's values q * 4 ... + 3 of token t, scaled by `down`
+    auto keep = [&](int t, int q, const float (&v)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const T h = from_f32<T>(v[i]);
+            hs[t * HROW + 4 * q + i] = h;
+            // (an infinity has no remainder: its difference to itself would be NaN)
+            if constexpr (!F32) hs[(16 + t) * HROW + 4 * q + i] = from_f32<T>(fabsf(to_f32(h)) == INFINITY ? 0.0f : v[i] - to_f32(h));
+        }
+    };
+    f32x4 alone[RT];                                              // ALONE: the sums of row l16 with its own adapter
     while (todo != 0) {
         // two adapters per pass, where there are two: of their products a lane keeps its own token's
         const int cur0 = next(), cur1 = todo != 0 ? next() : -1;
@@ -220,11 +237,11 @@ __global__ __launch_bounds__(64 * LORA_WAVES, 2) void token_lora_kernel(LoraArgs
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt) LoraStep<T>::run(dv[i][rt], xv[i], acc[rt]);      // rows: ranks, columns: tokens
             };
-            int s = wave * share;
+            int s = part * share;
             const int end = min(s + share, full);
             for (; s + AHEAD <= end; s += AHEAD) steps(std::integral_constant<int, AHEAD>(), s);
             for (; s < end; ++s) steps(std::integral_constant<int, 1>(), s);
-            if (tail != 0 && wave == LORA_WAVES - 1) {            // the last channels
+            if (tail != 0 && (ALONE || wave == LORA_WAVES - 1)) { // the last channels
                 const bool in = VW * quarter < tail;
                 const int at = full * KS - (in ? 0 : VW * quarter);
                 uint4 xv = *(const uint4*)(xr + at);
@@ -239,6 +256,12 @@ __global__ __launch_bounds__(64 * LORA_WAVES, 2) void token_lora_kernel(LoraArgs
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
                 if (n == 0 || id == cur) own[rt] = acc[rt];
+        }
+        if constexpr (ALONE) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+                if (id >= 0 && (id == cur0 || id == cur1)) alone[rt] = own[rt];
+            continue;
         }
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) *(f32x4*)&red[wave][l16][rt * 16 + 4 * quarter] = own[rt];
@@ -272,15 +295,35 @@ __global__ __launch_bounds__(64 * LORA_WAVES, 2) void token_lora_kernel(LoraArgs
                 if (q == 0) hscale[t] = __uint_as_float((unsigned)(e - 14) << 23);
             }
             if (!on) continue;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const T h = from_f32<T>(v[i]);
-                hs[t * HROW + 4 * q + i] = h;
-                // (an infinity has no remainder: its difference to itself would be NaN)
-                if constexpr (!F32) hs[(16 + t) * HROW + 4 * q + i] = from_f32<T>(fabsf(to_f32(h)) == INFINITY ? 0.0f : v[i] - to_f32(h));
-            }
+            keep(t, q, v);
         }
         __syncthreads();
+    }
+    if constexpr (ALONE) {
+        const float alpha = a.alpha != nullptr && id >= 0 ? a.alpha[id] : 1.0f;
+        float v[RT][4];
+        unsigned top = 0u;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[rt][i] = id >= 0 && rt * 16 + 4 * quarter + i < a.rank ? alpha * alone[rt][i] : 0.0f;
+                top = max(top, __float_as_uint(v[rt][i]) & 0x7fffffffu);
+            }
+        if constexpr (__is_same(T, f16)) {                        // (as above; the four quarters hold the row)
+            top = max(top, (unsigned)__shfl_xor((int)top, 16));
+            top = max(top, (unsigned)__shfl_xor((int)top, 32));
+            const int e = min(max((int)(top >> 23), 27), 254);
+            const float down = __uint_as_float((unsigned)(127 + 127 + 14 - e) << 23);
+            back = __uint_as_float((unsigned)(e - 14) << 23);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[rt][i] *= down;
+        }
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) keep(l16, rt * 4 + quarter, v[rt]);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");    // (read as other vectors below; a wave's LDS operations stay in order)
     }
 
     // y^T = up h^T: rows are output channels, so that a lane holds consecutive ones of one token.  Half types: two products of 16
@@ -291,9 +334,8 @@ __global__ __launch_bounds__(64 * LORA_WAVES, 2) void token_lora_kernel(LoraArgs
         hv[s] = *(const uint4*)(hs + l16 * HROW + s * KS + VW * quarter);
         if constexpr (!F32) hl[s] = *(const uint4*)(hs + (16 + l16) * HROW + s * KS + VW * quarter);
     }
-    float back = 1.0f;
-    if constexpr (__is_same(T, f16)) back = id >= 0 ? hscale[l16] : 1.0f;
-    int u0 = (blockIdx.y * LORA_WAVES + wave) * a.span;
+    if constexpr (__is_same(T, f16) && !ALONE) back = id >= 0 ? hscale[l16] : 1.0f;
+    int u0 = (blockIdx.y * (ALONE ? 1 : LORA_WAVES) + part) * a.span;
     const int u_end = min(u0 + a.span, (a.Cout + CU - 1) / CU);
     // A batch of stretches.  SAME: all rows that there are have one adapter; else what each makes is taken over by its own rows, not
     // added as zeros (what another adapter holds may be no number).
@@ -368,9 +410,9 @@ static int launch_lora(LoraArgs& a, int rows, hipStream_t st)
     const int per = a.rows_per_id;
     a.group = per <= (rows <= 512 ? 8 : 5) && rows > 3L * per && a.adapters > 2 && a.adapters < 1 << 24 ? 16 / per : 0;
     int tiles = (rows + 15) / 16;
+    // (of n runs at most this many groups, each of one adapter or none; those that there are not end at once)
+    auto groups = [&](int n) { return std::min(n, (int)((n + (long)std::min(a.adapters + 1, n) * (a.group - 1)) / a.group)); };
     if (a.group > 0) {
-        // (of n runs at most this many groups, each of one adapter or none; those that there are not end at once)
-        auto groups = [&](int n) { return std::min(n, (int)((n + (long)std::min(a.adapters + 1, n) * (a.group - 1)) / a.group)); };
         const int runs = (int)(((long)rows + per - 1) / per), section = groups(LORA_SECTION);
         tiles = runs / LORA_SECTION * section + groups(runs % LORA_SECTION);
         a.d_tiles = fast_div(section);
@@ -378,18 +420,36 @@ static int launch_lora(LoraArgs& a, int rows, hipStream_t st)
     }
     // workgroups per 16 rows: one per compute unit where the rows alone are fewer (two take 8.6 instead of 6.8 us for 1011 rows of
     // 640 -> 648 in single precision, half of one 7.8), a stretch of channels per wave at least
-    const int cut = std::max(std::min((256 + tiles - 1) / tiles, (units + LORA_WAVES - 1) / LORA_WAVES), 1);
-    a.span = (units + cut * LORA_WAVES - 1) / (cut * LORA_WAVES);
+    // Narrow rows, a tile for every SIMD: each wave by itself (16384 rows of 128 -> 128 10.9 -> 5.9 us, of 320 -> 320 13.8 -> 10.1, single
+    // tokens of 8 adapters 20 -> 9.4; 8192 of 320 -> 320 7.2 -> 9.0, 24576 of 640 -> 640 22.9 -> 25.9)
+    const bool alone = tiles >= 1024 && (long)(a.Cin + a.Cout) * (long)sizeof(T) <= 1280;
+    const int cut = alone ? 1 : std::max(std::min((256 + tiles - 1) / tiles, (units + LORA_WAVES - 1) / LORA_WAVES), 1);
+    a.span = alone ? units : (units + cut * LORA_WAVES - 1) / (cut * LORA_WAVES);
+    if (alone) {
+        auto quarters = [](int n) { return (n + LORA_WAVES - 1) / LORA_WAVES; };
+        if (a.group > 0) {
+            const int runs = (int)(((long)rows + per - 1) / per), section = quarters(groups(LORA_SECTION));
+            tiles = runs / LORA_SECTION * section + quarters(groups(runs % LORA_SECTION));
+            a.d_tiles = fast_div(section);
+        } else {
+            tiles = quarters(tiles);
+        }
+    }
     const dim3 grid(tiles, cut);
     auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(64 * LORA_WAVES), 0, st, a); };
-    const int rt = (a.rank + 15) / 16;
-    if (rt == 1) go(token_lora_kernel<T, 1>);
-    else if (rt == 2) go(token_lora_kernel<T, 2>);
-    else if (rt == 3) go(token_lora_kernel<T, 3>);
-    else if (rt == 4) go(token_lora_kernel<T, 4>);
-    else if (rt == 5) go(token_lora_kernel<T, 5>);
-    else if (rt == 6) go(token_lora_kernel<T, 6>);
-    else go(token_lora_kernel<T, 8>);
+    auto by_rank = [&](auto al) {
+        constexpr bool A = decltype(al)::value;
+        const int rt = (a.rank + 15) / 16;
+        if (rt == 1) go(token_lora_kernel<T, 1, A>);
+        else if (rt == 2) go(token_lora_kernel<T, 2, A>);
+        else if (rt == 3) go(token_lora_kernel<T, 3, A>);
+        else if (rt == 4) go(token_lora_kernel<T, 4, A>);
+        else if (rt == 5) go(token_lora_kernel<T, 5, A>);
+        else if (rt == 6) go(token_lora_kernel<T, 6, A>);
+        else go(token_lora_kernel<T, 8, A>);
+    };
+    if (alone) by_rank(std::true_type());
+    else by_rank(std::false_type());
     SIGE_LAUNCH_CHECK("sige_token_lora");
     return SIGE_OK;
 }

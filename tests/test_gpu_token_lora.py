@@ -80,6 +80,34 @@ def test_ranks(rank, dtype):
     close(y, want, mag, 136, rank, dtype, "rank %d" % rank)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,per,cin,cout,rank,n", [(16384, 64, 64, 40, 8, 3), (16500, 7, 72, 24, 24, 4), (20001, 13, 40, 72, 40, 2), (9000, 1, 48, 32, 16, 40),
+                                                      (12000, 2, 24, 64, 72, 9), (17777, 3, 64, 16, 88, 3), (16400, 20, 16, 8, 120, 5)])
+def test_many_narrow_rows(rows, per, cin, cout, rank, n, dtype):
+    """A tile of rows per wave: tiles of several adapters, of none, grouped runs, a device count, in place."""
+    x, down, up, ids, alpha, base = make(rows + rank, rows, per, cin, cout, rank, n, dtype, ld=8)
+    want, mag = expected(x, down, up, ids, per, alpha, base, cout)
+    y = torch.full((rows + 1, cout + 8), 7.0, dtype=DT[dtype], device="cuda")
+    api.sige_token_lora(x, y[:rows, :cout], cin, cout, down, up, ids, per, alpha=alpha, base=base, n_rows=rows)
+    torch.cuda.synchronize()
+    close(y[:rows, :cout], want, mag, cin, rank, dtype, "many rows")
+    assert (y[rows] == 7.0).all() and (y[:, cout:] == 7.0).all()
+    y = base.clone()
+    count = len(ids) - 5
+    api.sige_token_lora(x, y, cin, cout, down, up, ids, per, alpha=alpha, base=y, count=torch.tensor([count], dtype=torch.int32, device="cuda"), max_rows=rows)
+    torch.cuda.synchronize()
+    close(y[:count * per], want[:count * per], mag[:count * per], cin, rank, dtype, "a device count")
+    assert torch.equal(y[count * per:], base[count * per:])
+    if dtype == "f16":                            # middle vectors beyond the range of fp16
+        down, alpha = down * 2.0 ** 10, torch.full_like(alpha, 256.0)
+        up = up * 2.0 ** -12
+        want, mag = expected(x, down, up, ids, per, alpha, base, cout)
+        api.sige_token_lora(x, y, cin, cout, down, up, ids, per, alpha=alpha, base=base, n_rows=rows)
+        torch.cuda.synchronize()
+        bound = ((cin + rank + 4) * 2.0 ** -24 + 2.0 ** -16) * mag + 2.0 ** -11 * np.abs(want) + 2.0 ** -25
+        assert (np.abs(f64(y) - want) <= bound).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_ids_counts_and_neighbours(dtype):
     """Every row its own adapter, ids that name none, the same adapter twice; rows by a device count; rows and adapters of NaN reach
