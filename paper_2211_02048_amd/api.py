@@ -563,6 +563,9 @@ def _at(t):
     return None if t is None else t.data_ptr()
 
 
+_I32 = torch.int32
+
+
 def _like(x, *tensors):
     """The tensors a kernel takes for the type of x."""
     dtype = x.dtype
@@ -573,7 +576,7 @@ def _like(x, *tensors):
 
 def _table(what, t, dtype, n):
     """A table the kernels read entry by entry: at least n of them, one after the other."""
-    if t is not None and (t.dtype is not dtype or t.numel() < n or not t.is_contiguous()):
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
         raise SigeError(1, f"{what}: {n} entries of {dtype}, contiguous, not {tuple(t.shape)} of {t.dtype}")
 
 
@@ -591,8 +594,10 @@ def _lines(t):
 def _block_list(indices, count, n_blocks, max_blocks=None):
     """The most blocks of a list that a call may read."""
     mb = indices.shape[0] if max_blocks is None else max_blocks
-    _table("indices", indices, torch.int32, 2 * (mb if n_blocks < 0 else n_blocks))
-    _table("count", count, torch.int32, 1)
+    if indices.dtype is not _I32 or indices.numel() < 2 * (mb if n_blocks < 0 else n_blocks) or not indices.is_contiguous():
+        _table("indices", indices, _I32, 2 * (mb if n_blocks < 0 else n_blocks))
+    if count is not None and count.dtype is not _I32:
+        _table("count", count, _I32, 1)
     return mb
 
 
@@ -601,9 +606,10 @@ def sige_token_rope(x, y, heads, d, pairs, positions, *, layout=ROPE_ADJACENT, n
     """Rotates the `heads` heads of every row by the row's positions (fp32 [rows, axes]); y may be x."""
     _like(x, y)
     mr = x.numel() // x.shape[-1] if max_rows is None else max_rows
-    _table("pairs", pairs, torch.int32, 4 * pairs.shape[0])
+    _table("pairs", pairs, _I32, 4 * pairs.shape[0])
     _table("positions", positions, torch.float32, (mr if n_rows < 0 else n_rows) * positions.shape[-1])
-    _table("count", count, torch.int32, 1)
+    if count is not None:
+        _table("count", count, _I32, 1)
     stream = _stream_of(x, y, pairs, positions, count)
     rc = lib().sige_token_rope(x.data_ptr(), _DT[x.dtype], heads, d, _lines(x) if x_ld is None else x_ld, _at(count),
                                rows_per_count, mr, n_rows, pairs.data_ptr(), pairs.shape[0], layout, positions.data_ptr(),
@@ -616,7 +622,7 @@ def sige_token_rope_blocks(x, y, heads, d, pairs, g: Geom, indices, count, *, n_
                            n_blocks=-1, max_blocks=None, x_ld=None, y_ld=None):
     """The same with the positions (y, x) or (frame, y, x) of the listed blocks' pixels."""
     _like(x, y)
-    _table("pairs", pairs, torch.int32, 4 * pairs.shape[0])
+    _table("pairs", pairs, _I32, 4 * pairs.shape[0])
     mb = _block_list(indices, count, n_blocks, max_blocks)
     stream = _stream_of(x, y, pairs, indices, count)
     rc = lib().sige_token_rope_blocks(x.data_ptr(), _DT[x.dtype], heads, d, _lines(x) if x_ld is None else x_ld, ctypes.byref(g),
@@ -654,8 +660,10 @@ def sige_cache4_store(k, v, cache, capacity, heads, d, *, slots=None, first=0, n
     _check_cache(cache, heads, d, capacity)
     _like(k, v)
     mr = k.shape[0] if max_rows is None else max_rows
-    _table("slots", slots, torch.int32, mr if n_rows < 0 else n_rows)
-    _table("count", count, torch.int32, 1)
+    if slots is not None:
+        _table("slots", slots, _I32, mr if n_rows < 0 else n_rows)
+    if count is not None:
+        _table("count", count, _I32, 1)
     stream = _stream_of(k, v, cache, slots, count)
     rc = lib().sige_cache4_store(k.data_ptr(), _rows_ld(k, heads, d) if k_ld is None else k_ld, v.data_ptr(),
                                  _rows_ld(v, heads, d) if v_ld is None else v_ld, _DT[k.dtype], heads, d, _at(slots), first,
@@ -700,7 +708,8 @@ def sige_cache4_attn(q, cache, capacity, o, scale, *, T, heads, d, Nq=None, rang
     _check_cache(cache, heads, d, capacity)
     _like(q, o)
     nq = q.shape[0] if Nq is None else Nq
-    _table("ranges", ranges, torch.int32, 2 * nq)
+    if ranges is not None:
+        _table("ranges", ranges, _I32, 2 * nq)
     stream = _stream_of(q, cache, o, ranges, workspace)
     rc = lib().sige_cache4_attn(q.data_ptr(), _rows_ld(q, heads, d) if q_ld is None else q_ld, cache.data_ptr(), capacity, _DT[q.dtype],
                                 nq, T, heads, d, scale, _at(ranges), o.data_ptr(),
@@ -715,7 +724,8 @@ def sige_cache4_attn_blocks(q_full, g: Geom, indices, n_blocks, cache, capacity,
     _check_cache(cache, heads, d, capacity)
     _like(q_full, o)
     _block_list(indices, None, n_blocks)
-    _table("ranges", ranges, torch.int32, 2 * n_blocks * g.block_h * g.block_w)
+    if ranges is not None:
+        _table("ranges", ranges, _I32, 2 * n_blocks * g.block_h * g.block_w)
     stream = _stream_of(q_full, cache, o, indices, ranges, workspace)
     rc = lib().sige_cache4_attn_blocks(q_full.data_ptr(), _lines(q_full) if q_ld is None else q_ld, ctypes.byref(g),
                                        indices.data_ptr(), n_blocks, cache.data_ptr(), capacity, _DT[q_full.dtype], T, heads, d, scale,
@@ -733,9 +743,11 @@ def sige_token_lora(x, y, Cin, Cout, down, up, ids, rows_per_id, *, alpha=None, 
         raise SigeError(1, "sige_token_lora: down is [adapters, rank, Cin] and up [adapters, Cout, rank], contiguous")
     _like(x, y, down, up, base)
     mr = x.numel() // x.shape[-1] if max_rows is None else max_rows
-    _table("ids", ids, torch.int32, -(-(mr if n_rows < 0 else n_rows) // max(rows_per_id, 1)))
-    _table("alpha", alpha, torch.float32, n)
-    _table("count", count, torch.int32, 1)
+    _table("ids", ids, _I32, -(-(mr if n_rows < 0 else n_rows) // max(rows_per_id, 1)))
+    if alpha is not None:
+        _table("alpha", alpha, torch.float32, n)
+    if count is not None:
+        _table("count", count, _I32, 1)
     stream = _stream_of(x, y, down, up, ids, alpha, base, count)
     rc = lib().sige_token_lora(x.data_ptr(), _DT[x.dtype], Cin, _lines(x) if x_ld is None else x_ld, _at(count), rows_per_id, mr,
                                n_rows, down.data_ptr(), up.data_ptr(), rank, n, _at(alpha), ids.data_ptr(), _at(base),

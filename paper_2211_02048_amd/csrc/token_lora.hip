@@ -4,7 +4,7 @@
 // Bound by memory: per row and adapter 2 rank (Cin + Cout) operations against (Cin + 2 Cout) values.  One kernel, no workspace: a
 // workgroup takes 16 rows, its four waves share the contraction over Cin (the partial products meet in LDS), then each takes
 // stretches of the output channels.  Few rows alone would leave most compute units without work, so the output channels are cut
-// over workgroups too, each of which repeats the small first product.  Where the 16 rows have several adapters there is one pass
+// over workgroups too, each of which repeats the small first product.  Many narrow rows instead: 16 rows for every wave by itself.  Where the 16 rows have several adapters there is one pass
 // for each, of which its own rows keep the result; where runs are short (single tokens of many requests) every workgroup of a section
 // of 128 runs first counts them into the order of their adapters and takes up to 16 rows of one adapter from there, in any place of
 // the section: no sorted copy, no second launch (32 tokens of 32 adapters of rank 32, 1280 -> 1280: 63 -> 8.4 us).
@@ -408,8 +408,9 @@ static int launch_lora(LoraArgs& a, int rows, hipStream_t st)
     // against 7.6; 1263 in runs of 3 of two adapters 7.1 against 6.3), and of up to 8 where latency counts (128 rows of 1280 -> 1280 7.9
     // against 9.2); from four runs on
     const int per = a.rows_per_id;
-    a.group = per <= (rows <= 512 ? 8 : 5) && rows > 3L * per && a.adapters > 2 && a.adapters < 1 << 24 ? 16 / per : 0;
+    a.group = per <= (rows <= 512 ? 8 : 5) && rows > 3L * per && a.adapters > 2 && a.adapters < 1 << 24 && rows < 1 << 23 ? 16 / per : 0;
     int tiles = (rows + 15) / 16;
+    a.d_tiles = a.d_group = fast_div(1);
     // (of n runs at most this many groups, each of one adapter or none; those that there are not end at once)
     auto groups = [&](int n) { return std::min(n, (int)((n + (long)std::min(a.adapters + 1, n) * (a.group - 1)) / a.group)); };
     if (a.group > 0) {
@@ -418,11 +419,11 @@ static int launch_lora(LoraArgs& a, int rows, hipStream_t st)
         a.d_tiles = fast_div(section);
         a.d_group = fast_div(a.group);
     }
-    // workgroups per 16 rows: one per compute unit where the rows alone are fewer (two take 8.6 instead of 6.8 us for 1011 rows of
-    // 640 -> 648 in single precision, half of one 7.8), a stretch of channels per wave at least
     // Narrow rows, a tile for every SIMD: each wave by itself (16384 rows of 128 -> 128 10.9 -> 5.9 us, of 320 -> 320 13.8 -> 10.1, single
     // tokens of 8 adapters 20 -> 9.4; 8192 of 320 -> 320 7.2 -> 9.0, 24576 of 640 -> 640 22.9 -> 25.9)
     const bool alone = tiles >= 1024 && (long)(a.Cin + a.Cout) * (long)sizeof(T) <= 1280;
+    // Else workgroups per 16 rows: one per compute unit where the rows alone are fewer (two take 8.6 instead of 6.8 us for 1011 rows of
+    // 640 -> 648 in single precision, half of one 7.8), a stretch of channels per wave at least
     const int cut = alone ? 1 : std::max(std::min((256 + tiles - 1) / tiles, (units + LORA_WAVES - 1) / LORA_WAVES), 1);
     a.span = alone ? units : (units + cut * LORA_WAVES - 1) / (cut * LORA_WAVES);
     if (alone) {
