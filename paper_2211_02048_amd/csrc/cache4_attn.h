@@ -857,8 +857,9 @@ static int launch_cache4_as(const Cache4AttnArgs& a, const Cache4Form& f, hipStr
     const int P = a.splits <= 4 ? 1 : a.splits <= 16 ? 4 : 16;             // (at most 64 splits)
     SIGE_REQUIRE(tiles * a.splits * threads < (1L << 32) && (a.splits == 1 || groups * P < (1L << 32) - 256), SIGE_ERR_UNSUPPORTED,
                  "sige_cache4_attn: too many queries");                       // (what a launch can have of threads)
-    if (lds > 48 * 1024) {
-        const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (lds > 48 * 1024) {                         // (allowed: the same for all calls of a kernel, two may be made at once)
+        const size_t most = std::max(lds, NK * std::max((size_t)cache4_apart_bytes(DT, NP), 32 * (32 * DT + 4) * sizeof(float)));
+        const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)most);
         SIGE_REQUIRE(e == hipSuccess, SIGE_ERR_HIP, "sige_cache4_attn: cannot reserve %zu bytes of LDS: %s", lds, hipGetErrorString(e));
     }
     hipLaunchKernelGGL(kern, dim3((unsigned)tiles, 1, a.splits), dim3(threads), lds, st, a);

@@ -478,3 +478,35 @@ def test_attention_takes_the_form_for_many_queries():
             p = torch.softmax(s, -1)
             want, mag = (p @ v[:, h]).cpu().numpy()[:, None], ((p + 2.0 ** -30) @ v[:, h].abs()).cpu().numpy()[:, None]
             close(o[:, h * d:(h + 1) * d], want, mag, q64[:, h:h + 1].cpu().numpy(), k[:, h:h + 1].cpu().numpy(), scale, dtype, T, f"{nq} of {T} x {d}")
+
+
+def test_calls_at_once():
+    """Two threads, each on a stream of its own with a workspace of its own, calling the same kernel for heads of two sizes: bit for bit
+    what each call gives alone."""
+    import threading
+    jobs = []
+    for d, T in ((72, 3000), (80, 900)):
+        q, cache, cap, _, _ = case(d, 40, T, 3, d, "bf16")
+        alone = attend(q, cache, cap, T, 3, d, 0.1).clone()
+        ws = torch.empty(api.sige_cache4_attn_workspace_bytes(40, T, 3, d) // 4 + 1, dtype=torch.float32, device="cuda")
+        jobs.append((q, cache, cap, T, d, alone, ws, [torch.empty(40, 3 * d, dtype=torch.bfloat16, device="cuda") for _ in range(20)]))
+    torch.cuda.synchronize()
+    errors = []
+
+    def work(job):
+        q, cache, cap, T, d, _, ws, outs = job
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for o in outs:
+                    api.sige_cache4_attn(q, cache, cap, o, 0.1, T=T, heads=3, d=d, workspace=ws)
+        except Exception as e:                     # noqa: BLE001
+            errors.append(e)
+    threads = [threading.Thread(target=work, args=(j,)) for j in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors, errors
+    for _, _, _, _, _, alone, _, outs in jobs:
+        assert all(torch.equal(o, alone) for o in outs)
