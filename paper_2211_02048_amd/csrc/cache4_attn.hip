@@ -38,18 +38,20 @@ static int cache4_waves(const Cache4Cut& cut, long workgroups, int share, bool m
 //                     against 50, 2^21 74 against 87; 256: 2^18 46 against 45, 2^19 55 against 47, 2^20 67 against 83); with ranges, of which 256
 //                     rows span more than 32, up to d = 128 four times of it (1024 rows of 16384 x 8 of 96 76 against 85 us, of 128 69 against 94;
 //                     2048 of 4096 x 8 of 128 63 against 59)
-// Splits over workgroups: of one to six rounds of the chip (of common chunks up to d = 96 a compute unit holds three workgroups, else one)
-// the number that costs least at 2.5 us per round, 2 per chunk (measured: 1.3 - 2.2 over all forms), and 3 and the partial sums' bytes
-// for the merge (1500 queries of 16384 x 3 of 40, 141 tiles: 51 -> 39 us); none for fewer than four chunks per wave, which end before that (16 queries of 4096 x 8 of 40, eight chunks per wave:
-// 16.2 us alone, 12.9, 10.0 and 9.0 in 2, 4 and 8 splits; 160 tiles of 4096 x 80 22.6 alone, 29.6 in two), nor side by side.  Rows
-// with ranges of their own make workgroups of different lengths: up to four (side by side: eight) times as many then, of eight chunks per
-// wave at least (2379 rows with ranges of 20391 x 2 of 32 52 -> 31 us; 640 of 4096 x 8 of 64 18.3, 22.5 in two of four chunks).
+// Splits over workgroups: of one to six rounds of the chip (of common chunks up to d = 96 a compute unit holds three workgroups, else
+// one) the number that costs least at 2.5 us per round, 2 per chunk (measured: 1.3 - 2.2 over all forms), and 3 and the partial sums'
+// bytes for the merge (1500 queries of 16384 x 3 of 40, 141 tiles: 51 -> 39 us); none for fewer than four chunks per wave, which end
+// before that (16 queries of 4096 x 8 of 40, eight chunks per wave: 16.2 us alone, 12.9, 10.0 and 9.0 in 2, 4 and 8 splits; 160 tiles of
+// 4096 x 80 22.6 alone, 29.6 in two), nor side by side.  Rows with ranges of their own make workgroups of different lengths: up to four
+// (side by side: eight) times as many then, of eight chunks per wave at least (2379 rows with ranges of 20391 x 2 of 32 52 -> 31 us; 640
+// of 4096 x 8 of 64 18.3, 22.5 in two of four chunks).
 static Cache4Form plan_cache4(int Nq, int T, int heads, int d, sige_dtype dt, bool ranges, size_t room = ~(size_t)0)
 {
     const int target = knob(SIGE_KNOB_ATTN_WGS);
     const long tiles = (long)heads * (((long)Nq + 31) / 32);
     const int many = knob(SIGE_KNOB_CACHE4_MANY);
-    Cache4Form f = {dt != SIGE_F32 && (many >= 0 ? many != 0 : d <= 64 ? tiles > 256 : (double)tiles * T * d * d >= (double)(1L << (ranges && d <= 128 ? 37 : 35))), 1};
+    const bool crosses = d <= 64 ? tiles > 256 : (double)tiles * T * d * d >= (double)(1L << (ranges && d <= 128 ? 37 : 35));
+    Cache4Form f = {dt != SIGE_F32 && (many >= 0 ? many != 0 : crosses), 1};
     const Cache4Cut cut = cache4_cut(d, dt, f.many);
     const long chunks = ((long)T + cut.chunk - 1) / cut.chunk;
     const long base = (long)heads * (((long)Nq + cut.rows - 1) / cut.rows);

@@ -2,18 +2,17 @@
 // the active blocks:   y_r = base_r + alpha_i * up_i (down_i x_r),   i = the adapter of the row's block.
 //
 // Bound by memory: per row and adapter 2 rank (Cin + Cout) operations against (Cin + 2 Cout) values.  One kernel, no workspace: a
-// workgroup takes 16 rows, its four waves share the contraction over Cin (the partial products meet in LDS), then each takes
-// stretches of the output channels.  Few rows alone would leave most compute units without work, so the output channels are cut
-// over workgroups too, each of which repeats the small first product.  Many narrow rows instead: 16 rows for every wave by itself.  Where the 16 rows have several adapters there is one pass
-// for each, of which its own rows keep the result; where runs are short (single tokens of many requests) every workgroup of a section
-// of 128 runs first counts them into the order of their adapters and takes up to 16 rows of one adapter from there, in any place of
-// the section: no sorted copy, no second launch (32 tokens of 32 adapters of rank 32, 1280 -> 1280: 63 -> 8.4 us).
-// Measured: 8192 rows of 1280 -> 1280 in fp16, rank 32, 19.2 us, 3.3 TB/s (the first product, its sums in LDS and the second follow
-// each other, and all workgroups are in the same phase; 162 KB of weights per workgroup come from L2); 64 rows of 320 -> 960 4.4 us, of
-// which a launch is 3.
-// The middle vector down_i x_r stays in 32 bits; the half types' second product takes it as the sum of two halves (the rounded
-// value and the rounded remainder: 16 bits of bf16, 22 of fp16).  fp16 has a power of two per row taken off before and put back on the
-// sums, so that neither end of its range is in the way.
+// workgroup takes 16 rows, its four waves share the contraction over Cin (the partial products meet in LDS), then each takes stretches of
+// the output channels.  Few rows alone would leave most compute units without work, so the output channels are cut over workgroups too,
+// each of which repeats the small first product.  Many narrow rows instead: 16 rows for every wave by itself.  Where the 16 rows have
+// several adapters there is one pass for each, of which its own rows keep the result; where runs are short (single tokens of many
+// requests) every workgroup of a section of 128 runs first counts them into the order of their adapters and takes up to 16 rows of one
+// adapter from there, in any place of the section: no sorted copy, no second launch (32 tokens of 32 adapters of rank 32, 1280 -> 1280:
+// 63 -> 8.4 us). Measured: 8192 rows of 1280 -> 1280 in fp16, rank 32, 19.2 us, 3.3 TB/s (the first product, its sums in LDS and the
+// second follow each other, and all workgroups are in the same phase; 162 KB of weights per workgroup come from L2); 64 rows of 320 ->
+// 960 4.4 us, of which a launch is 3. The middle vector down_i x_r stays in 32 bits; the half types' second product takes it as the sum
+// of two halves (the rounded value and the rounded remainder: 16 bits of bf16, 22 of fp16).  fp16 has a power of two per row taken off
+// before and put back on the sums, so that neither end of its range is in the way.
 #include "common.h"
 
 #include <algorithm>
@@ -92,8 +91,9 @@ template <typename T> __device__ __forceinline__ uint4 lora_sum(const f32x4 (&su
 constexpr int LORA_WAVES = 4;
 constexpr int LORA_SECTION = 128;                                 // runs that are grouped by adapter
 
-// ALONE: every wave has 16 rows of its own and shares nothing: no barriers, no sums in LDS.  RT = 16-wide tiles over the rank.  The registers are bounded for two workgroups per compute unit.  No load is guarded (a guard is a branch of its own): lanes past the end read the last vector or
-// row again, and what they make of it is either multiplied by the zeros behind the rank, or not stored.
+// ALONE: every wave has 16 rows of its own and shares nothing: no barriers, no sums in LDS.  RT = 16-wide tiles over the rank.  The
+// registers are bounded for two workgroups per compute unit.  No load is guarded (a guard is a branch of its own): lanes past the end
+// read the last vector or row again, and what they make of it is either multiplied by the zeros behind the rank, or not stored.
 template <typename T, int RT, bool ALONE>
 __global__ __launch_bounds__(64 * LORA_WAVES, 2) void token_lora_kernel(LoraArgs a)
 {
