@@ -18,8 +18,8 @@
 // they meet.  cache4_common_kernel: four or eight waves of 32 queries each that expand every chunk once for all.  The vector instructions
 // bound the first where there is work (per 64 keys x 32 queries x 64: about 90 for the expansion, 110 for the softmax), LDS and the order
 // of the two kinds of instructions the second.  Measured: one query of 65536 x 8 of 64 in bf16 14.7 us (with the merge; 35.7 MB, 2.4 TB/s),
-// 614 of 4096 x 8 of 80 in fp16 21 us (300 TFLOP/s: 160 workgroups of eight chunks per wave), 4096 of 16384 x 8 of 128 in bf16 291 us (945
-// TFLOP/s; a library product reaches 1167).
+// 614 of 4096 x 8 of 80 in fp16 21 us (300 TFLOP/s: 160 workgroups of eight chunks per wave), 4096 of 16384 x 8 of 128 in bf16 265 - 302 us by
+// card (1040 - 910 TFLOP/s; a library product reaches 1167).
 #pragma once
 
 #include "cache4.h"

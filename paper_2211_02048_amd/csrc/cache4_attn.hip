@@ -16,15 +16,16 @@ static Cache4Cut cache4_cut(int d, sige_dtype dt, bool many)
 // Waves of a workgroup.  Of more workgroups than compute units those with all waves fill the chip in few uneven rounds, and with few
 // chunks leave most waves idle: as many waves as the chip holds at once by registers (heads from 136 on, single precision from 72 on: one
 // per SIMD runs best), a power of two, none without a chunk (4096 queries of 77 tokens x 8 of 80 22 -> 9 us, of 160 25 -> 15; of 1500
-// tokens x 80 43 -> 32, x 160 85 -> 72; the wrong way 1500 queries of 1500 x 160 42 -> 49).  Where rows have ranges workgroups differ in length,
+// tokens x 80 43 -> 32, x 160 85 -> 72; the wrong way 1500 queries of 1500 x 160 42 -> 49); half types' heads from 136 on, to the nearest
+// (1100 queries of 4000 x 8 of 160 110 us with two waves, 90 with four).  Where rows have ranges workgroups differ in length,
 // and large ones end sooner (2889 rows with ranges of 12052 x 10 of 32 68 us, 88 with four waves).  Fewer workgroups than
 // compute units: idle waves cost nothing, and all of them write.
-static int cache4_waves(const Cache4Cut& cut, long workgroups, int share, bool many, bool ranges)
+static int cache4_waves(const Cache4Cut& cut, long workgroups, int share, bool many, bool ranges, bool wide)
 {
     if (cut.waves == 1 || workgroups <= 256) return cut.waves;
-    const long hold = ranges ? cut.waves : 256L * cut.waves * (many ? 4 : 1) / workgroups;
+    const double hold = ranges ? cut.waves : 256.0 * cut.waves * (many ? 4 : 1) / workgroups;
     int w = cut.waves;
-    while (w > 1 && (w > hold || w / 2 >= share)) w /= 2;
+    while (w > 1 && (w > (wide ? hold + hold / 3 : hold) || w / 2 >= share)) w /= 2;
     return w;
 }
 
@@ -42,7 +43,8 @@ static int cache4_waves(const Cache4Cut& cut, long workgroups, int share, bool m
 // one) the number that costs least at 2.5 us per round, 2 per chunk (measured: 1.3 - 2.2 over all forms), and 3 and the partial sums'
 // bytes for the merge (1500 queries of 16384 x 3 of 40, 141 tiles: 51 -> 39 us); none for fewer than four chunks per wave, which end
 // before that (16 queries of 4096 x 8 of 40, eight chunks per wave: 16.2 us alone, 12.9, 10.0 and 9.0 in 2, 4 and 8 splits; 160 tiles of
-// 4096 x 80 22.6 alone, 29.6 in two), nor side by side.  Rows with ranges of their own make workgroups of different lengths: up to four
+// 4096 x 80 22.6 alone, 29.6 in two), nor side by
+// side, nor where every wave has tiles enough by itself (more tiles than compute units).  Rows with ranges of their own make workgroups of different lengths: up to four
 // (side by side: eight) times as many then, of eight chunks per wave at least (2379 rows with ranges of 20391 x 2 of 32 52 -> 31 us; 640
 // of 4096 x 8 of 64 18.3, 22.5 in two of four chunks).
 static Cache4Form plan_cache4(int Nq, int T, int heads, int d, sige_dtype dt, bool ranges, size_t room = ~(size_t)0)
@@ -59,7 +61,7 @@ static Cache4Form plan_cache4(int Nq, int T, int heads, int d, sige_dtype dt, bo
     const bool crowd = f.many && cut.waves > 1;
     const long most = std::max(std::min(chunks / cut.waves, 64L), 1L);
     long want = target >= 0 ? (target + base - 1) / base : 1;
-    if (target < 0 && !crowd && chunks >= 4 * cut.waves) {
+    if (target < 0 && !crowd && (cut.waves == 1 || base <= fill) && chunks >= 4 * cut.waves) {
         double least = INFINITY;
         for (int rounds = 1; rounds <= 6; ++rounds) {
             const long z = std::max(std::min(fill * rounds / base, most), 1L);
@@ -110,7 +112,8 @@ static int cache4_attn_entry(const char* who, Cache4AttnArgs& a, const void* q, 
     a.splits = f.splits;
     a.share = (int)((((long)T + cut.chunk - 1) / cut.chunk + f.splits - 1) / f.splits);
     a.d_splits = fast_div(f.splits);
-    a.waves = cache4_waves(cut, (((long)Nq + cut.rows - 1) / cut.rows) * heads * f.splits, a.share, f.many, ranges != nullptr);
+    a.waves = cache4_waves(cut, (((long)Nq + cut.rows - 1) / cut.rows) * heads * f.splits, a.share, f.many, ranges != nullptr,
+                           dt != SIGE_F32 && d > 128);
     hipStream_t st = (hipStream_t)stream;
     return dt == SIGE_F32 ? launch_cache4_f32(a, f, st) : dt == SIGE_F16 ? launch_cache4_f16(a, f, st) : launch_cache4_bf16(a, f, st);
 }
