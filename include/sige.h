@@ -498,6 +498,7 @@ int sige_cache4_load(const void* cache, int32_t capacity, sige_dtype dt, int32_t
  * what a row does not see - NaN, infinities - does not reach it.  0 <= T <= capacity.
  * The cached values enter the products exactly (they are bf16 numbers; for fp16 queries, fp16 numbers wherever an fp16 row was stored).
  * fp16 and bf16 round a probability to their type once; single precision loses nothing (operands in three parts).
+ * Finite queries and values give finite rows as long as the logits and a row's sum of values stay in the range of fp32.
  * scale >= 0.  workspace: as for sige_sparse_attn, sige_cache4_attn_workspace_bytes of it; two calls that may run at the same time (on
  * two streams, in two graphs) need one each.  T < 2^31 - 128.                              */
 int sige_cache4_attn(const void* q, int32_t q_ld, const void* cache, int32_t capacity, sige_dtype dt, int32_t Nq,

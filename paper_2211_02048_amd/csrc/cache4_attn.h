@@ -45,7 +45,7 @@ struct Cache4AttnArgs {
     int splits, share;         // workgroups that share the tokens of a query out, and their chunks of all T
     int waves;                 // of a workgroup, where they share its tokens out: 1, 2, 4 or 8
     int full, gs_log2;
-    float scale_log2e;
+    float scale_log2e, inv_scale;  // and its inverse
     int q_tpb, q_bw, q_H, q_W;
     FastDiv d_heads, d_tpb, d_qbw, d_dq, d_splits;
 };
@@ -195,6 +195,10 @@ __device__ __forceinline__ void cache4_queries(const Cache4AttnArgs& a, int qi, 
     }
 }
 
+// Maxima from here on (of logits times log2 e): their rounding, which the fused operation of the exponents keeps, is no longer small
+// beside the offset of fp16's probabilities (2^15, the type ends at 2^16), and from 2^31 on beside the range of single precision.
+constexpr float CACHE4_FAR = 1048576.0f;
+
 // The sums of a wave's 32 rows.  Of a 32-key tile of logits a lane holds keys 8 * (r / 4) + 4 * half + r % 4 of its row.
 template <typename T, int DT, bool ODD, int KT> struct Cache4Sums {
     using C = typename Cache4Compute<T>::type;
@@ -250,7 +254,7 @@ template <typename T, int DT, bool ODD, int KT> struct Cache4Sums {
     }
     // The running maximum, and the sums brought to it; returns what the exponents subtract.  Logits are compared raw: the scale
     // (> 0) goes into the exponent.
-    __device__ __forceinline__ float settle(float scale_log2e, const f32x16 (&sacc)[KT])
+    __device__ __forceinline__ float settle(float scale_log2e, float inv_scale, f32x16 (&sacc)[KT])
     {
         float mr = sacc[0][0];
 #pragma unroll
@@ -271,7 +275,23 @@ template <typename T, int DT, bool ODD, int KT> struct Cache4Sums {
         }
         // (fp16: probabilities times 2^15, numerator and denominator alike, so that those down to 2^-29 keep their 11 bits and
         // only what is below 2^-40 is lost)
-        return m_at - (__is_same(C, f16) ? 15.0f : 0.0f);
+        constexpr float up = __is_same(C, f16) ? 15.0f : 0.0f;
+        float m_sub = m_at - up;
+        if (__builtin_amdgcn_ballot_w64(fabsf(m_at) >= CACHE4_FAR) != 0ull) {
+            // The products of such a row are rounded as its maximum was and its logits measured from there: the largest exponent is
+            // exactly 0 (finite logits of 10^7 in fp16, of 2 10^9 in bf16 made infinite probabilities).  The other rows stay as they are.
+            const bool mine = fabsf(m_at) >= CACHE4_FAR;
+#pragma unroll
+            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    float e = sacc[kt][r] * scale_log2e;
+                    asm volatile("" : "+v"(e));                    // (a product of its own, not a part of a fused operation)
+                    sacc[kt][r] = mine ? (e - m_at) * inv_scale : sacc[kt][r];
+                }
+            m_sub = mine ? -up : m_sub;
+        }
+        return m_sub;
     }
     // The probabilities, and O^T += V^T P^T in steps of 16 keys; v(kt, s, nt): the V^T fragment.  URGENT: from the product on the wave
     // goes before the others of its SIMD
@@ -513,7 +533,7 @@ __global__ __launch_bounds__(64 * NK, WAVES) void cache4_apart_kernel(Cache4Attn
             }
         if (next < c_end) fetch(next);             // in flight during the softmax and the second product
         if (partial) sums.hide(a, seen, t0, half, marked, vsec + a.scales + (long)t0 * GS, sacc);
-        const float m_sub = sums.settle(a.scale_log2e, sacc);
+        const float m_sub = sums.settle(a.scale_log2e, a.inv_scale, sacc);
         sums.template add<false>(a.scale_log2e, m_sub, sacc, v_fragment);
         c = next;
     }
@@ -748,7 +768,7 @@ __global__ __launch_bounds__(64 * cache4_common_waves(DT), 2) void cache4_common
         if (seen.partial(t0, KCH))
             sums.hide(a, seen, t0, half, __builtin_amdgcn_readfirstlane(marked_chunk[buf]) == c + 1,
                       sec + a.section + a.scales + ((long)t0 << a.gs_log2), sacc);
-        const float m_sub = sums.settle(a.scale_log2e, sacc);
+        const float m_sub = sums.settle(a.scale_log2e, a.inv_scale, sacc);
         sums.template add<true>(a.scale_log2e, m_sub, sacc, [&](int kt, int s, int nt) {
             char* const at = rows + tr + (kt * 32 + 16 * s) * VROW + nt * 64;
             union { s16x4 h[2]; u32x4 u; } vf;

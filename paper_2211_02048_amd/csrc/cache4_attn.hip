@@ -105,6 +105,7 @@ static int cache4_attn_entry(const char* who, Cache4AttnArgs& a, const void* q, 
     a.q_ld = q_ld; a.o_ld = o_ld; a.Nq = Nq; a.T = T; a.heads = heads; a.d = d;
     // (never 0, which would make a number of the -inf of a token out of sight: the smallest float turns every finite logit into 0 too)
     a.scale_log2e = std::max(scale * 1.4426950408889634f, 1.4e-45f);
+    a.inv_scale = 1.0f / a.scale_log2e;
     a.d_heads = fast_div(heads); a.d_tpb = fast_div(a.q_tpb); a.d_qbw = fast_div(a.q_bw); a.d_dq = fast_div(d / 4);
     const bool room = workspace != nullptr && aligned16(workspace);
     const Cache4Form f = plan_cache4(Nq, T, heads, d, dt, ranges != nullptr, room ? workspace_bytes / sizeof(float) : 0);
