@@ -77,12 +77,15 @@ template <typename C> __device__ __forceinline__ uint32_t round2(float a, float 
     }
 }
 
-// Two floats as NP pairs of the compute type whose sums they are (to 8 NP bits of bf16).
-template <typename C, int NP> __device__ __forceinline__ void split2(float a, float b, uint32_t (&out)[NP])
+// Two floats as NP pairs of the compute type whose sums they are (to 8 NP bits of bf16).  ANY: of any size - single precision ends
+// above bf16, where the first part is bf16's largest number instead of an infinity (what is infinite becomes NaN with the others).
+template <typename C, int NP, bool ANY> __device__ __forceinline__ void split2(float a, float b, uint32_t (&out)[NP])
 {
+    constexpr float LARGEST = 0x1.fep127f;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-        out[i] = round2<C>(a, b);
+        if (ANY && i == 0) out[i] = round2<C>(fminf(fmaxf(a, -LARGEST), LARGEST), fminf(fmaxf(b, -LARGEST), LARGEST));
+        else out[i] = round2<C>(a, b);
         if (i + 1 < NP) {
             a -= __uint_as_float(out[i] << 16);
             b -= __uint_as_float(out[i] & 0xffff0000u);
@@ -184,7 +187,7 @@ __device__ __forceinline__ void cache4_queries(const Cache4AttnArgs& a, int qi, 
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     uint32_t w[NP];
-                    split2<C, NP>(f[2 * j], f[2 * j + 1], w);
+                    split2<C, NP, true>(f[2 * j], f[2 * j + 1], w);
 #pragma unroll
                     for (int p = 0; p < NP; ++p) qf[p][s][j] = w[p];
                 }
@@ -311,7 +314,7 @@ template <typename T, int DT, bool ODD, int KT> struct Cache4Sums {
                 for (int j = 0; j < 4; ++j) {
                     const float p0 = sacc[kt][8 * s + 2 * j], p1 = sacc[kt][8 * s + 2 * j + 1];
                     uint32_t w[NP];
-                    split2<C, NP>(p0, p1, w);
+                    split2<C, NP, false>(p0, p1, w);
 #pragma unroll
                     for (int p = 0; p < NP; ++p) pf[p][j] = w[p];
                     if constexpr (!ODD) {

@@ -21,13 +21,13 @@ def cache_of(k, v, dtype, capacity):
     return cache, ref.read(cache, heads, d, capacity, T, 0), ref.read(cache, heads, d, capacity, T, 1)
 
 
-def near(o, want, mag, dtype, T, what):
-    """As test_gpu_cache4.close for logits without an error of their own: |o - want| <= (p + s) sum_t p_t |v_t| + r |want| with p the rounding
+def near(o, want, mag, dtype, T, what, logits=0.0):
+    """As test_gpu_cache4.close for logits whose error is known (none: they are exact): |o - want| <= (p + s) sum_t p_t |v_t| + r |want| with p the rounding
     of the probabilities in numerator and denominator (single precision: three parts), s the exponential's 2^-21 in both and the
-    T terms of both sums, r the rounding of the result."""
+    T terms of both sums, twice the logits' error, r the rounding of the result."""
     eps = torch.finfo(DT[dtype]).eps
     p = eps if dtype != "f32" else 2.0 ** -22
-    bound = (p + 2.0 ** -20 + T * 2.0 ** -23) * mag + eps / 2 * np.abs(want) + (2.0 ** -25 if dtype == "f16" else 1e-30)
+    bound = (p + 2.0 ** -20 + T * 2.0 ** -23 + 2 * logits) * mag + eps / 2 * np.abs(want) + (2.0 ** -25 if dtype == "f16" else 1e-30)
     got = f64(o).reshape(want.shape)
     assert np.isfinite(got).all(), f"{what}: {int((~np.isfinite(got)).sum())} of {got.size} are no numbers"
     assert (np.abs(got - want) <= bound).all(), f"{what}: worst {np.max(np.abs(got - want) / bound):.2f} of the bound"
@@ -98,3 +98,29 @@ def test_large_logits_of_all_channels(d, dtype):
                     o = f64(attend(qt, cache, cap, T, heads, d, scale, None, ws)).reshape(nq, heads, d)
                 assert np.isfinite(o).all(), f"{size}, form {many}: {int((~np.isfinite(o)).sum())} of {o.size} are no numbers"
                 assert (o >= lo - room).all() and (o <= hi + room).all()
+
+
+@pytest.mark.parametrize("d", [24, 64, 96, 256])
+def test_queries_at_the_end_of_single_precision(d):
+    """Queries up to the largest float, beyond the largest number of bf16, on keys so small that the logits are ordinary."""
+    heads, nq, T = 2, 33, 50
+    rng = np.random.default_rng(d)
+    most = float(torch.finfo(torch.float32).max)
+    k = np.zeros((T, heads, d))
+    at = [0, d // 2, d - 1]
+    k[..., at] = rng.choice([-6.0, -2.0, -0.5, 0.5, 1.0, 4.0], (T, heads, 3)) * 2.0 ** -125
+    v = rng.standard_normal((T, heads, d))
+    q = np.zeros((nq, heads, d))
+    q[..., at] = rng.choice([most, -most, 3.4e38, 3.397e38, 3.39e38, 1e38, -3.0], (nq, heads, 3))
+    qt = torch.from_numpy(q.reshape(nq, heads * d)).float().cuda()
+    q = f64(qt).reshape(nq, heads, d)
+    cache, k, v = cache_of(k, v, "f32", T)
+    want, mag = ref.attention(q, k, v, 0.125)
+    o = attend(qt, torch.from_numpy(cache).cuda(), T, T, heads, d, 0.125)
+    # (nine products - three channels, three parts - are added in fp32: 2^-24 of at most 3 * 6 2^-125 * 2^128 / 8 = 18 each time)
+    near(o, want, mag, "f32", T, "the largest queries", logits=9 * 18 * 2.0 ** -24)
+    qt[5, 1] = float("inf")
+    qt[6, d] = float("nan")
+    o = attend(qt, torch.from_numpy(cache).cuda(), T, T, heads, d, 0.125).view(nq, heads, d)
+    assert torch.isnan(o[5, 0]).all() and torch.isnan(o[6, 1]).all()
+    assert torch.isfinite(o[:5]).all() and torch.isfinite(o[7:]).all()
