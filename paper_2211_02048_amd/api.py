@@ -586,9 +586,10 @@ def _lines(t):
     if len(st) == 2 and st[1] == 1:
         return st[0]
     sh = t.shape
-    if len(st) < 2 or st[-1] != 1 or any(sh[i] > 1 and st[i] != sh[i + 1] * st[i + 1] for i in range(len(sh) - 2)):
+    outer = [(n, s) for n, s in zip(sh[:-1], st[:-1]) if n != 1]           # (the stride of an axis of one is nobody's)
+    if len(st) < 2 or st[-1] != 1 or any(s != outer[i + 1][0] * outer[i + 1][1] for i, (_, s) in enumerate(outer[:-1])):
         raise SigeError(1, f"rows of channels at one distance, not {tuple(sh)} with strides {st}")
-    return st[-2]
+    return outer[-1][1] if outer else st[-2]
 
 
 def _block_list(indices, count, n_blocks, max_blocks=None):

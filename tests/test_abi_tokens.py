@@ -205,3 +205,16 @@ def test_the_binding_refuses_tables_and_types():
         for call in bad:
             with pytest.raises(api.SigeError, match=what):
                 call()
+
+
+def test_the_binding_refuses_gaps_between_rows():
+    """Tiles of 1 x 8 pixels out of tiles of 1 x 10: the rows do not follow each other at one distance, whatever the axis of one says;
+    an axis of one between rows that do is no gap."""
+    h, i = torch.bfloat16, torch.int32
+    wide, y = torch.zeros(4, 1, 10, 128, dtype=h), torch.zeros(40, 128, dtype=h)
+    down, up, ids = torch.zeros(2, 8, 128, dtype=h), torch.zeros(2, 128, 8, dtype=h), torch.zeros(10, dtype=i)
+    for x, n, what in ((wide[:, :, :8], 32, "one distance"), (wide, 40, "cpu"), (wide[:, :, :, :64], 40, "cpu"),
+                       (torch.zeros(4, 3, 10, 128, dtype=h)[:, :1], 40, "one distance"), (torch.zeros(4, 3, 128, dtype=h)[:, :1], 4, "cpu")):
+        c = x.shape[-1]
+        with pytest.raises(api.SigeError, match=what):
+            api.sige_token_lora(x, y, c, 128, down[:, :, :c].contiguous(), up, ids, 4, n_rows=n)
