@@ -580,16 +580,37 @@ def _table(what, t, dtype, n):
         raise SigeError(1, f"{what}: {n} entries of {dtype}, contiguous, not {tuple(t.shape)} of {t.dtype}")
 
 
-def _lines(t):
-    """Stride of the rows of t, [..., channels] with rows that follow each other at one distance."""
+def _holds(t, rows, width, ld=None):
+    """Refuses a tensor that has not the rows a call touches: by its shape, or, where the call gives the rows' stride itself, by
+    what its storage holds from its first element on."""
+    if rows <= 0:
+        return
+    if ld is not None:
+        room = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+        if (rows - 1) * ld + width > room:
+            raise SigeError(3, f"{rows} rows of {width} channels, {ld} apart, in a tensor with {room} elements behind its first")
+    elif t.shape[-1] < width or t.numel() // t.shape[-1] < rows:
+        raise SigeError(3, f"{rows} rows of {width} channels in a tensor of {tuple(t.shape)}")
+
+
+def _lines(t, rows, width, ld=None):
+    """Stride of the rows of t, [..., channels] with `rows` rows or more, of `width` channels or more, that follow each other at one
+    distance; ld: the caller's own."""
     st = t.stride()
-    if len(st) == 2 and st[1] == 1:
-        return st[0]
-    sh = t.shape
-    outer = [(n, s) for n, s in zip(sh[:-1], st[:-1]) if n != 1]           # (the stride of an axis of one is nobody's)
-    if len(st) < 2 or st[-1] != 1 or any(s != outer[i + 1][0] * outer[i + 1][1] for i, (_, s) in enumerate(outer[:-1])):
-        raise SigeError(1, f"rows of channels at one distance, not {tuple(sh)} with strides {st}")
-    return outer[-1][1] if outer else st[-2]
+    if ld is not None:
+        _holds(t, rows, width, ld)
+    elif len(st) == 2 and st[1] == 1:
+        ld = st[0]
+        if t.shape[0] < rows or t.shape[1] < width:
+            _holds(t, rows, width)
+    else:
+        sh = t.shape
+        outer = [(n, s) for n, s in zip(sh[:-1], st[:-1]) if n != 1]       # (the stride of an axis of one is nobody's)
+        if len(st) < 2 or st[-1] != 1 or any(s != outer[i + 1][0] * outer[i + 1][1] for i, (_, s) in enumerate(outer[:-1])):
+            raise SigeError(1, f"rows of channels at one distance, not {tuple(sh)} with strides {st}")
+        _holds(t, rows, width)
+        ld = outer[-1][1] if outer else st[-2]
+    return ld
 
 
 def _block_list(indices, count, n_blocks, max_blocks=None):
@@ -597,7 +618,7 @@ def _block_list(indices, count, n_blocks, max_blocks=None):
     mb = indices.shape[0] if max_blocks is None else max_blocks
     if indices.dtype is not _I32 or indices.numel() < 2 * (mb if n_blocks < 0 else n_blocks) or not indices.is_contiguous():
         _table("indices", indices, _I32, 2 * (mb if n_blocks < 0 else n_blocks))
-    if count is not None and count.dtype is not _I32:
+    if count is not None:
         _table("count", count, _I32, 1)
     return mb
 
@@ -606,15 +627,17 @@ def sige_token_rope(x, y, heads, d, pairs, positions, *, layout=ROPE_ADJACENT, n
                     max_rows=None, x_ld=None, y_ld=None):
     """Rotates the `heads` heads of every row by the row's positions (fp32 [rows, axes]); y may be x."""
     _like(x, y)
-    mr = x.numel() // x.shape[-1] if max_rows is None else max_rows
+    mr = x.numel() // max(x.shape[-1], 1) if max_rows is None else max_rows
+    rows = mr if n_rows < 0 else n_rows
     _table("pairs", pairs, _I32, 4 * pairs.shape[0])
-    _table("positions", positions, torch.float32, (mr if n_rows < 0 else n_rows) * positions.shape[-1])
+    _table("positions", positions, torch.float32, rows * positions.shape[-1])
     if count is not None:
         _table("count", count, _I32, 1)
+    x_ld, y_ld = _lines(x, rows, heads * d, x_ld), _lines(y, rows, heads * d, y_ld)
     stream = _stream_of(x, y, pairs, positions, count)
-    rc = lib().sige_token_rope(x.data_ptr(), _DT[x.dtype], heads, d, _lines(x) if x_ld is None else x_ld, _at(count),
+    rc = lib().sige_token_rope(x.data_ptr(), _DT[x.dtype], heads, d, x_ld, _at(count),
                                rows_per_count, mr, n_rows, pairs.data_ptr(), pairs.shape[0], layout, positions.data_ptr(),
-                               positions.shape[-1], y.data_ptr(), _lines(y) if y_ld is None else y_ld, stream)
+                               positions.shape[-1], y.data_ptr(), y_ld, stream)
     if rc:
         _check(rc)
 
@@ -625,10 +648,12 @@ def sige_token_rope_blocks(x, y, heads, d, pairs, g: Geom, indices, count, *, n_
     _like(x, y)
     _table("pairs", pairs, _I32, 4 * pairs.shape[0])
     mb = _block_list(indices, count, n_blocks, max_blocks)
+    rows = (mb if n_blocks < 0 else n_blocks) * g.block_h * g.block_w
+    x_ld, y_ld = _lines(x, rows, heads * d, x_ld), _lines(y, rows, heads * d, y_ld)
     stream = _stream_of(x, y, pairs, indices, count)
-    rc = lib().sige_token_rope_blocks(x.data_ptr(), _DT[x.dtype], heads, d, _lines(x) if x_ld is None else x_ld, ctypes.byref(g),
+    rc = lib().sige_token_rope_blocks(x.data_ptr(), _DT[x.dtype], heads, d, x_ld, ctypes.byref(g),
                                       indices.data_ptr(), _at(count), mb, n_blocks, pairs.data_ptr(), pairs.shape[0], layout, n_axes,
-                                      frame, y.data_ptr(), _lines(y) if y_ld is None else y_ld, stream)
+                                      frame, y.data_ptr(), y_ld, stream)
     if rc:
         _check(rc)
 
@@ -639,17 +664,30 @@ def sige_cache4_bytes(heads, d, capacity) -> int:
     return int(lib().sige_cache4_bytes(heads, d, capacity))
 
 
-def _rows_ld(t, heads, d):
-    """Stride of the rows of t, [rows, heads * d or more] or [rows, heads, d]."""
+def _rows_ld(t, rows, heads, d, ld=None):
+    """Stride of the rows of t, [rows or more, heads * d or more] or [rows or more, heads, d]; ld: the caller's own."""
     if t is None:
         return 0
-    st = t.stride()
-    if st[-1] == 1 and (len(st) == 2 or len(st) == 3 and st[1] == d and t.shape[1:] == (heads, d)):
-        return st[0]
-    raise SigeError(1, f"rows of {heads} heads of {d} channels, not {tuple(t.shape)} with strides {st}")
+    if ld is not None:
+        _holds(t, rows, heads * d, ld)
+        return ld
+    st, sh = t.stride(), t.shape
+    if st[-1] != 1 or not (len(st) == 2 or len(st) == 3 and st[1] == d and sh[1:] == (heads, d)):
+        raise SigeError(1, f"rows of {heads} heads of {d} channels, not {tuple(sh)} with strides {st}")
+    if sh[0] < rows or len(st) == 2 and rows > 0 and sh[1] < heads * d:
+        raise SigeError(3, f"{rows} rows of {heads} heads of {d} channels in a tensor of {tuple(sh)}")
+    return st[0]
+
+
+def _work_bytes(workspace):
+    if workspace is not None and not workspace.is_contiguous():
+        raise SigeError(1, "the workspace must be contiguous")
+    return _nbytes(workspace)
 
 
 def _check_cache(cache, heads, d, capacity):
+    if not cache.is_contiguous():
+        raise SigeError(1, "the cache must be contiguous")
     need = sige_cache4_bytes(heads, d, capacity)
     if _nbytes(cache) < need:
         raise SigeError(3, f"a cache of {capacity} tokens takes {need} bytes, the tensor has {_nbytes(cache)}")
@@ -661,13 +699,14 @@ def sige_cache4_store(k, v, cache, capacity, heads, d, *, slots=None, first=0, n
     _check_cache(cache, heads, d, capacity)
     _like(k, v)
     mr = k.shape[0] if max_rows is None else max_rows
+    rows = mr if n_rows < 0 else n_rows
     if slots is not None:
-        _table("slots", slots, _I32, mr if n_rows < 0 else n_rows)
+        _table("slots", slots, _I32, rows)
     if count is not None:
         _table("count", count, _I32, 1)
+    k_ld, v_ld = _rows_ld(k, rows, heads, d, k_ld), _rows_ld(v, rows, heads, d, v_ld)
     stream = _stream_of(k, v, cache, slots, count)
-    rc = lib().sige_cache4_store(k.data_ptr(), _rows_ld(k, heads, d) if k_ld is None else k_ld, v.data_ptr(),
-                                 _rows_ld(v, heads, d) if v_ld is None else v_ld, _DT[k.dtype], heads, d, _at(slots), first,
+    rc = lib().sige_cache4_store(k.data_ptr(), k_ld, v.data_ptr(), v_ld, _DT[k.dtype], heads, d, _at(slots), first,
                                  _at(count), rows_per_count, mr, n_rows, cache.data_ptr(), capacity, stream)
     if rc:
         _check(rc)
@@ -679,9 +718,10 @@ def sige_cache4_store_blocks(k, v, cache, capacity, heads, d, g: Geom, indices, 
     _check_cache(cache, heads, d, capacity)
     _like(k, v)
     mb = _block_list(indices, count, n_blocks, max_blocks)
+    rows = (mb if n_blocks < 0 else n_blocks) * g.block_h * g.block_w
+    k_ld, v_ld = _rows_ld(k, rows, heads, d, k_ld), _rows_ld(v, rows, heads, d, v_ld)
     stream = _stream_of(k, v, cache, indices, count)
-    rc = lib().sige_cache4_store_blocks(k.data_ptr(), _rows_ld(k, heads, d) if k_ld is None else k_ld, v.data_ptr(),
-                                        _rows_ld(v, heads, d) if v_ld is None else v_ld, _DT[k.dtype], heads, d, ctypes.byref(g),
+    rc = lib().sige_cache4_store_blocks(k.data_ptr(), k_ld, v.data_ptr(), v_ld, _DT[k.dtype], heads, d, ctypes.byref(g),
                                         indices.data_ptr(), _at(count), mb, n_blocks, first, cache.data_ptr(), capacity, stream)
     if rc:
         _check(rc)
@@ -691,11 +731,13 @@ def sige_cache4_load(cache, capacity, heads, d, k, v, *, first=0, n_tokens=None,
     """Tokens first, first + 1, ... of the cache as rows of k's and v's type (either may be None)."""
     _check_cache(cache, heads, d, capacity)
     t = k if k is not None else v
+    if t is None:
+        raise SigeError(1, "sige_cache4_load: k or v is required")
     _like(t, v)
+    n = t.shape[0] if n_tokens is None else n_tokens
+    k_ld, v_ld = _rows_ld(k, n, heads, d, k_ld), _rows_ld(v, n, heads, d, v_ld)
     stream = _stream_of(cache, k, v)
-    rc = lib().sige_cache4_load(cache.data_ptr(), capacity, _DT[t.dtype], heads, d, first, t.shape[0] if n_tokens is None else n_tokens,
-                                _at(k), _rows_ld(k, heads, d) if k_ld is None else k_ld, _at(v),
-                                _rows_ld(v, heads, d) if v_ld is None else v_ld, stream)
+    rc = lib().sige_cache4_load(cache.data_ptr(), capacity, _DT[t.dtype], heads, d, first, n, _at(k), k_ld, _at(v), v_ld, stream)
     if rc:
         _check(rc)
 
@@ -711,10 +753,10 @@ def sige_cache4_attn(q, cache, capacity, o, scale, *, T, heads, d, Nq=None, rang
     nq = q.shape[0] if Nq is None else Nq
     if ranges is not None:
         _table("ranges", ranges, _I32, 2 * nq)
+    q_ld, o_ld, wsb = _rows_ld(q, nq, heads, d, q_ld), _rows_ld(o, nq, heads, d, o_ld), _work_bytes(workspace)
     stream = _stream_of(q, cache, o, ranges, workspace)
-    rc = lib().sige_cache4_attn(q.data_ptr(), _rows_ld(q, heads, d) if q_ld is None else q_ld, cache.data_ptr(), capacity, _DT[q.dtype],
-                                nq, T, heads, d, scale, _at(ranges), o.data_ptr(),
-                                _rows_ld(o, heads, d) if o_ld is None else o_ld, _at(workspace), _nbytes(workspace), stream)
+    rc = lib().sige_cache4_attn(q.data_ptr(), q_ld, cache.data_ptr(), capacity, _DT[q.dtype], nq, T, heads, d, scale, _at(ranges),
+                                o.data_ptr(), o_ld, _at(workspace), wsb, stream)
     if rc:
         _check(rc)
 
@@ -725,13 +767,15 @@ def sige_cache4_attn_blocks(q_full, g: Geom, indices, n_blocks, cache, capacity,
     _check_cache(cache, heads, d, capacity)
     _like(q_full, o)
     _block_list(indices, None, n_blocks)
+    nq = n_blocks * g.block_h * g.block_w
     if ranges is not None:
-        _table("ranges", ranges, _I32, 2 * n_blocks * g.block_h * g.block_w)
+        _table("ranges", ranges, _I32, 2 * nq)
+    q_ld, o_ld = _lines(q_full, g.H_in * g.W_in if nq > 0 else 0, heads * d, q_ld), _rows_ld(o, nq, heads, d, o_ld)
+    wsb = _work_bytes(workspace)
     stream = _stream_of(q_full, cache, o, indices, ranges, workspace)
-    rc = lib().sige_cache4_attn_blocks(q_full.data_ptr(), _lines(q_full) if q_ld is None else q_ld, ctypes.byref(g),
-                                       indices.data_ptr(), n_blocks, cache.data_ptr(), capacity, _DT[q_full.dtype], T, heads, d, scale,
-                                       _at(ranges), o.data_ptr(), _rows_ld(o, heads, d) if o_ld is None else o_ld, _at(workspace),
-                                       _nbytes(workspace), stream)
+    rc = lib().sige_cache4_attn_blocks(q_full.data_ptr(), q_ld, ctypes.byref(g), indices.data_ptr(), n_blocks, cache.data_ptr(),
+                                       capacity, _DT[q_full.dtype], T, heads, d, scale, _at(ranges), o.data_ptr(), o_ld,
+                                       _at(workspace), wsb, stream)
     if rc:
         _check(rc)
 
@@ -743,17 +787,18 @@ def sige_token_lora(x, y, Cin, Cout, down, up, ids, rows_per_id, *, alpha=None, 
     if c != Cin or up.shape != (n, Cout, rank) or not (down.is_contiguous() and up.is_contiguous()):
         raise SigeError(1, "sige_token_lora: down is [adapters, rank, Cin] and up [adapters, Cout, rank], contiguous")
     _like(x, y, down, up, base)
-    mr = x.numel() // x.shape[-1] if max_rows is None else max_rows
-    _table("ids", ids, _I32, -(-(mr if n_rows < 0 else n_rows) // max(rows_per_id, 1)))
+    mr = x.numel() // max(x.shape[-1], 1) if max_rows is None else max_rows
+    rows = mr if n_rows < 0 else n_rows
+    _table("ids", ids, _I32, -(-rows // max(rows_per_id, 1)))
     if alpha is not None:
         _table("alpha", alpha, torch.float32, n)
     if count is not None:
         _table("count", count, _I32, 1)
+    x_ld, y_ld = _lines(x, rows, Cin, x_ld), _lines(y, rows, Cout, y_ld)
+    base_ld = 0 if base is None else _lines(base, rows, Cout, base_ld)
     stream = _stream_of(x, y, down, up, ids, alpha, base, count)
-    rc = lib().sige_token_lora(x.data_ptr(), _DT[x.dtype], Cin, _lines(x) if x_ld is None else x_ld, _at(count), rows_per_id, mr,
-                               n_rows, down.data_ptr(), up.data_ptr(), rank, n, _at(alpha), ids.data_ptr(), _at(base),
-                               0 if base is None else _lines(base) if base_ld is None else base_ld, Cout, y.data_ptr(),
-                               _lines(y) if y_ld is None else y_ld, stream)
+    rc = lib().sige_token_lora(x.data_ptr(), _DT[x.dtype], Cin, x_ld, _at(count), rows_per_id, mr, n_rows, down.data_ptr(), up.data_ptr(),
+                               rank, n, _at(alpha), ids.data_ptr(), _at(base), base_ld, Cout, y.data_ptr(), y_ld, stream)
     if rc:
         _check(rc)
 

@@ -218,3 +218,69 @@ def test_the_binding_refuses_gaps_between_rows():
         c = x.shape[-1]
         with pytest.raises(api.SigeError, match=what):
             api.sige_token_lora(x, y, c, 128, down[:, :, :c].contiguous(), up, ids, 4, n_rows=n)
+
+
+def test_the_binding_refuses_rows_that_are_not_there():
+    """Tensors with fewer rows or channels than the call touches, rows given by a stride of the caller's that pass the storage's end,
+    rows with gaps between them; the whole ones get as far as the refusal of CPU tensors."""
+    h, i = torch.bfloat16, torch.int32
+    R, C = 32, 128
+    x, y = torch.zeros(R, C, dtype=h), torch.zeros(R, C, dtype=h)
+    short, narrow, flat, small = x[:R - 1], x[:, :C - 8], torch.zeros(R * C, dtype=h), torch.zeros(R * C - 1, dtype=h)
+    cache = torch.zeros(api.sige_cache4_bytes(2, 64, 256), dtype=torch.uint8)
+    table, pos = torch.zeros(32, 4, dtype=i), torch.zeros(R, 2)
+    g = good()                                            # 16 x 16 pixels, blocks of 4 x 4
+    idx, cnt = torch.zeros(2, 2, dtype=i), torch.zeros(1, dtype=i)
+    full = torch.zeros(256, C, dtype=h)
+    down, up, ids = torch.zeros(2, 8, C, dtype=h), torch.zeros(2, C, 8, dtype=h), torch.zeros(8, dtype=i)
+
+    def rope(a, b, n=R, **kw):
+        return lambda: api.sige_token_rope(a, b, 2, 64, table, pos, n_rows=n, **{"max_rows": R, **kw})
+
+    def rope_blocks(a, b, n=2):
+        return lambda: api.sige_token_rope_blocks(a, b, 2, 64, table, g, idx, cnt, n_blocks=n)
+
+    def store(k, v, **kw):
+        return lambda: api.sige_cache4_store(k, v, cache, 256, 2, 64, **{"n_rows": R, "max_rows": R, **kw})
+
+    def store_blocks(k, v, n=2):
+        return lambda: api.sige_cache4_store_blocks(k, v, cache, 256, 2, 64, g, idx, cnt, n_blocks=n)
+
+    def load(k, v, **kw):
+        return lambda: api.sige_cache4_load(cache, 256, 2, 64, k, v, **kw)
+
+    def attn(q, o, **kw):
+        return lambda: api.sige_cache4_attn(q, cache, 256, o, 1.0, T=4, heads=2, d=64, **kw)
+
+    def attn_blocks(q, o):
+        return lambda: api.sige_cache4_attn_blocks(q, g, idx, 2, cache, 256, o, 1.0, T=4, heads=2, d=64)
+
+    def lora(a, b, base=None, **kw):
+        return lambda: api.sige_token_lora(a, b, C, C, down, up, ids, 4, base=base, **{"n_rows": R, "max_rows": R, **kw})
+
+    tiles = torch.zeros(4, 1, 10, C, dtype=h)             # rows of a tile of 1 x 8 out of tiles of 1 x 10
+    whole = [rope(x, y), rope(x, x), rope(flat, y, x_ld=C), rope(x.view(2, 4, 4, C), y), rope(short, y, n=R - 1), rope_blocks(x, y), rope_blocks(x, y, -1),
+             rope_blocks(short, short, 1), store(x, y), store(x.view(R, 2, 64), flat, v_ld=C), store(short, y, n_rows=-1, max_rows=R - 1, count=cnt, rows_per_count=4),
+             store_blocks(x, y), load(x, y), load(None, y), load(short, y), load(x, flat, v_ld=C), attn(x, y), attn(short, y), attn(x, flat, o_ld=C),
+             attn(x.view(R, 2, 64), y), attn_blocks(full, y), attn_blocks(full.view(16, 16, C), y), lora(x, y), lora(x, y, x), lora(x, flat, y_ld=C),
+             lora(x.view(8, 2, 2, C), y), lora(x.view(8, 1, 4, C), y), lora(tiles[:2, :, :, :], y, n_rows=20), lora(short, short, n_rows=R - 1),
+             attn(x, y, Nq=0), rope(x, y[:0], n=0)]
+    for call in whole:
+        with pytest.raises(api.SigeError, match="cpu"):
+            call()
+    missing = [rope(short, y), rope(x, short), rope(narrow, y), rope(x, narrow), rope(x, small, y_ld=C), rope(x, y, x_ld=C + 8), rope(x[1:], y, x_ld=C),
+               rope(x, short, n=-1, count=cnt, rows_per_count=4), rope(x.view(2, 16, C)[:, :15], y), rope_blocks(short, y), rope_blocks(x, short), rope_blocks(short, y, -1),
+               store(short, y), store(x, short), store(x, narrow), store(x, short, n_rows=-1, count=cnt, rows_per_count=4), store(x, flat[8:], v_ld=C),
+               store(x, x.view(R, 2, 64)[:R - 1]), store_blocks(x, short), store_blocks(short, y), store_blocks(x, short, -1),
+               load(x, short), load(short, y, n_tokens=R), load(x, narrow), load(x, y, n_tokens=R + 1), load(x, flat, v_ld=C + 8),
+               attn(x, short), attn(short, y, Nq=R), attn(x, narrow), attn(x, small, o_ld=C), attn_blocks(full[:255], y), attn_blocks(full, short),
+               attn_blocks(full[:, :120], y), lora(x, short), lora(short, y), lora(x, y, short), lora(x, narrow), lora(narrow, y), lora(x, y, narrow),
+               lora(x, flat[1:], y_ld=C), lora(x, y, flat[8:], base_ld=C), lora(tiles[:, :, :8], y), lora(x, y[:1].expand(R, C)[:R - 1])]
+    for call in missing:
+        with pytest.raises(api.SigeError, match="rows of"):
+            call()
+    for call, what in ((load(None, None), "k or v"), (lambda: api.sige_cache4_attn(x, cache.expand(2, -1), 256, y, 1.0, T=4, heads=2, d=64), "contiguous"),
+                       (lambda: api.sige_cache4_attn(x, cache, 256, y, 1.0, T=4, heads=2, d=64, workspace=torch.zeros(1).expand(4096)), "contiguous"),
+                       (lambda: api.sige_token_rope_blocks(x, y, 2, 64, table, g, idx, cnt[:0]), "count")):
+        with pytest.raises(api.SigeError, match=what):
+            call()
