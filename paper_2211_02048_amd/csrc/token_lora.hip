@@ -199,14 +199,16 @@ __global__ __launch_bounds__(64 * LORA_WAVES, 2) void token_lora_kernel(LoraArgs
     const int share = ALONE ? full : (full + LORA_WAVES - 1) / LORA_WAVES;       // of a wave, one after the other: whole lines of memory
     const int part = ALONE ? 0 : wave;
     float back = 1.0f;
+    constexpr float LARGEST = __is_same(T, f16) ? 65504.0f : 0x1.fep127f;
     // the middle vector's values q * 4 ... + 3 of token t, scaled by `down`
     auto keep = [&](int t, int q, const float (&v)[4]) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const T h = from_f32<T>(v[i]);
+            // (half types: single precision ends above bf16, where the value is the type's largest number and a remainder; an infinity
+            // is in the remainder: a difference of two would be NaN)
+            const T h = from_f32<T>(F32 ? v[i] : fminf(fmaxf(v[i], -LARGEST), LARGEST));
             hs[t * HROW + 4 * q + i] = h;
-            // (an infinity has no remainder: its difference to itself would be NaN)
-            if constexpr (!F32) hs[(16 + t) * HROW + 4 * q + i] = from_f32<T>(fabsf(to_f32(h)) == INFINITY ? 0.0f : v[i] - to_f32(h));
+            if constexpr (!F32) hs[(16 + t) * HROW + 4 * q + i] = from_f32<T>(v[i] - to_f32(h));
         }
     };
     f32x4 alone[RT];                                              // ALONE: the sums of row l16 with its own adapter

@@ -308,3 +308,29 @@ def test_calls_kept_and_made_again_and_what_the_binding_refuses():
     api.sige_token_lora(tiles, z, C, C, down, up, ids, 8, base=base, n_rows=rows)
     torch.cuda.synchronize()
     assert torch.equal(z, y)
+
+
+@pytest.mark.parametrize("rows,cin,cout,rank", [(37, 256, 72, 8), (5, 40, 1280, 24), (33, 64, 40, 72), (17000, 16, 24, 8)])
+def test_middle_vectors_at_the_end_of_single_precision(rows, cin, cout, rank):
+    """bf16: middle vectors between the type's largest number and that of single precision on small `up`; infinite ones stay infinite."""
+    per, n = 5, 3
+    _, _, up, ids, _, base = make(rank, rows, per, cin, cout, rank, n, "bf16")
+    big = float(torch.finfo(torch.bfloat16).max)
+    x = torch.zeros(rows, cin, dtype=torch.bfloat16, device="cuda")
+    x[:, 0] = torch.tensor([big, -big, big / 2, 3.0], device="cuda").bfloat16().repeat(rows)[:rows]
+    down = torch.zeros(n, rank, cin, dtype=torch.bfloat16, device="cuda")
+    down[:, :, 0] = torch.tensor([1.0, -1.0, 0.5, 2.0 ** -120], device="cuda").bfloat16().repeat(rank)[:rank]
+    alpha = torch.tensor([1.0035, 1.002, 1.0039], device="cuda")                # times the largest bf16 below 2^128
+    up = (up.float() * 2.0 ** -118).bfloat16()
+    want, mag = expected(x, down, up, ids, per, alpha, base, cout)
+    assert (np.abs(f64(x)[:, :1] * 1.0035) > big).any() and np.isfinite(f64(x) * 1.0039).all() and 1.0039 * big < torch.finfo(torch.float32).max
+    y = torch.empty_like(base)
+    api.sige_token_lora(x, y, cin, cout, down, up, ids, per, alpha=alpha, base=base, n_rows=rows)
+    torch.cuda.synchronize()
+    close(y, want, mag, cin, rank, "bf16", "the largest middle vectors")
+    x[3, 1] = float("inf")
+    down[:, :, 1] = 1.0
+    want, _ = expected(x, down, up, ids, per, alpha, base, cout)
+    api.sige_token_lora(x, y, cin, cout, down, up, ids, per, alpha=alpha, base=base, n_rows=rows)
+    torch.cuda.synchronize()
+    assert np.array_equal(np.isfinite(f64(y)), np.isfinite(want))
