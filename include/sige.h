@@ -518,7 +518,7 @@ int sige_cache4_attn_blocks(const void* q, int32_t q_ld, const sige_geom* g, con
  * without adapter.  base [rows][Cout] is the projection's output, or NULL: y is the adapters' share alone, which sige_conv_scatter
  * adds to its fp32 sums as residual_tiles.  y == base is allowed.  Sums in fp32, the middle vector in fp32 (half types multiply it as
  * the sum of two halves), rounded once.  Rows: n_rows >= 0 from the host, or -1 = min(*count * rows_per_id, max_rows).
- * Cin, Cout, rank and strides must be multiples of 16 bytes, rank <= 128.  y may not be x; y == base needs y_ld == base_ld.  */
+ * Cin, Cout, rank and strides must be multiples of 16 bytes, rank <= 128, Cin and Cout <= 2^28.  y may not be x; y == base needs y_ld == base_ld.  */
 int sige_token_lora(const void* x, sige_dtype dt, int32_t Cin, int32_t x_ld, const int32_t* count, int32_t rows_per_id,
                     int32_t max_rows, int32_t n_rows, const void* down, const void* up, int32_t rank,
                     int32_t n_adapters, const float* alpha, const int32_t* ids, const void* base, int32_t base_ld,

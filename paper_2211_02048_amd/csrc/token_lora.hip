@@ -478,6 +478,7 @@ extern "C" int sige_token_lora(const void* x, sige_dtype dt, int32_t Cin, int32_
                  "%s: row strides must be >= the channel counts", who);
     const int vw = (int)(16 / dtype_size(dt));
     SIGE_REQUIRE(rank <= 128, SIGE_ERR_UNSUPPORTED, "%s: the rank must be <= 128", who);
+    SIGE_REQUIRE(Cin <= 1 << 28 && Cout <= 1 << 28, SIGE_ERR_UNSUPPORTED, "%s: too many channels", who);      // (offsets within a row are ints)
     SIGE_REQUIRE(Cin % vw == 0 && Cout % vw == 0 && rank % vw == 0 && x_ld % vw == 0 && y_ld % vw == 0 && (base == nullptr || base_ld % vw == 0),
                  SIGE_ERR_UNSUPPORTED, "%s: channel counts, rank and row strides must be multiples of %d elements", who, vw);
     const int rows = n_rows >= 0 ? n_rows : max_rows;

@@ -284,3 +284,10 @@ def test_the_binding_refuses_rows_that_are_not_there():
                        (lambda: api.sige_token_rope_blocks(x, y, 2, 64, table, g, idx, cnt[:0]), "count")):
         with pytest.raises(api.SigeError, match=what):
             call()
+
+
+def test_adapters_of_more_channels_than_offsets_count(L):
+    for cin, cout in ((320, 2 ** 30 + 8), (320, 2 ** 31 - 8), (2 ** 30, 64), (320, 2 ** 28 + 8)):
+        for dt in (0, 1):
+            assert L.sige_token_lora(FAKE, dt, cin, cin, None, 4, 8, 8, FAKE, FAKE, 8, 2, None, FAKE, None, 0, cout, ctypes.c_void_p(0x20000), cout, None) == 2
+            assert "channels" in err(L)
