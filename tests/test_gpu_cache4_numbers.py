@@ -124,3 +124,39 @@ def test_queries_at_the_end_of_single_precision(d):
     o = attend(qt, torch.from_numpy(cache).cuda(), T, T, heads, d, 0.125).view(nq, heads, d)
     assert torch.isnan(o[5, 0]).all() and torch.isnan(o[6, 1]).all()
     assert torch.isfinite(o[:5]).all() and torch.isfinite(o[7:]).all()
+
+
+def in_parts(x, n):
+    """What n bf16 numbers hold of x, each the rounding of what the ones before left."""
+    left, held = torch.from_numpy(x).clone(), torch.zeros(x.shape, dtype=torch.float64)
+    for _ in range(n):
+        part = left.bfloat16().double()
+        held, left = held + part, left - part
+    return held.numpy()
+
+
+@pytest.mark.parametrize("d", [8, 24, 40, 64, 96, 128, 160, 200, 248, 256])
+def test_single_precision_keeps_24_bits(d):
+    """Queries that differ in their last 8 bits alone, keys of 2^18 in one channel each: exact logits of unlike tokens less than 3
+    apart, which the first 16 bits do not tell; values of both signs, so that what a probability loses is left over.  The bound
+    refuses two parts of a query, and two of a probability."""
+    heads, nq, T = 2, 70, 5
+    rng = np.random.default_rng(d)
+    k = np.zeros((T, heads, d))
+    at = np.arange(T) * d // T
+    k[np.arange(T), :, at] = 2.0 ** 18
+    v = rng.choice([-1.0, 1.0], (T, heads, d))
+    q = rng.standard_normal((nq, heads, d))
+    q[..., at] = 1 + rng.integers(0, 2 ** 15, (nq, heads, 1)) * 2.0 ** -15 + rng.integers(0, 96, (nq, heads, T)) * 2.0 ** -23
+    qt = torch.from_numpy(q.reshape(nq, heads * d)).float().cuda()
+    q = f64(qt).reshape(nq, heads, d)
+    cache, k, v = cache_of(k, v, "f32", T)
+    want, mag = ref.attention(q, k, v, 1.0)
+    near(attend(qt, torch.from_numpy(cache).cuda(), T, T, heads, d, 1.0), want, mag, "f32", T, "24 bits")
+    with pytest.raises(AssertionError, match="of the bound"):
+        near(torch.from_numpy(ref.attention(in_parts(q, 2), k, v, 1.0)[0]), want, mag, "f32", T, "two parts of a query")
+    s = np.einsum("ihc,thc->iht", q, k)
+    p = np.exp(s - s.max(-1, keepdims=True))
+    fewer = np.einsum("iht,thc->ihc", in_parts(p, 2), v) / p.sum(-1)[..., None]
+    with pytest.raises(AssertionError, match="of the bound"):
+        near(torch.from_numpy(fewer), want, mag, "f32", T, "two parts of a probability")
