@@ -5,7 +5,7 @@ import torch
 
 import cache4_oracle as ref
 from paper_2211_02048_amd import api
-from test_gpu_cache4 import DT, attend, f64, forms, some_ranges
+from test_gpu_cache4 import DT, attend, case, close, f64, forms, some_ranges
 
 pytestmark = pytest.mark.gpu
 
@@ -160,3 +160,28 @@ def test_single_precision_keeps_24_bits(d):
     fewer = np.einsum("iht,thc->ihc", in_parts(p, 2), v) / p.sum(-1)[..., None]
     with pytest.raises(AssertionError, match="of the bound"):
         near(torch.from_numpy(fewer), want, mag, "f32", T, "two parts of a probability")
+
+
+@pytest.mark.parametrize("dtype,nq,T,heads,d,many", [("bf16", 2100, 700, 8, 64, 1), ("f16", 1500, 1100, 12, 40, 1), ("bf16", 4200, 16400, 2, 96, 1), ("f16", 4100, 20000, 1, 128, 1),
+                                                     ("bf16", 2050, 12000, 2, 160, 1), ("f16", 1300, 700, 5, 64, 0), ("bf16", 4200, 8200, 2, 96, 0), ("f16", 1000, 16400, 1, 128, 0),
+                                                     ("bf16", 600, 9000, 1, 160, 0)])
+def test_which_form_a_call_takes(dtype, nq, T, heads, d, many):
+    """Half types take the form for many queries where heads of up to 64 have more tiles of 32 queries than compute units (256), and where
+    tiles x tokens x d^2 of larger ones passes 2^35: bit for bit what the knob makes of the call, and not what it makes the other way
+    (up to 64: the forms differ in a workgroup's waves, up to 256 and from 513 tiles on); every row against float64 on the GPU."""
+    tiles = -(-nq // 32) * heads
+    assert (tiles > 256 if d <= 64 else tiles * T * d * d >= 2 ** 35) == bool(many)
+    q, cache, cap, k, v = case(7, nq, T, heads, d, dtype)
+    k, v = torch.from_numpy(k).cuda(), torch.from_numpy(v).cuda()
+    scale = d ** -0.5
+    o = attend(q, cache, cap, T, heads, d, scale)
+    forced = {}
+    for m in (0, 1):
+        with api.knobs(CACHE4_MANY=m):
+            forced[m] = attend(q, cache, cap, T, heads, d, scale)
+    assert torch.equal(o, forced[many]) and not torch.equal(o, forced[1 - many])
+    q64 = q.double().view(nq, heads, d)
+    for h in range(heads):
+        p = torch.softmax(q64[:, h] @ k[:, h].t() * scale, -1)
+        want, mag = (p @ v[:, h]).cpu().numpy()[:, None], ((p + 2.0 ** -30) @ v[:, h].abs()).cpu().numpy()[:, None]
+        close(o[:, h * d:(h + 1) * d], want, mag, q64[:, h:h + 1].cpu().numpy(), k[:, h:h + 1].cpu().numpy(), scale, dtype, T, f"{nq} of {T} x {d}")
