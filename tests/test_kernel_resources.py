@@ -1,6 +1,7 @@
 """What the kernels of the built library take of a compute unit, from the metadata that the compiler writes beside the code (the
 notes of the code objects inside the library)."""
 import os
+import re
 import struct
 
 import msgpack
@@ -70,3 +71,24 @@ def test_no_scratch_memory(kernels, name):
     mine = {n: k[".private_segment_fixed_size"] for n, k in kernels.items() if name in n}
     assert mine
     assert not any(mine.values()), [n for n, size in mine.items() if size]
+
+
+@pytest.mark.parametrize("name", ["token_norm", "token_rope_kernel", "token_lora_kernel", "cache4_store_kernel", "cache4_load_kernel", "cache4_common_kernel", "cache4_merge_kernel"])
+def test_no_scratch_memory_of_stacked_tokens(kernels, name):
+    mine = {n: k[".private_segment_fixed_size"] for n, k in kernels.items() if name in n}
+    assert mine
+    assert not any(mine.values()), [n for n, size in mine.items() if size]
+
+
+def test_scratch_memory_of_waves_by_themselves(kernels):
+    """The attention on four bits, every wave by itself: half types, heads of 33 to 64 with four waves per SIMD, and of 193 to 224, and
+    heads of 225 to 256 in single precision are bounded below what they would take and keep some registers in memory (bytes per
+    lane, at most); all others hold everything."""
+    few = {("DF16", 2, 4): 64, ("DF16", 7, 2): 48, ("f", 8, 1): 224}
+    seen = 0
+    for n, k in kernels.items():
+        m = re.search(r"cache4_apart_kernelI(f|DF16)[_b]?Li(\d+)ELb[01]ELi\d+ELi(\d+)E", n)
+        if m:
+            seen += 1
+            assert k[".private_segment_fixed_size"] <= few.get((m.group(1), int(m.group(2)), int(m.group(3))), 0), n
+    assert seen == 16 * 3 + 2 * 4
