@@ -743,11 +743,11 @@ __global__ __launch_bounds__(64 * cache4_common_waves(DT), 2) void cache4_common
             stage(c + 1, buf ^ 1);
             if (c + 2 < c_end) fetch(c + 2);
         }
-        __builtin_amdgcn_s_setprio(0);
         const int t0 = c * KCH;
         char* const rows = lds + buf * CHUNK;
-        // Of the two waves on a SIMD the one in a product goes first: its matrix instructions fill while the other expands or
-        // does its softmax (4096 queries of 16384 x 8 of 128 299.5 -> 293 us, 2048 of 4096 x 160 78.8 -> 75.7; the reverse 299)
+        // Of the two waves on a SIMD the one in its softmax yields to the other, from here to the logits and again from the second
+        // product to the next chunk's rows (4096 queries of 16384 x 8 of 128 299.5 -> 293 us, 2048 of 4096 x 160 78.8 -> 75.7; the softmax
+        // first 299)
         __builtin_amdgcn_s_setprio(1);
         f32x16 sacc[KT];
 #pragma unroll
