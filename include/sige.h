@@ -497,7 +497,8 @@ int sige_cache4_load(const void* cache, int32_t capacity, sige_dtype dt, int32_t
  * part of the cache, or tokens that see only those before them); NULL: all T.  A row that sees no token is written as zeros, and
  * what a row does not see - NaN, infinities - does not reach it.  0 <= T <= capacity.
  * The cached values enter the products exactly (they are bf16 numbers; for fp16 queries, fp16 numbers wherever an fp16 row was stored).
- * fp16 and bf16 round a probability to their type once; single precision loses nothing (operands in three parts).
+ * fp16 and bf16 round a probability to their type once (sige_sparse_attn holds bf16 ones in two terms: the 4 bits of the cached values
+ * are off by far more); single precision loses nothing (operands in three parts).
  * Finite queries and values give finite rows as long as the logits and a row's sum of values stay in the range of fp32.
  * scale >= 0.  workspace: as for sige_sparse_attn, sige_cache4_attn_workspace_bytes of it; two calls that may run at the same time (on
  * two streams, in two graphs) need one each.  T < 2^31 - 128.                              */
@@ -518,7 +519,9 @@ int sige_cache4_attn_blocks(const void* q, int32_t q_ld, const sige_geom* g, con
  * without adapter.  base [rows][Cout] is the projection's output, or NULL: y is the adapters' share alone, which sige_conv_scatter
  * adds to its fp32 sums as residual_tiles.  y == base is allowed.  Sums in fp32, the middle vector in fp32 (half types multiply it as
  * the sum of two halves), rounded once.  Rows: n_rows >= 0 from the host, or -1 = min(*count * rows_per_id, max_rows).
- * Cin, Cout, rank and strides must be multiples of 16 bytes, rank <= 128, Cin and Cout <= 2^28.  y may not be x; y == base needs y_ld == base_ld.  */
+ * Cin, Cout, rank and strides must be multiples of 16 bytes, rank <= 128, Cin and Cout <= 2^28.  y may not be x; y == base needs
+ * y_ld == base_ld.  Adapters of a smaller rank than the call's are padded with zeros (rows of down, columns of up).  An infinity in up
+ * can come out as NaN.                                                                  */
 int sige_token_lora(const void* x, sige_dtype dt, int32_t Cin, int32_t x_ld, const int32_t* count, int32_t rows_per_id,
                     int32_t max_rows, int32_t n_rows, const void* down, const void* up, int32_t rank,
                     int32_t n_adapters, const float* alpha, const int32_t* ids, const void* base, int32_t base_ld,

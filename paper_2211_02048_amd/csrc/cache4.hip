@@ -4,9 +4,9 @@
 //
 // Both are bound by memory: a value is 2 or 4 bytes on one side and 0.53 on the other, and four instructions.  Four lanes share a
 // group of 32 channels (16 bytes of a half-type row each) and 16 tokens lie side by side in a wave, so that it reads 64 whole
-// bytes of 16 rows and writes 256 bytes of one plane in a run.  Measured: 16384 tokens of 8 heads of 128 in fp16, stored 21 us, read back
-// 18 us, 85 MB each, 4.0 and 4.7 TB/s (a large copy reaches 5.2); 640 tokens of 8 heads of 40 2.4 us each, which is a launch.  (The single
-// scale bytes make 52 MB of the 18 that a store writes; a wave with all groups of a head, which writes them in one piece, takes as long, and
+// bytes of 16 rows and writes 256 bytes of one plane in a run.  Measured: 16384 tokens of 8 heads of 128 in fp16, stored 23.6 us, read back
+// 15.9 us, 85 MB each, 3.6 and 5.3 TB/s (a large copy reaches 5.2); 640 tokens of 8 heads of 40 2.4 us each, which is a launch.  (The single
+// scale bytes make 51 MB of the 18 that a store writes; a wave with all groups of a head, which writes them in one piece, takes as long, and
 // 15 - 30 % longer on few rows.)
 #include "cache4.h"
 

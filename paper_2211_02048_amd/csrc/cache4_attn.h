@@ -10,16 +10,22 @@
 // instruction.  What differs by type is the other operand: bf16 and fp16 queries enter as they are; a single-precision
 // query, and the probabilities beside it, as the sum of three bf16 numbers (24 bits), so that single precision runs on the bf16 matrix
 // instructions at a third of their rate (the fp32 ones have a sixteenth) with exact products.
-// A probability is rounded to the compute type once (bf16: 2^-9 of each at most, without bias; the values behind it were
-// rounded to 2 bits of significand), and the denominator adds what was multiplied: through a column of ones beside V where the
-// head size leaves one free, else as dot products of the rounded pairs with ones (single precision: the values themselves).
+// A probability is rounded to the compute type once, by half a step at most (bf16 2^-8 of each, fp16 2^-11), without bias, and the
+// denominator adds what was multiplied: through a column of ones beside V where the head size leaves one free, else as dot
+// products of the rounded pairs with ones (single precision: the values themselves).  In bf16 this is a choice against two terms,
+// hi + lo, which sige_sparse_attn feeds.  One term: the result is off by 2.2e-3 of itself (rms; its own rounding is 1.65e-3 of that, and
+// what two terms come to).  Two terms: 34 % more time for 4096 queries of 16384 x 8 of 128 (274 -> 367 us), 27 - 37 % for 4096 of 4096 x
+// 40 - 80, 7 % for one query of 65536.  The cached values themselves, with 2 bits of significand, put the result 0.17 of itself away
+// from that on the rows that were stored.
 //
 // Two forms.  cache4_apart_kernel: every wave by itself, the waves of a workgroup share the keys out among them; no barrier until
 // they meet.  cache4_common_kernel: four or eight waves of 32 queries each that expand every chunk once for all.  The vector instructions
 // bound the first where there is work (per 64 keys x 32 queries x 64: about 90 for the expansion, 110 for the softmax), LDS and the order
 // of the two kinds of instructions the second.  Measured: one query of 65536 x 8 of 64 in bf16 14.7 us (with the merge; 35.7 MB, 2.4 TB/s),
 // 614 of 4096 x 8 of 80 in fp16 21 us (300 TFLOP/s: 160 workgroups of eight chunks per wave), 4096 of 16384 x 8 of 128 in bf16 265 - 302 us by
-// card (1040 - 910 TFLOP/s; a library product reaches 1167).
+// card (1040 - 910 TFLOP/s; a library product reaches 1167).  Where the registers are bounded for more waves side by side some kernels keep a
+// few values in scratch memory: heads of 33 to 64 with four waves per SIMD 1 and 17 registers, half-type heads of 193 to 224 2 and 9;
+// single-precision heads of 225 to 256 66 and 96, all of a SIMD's.
 #pragma once
 
 #include "cache4.h"
@@ -297,7 +303,7 @@ template <typename T, int DT, bool ODD, int KT> struct Cache4Sums {
         return m_sub;
     }
     // The probabilities, and O^T += V^T P^T in steps of 16 keys; v(kt, s, nt): the V^T fragment.  URGENT: from the product on the wave
-    // goes before the others of its SIMD
+    // goes before the others of its SIMD (until its next softmax)
     template <bool URGENT, typename V> __device__ __forceinline__ void add(float scale_log2e, float m_sub, f32x16 (&sacc)[KT], V v)
     {
 #pragma unroll
@@ -372,7 +378,9 @@ constexpr int cache4_apart_waves(int DT, int parts) { return DT <= (parts > 1 ? 
 // waves per SIMD: their registers hold the next chunk beside everything, and the waves of one workgroup are two per SIMD anyway
 constexpr int cache4_apart_side(int DT, int parts) { return parts > 1 ? (DT <= 3 ? 2 : 1) : DT <= 7 ? 2 : 1; }
 // Many queries, half types.  Heads up to 64: four waves per SIMD, two workgroups side by side (4096 queries of 4096 x 8 of 64 74 -> 64 us,
-// of 40 62 -> 50; one query of 65536 keys 15.1 -> 16.1).  Larger heads have no registers for that: the common form.
+// of 40 62 -> 50; one query of 65536 keys 15.1 -> 16.1).  Larger heads have no registers for that: the common form.  For heads up to 64
+// the common form wins on long caches alone (bf16, us, this one | common chunks: 4096 of 16384 x 8 of 64 202 | 180, of 40 162 | 153; 4096 of 4096
+// x 64 61 | 61, x 40 46 | 51, x 32 36 | 44; 2048 of 4096 x 64 32 | 42; 1500 of 1500 x 64 16 | 29; 4096 of 1024 x 32 12 | 23) and is not built.
 constexpr bool cache4_crowds(int DT, int parts) { return parts == 1 && DT <= 2; }
 constexpr int CACHE4_CROWD_WAVES = 4;              // of a workgroup (eight: 1500 queries of 1500 x 8 of 64 18.4 -> 19.2 us)
 constexpr bool cache4_has_common(int DT, int parts) { return parts == 1 && DT > 2; }

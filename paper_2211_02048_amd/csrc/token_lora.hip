@@ -393,6 +393,8 @@ __global__ __launch_bounds__(64 * LORA_WAVES, 2) void token_lora_kernel(LoraArgs
             if (live && u0 + i < u_end && c < a.Cout) *(uint4*)((T*)a.y + row * a.y_ld + c) = lora_sum<T>(sum[i], back, bv[i]);
         }
     };
+    // (single precision keeps to the general form, one of which it needs anyway: 8192 rows of 640 -> 640 16.6 us against 16.5 as one
+    // adapter, 4096 of 1280 -> 1280 25.3 against 24.3, the smaller calls within 0.1)
     const int first = __builtin_amdgcn_readlane(id, 0);
     const bool same = !F32 && first >= 0 && __builtin_amdgcn_ballot_w64(live && id != first) == 0ul;
     if (same)
