@@ -206,6 +206,7 @@ __device__ __forceinline__ void cache4_queries(const Cache4AttnArgs& a, int qi, 
 
 // Maxima from here on (of logits times log2 e): their rounding, which the fused operation of the exponents keeps, is no longer small
 // beside the offset of fp16's probabilities (2^15, the type ends at 2^16), and from 2^31 on beside the range of single precision.
+// (The test for it and a register take 0.8 % of 4096 queries of 16384 x 8 of 128, 270 -> 272 us, and nothing that shows elsewhere.)
 constexpr float CACHE4_FAR = 1048576.0f;
 
 // The sums of a wave's 32 rows.  Of a 32-key tile of logits a lane holds keys 8 * (r / 4) + 4 * half + r % 4 of its row.
