@@ -527,6 +527,62 @@ int sige_token_lora(const void* x, sige_dtype dt, int32_t Cin, int32_t x_ld, con
                     int32_t n_adapters, const float* alpha, const int32_t* ids, const void* base, int32_t base_ld,
                     int32_t Cout, void* y, int32_t y_ld, void* stream);
 
+/* ---- token-wise layers on rows held in 8 bits ------------------------------------------------- */
+
+/* A matrix of rows x C in 8 bits, one row per token (or, for weights, per output channel):
+ *   codes   [rows][q_ld]  floats of eight bits (sign, 4 bits of exponent, 3 of significand, no infinities, largest 448; the code 0x7f is
+ *                         NaN), 128 * ceil(C / 128) of them per row, those behind C are 0
+ *   scales  [rows][s_ld]  a byte s = 2^(s - 127) per 128 channels, 4 * ceil(C / 512) bytes per row, those of blocks behind C are 0
+ * a value is its code times its block's scale.  q_ld >= 128 * ceil(C / 128), a multiple of 16; s_ld >= 4 * ceil(C / 512), a multiple of 4;
+ * codes 16-byte, scales 4-byte aligned.  A scale byte of 255 is NaN.  Half of a half type's size; the powers of two lose nothing
+ * against other factors (the codes have exponents of their own), and the matrix instruction applies them by itself.
+ * Rows as in sige_token_norm: n_rows >= 0 from the host, or -1 = min(*count * rows_per_count, max_rows); rows behind them are
+ * neither read nor written.
+ *
+ * sige_rows8_store: x [rows][C] of dt to 8 bits.  A block's scale is the smallest power of two, at least 2^-126, with max|x| <= 448 * scale over its
+ * finite values; codes are the nearest, ties to the even one; an infinity or NaN becomes a NaN and leaves the others alone.
+ * Weights are stored once by the same call.
+ * sige_rows8_load: the values as rows of dt (rounded once; fp16 and bf16 lose nothing but what lies outside of their range).  */
+int sige_rows8_store(const void* x, sige_dtype dt, int32_t C, int32_t x_ld, const int32_t* count, int32_t rows_per_count,
+                     int32_t max_rows, int32_t n_rows, void* q, int32_t q_ld, void* scales, int32_t s_ld, void* stream);
+int sige_rows8_load(const void* q, int32_t q_ld, const void* scales, int32_t s_ld, int32_t C, const int32_t* count,
+                    int32_t rows_per_count, int32_t max_rows, int32_t n_rows, void* y, sige_dtype dt, int32_t y_ld, void* stream);
+
+/* The root-mean-square norm, beside sige_token_norm for models that have it, with the residual's addition before it:
+ *   h[r][c] = x[r][c] + residual[r][c], rounded to dt (residual NULL: h = x),
+ *   y[r][c] = h[r][c] / sqrt(mean_c(h[r][c]^2) + eps) * gamma[c],
+ * the mean in fp32 (a sum of squares beyond its range gives a row of zeros), gamma fp32 [C] or NULL (1).  Outputs, each of its own: total = h [rows][C] (beside a
+ * residual; may be NULL), y [rows][C] of dt, and q / scales: y in 8 bits, from the values before they are rounded to dt; y or
+ * q may be NULL, not both.  total or y may be x or residual (same row stride).  C * size and the strides must be multiples of 16 bytes; at
+ * most 32 KiB per token.                                                                */
+int sige_token_rms(const void* x, sige_dtype dt, int32_t C, int32_t x_ld, const void* residual, int32_t res_ld, const int32_t* count,
+                   int32_t rows_per_count, int32_t max_rows, int32_t n_rows, const float* gamma, float eps, void* total,
+                   int32_t total_ld, void* y, int32_t y_ld, void* q, int32_t q_ld, void* scales, int32_t s_ld, void* stream);
+
+/* A 1x1 layer on stacked tokens with both operands in 8 bits:
+ *   y[r][o] = sum_c x[r][c] * w[o][c] + bias[o] + base[r][o],
+ * x (codes and scales) [rows][Cin], w [Cout][Cin], bias fp32 [Cout] or NULL, base [rows][Cout] of dt or NULL (a residual, or what another layer
+ * left), y [rows][Cout] of dt, rounded once; y == base is allowed (same row stride).  Sums in fp32.  Half types: the matrix instruction for 8 bits, which cuts off
+ * of a product what lies 13 places and more below the largest one that it adds in the same step (within a block of 128 channels; 1.5e-5 of
+ * the result in the mean over normal numbers, the codes' own rounding is 1000 times as much).  Single precision cuts off nothing:
+ * the codes are multiplied as bf16 numbers, which they are (scales of 2^-110 to 2^110; below 2^-126 values become 0).
+ * Cout must be a multiple of 16 bytes' worth of dt, Cin may be anything.                       */
+int sige_rows8_linear(const void* x, int32_t x_ld, const void* x_scales, int32_t xs_ld, int32_t Cin, const int32_t* count,
+                      int32_t rows_per_count, int32_t max_rows, int32_t n_rows, const void* w, int32_t w_ld, const void* w_scales,
+                      int32_t ws_ld, int32_t Cout, const float* bias, const void* base, int32_t base_ld, void* y, sige_dtype dt,
+                      int32_t y_ld, void* stream);
+
+/* The first feed-forward layer: the same product with 2 * Cout output channels, the values in rows 0..Cout-1 of w, their gates in the
+ * rows Cout..2*Cout-1 (bias likewise, fp32 [2 * Cout]), and the gated activation behind it, to 8 bits:
+ *   v[r][o] = u[r][o] * act(g[r][o]),  act = gelu(g) = g/2 * (1 + erf(g / sqrt 2)) or silu(g) = g / (1 + exp(-g)),
+ * from the fp32 sums (with the matrix instruction for 8 bits) to codes and scales [rows][Cout] as sige_rows8_store makes them, so that the
+ * next layer takes them as they are.  Cout must be a multiple of 8.                           */
+typedef enum { SIGE_GATE_GELU = 0, SIGE_GATE_SILU = 1 } sige_gate;
+int sige_rows8_linear_gated(const void* x, int32_t x_ld, const void* x_scales, int32_t xs_ld, int32_t Cin, const int32_t* count,
+                            int32_t rows_per_count, int32_t max_rows, int32_t n_rows, const void* w, int32_t w_ld,
+                            const void* w_scales, int32_t ws_ld, int32_t Cout, const float* bias, sige_gate gate, void* q,
+                            int32_t q_ld, void* scales, int32_t s_ld, void* stream);
+
 /* ---- helpers beside the path --------------------------------------------------- */
 
 /* Re-lays an OIHW weight tensor (device, dtype dt, [Cout][Cin][k][k]) into the

@@ -20,6 +20,7 @@ LIB_PATH = os.path.join(_HERE, "libsige_hip.so")
 SIGE_F32, SIGE_F16, SIGE_BF16 = 0, 1, 2
 ACT_NONE, ACT_SILU, ACT_RELU, ACT_LEAKY_RELU = 0, 1, 2, 3
 ROPE_ADJACENT, ROPE_HALVES = 0, 1
+GATE_GELU, GATE_SILU = 0, 1
 _DT = {torch.float32: SIGE_F32, torch.float16: SIGE_F16, torch.bfloat16: SIGE_BF16}
 STATUS = {0: "SIGE_OK", 1: "SIGE_ERR_INVALID_ARG", 2: "SIGE_ERR_UNSUPPORTED", 3: "SIGE_ERR_CAPACITY",
           4: "SIGE_ERR_HIP"}
@@ -29,7 +30,8 @@ EXPORTS = ["sige_reduce_mask", "sige_reduce_mask_workspace_bytes", "sige_reduce_
            "sige_gn_stats", "sige_gn_stats_act", "sige_last_error", "sige_version", "sige_set_knob", "sige_get_knob", "sige_conv_plan", "sige_reduce_mask_noalloc", "sige_mark_blocks",
            "sige_fused_conv_pair_marked", "sige_rope_pairs", "sige_token_rope", "sige_token_rope_blocks", "sige_cache4_bytes",
            "sige_cache4_store", "sige_cache4_store_blocks", "sige_cache4_load", "sige_cache4_attn", "sige_cache4_attn_blocks",
-           "sige_cache4_attn_workspace_bytes", "sige_token_lora"]
+           "sige_cache4_attn_workspace_bytes", "sige_token_lora", "sige_rows8_store", "sige_rows8_load", "sige_token_rms",
+           "sige_rows8_linear", "sige_rows8_linear_gated"]
 
 # sige_knob of the header
 KNOBS = {"CONV_CFG": 0, "CONV_KC": 1, "CONV_SPLIT": 2, "CONV_HALF": 3, "CONV_SPLIT_WGS": 4, "CONV_POINTWISE": 5,
@@ -149,6 +151,11 @@ def lib() -> ctypes.CDLL:
         L.sige_cache4_attn_blocks.argtypes = [vp, i32, gp, vp, i32, vp, i32, i32, i32, i32, i32, f32, vp, vp, i32, vp, sz, vp]
         L.sige_cache4_attn_workspace_bytes.argtypes = [i32, i32, i32, i32]
         L.sige_token_lora.argtypes = [vp, i32, i32, i32, vp, i32, i32, i32, vp, vp, i32, i32, vp, vp, vp, i32, i32, vp, i32, vp]
+        L.sige_rows8_store.argtypes = [vp, i32, i32, i32, vp, i32, i32, i32, vp, i32, vp, i32, vp]
+        L.sige_rows8_load.argtypes = [vp, i32, vp, i32, i32, vp, i32, i32, i32, vp, i32, i32, vp]
+        L.sige_token_rms.argtypes = [vp, i32, i32, i32, vp, i32, vp, i32, i32, i32, vp, f32, vp, i32, vp, i32, vp, i32, vp, i32, vp]
+        L.sige_rows8_linear.argtypes = [vp, i32, vp, i32, i32, vp, i32, i32, i32, vp, i32, vp, i32, i32, vp, vp, i32, vp, i32, i32, vp]
+        L.sige_rows8_linear_gated.argtypes = [vp, i32, vp, i32, i32, vp, i32, i32, i32, vp, i32, vp, i32, i32, vp, i32, vp, i32, vp, i32, vp]
         L.sige_set_knob.argtypes = [i32, i32]
         L.sige_get_knob.argtypes = [i32]
         L.sige_get_knob.restype = i32
@@ -799,6 +806,125 @@ def sige_token_lora(x, y, Cin, Cout, down, up, ids, rows_per_id, *, alpha=None, 
     stream = _stream_of(x, y, down, up, ids, alpha, base, count)
     rc = lib().sige_token_lora(x.data_ptr(), _DT[x.dtype], Cin, x_ld, _at(count), rows_per_id, mr, n_rows, down.data_ptr(), up.data_ptr(),
                                rank, n, _at(alpha), ids.data_ptr(), _at(base), base_ld, Cout, y.data_ptr(), y_ld, stream)
+    if rc:
+        _check(rc)
+
+
+# ---- rows in 8 bits ------------------------------------------------------------------------------------
+
+def rows8_lds(C):
+    """Codes and scale bytes that a row of C channels takes."""
+    return -(-C // 128) * 128, -(-C // 512) * 4
+
+
+def rows8(rows, C, device="cuda"):
+    """Room for `rows` rows of C channels in 8 bits: codes and scales."""
+    ld, sld = rows8_lds(C)
+    return torch.empty((rows, ld), dtype=torch.uint8, device=device), torch.empty((rows, sld), dtype=torch.uint8, device=device)
+
+
+_U8 = torch.uint8
+
+
+def _rows8(what, q, scales, rows, C):
+    """Row strides of a matrix in 8 bits, [rows or more, codes] and [rows or more, scale bytes]."""
+    ld, sld = rows8_lds(C)
+    if q.dtype is not _U8 or scales.dtype is not _U8:
+        raise SigeError(1, f"{what}: codes and scales are {_U8}, not {q.dtype} and {scales.dtype}")
+    (a, b), (c, d) = q.stride(), scales.stride()
+    if b != 1 or d != 1:
+        raise SigeError(1, f"{what}: codes and scale bytes of a row side by side, not with strides {q.stride()} and {scales.stride()}")
+    (n, wide), (m, swide) = q.shape, scales.shape
+    if n < rows or m < rows or wide < ld or swide < sld:
+        raise SigeError(3, f"{what}: {rows} rows of {C} channels take codes [{rows}, {ld}] and scales [{rows}, {sld}], not "
+                           f"{tuple(q.shape)} and {tuple(scales.shape)}")
+    # (the stride of an axis of one is nobody's)
+    return a if n > 1 else max(ld, a), c if m > 1 else max(sld, c)
+
+
+def _row_count(x, n_rows, max_rows, count):
+    """The most rows that a call may have, and those that it may touch."""
+    mr = x.numel() // max(x.shape[-1], 1) if max_rows is None else max_rows
+    if count is not None:
+        _table("count", count, _I32, 1)
+    return mr, mr if n_rows < 0 else n_rows
+
+
+def sige_rows8_store(x, q, scales, C, *, n_rows=-1, count=None, rows_per_count=0, max_rows=None, x_ld=None):
+    """Rows of x to 8 bits: codes q and scales."""
+    mr, rows = _row_count(x, n_rows, max_rows, count)
+    x_ld = _lines(x, rows, C, x_ld)
+    q_ld, s_ld = _rows8("q", q, scales, rows, C)
+    stream = _stream_of(x, q, scales, count)
+    rc = lib().sige_rows8_store(x.data_ptr(), _DT[x.dtype], C, x_ld, _at(count), rows_per_count, mr, n_rows, q.data_ptr(), q_ld,
+                                scales.data_ptr(), s_ld, stream)
+    if rc:
+        _check(rc)
+
+
+def sige_rows8_load(q, scales, y, C, *, n_rows=-1, count=None, rows_per_count=0, max_rows=None, y_ld=None):
+    """Rows in 8 bits back to rows of y's type."""
+    mr, rows = _row_count(y, n_rows, max_rows, count)
+    y_ld = _lines(y, rows, C, y_ld)
+    q_ld, s_ld = _rows8("q", q, scales, rows, C)
+    stream = _stream_of(y, q, scales, count)
+    rc = lib().sige_rows8_load(q.data_ptr(), q_ld, scales.data_ptr(), s_ld, C, _at(count), rows_per_count, mr, n_rows, y.data_ptr(),
+                               _DT[y.dtype], y_ld, stream)
+    if rc:
+        _check(rc)
+
+
+def sige_token_rms(x, C, gamma=None, eps=1e-6, *, residual=None, total=None, y=None, q=None, scales=None, n_rows=-1, count=None,
+                   rows_per_count=0, max_rows=None, x_ld=None, res_ld=None, total_ld=None, y_ld=None):
+    """h = x + residual (to total), its root-mean-square norm times gamma to y and, in 8 bits, to q and scales."""
+    _like(x, residual, total, y)
+    mr, rows = _row_count(x, n_rows, max_rows, count)
+    if gamma is not None:
+        _table("gamma", gamma, torch.float32, C)
+    if (q is None) != (scales is None):
+        raise SigeError(1, "sige_token_rms: codes and scales go together")
+    x_ld = _lines(x, rows, C, x_ld)
+    res_ld = 0 if residual is None else _lines(residual, rows, C, res_ld)
+    total_ld = 0 if total is None else _lines(total, rows, C, total_ld)
+    y_ld = 0 if y is None else _lines(y, rows, C, y_ld)
+    q_ld, s_ld = (0, 0) if q is None else _rows8("q", q, scales, rows, C)
+    stream = _stream_of(x, residual, total, y, q, scales, gamma, count)
+    rc = lib().sige_token_rms(x.data_ptr(), _DT[x.dtype], C, x_ld, _at(residual), res_ld, _at(count), rows_per_count, mr, n_rows, _at(gamma),
+                              eps, _at(total), total_ld, _at(y), y_ld, _at(q), q_ld, _at(scales), s_ld, stream)
+    if rc:
+        _check(rc)
+
+
+def sige_rows8_linear(x, x_scales, w, w_scales, y, Cin, Cout, *, bias=None, base=None, n_rows=-1, count=None, rows_per_count=0,
+                      max_rows=None, base_ld=None, y_ld=None):
+    """y = x w^T + bias + base with x [rows, Cin] and w [Cout, Cin] in 8 bits."""
+    _like(y, base)
+    mr, rows = _row_count(y, n_rows, max_rows, count)
+    if bias is not None:
+        _table("bias", bias, torch.float32, Cout)
+    y_ld = _lines(y, rows, Cout, y_ld)
+    base_ld = 0 if base is None else _lines(base, rows, Cout, base_ld)
+    (q_ld, s_ld), (w_ld, ws_ld) = _rows8("x", x, x_scales, rows, Cin), _rows8("w", w, w_scales, Cout, Cin)
+    stream = _stream_of(y, x, x_scales, w, w_scales, bias, base, count)
+    rc = lib().sige_rows8_linear(x.data_ptr(), q_ld, x_scales.data_ptr(), s_ld, Cin, _at(count), rows_per_count, mr, n_rows, w.data_ptr(),
+                                 w_ld, w_scales.data_ptr(), ws_ld, Cout, _at(bias), _at(base), base_ld, y.data_ptr(), _DT[y.dtype], y_ld,
+                                 stream)
+    if rc:
+        _check(rc)
+
+
+def sige_rows8_linear_gated(x, x_scales, w, w_scales, q, scales, Cin, Cout, *, gate=GATE_GELU, bias=None, n_rows=-1, count=None,
+                            rows_per_count=0, max_rows=None):
+    """The product with the values (rows 0 .. Cout - 1 of w) times the activated gates (rows Cout .. 2 Cout - 1), in 8 bits to q and scales."""
+    mr, rows = _row_count(q, n_rows, max_rows, count)
+    if bias is not None:
+        _table("bias", bias, torch.float32, 2 * Cout)
+    (x_ld, xs_ld), (w_ld, ws_ld) = _rows8("x", x, x_scales, rows, Cin), _rows8("w", w, w_scales, 2 * Cout, Cin)
+    q_ld, s_ld = _rows8("q", q, scales, rows, Cout)
+    stream = _stream_of(q, scales, x, x_scales, w, w_scales, bias, count)
+    rc = lib().sige_rows8_linear_gated(x.data_ptr(), x_ld, x_scales.data_ptr(), xs_ld, Cin, _at(count), rows_per_count, mr, n_rows,
+                                       w.data_ptr(), w_ld, w_scales.data_ptr(), ws_ld, Cout, _at(bias), gate, q.data_ptr(), q_ld,
+                                       scales.data_ptr(), s_ld, stream)
     if rc:
         _check(rc)
 

@@ -1,0 +1,147 @@
+"""What the calls for rows in 8 bits refuse, and the oracle's own conversions (no GPU: nothing below is enqueued)."""
+import ctypes
+import os
+
+import numpy as np
+import pytest
+import torch
+
+import rows8_oracle as ref
+from paper_2211_02048_amd import api
+
+FAKE = ctypes.c_void_p(0x10000)  # never dereferenced: every call below fails validation first
+OTHER = ctypes.c_void_p(0x20000)
+ODD = ctypes.c_void_p(0x10008)
+ODDER = ctypes.c_void_p(0x10002)
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(api.LIB_PATH):
+        from paper_2211_02048_amd import build
+        build.build()
+    return api.lib()
+
+
+def err(L):
+    return L.sige_last_error().decode()
+
+
+def test_oracle_conversion_against_torch():
+    """The oracle's codes are those of torch's cast to the type."""
+    rng = np.random.default_rng(0)
+    x = np.concatenate([rng.normal(size=4096) * 2.0 ** rng.integers(-12, 8, 4096), ref.MAG, -ref.MAG, ref.EDGES, -ref.EDGES, [0.0, -0.0]])
+    x = x[np.abs(x) <= 448].astype(np.float32)
+    want = torch.from_numpy(x).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+    got = ref.nearest_code(np.abs(x).astype(float)) | np.where(np.signbit(x), 0x80, 0).astype(np.uint8)
+    np.testing.assert_array_equal(got, want)
+    x = rng.normal(size=(5, 300)) * np.exp(3 * rng.normal(size=(5, 1)))
+    q, s = ref.store(x)
+    v = ref.values(q, s, 300)
+    top = np.abs(np.pad(x, ((0, 0), (0, 84)))).reshape(5, 3, 128).max(-1)
+    scale = 2.0 ** (s[:, :3].astype(float) - 127)
+    assert (top <= 448 * scale).all() and (top > 224 * scale).all() and (s[:, 3:] == 0).all() and (q[:, 300:] == 0).all()
+    assert (np.abs(v - x) <= 2.0 ** -4 * np.abs(x) + 2.0 ** -10 * np.repeat(scale, 128, 1)[:, :300]).all()
+
+
+def test_sizes():
+    for C, want in ((1, (128, 4)), (128, (128, 4)), (129, (256, 4)), (512, (512, 4)), (513, (640, 8)), (1288, (1408, 12))):
+        assert api.rows8_lds(C) == want == ref.lds(C)
+
+
+def test_store_and_load_refusals(L):
+    def store(x=FAKE, dt=1, C=320, x_ld=320, count=None, per=0, mr=8, n=8, q=FAKE, q_ld=384, s=FAKE, s_ld=4):
+        return L.sige_rows8_store(x, dt, C, x_ld, count, per, mr, n, q, q_ld, s, s_ld, None)
+
+    def load(x=FAKE, dt=1, C=320, x_ld=320, count=None, per=0, mr=8, n=8, q=FAKE, q_ld=384, s=FAKE, s_ld=4):
+        return L.sige_rows8_load(q, q_ld, s, s_ld, C, count, per, mr, n, x, dt, x_ld, None)
+    for call in (store, load):
+        assert call(n=0) == 0 and err(L) == ""
+        assert call(n=0, x=None, q=None, s=None) == 0
+        for kw in (dict(x=None), dict(q=None), dict(s=None), dict(dt=3), dict(C=0), dict(C=-8), dict(x_ld=312), dict(q_ld=368), dict(s_ld=0), dict(C=520, x_ld=520, q_ld=640),
+                   dict(n=-1), dict(n=-1, count=FAKE), dict(n=-2), dict(mr=-1, n=-1, count=FAKE, per=1)):
+            assert call(**kw) == 1, kw
+        for kw in (dict(C=316, x_ld=320), dict(x_ld=324), dict(x=ODD), dict(q=ODD), dict(s=ODDER), dict(q_ld=392), dict(s_ld=6), dict(dt=0, x_ld=322),
+                   dict(mr=2 ** 31 - 1, n=2 ** 31 - 1)):
+            assert call(**kw) == 2, kw
+        assert call(n=9) == 3
+
+
+def test_rms_refusals(L):
+    def rms(x=FAKE, dt=1, C=320, x_ld=320, res=None, res_ld=0, count=None, per=0, mr=8, n=8, gamma=None, eps=1e-6, total=None, total_ld=0, y=OTHER, y_ld=320,
+            q=None, q_ld=0, s=None, s_ld=0):
+        return L.sige_token_rms(x, dt, C, x_ld, res, res_ld, count, per, mr, n, gamma, ctypes.c_float(eps), total, total_ld, y, y_ld, q, q_ld, s, s_ld, None)
+    assert rms(n=0) == 0 and err(L) == ""
+    for kw in (dict(x=None), dict(y=None), dict(dt=3), dict(C=0), dict(x_ld=312), dict(y_ld=312), dict(res=FAKE, res_ld=312), dict(total=FAKE, total_ld=320),
+               dict(res=FAKE, res_ld=320, total=FAKE, total_ld=312), dict(q=FAKE, q_ld=368, s=FAKE, s_ld=4), dict(q=FAKE, q_ld=384, s=None, s_ld=4),
+               dict(eps=-1.0), dict(eps=float("nan")), dict(n=-1), dict(n=-2), dict(res=FAKE, res_ld=320, total=OTHER, total_ld=320)):
+        assert rms(**kw) == 1, kw
+    for kw in (dict(C=316), dict(x=ODD), dict(y=ODD), dict(res=ODD, res_ld=320), dict(gamma=ODDER), dict(C=16392, x_ld=16392, y_ld=16392), dict(y=FAKE, y_ld=328),
+               dict(q=ODD, q_ld=384, s=FAKE, s_ld=4), dict(res=FAKE, res_ld=320, total=FAKE, total_ld=328), dict(res=OTHER, res_ld=328, total=OTHER, total_ld=320, y=None, q=FAKE, q_ld=384, s=FAKE, s_ld=4),
+               dict(dt=0, C=8196, x_ld=8196, y_ld=8196)):
+        assert rms(**kw) == 2, kw
+    assert rms(n=9) == 3
+
+
+def test_linear_refusals(L):
+    def linear(x=FAKE, x_ld=384, xs=FAKE, xs_ld=4, cin=320, count=None, per=0, mr=8, n=8, w=FAKE, w_ld=384, ws=FAKE, ws_ld=4, cout=640, bias=None, base=None, base_ld=0,
+               y=OTHER, dt=1, y_ld=640):
+        return L.sige_rows8_linear(x, x_ld, xs, xs_ld, cin, count, per, mr, n, w, w_ld, ws, ws_ld, cout, bias, base, base_ld, y, dt, y_ld, None)
+
+    def gated(x=FAKE, x_ld=384, xs=FAKE, xs_ld=4, cin=320, count=None, per=0, mr=8, n=8, w=FAKE, w_ld=384, ws=FAKE, ws_ld=4, cout=640, bias=None, gate=0, q=OTHER, q_ld=640,
+              s=OTHER, s_ld=8):
+        return L.sige_rows8_linear_gated(x, x_ld, xs, xs_ld, cin, count, per, mr, n, w, w_ld, ws, ws_ld, cout, bias, gate, q, q_ld, s, s_ld, None)
+    for call in (linear, gated):
+        assert call(n=0) == 0 and err(L) == ""
+        for kw in (dict(x=None), dict(xs=None), dict(w=None), dict(ws=None), dict(cin=0), dict(cout=0), dict(x_ld=368), dict(w_ld=368), dict(xs_ld=0), dict(cin=520, x_ld=640, w_ld=640, ws_ld=8),
+                   dict(n=-1), dict(n=-1, count=FAKE), dict(n=-2)):
+            assert call(**kw) == 1, kw
+        for kw in (dict(x=ODD), dict(w=ODD), dict(xs=ODDER), dict(ws=ODDER), dict(x_ld=392), dict(w_ld=392), dict(xs_ld=6), dict(ws_ld=6), dict(cout=636), dict(bias=ODDER),
+                   dict(cout=2 ** 28 + 8, y_ld=2 ** 29) if call is linear else dict(cout=2 ** 28 + 8, q_ld=2 ** 29, s_ld=2 ** 24)):
+            assert call(**kw) == 2, kw
+        assert call(n=9) == 3
+    for kw in (dict(y=None), dict(dt=3), dict(y_ld=632), dict(base=FAKE, base_ld=632)):
+        assert linear(**kw) == 1, kw
+    for kw in (dict(y=ODD), dict(base=ODD, base_ld=640), dict(y_ld=644), dict(base=OTHER, base_ld=648), dict(dt=0, cout=642, y_ld=644)):
+        assert linear(**kw) == 2, kw
+    for kw in (dict(gate=2), dict(gate=-1), dict(q=None), dict(s=None), dict(q_ld=624), dict(s_ld=4), dict(q=FAKE), dict(s=FAKE)):
+        assert gated(**kw) == 1, kw
+    for kw in (dict(q=ODD), dict(s=ODDER), dict(q_ld=648), dict(s_ld=10)):
+        assert gated(**kw) == 2, kw
+
+
+def test_binding_refusals():
+    """What the binding refuses before it asks the library."""
+    x, y = torch.zeros(4, 320, dtype=torch.float16), torch.zeros(4, 640, dtype=torch.float16)
+    q, s = api.rows8(4, 320, "cpu")
+    w, ws = api.rows8(640, 320, "cpu")
+    o, os_ = api.rows8(4, 640, "cpu")
+
+    def refused(code, fn, *a, **kw):
+        with pytest.raises(api.SigeError) as e:
+            fn(*a, **kw)
+        assert e.value.code == code, e.value
+    refused(1, api.sige_rows8_store, x, q, s, 320, n_rows=4)                                       # on the CPU
+    refused(1, api.sige_rows8_store, x, q.char(), s, 320, n_rows=4)
+    refused(3, api.sige_rows8_store, x, q[:3], s, 320, n_rows=4)
+    refused(3, api.sige_rows8_store, x, q[:, :368], s, 320, n_rows=4)
+    refused(3, api.sige_rows8_store, x, q, s[:, :3], 320, n_rows=4)
+    refused(1, api.sige_rows8_store, x, q.t().contiguous().t(), s, 320, n_rows=4)
+    refused(3, api.sige_rows8_store, x, q, s, 320, n_rows=5)
+    refused(3, api.sige_rows8_store, x, q, s, 328, n_rows=4)
+    refused(3, api.sige_rows8_load, q, s, x[:, :312], 320, n_rows=4)
+    refused(1, api.sige_token_rms, x, 320, torch.ones(320, dtype=torch.float16), y=x, n_rows=4)
+    refused(1, api.sige_token_rms, x, 320, torch.ones(312), y=x, n_rows=4)
+    refused(1, api.sige_token_rms, x, 320, y=x.float(), n_rows=4)
+    refused(1, api.sige_token_rms, x, 320, q=q, n_rows=4)
+    refused(3, api.sige_token_rms, x, 320, q=q, scales=s[:3], n_rows=4)
+    refused(3, api.sige_token_rms, x, 320, y=x, residual=x[:3], n_rows=4)
+    refused(1, api.sige_rows8_linear, q, s, w, ws, y, 320, 640, bias=torch.zeros(632), n_rows=4)
+    refused(1, api.sige_rows8_linear, q, s, w, ws, y, 320, 640, base=y.float(), n_rows=4)
+    refused(3, api.sige_rows8_linear, q, s, w[:639], ws, y, 320, 640, n_rows=4)
+    refused(3, api.sige_rows8_linear, q[:3], s, w, ws, y, 320, 640, n_rows=4)
+    refused(3, api.sige_rows8_linear, q, s, w, ws, y, 520, 640, n_rows=4)
+    refused(3, api.sige_rows8_linear_gated, q, s, w, ws, o, os_, 320, 640, n_rows=4)               # 2 * 640 rows of weights
+    refused(3, api.sige_rows8_linear_gated, q, s, w, ws, o[:, :304], os_, 320, 320, n_rows=4)
+    refused(1, api.sige_rows8_linear_gated, q, s, w, ws, o, os_, 320, 320, bias=torch.zeros(320), n_rows=4)
+    refused(1, api.sige_rows8_linear_gated, q, s, w, ws, o, os_, 320, 320, n_rows=-1, count=torch.zeros(1), rows_per_count=1)

@@ -1,0 +1,552 @@
+"""Rows in 8 bits on the GPU against their definitions in float64: store, load, the root-mean-square norm, the product and its gated form."""
+import numpy as np
+import pytest
+import torch
+
+import rows8_oracle as ref
+from paper_2211_02048_amd import api
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+TINY = {"f32": 2.0 ** -150, "f16": 2.0 ** -25, "bf16": 2.0 ** -134}     # half a step of the type's smallest numbers
+
+
+def f64(t):
+    return t.detach().cpu().double().numpy()
+
+
+def rounded(a, dtype):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(DT[dtype]).double().numpy()
+
+
+def rows(seed, n, C, dtype, extra=8):
+    """Rows of a wider tensor, channels of unlike size."""
+    g = torch.Generator().manual_seed(seed)
+    x = torch.full((n, C + extra), 3.0, dtype=torch.float64)
+    x[:, :C] = torch.randn(n, C, generator=g, dtype=torch.float64) * torch.exp(torch.randn(C, generator=g, dtype=torch.float64))
+    return x.to(DT[dtype]).cuda()[:, :C]
+
+
+def room(n, C, more=1, wide=16):
+    """Codes and scales with a row and bytes behind, all 0xa5."""
+    ld, sld = ref.lds(C)
+    return (torch.full((n + more, ld + wide), 0xa5, dtype=torch.uint8, device="cuda"), torch.full((n + more, sld + 4), 0xa5, dtype=torch.uint8, device="cuda"))
+
+
+def check_room(q, s, n, C):
+    """Nothing behind the rows or their bytes was written; codes and scale bytes behind C are 0."""
+    ld, sld = ref.lds(C)
+    assert (q[n:] == 0xa5).all() and (s[n:] == 0xa5).all() and (q[:, ld:] == 0xa5).all() and (s[:, sld:] == 0xa5).all()
+    assert (q[:n, C:ld] == 0).all() and (s[:n, -(-C // 128):sld] == 0).all()
+
+
+def same_codes(q, s, x64, C):
+    wq, ws = ref.store(x64)
+    gq, gs = q.cpu().numpy()[:, :wq.shape[1]], s.cpu().numpy()[:, :ws.shape[1]]
+    np.testing.assert_array_equal(gs, ws)
+    nan = wq & 0x7f == 0x7f
+    np.testing.assert_array_equal(gq[~nan], wq[~nan])
+    assert (gq[nan] & 0x7f == 0x7f).all()
+
+
+# ---- store, load ---------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("n,C", [(1, 8), (1, 128), (3, 136), (17, 320), (640, 40), (5, 512), (33, 520), (7, 1288), (4, 8192), (2, 16384)])
+def test_store_and_load(n, C, dtype):
+    x = rows(n + C, n, C, dtype)
+    q, s = room(n, C)
+    api.sige_rows8_store(x, q, s, C, n_rows=n)
+    torch.cuda.synchronize()
+    same_codes(q[:n], s[:n], f64(x), C)
+    check_room(q, s, n, C)
+    for out in ("bf16", "f16", "f32"):
+        y = torch.full((n + 1, C + 8), 7.0, dtype=DT[out], device="cuda")
+        api.sige_rows8_load(q, s, y[:n, :C], C, n_rows=n)
+        torch.cuda.synchronize()
+        np.testing.assert_array_equal(f64(y[:n, :C]), rounded(ref.values(q[:n].cpu().numpy(), s[:n].cpu().numpy(), C), out))
+        assert (y[n] == 7.0).all() and (y[:, C:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_store_borders(dtype):
+    """Every code and every tie at several scales, maxima at and beside 448 times a power of two, zeros, subnormal numbers, the type's ends."""
+    cases = []
+    for e in (-3, 0, 5):
+        v = np.concatenate([ref.MAG, ref.EDGES])
+        for part in np.array_split(np.concatenate([v, -v]), 5):
+            cases.append(np.concatenate([part, [448.0]]) * 2.0 ** (e if dtype != "f16" else min(e, 3)))
+    end = float(torch.finfo(DT[dtype]).max)
+    least = float(torch.finfo(DT[dtype]).smallest_normal)
+    for top in (448.0, 449.0, 450.0, 447.0, 480.0, 1.75, 1.7578125, 1.75 * 2.0 ** -10, end, least, least / 4, 0.0, least * 448, least * 450):
+        cases.append(np.array([top, -top / 2, top / 3, 0.0, -0.0, top / 1000]))
+    x = np.zeros((len(cases), 128))
+    for r, c in enumerate(cases):
+        x[r, :len(c)] = c
+    t = torch.from_numpy(x).to(DT[dtype]).cuda()
+    q, s = room(len(cases), 128)
+    api.sige_rows8_store(t, q, s, 128, n_rows=len(cases))
+    torch.cuda.synchronize()
+    same_codes(q[:-1], s[:-1], f64(t), 128)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_store_of_what_is_not_finite(dtype):
+    """Infinities and NaN become NaN by themselves; a block of nothing else has the smallest scale."""
+    x = rows(3, 6, 264, dtype, 0).clone()
+    x[0, 5], x[1, 200], x[2, 130] = float("inf"), float("-inf"), float("nan")
+    x[3, 128:256] = float("nan")
+    x[4] = float("inf")
+    q, s = room(6, 264)
+    api.sige_rows8_store(x, q, s, 264, n_rows=6)
+    y = torch.empty(6, 264, dtype=DT[dtype], device="cuda")
+    api.sige_rows8_load(q, s, y, 264, n_rows=6)
+    torch.cuda.synchronize()
+    same_codes(q[:6], s[:6], f64(x), 264)
+    assert torch.equal(torch.isnan(y), ~torch.isfinite(x))
+    s[5, 0] = 255                                  # a block whose scale is NaN
+    api.sige_rows8_load(q, s, y, 264, n_rows=6)
+    torch.cuda.synchronize()
+    assert torch.isnan(y[5, :128]).all() and torch.isfinite(y[5, 128:]).all()
+
+
+def test_rows_by_a_count_on_the_device():
+    n, C = 40, 320
+    x = rows(1, n, C, "bf16")
+    for count, per in ((3, 7), (0, 7), (9, 5), (-4, 7)):
+        have = max(0, min(count * per, n))
+        q, s = room(n, C)
+        kw = dict(count=torch.tensor([count], dtype=torch.int32, device="cuda"), rows_per_count=per, max_rows=n)
+        api.sige_rows8_store(x, q, s, C, **kw)
+        y, z = (torch.full((n, C), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        api.sige_rows8_load(q, s, y, C, **kw)
+        o, os_ = room(n, C)
+        api.sige_token_rms(x, C, y=z, q=o, scales=os_, **kw)
+        torch.cuda.synchronize()
+        check_room(q, s, have, C)
+        check_room(o, os_, have, C)
+        assert (y[have:] == 7.0).all() and (z[have:] == 7.0).all()
+        if have:
+            same_codes(q[:have], s[:have], f64(x[:have]), C)
+            np.testing.assert_array_equal(f64(y[:have]), ref.values(q[:have].cpu().numpy(), s[:have].cpu().numpy(), C))
+            assert (z[:have] != 7.0).any(1).all()
+
+
+# ---- norm ----------------------------------------------------------------------------------------------
+
+def rms_expected(x, res, gamma, eps, dtype):
+    h = f64(x)
+    if res is not None:
+        # (the sum is added in fp32 and rounded: two roundings, the second of a value that the first has moved by 2^-24 of itself)
+        h = rounded(rounded(h + f64(res), "f32"), dtype)
+    n = h / np.sqrt((h * h).mean(1, keepdims=True) + eps)
+    return h, n if gamma is None else n * f64(gamma)
+
+
+def close_codes(q, s, want, err, C, what=""):
+    """8-bit rows of values that are off by at most err from `want`: half a step of e4m3 (2^-4 of the value, 2^-10 of the scale, or of
+    twice the scale where the block's maximum lies beside a border)."""
+    n = want.shape[0]
+    got = ref.values(q[:n].cpu().numpy(), s[:n].cpu().numpy(), C)
+    top = np.zeros((n, -(-C // 128)))
+    for b in range(top.shape[1]):
+        top[:, b] = (np.abs(want) + err)[:, 128 * b:128 * b + 128].max(1)
+    scale = 2.0 ** np.vectorize(ref.scale_exponent)(top).astype(float)
+    scale = np.repeat(scale, 128, 1)[:, :C]
+    bound = err + 2.0 ** -4 * (np.abs(want) + err) + 2.0 ** -10 * scale
+    off = np.abs(got - want)
+    assert (off <= bound).all(), f"{what}: {np.nanmax(off / bound):.2f} of the bound"
+    # the scale byte itself: that of the largest value, or its neighbour where err reaches the border
+    low = np.zeros_like(top)
+    for b in range(top.shape[1]):
+        low[:, b] = np.maximum(np.abs(want) - err, 0)[:, 128 * b:128 * b + 128].max(1)
+    e = s[:n, :top.shape[1]].cpu().numpy().astype(int) - 127
+    assert (e <= np.vectorize(ref.scale_exponent)(top)).all() and (e >= np.vectorize(ref.scale_exponent)(low)).all(), what
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("n,C", [(1, 8), (5, 128), (3, 136), (19, 320), (6, 512), (7, 640), (5, 1288), (9, 2048), (3, 2056), (1, 4096), (4, 5120), (2, 8192)])
+def test_rms(n, C, dtype):
+    x, res = rows(C + n, n, C, dtype), rows(C + n + 1, n, C, dtype, 16)
+    gamma = (torch.rand(C + 3, dtype=torch.float32) + 0.5).cuda()[3:] if C % 16 else (torch.rand(C) + 0.5).cuda()     # (also not 16-byte aligned)
+    for r, gm, eps in ((res, gamma, 1e-6), (None, gamma, 1e-5), (res, None, 0.0)):
+        h, want = rms_expected(x, r, gm, eps, dtype)
+        rel = (C / 2 + 16) * 2.0 ** -24         # the sum of C squares in fp32 under a root; division, root, two products
+        y = torch.full((n + 1, C + 8), 7.0, dtype=DT[dtype], device="cuda")
+        total = torch.full((n + 1, C + 8), 7.0, dtype=DT[dtype], device="cuda")
+        q, s = room(n, C)
+        api.sige_token_rms(x, C, gm, eps, residual=r, total=None if r is None else total[:n, :C], y=y[:n, :C], q=q, scales=s, n_rows=n)
+        torch.cuda.synchronize()
+        err = np.abs(f64(y[:n, :C]) - want)
+        bound = rel * np.abs(want) + torch.finfo(DT[dtype]).eps / 2 * (1 + rel) * np.abs(want) + TINY[dtype]
+        assert (err <= bound).all(), np.max(err / bound)
+        close_codes(q, s, want, rel * np.abs(want), C, "norm")
+        check_room(q, s, n, C)
+        assert (y[n] == 7.0).all() and (y[:, C:] == 7.0).all() and (total[n] == 7.0).all() and (total[:, C:] == 7.0).all()
+        if r is None:
+            assert (total == 7.0).all()
+        else:
+            np.testing.assert_array_equal(f64(total[:n, :C]), h)
+        # one output at a time: the same bits; in place
+        y2, (q2, s2) = torch.empty_like(x), room(n, C)
+        api.sige_token_rms(x, C, gm, eps, residual=r, q=q2, scales=s2, n_rows=n)
+        api.sige_token_rms(x, C, gm, eps, residual=r, y=y2, n_rows=n)
+        z = x.clone()
+        api.sige_token_rms(z, C, gm, eps, residual=r, y=z, n_rows=n)
+        torch.cuda.synchronize()
+        assert torch.equal(y2, y[:n, :C]) and torch.equal(z, y2) and torch.equal(q, q2) and torch.equal(s, s2)
+        if r is not None:
+            z, w = x.clone(), r.clone()
+            api.sige_token_rms(z, C, gm, eps, residual=w, total=w, y=z, n_rows=n)
+            torch.cuda.synchronize()
+            assert torch.equal(z, y2) and torch.equal(w, total[:n, :C])
+
+
+def test_rms_widest_rows():
+    for dtype, C in (("bf16", 16384), ("f16", 12296), ("f32", 8192), ("f32", 6148)):
+        x = rows(C, 3, C, dtype)
+        _, want = rms_expected(x, None, None, 1e-6, dtype)
+        y, (q, s) = torch.empty_like(x), room(3, C)
+        api.sige_token_rms(x, C, None, 1e-6, y=y, q=q, scales=s, n_rows=3)
+        torch.cuda.synchronize()
+        rel = (C / 2 + 16) * 2.0 ** -24
+        assert (np.abs(f64(y) - want) <= (rel + torch.finfo(DT[dtype]).eps / 2 * (1 + rel)) * np.abs(want) + TINY[dtype]).all()
+        close_codes(q, s, want, rel * np.abs(want), C)
+        check_room(q, s, 3, C)
+
+
+@pytest.mark.parametrize("C", [320, 4096])
+def test_rms_rows_that_are_not_finite(C):
+    """A NaN makes its row NaN, an infinity its row 0 and itself NaN; a row of zeros stays zeros; neighbours do not notice."""
+    x = rows(2, 6, C, "bf16").clone()
+    x[1, 7], x[2, 9], x[3] = float("nan"), float("inf"), 0.0
+    y, (q, s) = torch.empty_like(x), room(6, C)
+    api.sige_token_rms(x, C, None, 1e-6, y=y, q=q, scales=s, n_rows=6)
+    back = torch.empty_like(x)
+    api.sige_rows8_load(q, s, back, C, n_rows=6)
+    torch.cuda.synchronize()
+    for t in (y, back):
+        assert torch.isnan(t[1]).all() and torch.isnan(t[2, 9]) and (torch.cat([t[2, :9], t[2, 10:]]) == 0).all() and (t[3] == 0).all()
+        assert torch.isfinite(t[[0, 4, 5]]).all()
+    want = rms_expected(x[[0, 4, 5]], None, None, 1e-6, "bf16")[1]
+    assert (np.abs(f64(y[[0, 4, 5]]) - want) <= 2.0 ** -7.9 * np.abs(want)).all()
+
+
+# ---- products ------------------------------------------------------------------------------------------
+
+def matrix(seed, n, C, size=1.0, wide=0):
+    """A matrix in 8 bits and its values; scales of unlike size from block to block."""
+    rng = np.random.default_rng(seed)
+    x = rng.normal(size=(n, C)) * np.exp(0.7 * rng.normal(size=C)) * 2.0 ** rng.integers(-2, 3, (n, 1)) * size
+    q, s = ref.store(x)
+    return wide_codes(q, s, wide) + (ref.values(q, s, C),)
+
+
+def wide_codes(q, s, wide):
+    a = torch.full((q.shape[0], q.shape[1] + wide), 0x7f, dtype=torch.uint8)       # what lies behind the codes is never read: NaN
+    b = torch.full((s.shape[0], s.shape[1] + wide // 4), 0xff, dtype=torch.uint8)
+    a[:, :q.shape[1]], b[:, :s.shape[1]] = torch.from_numpy(q), torch.from_numpy(s)
+    return a.cuda(), b.cuda()
+
+
+def product(xv, wv, cin):
+    """The product, the sum of the magnitudes and what the 8-bit instruction may cut off: per product less than 2^-13 of the largest of its block."""
+    y, mag = xv @ wv.T, np.abs(xv) @ np.abs(wv).T
+    cut = np.zeros_like(y)
+    for b in range(0, cin, 128):
+        p, w = np.abs(xv[:, b:b + 128]), np.abs(wv[:, b:b + 128])
+        for i in range(len(p)):
+            cut[i] += p.shape[1] * 2.0 ** -13 * (p[i] * w).max(1)
+    return y, mag, cut
+
+
+SIZES = [(1, 8, 8), (1, 320, 960), (16, 1280, 136), (17, 128, 24), (5, 136, 16), (33, 640, 320), (64, 384, 256), (100, 520, 264), (257, 264, 72), (130, 1288, 144), (300, 1024, 520),
+         (31, 2560, 640)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("n,cin,cout", SIZES)
+def test_linear(n, cin, cout, dtype):
+    xq, xs, xv = matrix(n + cin, n, cin, wide=16)
+    wq, ws, wv = matrix(cout + cin, cout, cin, cin ** -0.5, wide=32)
+    rng = np.random.default_rng(5)
+    bias = torch.from_numpy(rng.normal(size=cout)).float().cuda()
+    base = torch.from_numpy(rng.normal(size=(n, cout + 8))).to(DT[dtype]).cuda()[:, :cout]
+    want, mag, cut = product(xv, wv, cin)
+    for b, r in ((bias, base), (None, None), (None, base)):
+        y = torch.full((n + 1, cout + 8), 7.0, dtype=DT[dtype], device="cuda")
+        api.sige_rows8_linear(xq, xs, wq, ws, y[:n, :cout], cin, cout, bias=b, base=r, n_rows=n)
+        torch.cuda.synchronize()
+        more = (0 if b is None else f64(b)) + (0 if r is None else f64(r))
+        w = want + more
+        bound = (cin + 4) * 2.0 ** -24 * (mag + np.abs(more)) + (0 if dtype == "f32" else cut)
+        bound = bound + torch.finfo(DT[dtype]).eps / 2 * (np.abs(w) + bound) + TINY[dtype]
+        err = np.abs(f64(y[:n, :cout]) - w)
+        assert (err <= bound).all(), f"{np.max(err / bound):.2f} of the bound"
+        assert (y[n] == 7.0).all() and (y[:, cout:] == 7.0).all()
+    z = base.clone()
+    api.sige_rows8_linear(xq, xs, wq, ws, z, cin, cout, base=z, n_rows=n)
+    torch.cuda.synchronize()
+    assert torch.equal(z, y[:n, :cout])
+
+
+@pytest.mark.parametrize("gate", [api.GATE_GELU, api.GATE_SILU])
+@pytest.mark.parametrize("n,cin,cout", SIZES)
+def test_gated(n, cin, cout, gate):
+    xq, xs, xv = matrix(n + cin, n, cin, wide=16)
+    wq, ws, wv = matrix(cout + cin, 2 * cout, cin, 0.5 * cin ** -0.5, wide=32)
+    bias = torch.from_numpy(np.random.default_rng(5).normal(size=2 * cout)).float().cuda()
+    want, mag, cut = product(xv, wv, cin)
+    for b in (bias, None):
+        more = 0 if b is None else f64(b)
+        err = (cin + 4) * 2.0 ** -24 * (mag + np.abs(more)) + cut
+        u, g = (want + more)[:, :cout], (want + more)[:, cout:]
+        v = u * ref.gate(g, gate)
+        # the sums' errors (the gates' slope is below 1.13), then fp32: the error function or the exponential beside 1, some roundings
+        off = err[:, :cout] * (np.abs(ref.gate(g, gate)) + 1.13 * err[:, cout:]) + np.abs(u) * 1.13 * err[:, cout:] + 2.0 ** -20 * np.abs(u * g)
+        q, s = room(n, cout)
+        api.sige_rows8_linear_gated(xq, xs, wq, ws, q, s, cin, cout, gate=gate, bias=b, n_rows=n)
+        torch.cuda.synchronize()
+        close_codes(q, s, v, off, cout, "gated")
+        check_room(q, s, n, cout)
+
+
+def test_single_precision_loses_nothing():
+    """Numbers whose products lie far apart, with a sum that cancels the large ones: the 8-bit instruction would cut the small ones off."""
+    cin, n, cout = 256, 20, 24
+    rng = np.random.default_rng(0)
+    x, w = np.zeros((n, cin)), np.zeros((cout, cin))
+    x[:, :64], w[:, :64] = 448.0, 448.0
+    w[:, 32:64] = -448.0
+    x[:, 64:128], w[:, 64:128] = rng.integers(1, 16, (n, 64)) / 64.0, rng.integers(1, 16, (cout, 64)) / 64.0
+    (xq, xs), (wq, ws) = (wide_codes(*ref.store(v), 0) for v in (x, w))
+    y = torch.empty(n, cout, device="cuda")
+    api.sige_rows8_linear(xq, xs, wq, ws, y, cin, cout, n_rows=n)
+    torch.cuda.synchronize()
+    # partial sums of 32 products of 2^17.6 have 24 bits: 2^-1.4 each
+    assert (np.abs(f64(y) - x @ w.T) <= cin * 2.0 ** -24 * 32 * 448.0 ** 2).all()
+    x[:, :64] = 0
+    xq, xs = wide_codes(*ref.store(x), 0)
+    api.sige_rows8_linear(xq, xs, wq, ws, y, cin, cout, n_rows=n)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(f64(y), x @ w.T)     # 64 products of 8 bits: exact
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_products_with_what_is_not_finite(dtype):
+    """NaN codes and NaN scales reach the rows and channels that read them and no others."""
+    n, cin, cout = 37, 392, 136
+    xq, xs, _ = matrix(1, n, cin)
+    wq, ws, _ = matrix(2, 2 * cout, cin)
+    xq[3, 100] = 0x7f
+    xs[20, 2] = 255
+    wq[50, 391] = 0xff
+    ws[77, 0] = 255
+    y = torch.empty(n, cout, dtype=DT[dtype], device="cuda")
+    api.sige_rows8_linear(xq, xs, wq, ws, y, cin, cout, n_rows=n)
+    q, s = room(n, cout)
+    api.sige_rows8_linear_gated(xq, xs, wq, ws, q, s, cin, cout, n_rows=n)
+    back = torch.empty(n, cout, device="cuda")
+    api.sige_rows8_load(q, s, back, cout, n_rows=n)
+    torch.cuda.synchronize()
+    for t in (y, back):
+        bad = torch.zeros(n, cout, dtype=torch.bool, device="cuda")
+        bad[[3, 20]], bad[:, [50, 77]] = True, True
+        assert torch.equal(torch.isnan(t), bad)
+
+
+def test_extreme_scales():
+    """Scales from one end to the other: sums beyond fp16 become infinite, tiny ones keep their bits in single precision."""
+    n, cin, cout = 16, 256, 16
+    for ex, ew in ((60, 40), (-60, -40), (100, -100), (-100, 100), (-55, -55)):
+        rng = np.random.default_rng(1)
+        x, w = rng.normal(size=(n, cin)) * 2.0 ** ex, rng.normal(size=(cout, cin)) * 2.0 ** ew
+        (xq, xs), (wq, ws) = (wide_codes(*ref.store(v), 0) for v in (x, w))
+        xv, wv = ref.values(xq.cpu().numpy(), xs.cpu().numpy(), cin), ref.values(wq.cpu().numpy(), ws.cpu().numpy(), cin)
+        want, mag, cut = product(xv, wv, cin)
+        for dtype in ("f32", "bf16"):
+            y = torch.empty(n, cout, dtype=DT[dtype], device="cuda")
+            api.sige_rows8_linear(xq, xs, wq, ws, y, cin, cout, n_rows=n)
+            torch.cuda.synchronize()
+            bound = (cin + 4) * 2.0 ** -24 * mag + (0 if dtype == "f32" else cut)
+            bound = bound + torch.finfo(DT[dtype]).eps / 2 * (np.abs(want) + bound)
+            assert (np.abs(f64(y) - want) <= bound + 2.0 ** -126).all(), (ex, ew, dtype)
+    big = wide_codes(*ref.store(np.full((n, cin), 1000.0)), 0)
+    y = torch.empty(n, cout, dtype=torch.float16, device="cuda")
+    api.sige_rows8_linear(*big, *(t[:cout] for t in big), y, cin, cout, n_rows=n)
+    torch.cuda.synchronize()
+    assert torch.isinf(y).all()
+
+
+def test_product_rows_by_a_count_on_the_device():
+    n, cin, cout = 200, 264, 136
+    xq, xs, xv = matrix(1, n, cin)
+    wq, ws, wv = matrix(2, 2 * cout, cin)
+    full = torch.empty(n, cout, device="cuda")
+    api.sige_rows8_linear(xq, xs, wq, ws, full, cin, cout, n_rows=n)
+    fq, fs = room(n, cout)
+    api.sige_rows8_linear_gated(xq, xs, wq, ws, fq, fs, cin, cout, n_rows=n)
+    for count, per in ((3, 16), (0, 16), (100, 16), (-1, 16), (1, 1), (5, 29)):
+        have = max(0, min(count * per, n))
+        kw = dict(count=torch.tensor([count], dtype=torch.int32, device="cuda"), rows_per_count=per, max_rows=n)
+        y, (q, s) = torch.full((n, cout), 7.0, device="cuda"), room(n, cout)
+        api.sige_rows8_linear(xq, xs, wq, ws, y, cin, cout, **kw)
+        api.sige_rows8_linear_gated(xq, xs, wq, ws, q, s, cin, cout, **kw)
+        torch.cuda.synchronize()
+        assert torch.equal(y[:have], full[:have]) and (y[have:] == 7.0).all()
+        assert torch.equal(q[:have], fq[:have]) and torch.equal(s[:have], fs[:have])
+        check_room(q, s, have, cout)
+
+
+@pytest.mark.parametrize("kind", ["store", "rms", "linear"])
+def test_offsets_beyond_32_bits(kind):
+    """The last rows of tensors whose offsets do not fit 32 bits."""
+    C, n = 8192, 2 ** 31 // 8192 + 300
+    if kind == "linear":
+        xq, xs, xv = matrix(1, 3, C)
+        wq, ws, wv = matrix(2, 16, C, C ** -0.5)
+        q, s = api.rows8(n, C)
+        q[-3:], s[-3:] = xq, xs
+        q[:-3], s[:-3] = 0, 0
+        y = torch.empty(n, 16, dtype=torch.bfloat16, device="cuda")
+        api.sige_rows8_linear(q, s, wq, ws, y, C, 16, n_rows=n)
+        torch.cuda.synchronize()
+        want, mag, cut = product(xv, wv, C)
+        assert (np.abs(f64(y[-3:]) - want) <= C * 2.0 ** -24 * mag + cut + 2.0 ** -8 * (np.abs(want) + cut)).all() and (y[:-3] == 0).all()
+        return
+    x = torch.zeros(n, C, dtype=torch.bfloat16, device="cuda")
+    x[-2:] = rows(1, 2, C, "bf16", 0)
+    q, s = api.rows8(n, C)
+    if kind == "store":
+        api.sige_rows8_store(x, q, s, C, n_rows=n)
+        y = torch.empty_like(x)
+        api.sige_rows8_load(q, s, y, C, n_rows=n)
+        torch.cuda.synchronize()
+        same_codes(q[-2:], s[-2:], f64(x[-2:]), C)
+        np.testing.assert_array_equal(f64(y[-2:]), ref.values(q[-2:].cpu().numpy(), s[-2:].cpu().numpy(), C))
+    else:
+        y = torch.empty_like(x)
+        api.sige_token_rms(x, C, y=y, q=q, scales=s, n_rows=n)
+        torch.cuda.synchronize()
+        want = rms_expected(x[-2:], None, None, 1e-6, "bf16")[1]
+        assert (np.abs(f64(y[-2:]) - want) <= (2.0 ** -8 + 2.0 ** -10) * np.abs(want)).all()
+        close_codes(q[-2:], s[-2:], want, C * 2.0 ** -24 * np.abs(want), C)
+    assert (y[:-2] == 0).all()
+
+
+# ---- as they are used ----------------------------------------------------------------------------------
+
+def feed_forward(x, indices, g, n_blocks, p, tiles, h, q, s, v, vs, y, full, C):
+    """A feed-forward layer on the tokens of an edit, from the full tensor back into it."""
+    api.sige_gather(x, g, indices, None, tiles, n_blocks=n_blocks)
+    t, n = tiles.view(-1, C), n_blocks * g.block_h * g.block_w
+    api.sige_token_rms(t, C, p["gamma"], 1e-6, q=q, scales=s, n_rows=n)
+    api.sige_rows8_linear_gated(q, s, *p["first"], v, vs, C, 4 * C, bias=p["b1"], n_rows=n)
+    api.sige_rows8_linear(v, vs, *p["second"], y, 4 * C, C, bias=p["b2"], base=t, n_rows=n)
+    api.sige_scatter(y.view(tiles.shape), g, indices, None, full, n_blocks=n_blocks)
+
+
+def layer(seed, C, dtype="bf16"):
+    gen = torch.Generator().manual_seed(seed)
+    r = lambda *shape: torch.randn(*shape, generator=gen, dtype=torch.float64)   # noqa: E731
+    p = {"gamma": (1 + 0.1 * r(C)).float().cuda(), "b1": (0.1 * r(8 * C)).float().cuda(), "b2": (0.1 * r(C)).float().cuda()}
+    for name, shape in (("first", (8 * C, C)), ("second", (C, 4 * C))):
+        w = (r(*shape) / shape[1] ** 0.5).to(DT[dtype]).cuda()
+        p[name] = api.rows8(*shape)
+        api.sige_rows8_store(w, *p[name], shape[1], n_rows=shape[0])
+    return p
+
+
+def test_feed_forward_layer_of_an_edit():
+    """Gather, norm, the gated product, the product with the residual, scatter: every stored tensor against its definition on what the call
+    read; then captured into a graph and replayed on other edits, between eager calls."""
+    C, side, nb = 72, 32, 6
+    p = layer(0, C)
+    g = api.geom(side, side, 4, 1, 1, 0)
+    x = torch.randn(side, side, C, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    pick = torch.tensor([3, 9, 20, 33, 40, 63])
+    indices = torch.stack([pick // 8 * 4, pick % 8 * 4], 1).int().cuda()
+    n = nb * 16
+    tiles, y, full = torch.empty(nb, 4, 4, C).bfloat16().cuda(), torch.empty(n, C).bfloat16().cuda(), x.clone()
+    q, s, v, vs = *api.rows8(n, C), *api.rows8(n, 4 * C)
+    args = (x, indices, g, nb, p, tiles, None, q, s, v, vs, y, full, C)
+    feed_forward(*args)
+    torch.cuda.synchronize()
+    t = f64(tiles.view(n, C))
+    nrm = t / np.sqrt((t * t).mean(1, keepdims=True) + 1e-6) * f64(p["gamma"])
+    close_codes(q, s, nrm, (C + 16) * 2.0 ** -24 * np.abs(nrm), C, "norm")
+    val = lambda m, c: ref.values(m[0].cpu().numpy(), m[1].cpu().numpy(), c)   # noqa: E731
+    want, mag, cut = product(val((q, s), C), val(p["first"], C), C)
+    want, err = want + f64(p["b1"]), (C + 4) * 2.0 ** -24 * (mag + 1) + cut
+    u, gt = want[:, :4 * C], want[:, 4 * C:]
+    off = err[:, :4 * C] * (np.abs(ref.gate(gt, 0)) + 1.13 * err[:, 4 * C:]) + np.abs(u) * 1.13 * err[:, 4 * C:] + 2.0 ** -20 * np.abs(u * gt)
+    close_codes(v, vs, u * ref.gate(gt, 0), off, 4 * C, "gated")
+    want, mag, cut = product(val((v, vs), 4 * C), val(p["second"], 4 * C), 4 * C)
+    want = want + f64(p["b2"]) + t
+    bound = (4 * C + 4) * 2.0 ** -24 * (mag + np.abs(t) + 1) + cut
+    assert (np.abs(f64(y) - want) <= bound + 2.0 ** -8 * (np.abs(want) + bound)).all()
+    for i, (y0, x0) in enumerate(indices.tolist()):
+        assert torch.equal(full[y0:y0 + 4, x0:x0 + 4], y.view(nb, 4, 4, C)[i])
+
+    side_stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side_stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side_stream):
+        feed_forward(*args)
+    for k in range(4):
+        x.copy_(torch.randn(side, side, C, generator=torch.Generator().manual_seed(10 + k)).bfloat16())
+        indices.copy_(torch.tensor([[4 * ((i + k) % 8), 4 * ((3 * i + k) % 8)] for i in range(nb)]).int())
+        full.copy_(x)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = full.clone()
+        full.copy_(x)
+        feed_forward(*args)
+        torch.cuda.synchronize()
+        assert torch.equal(got, full) and not torch.equal(full, x)
+
+
+def test_two_streams_at_once():
+    """The calls hold no state: the same layers on two streams at the same time, each with buffers of its own."""
+    C, n = 320, 48
+    p = layer(3, C)
+    sets = []
+    for k in range(2):
+        x = rows(k, n, C, "bf16", 0)
+        sets.append((x, *api.rows8(n, C), *api.rows8(n, 4 * C), torch.empty_like(x)))
+
+    def run(x, q, s, v, vs, y):
+        api.sige_token_rms(x, C, p["gamma"], q=q, scales=s, n_rows=n)
+        api.sige_rows8_linear_gated(q, s, *p["first"], v, vs, C, 4 * C, gate=api.GATE_SILU, bias=p["b1"], n_rows=n)
+        api.sige_rows8_linear(v, vs, *p["second"], y, 4 * C, C, base=x, n_rows=n)
+    want = []
+    for a in sets:
+        run(*a)
+        torch.cuda.synchronize()
+        want.append(a[-1].clone())
+        a[-1].zero_()
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for st, a in zip(streams, sets):
+            with torch.cuda.stream(st):
+                run(*a)
+    torch.cuda.synchronize()
+    for a, w in zip(sets, want):
+        assert torch.equal(a[-1], w)
+
+
+def test_recorded_calls():
+    """Calls marshalled once and repeated."""
+    C, n = 320, 5
+    x = rows(0, n, C, "f16", 0)
+    q, s = api.rows8(n, C)
+    y = torch.empty_like(x)
+    with api.record() as calls:
+        api.sige_token_rms(x, C, q=q, scales=s, n_rows=n)
+        api.sige_rows8_load(q, s, y, C, n_rows=n)
+    torch.cuda.synchronize()
+    want = y.clone()
+    y.zero_()
+    calls.run()
+    torch.cuda.synchronize()
+    assert len(calls) == 2 and torch.equal(y, want)
