@@ -643,7 +643,7 @@ typedef enum {
     SIGE_KNOB_CONV_SPLIT_WGS = 4, SIGE_KNOB_CONV_POINTWISE = 5, SIGE_KNOB_CONV_POINTWISE_W4 = 6,
     SIGE_KNOB_CONV_PAIR_WGS = 7, SIGE_KNOB_ATTN_WGS = 8, SIGE_KNOB_DIFF_LOADS = 9, SIGE_KNOB_DIFF_WGS = 10,
     SIGE_KNOB_CONV_DIRECT = 11, SIGE_KNOB_CONV_LDS_PAD = 12, SIGE_KNOB_CONV_AHEAD = 13,
-    SIGE_KNOB_CACHE4_MANY = 14, SIGE_KNOB_COUNT = 15
+    SIGE_KNOB_CACHE4_MANY = 14, SIGE_KNOB_ROWS8_FORM = 15, SIGE_KNOB_COUNT = 16
 } sige_knob;
 int sige_set_knob(sige_knob knob, int32_t value);
 int32_t sige_get_knob(sige_knob knob);

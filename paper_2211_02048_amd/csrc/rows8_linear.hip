@@ -1,145 +1,75 @@
-// sige_rows8_linear, sige_rows8_linear_gated: products of two matrices in 8 bits on the stacked tokens of the active blocks.
-//
-// One instruction of the matrix unit, v_mfma_scale_f32_16x16x128_f8f6f4, multiplies 16 weight rows by 16 token rows over a whole block of 128
-// channels and applies the two blocks' scales: the sums stay where they are from the first block to the last.  The weights are the
-// instruction's first operand, so that a lane holds consecutive output channels of one token.
-#include "rows8.h"
+// sige_rows8_linear, sige_rows8_linear_gated: products of two matrices in 8 bits on the stacked tokens of the active blocks; checks, and which
+// kernel takes a call.
+#include "rows8_forms.h"
+
+#include <cmath>
 
 namespace sige {
 
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-struct Linear8Args {
-    const unsigned char* x;
-    const unsigned char* xs;
-    const unsigned char* w;
-    const unsigned char* ws;
-    const float* bias;
-    const void* base;
-    void* y;
-    unsigned char* q;
-    unsigned char* s;
-    Rows8 rows;
-    int blocks;                 // of 128 input channels
-    int Cout, x_ld, xs_ld, w_ld, ws_ld, base_ld, y_ld, q_ld, s_ld;
-    int gate;
+// What a form takes, in microseconds, by a model of measured calls (360 calls over the ranges 1 to 8192 rows and 16 to 8192 channels, replayed from a
+// graph with inputs that change: off by 6 to 14 %): start + rounds of workgroups over the chip * (tile + block * blocks of 128 channels that
+// a wave goes through).  The few-row kernel's workgroups are small and many: its time goes by blocks and tiles in all.
+struct Linear8Cost {
+    int rows, cols, slots, shares;
+    float start, tile, block;
 };
 
-// 32 codes of a lane: channels 16 k .. 16 k + 15 and 64 + 16 k .. of a block, k = lane / 16 (any order serves, as long as both operands have it).
-struct Codes32 { uint4 lo, hi; };
-
-__device__ __forceinline__ Codes32 load_codes(const unsigned char* row, int k)
+static float linear8_cost(const Linear8Cost& c, int rows, int cols, int blocks)
 {
-    return {*(const uint4*)(row + 16 * k), *(const uint4*)(row + 64 + 16 * k)};
+    const float tiles = (float)((rows + c.rows - 1) / c.rows) * (float)((cols + c.cols - 1) / c.cols), units = tiles / COMPUTE_UNITS;
+    float rounds = std::ceil(units / c.slots);
+    if (c.slots == 2) rounds = units <= 1.0f ? 0.62f : units <= 2.0f ? 1.0f : units / 2.0f;     // (one workgroup by itself has the compute unit's time)
+    if (c.rows == 256) {
+        const float whole = std::floor(units), over = units - whole;
+        rounds = whole + (over == 0.0f ? 0.0f : whole >= 1.0f && over <= 0.5f ? 0.62f : 1.0f);  // (the rest as halves)
+    }
+    return c.start + rounds * (c.tile + c.block * (float)((blocks + c.shares - 1) / c.shares));
 }
 
-// c += 16 weight rows x 16 token rows over a block of 128 channels; the scale words' low bytes count.
-template <bool EXACT> struct Step8;
-template <> struct Step8<false> {
-    static __device__ __forceinline__ void run(const Codes32& a, unsigned sa, const Codes32& b, unsigned sb, f32x4& c)
-    {
-        const i32x8 u = {(int)a.lo.x, (int)a.lo.y, (int)a.lo.z, (int)a.lo.w, (int)a.hi.x, (int)a.hi.y, (int)a.hi.z, (int)a.hi.w};
-        const i32x8 v = {(int)b.lo.x, (int)b.lo.y, (int)b.lo.z, (int)b.lo.w, (int)b.hi.x, (int)b.hi.y, (int)b.hi.z, (int)b.hi.w};
-        c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u, v, c, 0, 0, 0, (int)sa, 0, (int)sb);
-    }
-};
-template <> struct Step8<true> {
-    // codes times scales are bf16 numbers: four instructions of 32 channels
-    static __device__ __forceinline__ uint4 expand(unsigned lo, unsigned hi, float scale)
-    {
-        union { decltype(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(0u, 1.0f, false)) v; unsigned u; } p, q, r, t;
-        p.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false);
-        q.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
-        r.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false);
-        t.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
-        return make_uint4(p.u, q.u, r.u, t.u);
-    }
-    static __device__ __forceinline__ void run(const Codes32& a, unsigned sa, const Codes32& b, unsigned sb, f32x4& c)
-    {
-        typedef __bf16 v8 __attribute__((ext_vector_type(8)));
-        const float fa = scale_value(sa & 255u), fb = scale_value(sb & 255u);
-        const auto one = [&](unsigned a0, unsigned a1, unsigned b0, unsigned b1) {
-            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, expand(a0, a1, fa)), __builtin_bit_cast(v8, expand(b0, b1, fb)), c, 0, 0, 0);
-        };
-        one(a.lo.x, a.lo.y, b.lo.x, b.lo.y);
-        one(a.lo.z, a.lo.w, b.lo.z, b.lo.w);
-        one(a.hi.x, a.hi.y, b.hi.x, b.hi.y);
-        one(a.hi.z, a.hi.w, b.hi.z, b.hi.w);
-    }
-};
-
-__device__ __forceinline__ float gate_value(float u, float g, int gate)
+static float linear8_few_cost(bool exact, int rows, int cols, int blocks)
 {
-    return gate == SIGE_GATE_GELU ? u * (0.5f * g * (1.0f + erff(g * 0.70710678118654752f))) : u * g / (1.0f + expf(-g));
+    const int words = (blocks + 3) / 4, waves = words < 8 ? words : 8, fit = 160 * 1024 / (waves * Few8<false, 1, 1, 2>::WAVE), slots = fit < 32 / waves ? fit : 32 / waves;
+    const float units = (float)((rows + 15) / 16) * (float)((cols + 15) / 16) / COMPUTE_UNITS, steps = (float)(4 * ((words + waves - 1) / waves));
+    const float more = units / (float)slots > 1.0f ? units / (float)slots - 1.0f : 0.0f;
+    return exact ? 1.04f + 0.489f * steps + 0.057f * units * (float)blocks + 0.112f * units
+                 : 1.24f + 0.379f * steps + 0.053f * units * (float)blocks + 0.079f * units + 0.488f * more;
 }
 
-// 16 rows x 128 output channels per workgroup, 16 channels per wave.
-template <typename T, bool GATED>
-__global__ __launch_bounds__(512) void rows8_linear_kernel(Linear8Args a)
+// The form with the smallest cost that can take the call: the kernels for tiles have 32-bit offsets into a tile's rows.
+static int linear8_form(const Linear8Args& a, int rows, bool exact)
 {
-    __shared__ unsigned top[8][16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = lane & 15, k = lane >> 4;
-    const int rows = rows8_effective(a.rows);
-    const int row0 = blockIdx.y * 16, c0 = blockIdx.x * 128 + wave * 16;
-    if (row0 >= rows) return;
-    const int row = row0 + m < rows ? row0 + m : rows - 1;
-    const int ch = c0 + m < a.Cout ? c0 + m : a.Cout - 1;
-    const unsigned char* x = a.x + (long)row * a.x_ld;
-    const unsigned char* xs = a.xs + (long)row * a.xs_ld;
-    const unsigned char* w = a.w + (long)ch * a.w_ld;
-    const unsigned char* ws = a.ws + (long)ch * a.ws_ld;
-    const long gw = (long)a.Cout * a.w_ld, gs = (long)a.Cout * a.ws_ld;
-    f32x4 u = {0, 0, 0, 0}, g = {0, 0, 0, 0};
-    for (int b = 0; b < a.blocks; ++b) {
-        const Codes32 xc = load_codes(x + 128 * b, k);
-        const unsigned sx = xs[b];
-        Step8<sizeof(T) == 4>::run(load_codes(w + 128 * b, k), ws[b], xc, sx, u);
-        if (GATED) Step8<sizeof(T) == 4>::run(load_codes(w + gw + 128 * b, k), ws[gs + b], xc, sx, g);
+    static const Linear8Cost half[LINEAR8_FORMS] = {{}, {32, 32, 1, 4, 1.32f, 1.38f, 0.352f}, {32, 64, 1, 4, 1.23f, 1.63f, 0.520f}, {64, 64, 1, 4, 0.84f, 2.41f, 0.679f},
+                                                   {128, 64, 2, 1, 0.92f, 2.97f, 0.512f}, {128, 128, 2, 1, 0.19f, 4.63f, 0.731f}, {128, 128, 1, 1, 0.0f, 3.50f, 0.402f},
+                                                   {256, 256, 1, 1, 0.0f, 6.44f, 0.973f}};
+    static const Linear8Cost single[LINEAR8_FORMS] = {{}, {32, 32, 1, 4, 1.27f, 1.58f, 0.525f}, {32, 64, 1, 4, 1.20f, 2.10f, 0.750f}, {64, 64, 1, 4, 0.32f, 3.22f, 1.024f},
+                                                     {128, 64, 2, 1, 0.0f, 4.96f, 0.858f}, {128, 128, 2, 1, 0.0f, 6.32f, 1.240f}, {128, 128, 1, 1, 0.0f, 4.25f, 0.776f}, {}};
+    const int set = knob(SIGE_KNOB_ROWS8_FORM);
+    const bool offsets = a.x_ld < (1 << 22) && a.w_ld < (1 << 22);
+    if (set >= 0 && (set < LINEAR8_TILE_128X64 || offsets)) return set;
+    int best = LINEAR8_FEW;
+    float least = rows <= 65535 * 16 ? linear8_few_cost(exact, rows, a.Cout, a.blocks) : INFINITY;
+    for (int f = LINEAR8_WAVES_32; f < (exact ? LINEAR8_TILE_256 : LINEAR8_FORMS); ++f) {
+        if (f >= LINEAR8_TILE_128X64 && !offsets) break;
+        const float c = linear8_cost(exact ? single[f] : half[f], rows, a.Cout, a.blocks);
+        if (c < least) { least = c; best = f; }
     }
-    asm volatile("" : "+v"(u), "+v"(g));         // (the instruction works on all lanes: nothing of it may move into the branches below)
-    const int c = c0 + 4 * k;                    // the lane's channels c .. c + 3 of token row0 + m
-    const bool in = row0 + m < rows;
-    if constexpr (!GATED) {
-        if (!in || c >= a.Cout) return;
-        const T* base = a.base ? (const T*)a.base + (long)row * a.base_ld + c : nullptr;
-        T* y = (T*)a.y + (long)row * a.y_ld + c;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float v = u[i];
-            if (a.bias) v += a.bias[c + i];
-            if (base) v += to_f32(base[i]);
-            y[i] = from_f32<T>(v);
-        }
-    } else {
-        float v[4];
-        unsigned most = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bool real = c + i < a.Cout;
-            const float bu = a.bias && real ? a.bias[c + i] : 0.0f, bg = a.bias && real ? a.bias[a.Cout + c + i] : 0.0f;
-            v[i] = real ? gate_value(u[i] + bu, g[i] + bg, a.gate) : 0.0f;
-            const unsigned bits = finite_bits(v[i]);
-            most = bits > most ? bits : most;
-        }
-        unsigned o = (unsigned)__shfl_xor((int)most, 16);
-        most = o > most ? o : most;
-        o = (unsigned)__shfl_xor((int)most, 32);
-        most = o > most ? o : most;
-        if (k == 0) top[wave][m] = most;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 8; ++i) most = top[i][m] > most ? top[i][m] : most;
-        if (!in) return;
-        const int sb = scale_byte(most);
-        *(unsigned*)(a.q + (long)row * a.q_ld + c) = codes4(v[0], v[1], v[2], v[3], scale_inverse(sb));
-        if (wave == 0 && k == 0) {
-            unsigned char* s = a.s + (long)row * a.s_ld;
-            s[blockIdx.x] = (unsigned char)sb;
-            if (blockIdx.x == gridDim.x - 1)
-                for (int b = gridDim.x; b & 3; ++b) s[b] = 0;
-        }
+    return best;
+}
+
+static int linear8_gated_form(const Linear8Args& a, int rows)
+{
+    static const Linear8Cost cost[GATED8_FORMS] = {{16, 128, 1, 1, 1.15f, 2.56f, 0.389f}, {64, 128, 1, 1, 0.70f, 5.32f, 0.468f}, {128, 128, 1, 1, 0.0f, 8.59f, 0.648f},
+                                                  {256, 128, 1, 1, 0.0f, 15.83f, 0.967f}};
+    const int set = knob(SIGE_KNOB_ROWS8_FORM);
+    const bool offsets = a.x_ld < (1 << 22) && 2L * a.Cout * a.w_ld < (1L << 31);
+    if (set >= 0 && (set < GATED8_TILE_64 || offsets)) return set;
+    int best = GATED8_FEW;
+    float least = INFINITY;
+    for (int f = GATED8_FEW; f < (offsets ? GATED8_FORMS : GATED8_TILE_64); ++f) {
+        const float c = linear8_cost(cost[f], rows, a.Cout, a.blocks);
+        if (c < least) { least = c; best = f; }
     }
+    return best;
 }
 
 }  // namespace sige
@@ -183,15 +113,9 @@ extern "C" int sige_rows8_linear(const void* x, int32_t x_ld, const void* x_scal
     SIGE_REQUIRE(y, SIGE_ERR_INVALID_ARG, "%s: y is required", who);
     SIGE_REQUIRE(aligned16(y) && aligned16(base), SIGE_ERR_UNSUPPORTED, "%s: y and base must be 16-byte aligned", who);
     a.base = base; a.base_ld = base_ld; a.y = y; a.y_ld = y_ld;
-    const dim3 grid((Cout + 127) / 128, (rows + 15) / 16);
-    SIGE_REQUIRE(grid.y < 65536, SIGE_ERR_UNSUPPORTED, "%s: too many rows", who);
     hipStream_t st = (hipStream_t)stream;
-    auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(512), 0, st, a); };
-    if (dt == SIGE_F32) go(rows8_linear_kernel<float, false>);
-    else if (dt == SIGE_F16) go(rows8_linear_kernel<f16, false>);
-    else go(rows8_linear_kernel<bf16, false>);
-    SIGE_LAUNCH_CHECK(who);
-    return SIGE_OK;
+    const int form = linear8_form(a, rows, dt == SIGE_F32);
+    return dt == SIGE_F32 ? linear8_f32(who, a, rows, form, st) : dt == SIGE_F16 ? linear8_f16(who, a, rows, form, st) : linear8_bf16(who, a, rows, form, st);
 }
 
 extern "C" int sige_rows8_linear_gated(const void* x, int32_t x_ld, const void* x_scales, int32_t xs_ld, int32_t Cin, const int32_t* count,
@@ -211,9 +135,5 @@ extern "C" int sige_rows8_linear_gated(const void* x, int32_t x_ld, const void* 
     SIGE_REQUIRE(rows == 0 || (q != x && scales != x_scales), SIGE_ERR_INVALID_ARG, "%s: the output may not be x", who);
     if (rows == 0) return SIGE_OK;
     a.gate = gate; a.q = (unsigned char*)q; a.q_ld = q_ld; a.s = (unsigned char*)scales; a.s_ld = s_ld;
-    const dim3 grid((Cout + 127) / 128, (rows + 15) / 16);
-    SIGE_REQUIRE(grid.y < 65536, SIGE_ERR_UNSUPPORTED, "%s: too many rows", who);
-    hipLaunchKernelGGL((rows8_linear_kernel<bf16, true>), grid, dim3(512), 0, (hipStream_t)stream, a);
-    SIGE_LAUNCH_CHECK(who);
-    return SIGE_OK;
+    return linear8_gated(who, a, rows, linear8_gated_form(a, rows), (hipStream_t)stream);
 }

@@ -1,0 +1,6 @@
+// The products of two matrices in 8 bits with results in single precision.
+#include "rows8_forms.h"
+
+namespace sige {
+int linear8_f32(const char* who, const Linear8Args& a, int rows, int form, hipStream_t st) { return linear8_launch<float>(who, a, rows, form, st); }
+}  // namespace sige

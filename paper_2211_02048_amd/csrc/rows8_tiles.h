@@ -1,0 +1,394 @@
+// The product of two matrices in 8 bits for many rows: tiles of 64 RT rows x 64 CT output channels, four waves of 32 RT x 32 CT each.
+//
+// Bound by the matrix pipes for large calls.  v_mfma_scale_f32_32x32x64_f8f6f4 (weights as its first operand, so that a lane holds consecutive
+// channels of one token; its two scales are those of the block of 128 channels that its 64 lie in).  A block of 128 channels of both operands
+// comes into LDS by direct loads, whole 128-byte lines (halves of lines took 1.4 times as long: twice the requests), NS blocks
+// deep; the 16-byte pieces of a row are permuted by the row's number, so that neither the loads nor the reads meet in a bank.  While the
+// pipe works on one half of a block, the next half's operands are read into registers, one read or request between two
+// matrix instructions: there is one wave per SIMD in the largest form, and whatever it waits for the pipe waits for too.  One barrier per
+// block, in the middle of its first half, when its last reads are done: from there on its place takes the block NS further on.
+// Measured: 8192 x 8192 x 8192 in 401 us, 2746 TFLOP/s; the same kernel without any loads or reads reaches 4065.
+#pragma once
+
+#include "rows8_linear.h"
+
+namespace sige {
+
+constexpr int COMPUTE_UNITS = 256;
+
+// LDS rows of the weights: which output channel of the wave's (of its values and of its gates, if gated) lies at place p of the tile.  In the
+// result, place 8 (r / 4) + 4 h + r % 4 of 32 is in register r of the lanes of half h.
+template <bool GATED>
+__device__ __forceinline__ int tile_channel(int p)
+{
+    const int u = p & 31;
+    if (!GATED)         // registers 8 v .. 8 v + 7: channels 16 v + 8 h ...
+        return (p & ~31) + 16 * (u >> 4) + 8 * (u >> 2 & 1) + 4 * (u >> 3 & 1) + (u & 3);
+    // (four tiles of 32 per wave: two of values, two of their gates; tile t's registers: channels 32 h + 16 t ...)
+    return (p >> 7) * 64 + 32 * (u >> 2 & 1) + 16 * (p >> 5 & 1) + 4 * (u >> 3) + (u & 3);
+}
+
+template <typename T, bool GATED, int RT, int CT, int NS>
+struct Tile8 {
+    static constexpr bool EXACT = sizeof(T) == 4;
+    static constexpr int BM = 64 * RT, BN = 64 * CT, OUT = GATED ? BN / 2 : BN;          // rows, weight rows and output channels of a tile
+    static constexpr int XB = BM * 128, STAGE = XB + BN * 128, SC = NS * STAGE;          // bytes in LDS; where the scale words are
+    static constexpr int XI = BM / 32, WI = BN / 32, REQ = XI + WI;                      // direct loads of a wave per block
+    static constexpr int N = RT * CT;                                                    // matrix instructions of a wave per half block
+    // a block's 2 N matrix instructions are its time: operands of its second half are read beside the first of them, READS at a time; behind
+    // number FREE its place is requested into again, PER requests at a time, and at number COME the next block has to have come
+    static constexpr int READS = (RT + CT + N - 1) / N, READ = (RT + CT + READS - 1) / READS;
+    static constexpr int FREE = READ + (N >= 16 ? 2 : N >= 8 ? 1 : 0), COME = 2 * N - READ - (N >= 16 ? 2 : 0);
+    static constexpr int PER = (REQ + 2 * N - FREE - 1) / (2 * N - FREE);
+    static_assert(FREE <= COME && COME >= N, "");
+    static constexpr int GROUPS = (BM + BN) / 64;                                        // of scale words, 64 rows each
+    static constexpr int LDS = SC + 4 * (BM + BN) * 4;                                   // the stages, four scale words of every row
+
+    static __device__ __forceinline__ void mma(const i32x8& w, unsigned ws, const i32x8& x, unsigned xs, f32x16& c)
+    {
+        if constexpr (!EXACT) {
+            c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(w, x, c, 0, 0, 0, (int)ws, 0, (int)xs);
+        } else {
+            const float fw = scale_value(ws & 255u), fx = scale_value(xs & 255u);
+#pragma unroll
+            for (int i = 0; i < 8; i += 2)
+                c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(expand8(w[i], w[i + 1], fw), expand8(x[i], x[i + 1], fx), c, 0, 0, 0);
+        }
+    }
+
+    // The tile of rows row0 ... and output channels col0 ...
+    static __device__ __forceinline__ void run(const Linear8Args& a, unsigned char* lds, int all_rows, int row0, int col0)
+    {
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 31, h = lane >> 5;
+        const int wm = wave & 1, wn = wave >> 1;
+        const int rows = all_rows - row0 < BM ? all_rows - row0 : BM, cols = a.Cout - col0 < OUT ? a.Cout - col0 : OUT;
+        const auto xr = __builtin_amdgcn_make_buffer_rsrc((void*)(a.x + (long)row0 * a.x_ld), 0, rows * a.x_ld, 0x00027000);
+        const auto wr = __builtin_amdgcn_make_buffer_rsrc((void*)(a.w + (long)col0 * a.w_ld), 0, ((GATED ? a.Cout : 0) + cols) * a.w_ld, 0x00027000);
+        // what a wave requests: 8 rows of 128 bytes at a time, lane l piece (l % 8) ^ (row / 2 % 8) of row l / 8 (rows that are not there: the last one)
+        int xo[XI], wo[WI];
+        const int piece = ((lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7)) * 16;
+        const auto weight_row = [&](int p) {
+            const int c = tile_channel<GATED>(p);
+            return (GATED && (p >> 6 & 1) ? a.Cout : 0) + (c < cols ? c : cols - 1);
+        };
+#pragma unroll
+        for (int i = 0; i < XI; ++i) {
+            const int p = 8 * (wave + 4 * i) + (lane >> 3);
+            xo[i] = (p < rows ? p : rows - 1) * a.x_ld + piece;
+        }
+#pragma unroll
+        for (int i = 0; i < WI; ++i) wo[i] = weight_row(8 * (wave + 4 * i) + (lane >> 3)) * a.w_ld + piece;
+        typedef __attribute__((address_space(3))) void* lds_ptr;
+        const auto request = [&](int b, int place, int i) {
+            if (i < WI)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_ptr)(lds + place + XB + (wave + 4 * i) * 1024), 16, wo[i], 128 * b, 0, 0);
+            else
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, (lds_ptr)(lds + place + (wave + 4 * (i - WI)) * 1024), 16, xo[i - WI], 128 * b, 0, 0);
+        };
+#pragma unroll
+        for (int i = 0; i < REQ; ++i) request(0, 0, i);
+        // scale words, [word of four blocks % 4][BM + BN rows]: a wave requests two groups of 64 rows in turn
+        const int words = (a.blocks + 3) / 4;
+        const unsigned char* sp[2];
+        int sat[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int p = ((2 * wave + e) % GROUPS) * 64 + lane;
+            sp[e] = p < BM ? a.xs + (long)(row0 + (p < rows ? p : rows - 1)) * a.xs_ld : a.ws + (long)(col0 + weight_row(p - BM)) * a.ws_ld;
+            sat[e] = SC + ((2 * wave + e) % GROUPS) * 256;
+        }
+        typedef const __attribute__((address_space(1))) void* global_ptr;
+        const auto request_word = [&](int word, int e) {
+            const int w = word < words ? word : words - 1;
+            __builtin_amdgcn_global_load_lds((global_ptr)((e ? sp[1] : sp[0]) + 4 * (long)w), (lds_ptr)(lds + (e ? sat[1] : sat[0]) + (word & 3) * (BM + BN) * 4), 4, 0, 0);
+        };
+#pragma unroll
+        for (int e = 0; e < 4; ++e) request_word(e >> 1, e & 1);
+#pragma unroll
+        for (int b = 1; b < NS; ++b)
+            if (b < a.blocks) {
+#pragma unroll
+                for (int i = 0; i < REQ; ++i) request(b, b * STAGE, i);
+            }
+        // the bias waits in a register
+        float bias = 0.0f;
+        if (a.bias && (int)threadIdx.x < BN) {
+            const int c = (int)threadIdx.x % OUT;
+            bias = a.bias[((int)threadIdx.x < OUT ? 0 : a.Cout) + col0 + (c < cols ? c : cols - 1)];
+        }
+        f32x16 acc[RT][CT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int j = 0; j < CT; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+        // operands: row m of a tile of 32, pieces h and 2 + h of the first half of the block, 4 + h and 6 + h of the second
+        const int off = m * 128 + ((h ^ (m >> 1)) & 7) * 16;
+        int xb = wm * RT * 4096 + off, wb = XB + wn * CT * 4096 + off, place = 0;
+        i32x8 xf[2][RT], wf[2][CT];
+        unsigned xs[RT], ws[CT], xn[RT], wn_[CT];
+        const auto operand = [&](int at, int tile) {
+            return both(*(const i32x4*)(lds + at + tile * 4096), *(const i32x4*)(lds + (at ^ 32) + tile * 4096));
+        };
+        const auto read_words = [&](int b) {
+            const int at = SC + ((b >> 2 & 3) * (BM + BN) + m) * 4;
+#pragma unroll
+            for (int i = 0; i < RT; ++i) xn[i] = *(const unsigned*)(lds + at + (wm * RT + i) * 128);
+#pragma unroll
+            for (int j = 0; j < CT; ++j) wn_[j] = *(const unsigned*)(lds + at + BM * 4 + (wn * CT + j) * 128);
+        };
+        // the first block and the scale words have come, the others may be on their way (and the bias, which is newer still)
+        if (a.blocks >= NS) __builtin_amdgcn_s_waitcnt(0x0070 | ((NS - 1) * REQ & 15) | ((NS - 1) * REQ >> 4) << 14);
+        else __builtin_amdgcn_s_waitcnt(0x0070);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < CT; ++j) wf[0][j] = operand(wb, j);
+#pragma unroll
+        for (int i = 0; i < RT; ++i) xf[0][i] = operand(xb, i);
+        read_words(0);
+        // MORE: block b + NS exists; NEXT: block b + 1 does
+        const auto block = [&](int b, auto more_, auto next_) {
+            constexpr bool MORE = decltype(more_)::value, NEXT = decltype(next_)::value;
+#pragma unroll
+            for (int i = 0; i < RT; ++i) xs[i] = xn[i] >> 8 * (b & 3);
+#pragma unroll
+            for (int j = 0; j < CT; ++j) ws[j] = wn_[j] >> 8 * (b & 3);
+            const int next = NS == 2 ? place ^ STAGE : place + STAGE < SC ? place + STAGE : 0, step = next - place;
+            constexpr int issued = PER * (COME - FREE) < REQ ? PER * (COME - FREE) : REQ;
+            constexpr int newer = (NS - 2) * REQ + (COME > FREE ? issued + 1 : 0);
+#pragma unroll
+            for (int n = 0; n < 2 * N; ++n) {
+                constexpr auto wait = [](int vm, int lgkm) { return (vm & 15) | 0x70 | lgkm << 8 | (vm >> 4) << 14; };
+                const int u = n / N, i = n % N / CT, j = n % CT;
+                if (NEXT && n == FREE && FREE < COME) {
+                    // the block's last reads are done once the barrier is passed
+                    __builtin_amdgcn_s_waitcnt(wait(63, 0));
+                    asm volatile("" ::: "memory");
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (NEXT && n == COME) {
+                    __builtin_amdgcn_s_waitcnt(wait(MORE ? newer : 0, FREE < COME ? 15 : 0));
+                    asm volatile("" ::: "memory");
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                const int first = n < N ? n * READS : NEXT && n >= COME ? (n - COME) * READS : RT + CT;
+#pragma unroll
+                for (int r = first; r < first + READS && r < RT + CT; ++r) {
+                    if (r < CT) wf[n < N][r] = operand(n < N ? wb ^ 64 : wb + step, r);
+                    else xf[n < N][r - CT] = operand(n < N ? xb ^ 64 : xb + step, r - CT);
+                }
+                if (NEXT && n == (COME + READ < 2 * N ? COME + READ : 2 * N - 1)) read_words(b + 1);
+                mma(wf[u][j], ws[j], xf[u][i], xs[i], acc[i][j]);
+                if (MORE && n >= FREE) {
+                    if (n == FREE) request_word((b >> 2) + 2, b & 1);
+#pragma unroll
+                    for (int e = PER * (n - FREE); e < PER * (n - FREE + 1) && e < REQ; ++e) request(b + NS, place, e);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            xb += step;
+            wb += step;
+            place = next;
+        };
+        int b = 0;
+        for (; b + NS < a.blocks; ++b) block(b, std::true_type(), std::true_type());
+        for (; b + 1 < a.blocks; ++b) block(b, std::false_type(), std::true_type());
+        block(b, std::false_type(), std::false_type());
+        // (the instruction works on all lanes: nothing of it may move into the branches below)
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int j = 0; j < CT; ++j) asm volatile("" : "+v"(acc[i][j]));
+        __syncthreads();                                     // (the last block's reads are done)
+        if ((int)threadIdx.x < BN) ((float*)lds)[threadIdx.x] = bias;
+        __syncthreads();
+        if constexpr (GATED) gated(a, lds, acc, row0, col0, rows, cols, lane, wm, wn);
+        else plain(a, (const float*)lds, acc, row0, col0, rows, cols, m, h, wm, wn);
+    }
+
+    static __device__ __forceinline__ void plain(const Linear8Args& a, const float* bias, f32x16 (&acc)[RT][CT], int row0, int col0, int rows, int cols, int m, int h,
+                                                 int wm, int wn)
+    {
+        constexpr int V = Vec16<T>::N, P = 8 / V;            // a lane's runs of 8 channels are P vectors
+        long at[RT], from[RT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            const int r = (wm * RT + i) * 32 + m;
+            at[i] = (long)(row0 + r) * a.y_ld + col0;
+            from[i] = (long)(row0 + (r < rows ? r : rows - 1)) * a.base_ld + col0;
+        }
+#pragma unroll
+        for (int j = 0; j < CT; ++j)
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                const int c = (wn * CT + j) * 32 + 16 * v + 8 * h;
+                uint4 g[RT][P];
+                if (a.base) {
+#pragma unroll
+                    for (int i = 0; i < RT; ++i)
+#pragma unroll
+                        for (int w = 0; w < P; ++w) {
+                            const int cw = c + V * w < cols ? c + V * w : 0;
+                            g[i][w] = *(const uint4*)((const T*)a.base + from[i] + cw);
+                        }
+                }
+                float b8[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) b8[e] = bias[c + e];
+#pragma unroll
+                for (int i = 0; i < RT; ++i)
+#pragma unroll
+                    for (int w = 0; w < P; ++w) {
+                        float f[V];
+#pragma unroll
+                        for (int e = 0; e < V; ++e) f[e] = acc[i][j][8 * v + V * w + e] + b8[V * w + e];
+                        if (a.base) {
+                            float o[V];
+                            unpack<T>(g[i][w], o);
+#pragma unroll
+                            for (int e = 0; e < V; ++e) f[e] += o[e];
+                        }
+                        if ((wm * RT + i) * 32 + m < rows && c + V * w < cols) *(uint4*)((T*)a.y + at[i] + c + V * w) = pack<T>(f);
+                    }
+            }
+    }
+
+    // Tiles 0, 1 of a wave are values, 2, 3 their gates; a block of 128 output channels is the workgroup's, so that a row's scale is the
+    // maximum over two waves.
+    static __device__ __forceinline__ void gated(const Linear8Args& a, unsigned char* lds, f32x16 (&acc)[RT][CT], int row0, int col0, int rows, int cols, int lane,
+                                                 int wm, int wn)
+    {
+        static_assert(!GATED || CT == 4, "a workgroup has a block of 128 output channels");
+        const int m = lane & 31, h = lane >> 5;
+        const float* bias = (const float*)lds;               // [128] of values, [128] of gates
+        float* top = (float*)lds + BN;                       // [2][BM]
+        float most[RT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) most[i] = 0.0f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int c = wn * 64 + 32 * h + 16 * t;
+            // (Cout is a multiple of 8)
+#pragma unroll
+            for (int v = 0; v < 16; v += 8) {
+                const bool real = c + v < cols;
+                float bu[8], bg[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) { bu[e] = bias[c + v + e]; bg[e] = bias[OUT + c + v + e]; }
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float f = real ? gate_value(acc[i][t][v + e] + bu[e], acc[i][t + CT / 2][v + e] + bg[e], a.gate) : 0.0f;
+                        acc[i][t][v + e] = f;
+                        most[i] = fmaxf(most[i], fabsf(f));
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            if (most[i] == __uint_as_float(0x7f800000u)) {       // (a NaN is passed over by the maximum, an infinity has to be)
+                most[i] = 0.0f;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) most[i] = fmaxf(most[i], finite_or_0(acc[i][t][e]));
+            }
+            most[i] = fmaxf(most[i], __shfl_xor(most[i], 32));
+            if (h == 0) top[wn * BM + (wm * RT + i) * 32 + m] = most[i];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            const int r = (wm * RT + i) * 32 + m;
+            if (r >= rows) continue;
+            const int sb = scale_byte(__float_as_uint(fmaxf(most[i], top[(wn ^ 1) * BM + r])));
+            const float inv = scale_inverse(sb);
+            unsigned char* q = a.q + (long)(row0 + r) * a.q_ld + col0 + wn * 64 + 32 * h;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                uint4 w;
+                w.x = codes4(acc[i][t][0], acc[i][t][1], acc[i][t][2], acc[i][t][3], inv);
+                w.y = codes4(acc[i][t][4], acc[i][t][5], acc[i][t][6], acc[i][t][7], inv);
+                w.z = codes4(acc[i][t][8], acc[i][t][9], acc[i][t][10], acc[i][t][11], inv);
+                w.w = codes4(acc[i][t][12], acc[i][t][13], acc[i][t][14], acc[i][t][15], inv);
+                *(uint4*)(q + 16 * t) = w;
+            }
+            if (wn == 0 && h == 0) {
+                unsigned char* s = a.s + (long)(row0 + r) * a.s_ld;
+                const int block = col0 / 128, last = (a.Cout - 1) / 128;
+                s[block] = (unsigned char)sb;
+                if (block == last)
+                    for (int e = block + 1; e & 3; ++e) s[e] = 0;
+            }
+        }
+    }
+};
+
+// Number `t` of tiles of my x nx: the tiles that are worked on at a time lie in strips of 8 tiles of rows, so that the workgroups of an XCD share
+// both operands in its L2.
+__device__ __forceinline__ void tile_place(int t, int nx, int my, int& row, int& col)
+{
+    const int g = t / (8 * nx), rem = t - g * 8 * nx, high = my - g * 8 < 8 ? my - g * 8 : 8;
+    col = rem / high;
+    row = g * 8 + rem - col * high;
+}
+
+// The workgroup's number among n, so that each XCD (workgroups go to the eight in turn) has a run of them.
+__device__ __forceinline__ int xcd_run(int id, int n)
+{
+    const int per = n / 8, more = n % 8, x = id & 7;
+    return x * per + (x < more ? x : more) + (id >> 3);
+}
+
+// HALVES: what the last, partial round of tiles over the compute units leaves idle is used by tiles of half the rows, if that takes one round.
+template <typename T, bool GATED, int RT, int CT, int NS, int WGS, bool HALVES>
+__global__ __launch_bounds__(256, WGS) void rows8_tile_kernel(Linear8Args a)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char tile_lds[];
+    using Tile = Tile8<T, GATED, RT, CT, NS>;
+    const int rows = rows8_effective(a.rows), id = blockIdx.x;
+    const int nx = (a.Cout + Tile::OUT - 1) / Tile::OUT, my = (rows + Tile::BM - 1) / Tile::BM, n = nx * my;
+    const int over = n % COMPUTE_UNITS, whole = HALVES && n > COMPUTE_UNITS && over <= COMPUTE_UNITS / 2 ? n - over : n;
+    int row, col;
+    if (id < whole) {
+        tile_place(xcd_run(id, whole), nx, my, row, col);
+        Tile::run(a, tile_lds, rows, row * Tile::BM, col * Tile::OUT);
+    } else if constexpr (HALVES) {
+        if (id >= 2 * n - whole) return;
+        const int half = xcd_run(id - whole, 2 * (n - whole));
+        tile_place(whole + half / 2, nx, my, row, col);
+        const int row0 = row * Tile::BM + (half & 1) * (Tile::BM / 2);
+        if (row0 < rows) Tile8<T, GATED, RT / 2, CT, NS>::run(a, tile_lds, rows, row0, col * Tile::OUT);
+    }
+}
+
+// One launch of the kernel, for an instantiation per file.
+template <typename T, bool GATED, int RT, int CT, int NS, int WGS, bool HALVES = false>
+inline int launch_tiles(const char* who, const Linear8Args& a, int rows, hipStream_t st)
+{
+    using Tile = Tile8<T, GATED, RT, CT, NS>;
+    const long n = (long)((a.Cout + Tile::OUT - 1) / Tile::OUT) * ((rows + Tile::BM - 1) / Tile::BM);
+    SIGE_REQUIRE(n < (1L << 23), SIGE_ERR_UNSUPPORTED, "%s: too many rows and channels", who);
+    const auto kern = rows8_tile_kernel<T, GATED, RT, CT, NS, WGS, HALVES>;
+    static thread_local bool room = false;                    // (the attribute is a kernel's, the same whatever the call)
+    if (!room) {
+        hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+        SIGE_REQUIRE(e == hipSuccess, SIGE_ERR_HIP, "%s: %s", who, hipGetErrorString(e));
+        room = true;
+    }
+    hipLaunchKernelGGL(kern, dim3((unsigned)(n + (HALVES ? COMPUTE_UNITS / 2 : 0))), dim3(256), Tile::LDS, st, a);
+    SIGE_LAUNCH_CHECK(who);
+    return SIGE_OK;
+}
+
+}  // namespace sige
