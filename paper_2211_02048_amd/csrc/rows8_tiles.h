@@ -42,7 +42,7 @@ struct Tile8 {
     static constexpr int PER = (REQ + 2 * N - FREE - 1) / (2 * N - FREE);
     static_assert(FREE <= COME && COME >= N, "");
     static constexpr int GROUPS = (BM + BN) / 64;                                        // of scale words, 64 rows each
-    static constexpr int LDS = SC + 4 * (BM + BN) * 4;                                   // the stages, four scale words of every row
+    static constexpr int EPI = SC + 4 * (BM + BN) * 4, LDS = EPI + BN * 4 + (GATED ? 2 * BM * 4 : 0);   // four scale words of every row; bias, rows' maxima
 
     static __device__ __forceinline__ void mma(const i32x8& w, unsigned ws, const i32x8& x, unsigned xs, f32x16& c)
     {
@@ -56,66 +56,94 @@ struct Tile8 {
         }
     }
 
-    // The tile of rows row0 ... and output channels col0 ...
-    static __device__ __forceinline__ void run(const Linear8Args& a, unsigned char* lds, int all_rows, int row0, int col0)
+    // Where a tile's operands come from.
+    struct Source {
+        int row0, col0, rows, cols;                          // of the tile (rows and output channels that are there)
+        int xo[XI], wo[WI];                                  // a lane's places in the tile's rows, for each of its requests per block
+        const unsigned char* sp[2];                          // its scale words
+        float bias;                                          // thread t's: that of the t-th row of weights of the tile, in the order of the channels
+    };
+
+    // Tiles from next(row0, col0), one after the other: a tile's first blocks are requested before the results of the one before are worked on
+    // (4096 x 2560 -> 2 x 10240 gated by tiles of 128 rows 267 -> 254 us; tiles of 256 x 256 have no registers for it: ONCE, one tile).
+    template <bool ONCE, typename Next>
+    static __device__ __forceinline__ void run(const Linear8Args& a, unsigned char* lds, int all_rows, Next&& next_tile)
     {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), m = lane & 31, h = lane >> 5;
         const int wm = wave & 1, wn = wave >> 1;
-        const int rows = all_rows - row0 < BM ? all_rows - row0 : BM, cols = a.Cout - col0 < OUT ? a.Cout - col0 : OUT;
-        const auto xr = __builtin_amdgcn_make_buffer_rsrc((void*)(a.x + (long)row0 * a.x_ld), 0, rows * a.x_ld, 0x00027000);
-        const auto wr = __builtin_amdgcn_make_buffer_rsrc((void*)(a.w + (long)col0 * a.w_ld), 0, ((GATED ? a.Cout : 0) + cols) * a.w_ld, 0x00027000);
-        // what a wave requests: 8 rows of 128 bytes at a time, lane l piece (l % 8) ^ (row / 2 % 8) of row l / 8 (rows that are not there: the last one)
-        int xo[XI], wo[WI];
-        const int piece = ((lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7)) * 16;
-        const auto weight_row = [&](int p) {
-            const int c = tile_channel<GATED>(p);
-            return (GATED && (p >> 6 & 1) ? a.Cout : 0) + (c < cols ? c : cols - 1);
-        };
-#pragma unroll
-        for (int i = 0; i < XI; ++i) {
-            const int p = 8 * (wave + 4 * i) + (lane >> 3);
-            xo[i] = (p < rows ? p : rows - 1) * a.x_ld + piece;
-        }
-#pragma unroll
-        for (int i = 0; i < WI; ++i) wo[i] = weight_row(8 * (wave + 4 * i) + (lane >> 3)) * a.w_ld + piece;
-        typedef __attribute__((address_space(3))) void* lds_ptr;
-        const auto request = [&](int b, int place, int i) {
-            if (i < WI)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_ptr)(lds + place + XB + (wave + 4 * i) * 1024), 16, wo[i], 128 * b, 0, 0);
-            else
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, (lds_ptr)(lds + place + (wave + 4 * (i - WI)) * 1024), 16, xo[i - WI], 128 * b, 0, 0);
-        };
-#pragma unroll
-        for (int i = 0; i < REQ; ++i) request(0, 0, i);
-        // scale words, [word of four blocks % 4][BM + BN rows]: a wave requests two groups of 64 rows in turn
         const int words = (a.blocks + 3) / 4;
-        const unsigned char* sp[2];
-        int sat[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const int p = ((2 * wave + e) % GROUPS) * 64 + lane;
-            sp[e] = p < BM ? a.xs + (long)(row0 + (p < rows ? p : rows - 1)) * a.xs_ld : a.ws + (long)(col0 + weight_row(p - BM)) * a.ws_ld;
-            sat[e] = SC + ((2 * wave + e) % GROUPS) * 256;
-        }
+        Source t;
+        typedef __attribute__((address_space(3))) void* lds_ptr;
         typedef const __attribute__((address_space(1))) void* global_ptr;
+        const auto request = [&](int b, int place, int i) {
+            if (i < WI) {
+                const auto wr = __builtin_amdgcn_make_buffer_rsrc((void*)(a.w + (long)t.col0 * a.w_ld), 0, ((GATED ? a.Cout : 0) + t.cols) * a.w_ld, 0x00027000);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_ptr)(lds + place + XB + (wave + 4 * i) * 1024), 16, t.wo[i], 128 * b, 0, 0);
+            } else {
+                const auto xr = __builtin_amdgcn_make_buffer_rsrc((void*)(a.x + (long)t.row0 * a.x_ld), 0, t.rows * a.x_ld, 0x00027000);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, (lds_ptr)(lds + place + (wave + 4 * (i - WI)) * 1024), 16, t.xo[i - WI], 128 * b, 0, 0);
+            }
+        };
+        // scale words, [word of four blocks % 4][BM + BN rows]: a wave requests two groups of 64 rows in turn
+        const int sat[2] = {SC + (2 * wave % GROUPS) * 256, SC + ((2 * wave + 1) % GROUPS) * 256};
         const auto request_word = [&](int word, int e) {
             const int w = word < words ? word : words - 1;
-            __builtin_amdgcn_global_load_lds((global_ptr)((e ? sp[1] : sp[0]) + 4 * (long)w), (lds_ptr)(lds + (e ? sat[1] : sat[0]) + (word & 3) * (BM + BN) * 4), 4, 0, 0);
+            __builtin_amdgcn_global_load_lds((global_ptr)((e ? t.sp[1] : t.sp[0]) + 4 * (long)w), (lds_ptr)(lds + (e ? sat[1] : sat[0]) + (word & 3) * (BM + BN) * 4), 4, 0, 0);
         };
+        const auto begin = [&](int row0, int col0) {
+            t.row0 = row0;
+            t.col0 = col0;
+            t.rows = all_rows - row0 < BM ? all_rows - row0 : BM;
+            t.cols = a.Cout - col0 < OUT ? a.Cout - col0 : OUT;
+            // what a wave requests: 8 rows of 128 bytes at a time, lane l piece (l % 8) ^ (row / 2 % 8) of row l / 8 (rows that are not there: the last one)
+            const int piece = ((lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7)) * 16;
+            const auto weight_row = [&](int p) {
+                const int c = tile_channel<GATED>(p);
+                return (GATED && (p >> 6 & 1) ? a.Cout : 0) + (c < t.cols ? c : t.cols - 1);
+            };
 #pragma unroll
-        for (int e = 0; e < 4; ++e) request_word(e >> 1, e & 1);
-#pragma unroll
-        for (int b = 1; b < NS; ++b)
-            if (b < a.blocks) {
-#pragma unroll
-                for (int i = 0; i < REQ; ++i) request(b, b * STAGE, i);
+            for (int i = 0; i < XI; ++i) {
+                const int p = 8 * (wave + 4 * i) + (lane >> 3);
+                t.xo[i] = (p < t.rows ? p : t.rows - 1) * a.x_ld + piece;
             }
-        // the bias waits in a register
-        float bias = 0.0f;
-        if (a.bias && (int)threadIdx.x < BN) {
-            const int c = (int)threadIdx.x % OUT;
-            bias = a.bias[((int)threadIdx.x < OUT ? 0 : a.Cout) + col0 + (c < cols ? c : cols - 1)];
-        }
+#pragma unroll
+            for (int i = 0; i < WI; ++i) t.wo[i] = weight_row(8 * (wave + 4 * i) + (lane >> 3)) * a.w_ld + piece;
+#pragma unroll
+            for (int i = 0; i < REQ; ++i) request(0, 0, i);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int p = ((2 * wave + e) % GROUPS) * 64 + lane;
+                t.sp[e] = p < BM ? a.xs + (long)(row0 + (p < t.rows ? p : t.rows - 1)) * a.xs_ld : a.ws + (long)(col0 + weight_row(p - BM)) * a.ws_ld;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) request_word(e >> 1, e & 1);
+#pragma unroll
+            for (int b = 1; b < NS; ++b)
+                if (b < a.blocks) {
+#pragma unroll
+                    for (int i = 0; i < REQ; ++i) request(b, b * STAGE, i);
+                }
+            t.bias = 0.0f;
+            if (a.bias && (int)threadIdx.x < BN) {
+                const int c = (int)threadIdx.x % OUT;
+                t.bias = a.bias[((int)threadIdx.x < OUT ? 0 : a.Cout) + col0 + (c < t.cols ? c : t.cols - 1)];
+            }
+        };
+        constexpr auto wait = [](int vm, int lgkm) { return (vm & 15) | 0x70 | lgkm << 8 | (vm >> 4) << 14; };
+        const auto barrier = [] {
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        int row0, col0;
+        if (!next_tile(row0, col0)) return;
+        begin(row0, col0);
+        // the first block and the scale words have come, the others may be on their way
+        if (a.blocks >= NS) __builtin_amdgcn_s_waitcnt(wait((NS - 1) * REQ, 0));
+        else __builtin_amdgcn_s_waitcnt(wait(0, 0));
+        for (;;) {
+        barrier();
         f32x16 acc[RT][CT];
 #pragma unroll
         for (int i = 0; i < RT; ++i)
@@ -138,13 +166,6 @@ struct Tile8 {
 #pragma unroll
             for (int j = 0; j < CT; ++j) wn_[j] = *(const unsigned*)(lds + at + BM * 4 + (wn * CT + j) * 128);
         };
-        // the first block and the scale words have come, the others may be on their way (and the bias, which is newer still)
-        if (a.blocks >= NS) __builtin_amdgcn_s_waitcnt(0x0070 | ((NS - 1) * REQ & 15) | ((NS - 1) * REQ >> 4) << 14);
-        else __builtin_amdgcn_s_waitcnt(0x0070);
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int j = 0; j < CT; ++j) wf[0][j] = operand(wb, j);
 #pragma unroll
@@ -162,22 +183,15 @@ struct Tile8 {
             constexpr int newer = (NS - 2) * REQ + (COME > FREE ? issued + 1 : 0);
 #pragma unroll
             for (int n = 0; n < 2 * N; ++n) {
-                constexpr auto wait = [](int vm, int lgkm) { return (vm & 15) | 0x70 | lgkm << 8 | (vm >> 4) << 14; };
                 const int u = n / N, i = n % N / CT, j = n % CT;
                 if (NEXT && n == FREE && FREE < COME) {
                     // the block's last reads are done once the barrier is passed
                     __builtin_amdgcn_s_waitcnt(wait(63, 0));
-                    asm volatile("" ::: "memory");
-                    __builtin_amdgcn_s_barrier();
-                    asm volatile("" ::: "memory");
-                    __builtin_amdgcn_sched_barrier(0);
+                    barrier();
                 }
                 if (NEXT && n == COME) {
                     __builtin_amdgcn_s_waitcnt(wait(MORE ? newer : 0, FREE < COME ? 15 : 0));
-                    asm volatile("" ::: "memory");
-                    __builtin_amdgcn_s_barrier();
-                    asm volatile("" ::: "memory");
-                    __builtin_amdgcn_sched_barrier(0);
+                    barrier();
                 }
                 const int first = n < N ? n * READS : NEXT && n >= COME ? (n - COME) * READS : RT + CT;
 #pragma unroll
@@ -206,59 +220,86 @@ struct Tile8 {
 #pragma unroll
         for (int i = 0; i < RT; ++i)
 #pragma unroll
-            for (int j = 0; j < CT; ++j) asm volatile("" : "+v"(acc[i][j]));
-        __syncthreads();                                     // (the last block's reads are done)
-        if ((int)threadIdx.x < BN) ((float*)lds)[threadIdx.x] = bias;
-        __syncthreads();
-        if constexpr (GATED) gated(a, lds, acc, row0, col0, rows, cols, lane, wm, wn);
-        else plain(a, (const float*)lds, acc, row0, col0, rows, cols, m, h, wm, wn);
+            for (int j = 0; j < CT; ++j) {
+                if constexpr (N == 16) asm volatile("" : "+a"(acc[i][j]));
+                else asm volatile("" : "+v"(acc[i][j]));
+            }
+        // every wave has read its last operands; the bias to where the channels' lanes find it
+        if ((int)threadIdx.x < BN) ((float*)(lds + EPI))[threadIdx.x] = t.bias;
+        const int r0 = t.row0, c0 = t.col0, rows = t.rows, cols = t.cols;
+        __builtin_amdgcn_s_waitcnt(wait(63, 0));
+        barrier();
+        const bool more = !ONCE && next_tile(row0, col0);
+        if (more) begin(row0, col0);
+        if constexpr (GATED) gated(a, lds + EPI, acc, r0, c0, rows, cols, lane, wm, wn);
+        else if (rows == BM && cols == OUT) plain<true>(a, (const float*)(lds + EPI), acc, r0, c0, rows, cols, m, h, wm, wn);
+        else plain<false>(a, (const float*)(lds + EPI), acc, r0, c0, rows, cols, m, h, wm, wn);
+        if (!more) return;
+        // (the stores above are newer than the next tile's requests: all of a whole tile's may be on their way)
+        constexpr int stores = GATED ? 2 * RT : 2 * RT * CT * (8 / Vec16<T>::N), most = (NS - 1) * REQ + stores < 63 ? (NS - 1) * REQ + stores : 63;
+        if (a.blocks >= NS && rows == BM && cols == OUT) __builtin_amdgcn_s_waitcnt(wait(most, 0));
+        else __builtin_amdgcn_s_waitcnt(wait(0, 0));
+        }
     }
 
+    // FULL: every row and channel of the tile is there.
+    template <bool FULL>
     static __device__ __forceinline__ void plain(const Linear8Args& a, const float* bias, f32x16 (&acc)[RT][CT], int row0, int col0, int rows, int cols, int m, int h,
                                                  int wm, int wn)
     {
         constexpr int V = Vec16<T>::N, P = 8 / V;            // a lane's runs of 8 channels are P vectors
-        long at[RT], from[RT];
+        constexpr int JS = FULL && RT * CT < 16 ? CT : FULL ? 2 : 1;         // columns of tiles whose base is on its way at a time
+        const int c0 = wn * CT * 32 + 8 * h;
+        long row[RT];
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
             const int r = (wm * RT + i) * 32 + m;
-            at[i] = (long)(row0 + r) * a.y_ld + col0;
-            from[i] = (long)(row0 + (r < rows ? r : rows - 1)) * a.base_ld + col0;
+            row[i] = row0 + (FULL || r < rows ? r : rows - 1);
         }
 #pragma unroll
-        for (int j = 0; j < CT; ++j)
+        for (int j0 = 0; j0 < CT; j0 += JS) {
+            uint4 g[JS][2][RT][P];
+            if (a.base) {
 #pragma unroll
-            for (int v = 0; v < 2; ++v) {
-                const int c = (wn * CT + j) * 32 + 16 * v + 8 * h;
-                uint4 g[RT][P];
-                if (a.base) {
+                for (int i = 0; i < RT; ++i) {
+                    const T* base = (const T*)a.base + row[i] * a.base_ld + col0;
+#pragma unroll
+                    for (int j = 0; j < JS; ++j)
+#pragma unroll
+                        for (int v = 0; v < 2; ++v)
+#pragma unroll
+                            for (int w = 0; w < P; ++w) {
+                                const int c = c0 + (j0 + j) * 32 + 16 * v + V * w;
+                                g[j][v][i][w] = *(const uint4*)(base + (FULL || c < cols ? c : 0));
+                            }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int j = 0; j < JS; ++j)
+#pragma unroll
+                for (int v = 0; v < 2; ++v) {
+                    const int c = c0 + (j0 + j) * 32 + 16 * v;
+                    float b8[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) b8[e] = bias[c + e];
 #pragma unroll
                     for (int i = 0; i < RT; ++i)
 #pragma unroll
                         for (int w = 0; w < P; ++w) {
-                            const int cw = c + V * w < cols ? c + V * w : 0;
-                            g[i][w] = *(const uint4*)((const T*)a.base + from[i] + cw);
+                            float f[V];
+#pragma unroll
+                            for (int e = 0; e < V; ++e) f[e] = acc[i][j0 + j][8 * v + V * w + e] + b8[V * w + e];
+                            if (a.base) {
+                                float o[V];
+                                unpack<T>(g[j][v][i][w], o);
+#pragma unroll
+                                for (int e = 0; e < V; ++e) f[e] += o[e];
+                            }
+                            if (FULL || ((wm * RT + i) * 32 + m < rows && c + V * w < cols)) *(uint4*)((T*)a.y + row[i] * a.y_ld + col0 + c + V * w) = pack<T>(f);
                         }
                 }
-                float b8[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) b8[e] = bias[c + e];
-#pragma unroll
-                for (int i = 0; i < RT; ++i)
-#pragma unroll
-                    for (int w = 0; w < P; ++w) {
-                        float f[V];
-#pragma unroll
-                        for (int e = 0; e < V; ++e) f[e] = acc[i][j][8 * v + V * w + e] + b8[V * w + e];
-                        if (a.base) {
-                            float o[V];
-                            unpack<T>(g[i][w], o);
-#pragma unroll
-                            for (int e = 0; e < V; ++e) f[e] += o[e];
-                        }
-                        if ((wm * RT + i) * 32 + m < rows && c + V * w < cols) *(uint4*)((T*)a.y + at[i] + c + V * w) = pack<T>(f);
-                    }
-            }
+        }
     }
 
     // Tiles 0, 1 of a wave are values, 2, 3 their gates; a block of 128 output channels is the workgroup's, so that a row's scale is the
@@ -359,16 +400,30 @@ __global__ __launch_bounds__(256, WGS) void rows8_tile_kernel(Linear8Args a)
     const int rows = rows8_effective(a.rows), id = blockIdx.x;
     const int nx = (a.Cout + Tile::OUT - 1) / Tile::OUT, my = (rows + Tile::BM - 1) / Tile::BM, n = nx * my;
     const int over = n % COMPUTE_UNITS, whole = HALVES && n > COMPUTE_UNITS && over <= COMPUTE_UNITS / 2 ? n - over : n;
-    int row, col;
+    constexpr bool ONCE = HALVES || WGS > 1;                  // (else the grid is the chip at most, and a workgroup goes from tile to tile)
     if (id < whole) {
-        tile_place(xcd_run(id, whole), nx, my, row, col);
-        Tile::run(a, tile_lds, rows, row * Tile::BM, col * Tile::OUT);
+        int turn = 0;
+        Tile::template run<ONCE>(a, tile_lds, rows, [&](int& row0, int& col0) {
+            const int i = id + turn++ * (int)gridDim.x;
+            if (i >= whole) return false;
+            int row, col;
+            tile_place(xcd_run(i, whole), nx, my, row, col);
+            row0 = row * Tile::BM;
+            col0 = col * Tile::OUT;
+            return true;
+        });
     } else if constexpr (HALVES) {
-        if (id >= 2 * n - whole) return;
+        if (id >= whole + 2 * (n - whole)) return;
         const int half = xcd_run(id - whole, 2 * (n - whole));
+        int row, col;
         tile_place(whole + half / 2, nx, my, row, col);
-        const int row0 = row * Tile::BM + (half & 1) * (Tile::BM / 2);
-        if (row0 < rows) Tile8<T, GATED, RT / 2, CT, NS>::run(a, tile_lds, rows, row0, col * Tile::OUT);
+        const int first = row * Tile::BM + (half & 1) * (Tile::BM / 2);
+        if (first >= rows) return;
+        Tile8<T, GATED, RT / 2, CT, NS>::template run<true>(a, tile_lds, rows, [&](int& row0, int& col0) {
+            row0 = first;
+            col0 = col * Tile::OUT;
+            return true;
+        });
     }
 }
 
@@ -386,7 +441,7 @@ inline int launch_tiles(const char* who, const Linear8Args& a, int rows, hipStre
         SIGE_REQUIRE(e == hipSuccess, SIGE_ERR_HIP, "%s: %s", who, hipGetErrorString(e));
         room = true;
     }
-    hipLaunchKernelGGL(kern, dim3((unsigned)(n + (HALVES ? COMPUTE_UNITS / 2 : 0))), dim3(256), Tile::LDS, st, a);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(HALVES ? n + COMPUTE_UNITS / 2 : WGS > 1 || n < COMPUTE_UNITS ? n : COMPUTE_UNITS)), dim3(256), Tile::LDS, st, a);
     SIGE_LAUNCH_CHECK(who);
     return SIGE_OK;
 }
