@@ -178,7 +178,8 @@ __global__ __launch_bounds__(512) void rows8_few_kernel(Linear8Args a)
             most[i] = 0.0f;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                acc[i][0][e] = real ? gate_value(acc[i][0][e] + bu[e], acc[i][1][e] + bg[e], a.gate) : 0.0f;
+                const float u = real ? acc[i][0][e] + bu[e] : 0.0f, g = real ? acc[i][1][e] + bg[e] : 0.0f;
+                acc[i][0][e] = a.gate == SIGE_GATE_GELU ? gate_value<SIGE_GATE_GELU>(u, g) : gate_value<SIGE_GATE_SILU>(u, g);
                 most[i] = fmaxf(most[i], finite_or_0(acc[i][0][e]));
             }
             most[i] = fmaxf(most[i], __shfl_xor(most[i], 16));

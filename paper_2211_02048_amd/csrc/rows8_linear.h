@@ -49,13 +49,15 @@ __device__ __forceinline__ float finite_or_0(float f)
     return m < __uint_as_float(0x7f800000u) ? m : 0.0f;
 }
 
-// The gated activation: u * gelu(g) or u * silu(g).  gelu(g) = max(g, 0) - z erfc(z / sqrt 2) / 2 with z = |g|, which holds far below zero too, and
+// The gated activation: u * gelu(g) or u * silu(g).  (Chosen per call, not per value: a choice between every two values keeps their chains from
+// overlapping.)  gelu(g) = max(g, 0) - z erfc(z / sqrt 2) / 2 with z = |g|, which holds far below zero too, and
 // erfc(z / sqrt 2) / 2 = t R(t) exp(-z^2 / 2) with t = 1 / (1 + z / 5): R is the polynomial of degree 6 whose largest relative
 // error over 0 <= z <= 14 is smallest (1.2e-6; fitted by linear programming to values in 64 bits; with fp32 arithmetic 1.7e-6).  The
 // library's functions took five times as long as this: 23 us behind a tile of 256 x 256.
-__device__ __forceinline__ float gate_value(float u, float g, int gate)
+template <int GATE>
+__device__ __forceinline__ float gate_value(float u, float g)
 {
-    if (gate == SIGE_GATE_SILU) return u * (g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f)));
+    if constexpr (GATE == SIGE_GATE_SILU) return u * (g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(g * -1.4426950408889634f)));
     const float z = fabsf(g), t = __builtin_amdgcn_rcpf(fmaf(z, 0.2f, 1.0f));
     float r = fmaf(0.27912187576293945f, t, -0.3869353234767914f);
     r = fmaf(r, t, 0.4471128284931183f);

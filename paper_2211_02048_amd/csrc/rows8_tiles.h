@@ -124,10 +124,8 @@ struct Tile8 {
                     for (int i = 0; i < REQ; ++i) request(b, b * STAGE, i);
                 }
             t.bias = 0.0f;
-            if (a.bias && (int)threadIdx.x < BN) {
-                const int c = (int)threadIdx.x % OUT;
-                t.bias = a.bias[((int)threadIdx.x < OUT ? 0 : a.Cout) + col0 + (c < t.cols ? c : t.cols - 1)];
-            }
+            const int c = (int)threadIdx.x % OUT;
+            if (a.bias && (int)threadIdx.x < BN && c < t.cols) t.bias = a.bias[((int)threadIdx.x < OUT ? 0 : a.Cout) + col0 + c];
         };
         constexpr auto wait = [](int vm, int lgkm) { return (vm & 15) | 0x70 | lgkm << 8 | (vm >> 4) << 14; };
         const auto barrier = [] {
@@ -302,6 +300,34 @@ struct Tile8 {
         }
     }
 
+    // acc[i][t] becomes the gated value of tile t and its gates, most[i] the largest magnitude of a lane's row of tile i.
+    template <int GATE>
+    static __device__ __forceinline__ void gate_values(const float* bias, f32x16 (&acc)[RT][CT], float (&most)[RT], int h, int wn)
+    {
+#pragma unroll
+        for (int i = 0; i < RT; ++i) most[i] = 0.0f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int v = 0; v < 16; v += 8) {
+                const int c = wn * 64 + 32 * h + 16 * t + v;
+                float bu[8], bg[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) { bu[e] = bias[c + e]; bg[e] = bias[OUT + c + e]; }
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float f = gate_value<GATE>(acc[i][t][v + e] + bu[e], acc[i][t + CT / 2][v + e] + bg[e]);
+                        acc[i][t][v + e] = f;
+                        most[i] = fmaxf(most[i], fabsf(f));
+                    }
+                    if constexpr (RT > 1) __builtin_amdgcn_sched_barrier(0);     // (eight chains overlap; more of them do not fit the registers)
+                }
+            }
+        }
+    }
+
     // Tiles 0, 1 of a wave are values, 2, 3 their gates; a block of 128 output channels is the workgroup's, so that a row's scale is the
     // maximum over two waves.
     static __device__ __forceinline__ void gated(const Linear8Args& a, unsigned char* lds, f32x16 (&acc)[RT][CT], int row0, int col0, int rows, int cols, int lane,
@@ -312,29 +338,19 @@ struct Tile8 {
         const float* bias = (const float*)lds;               // [128] of values, [128] of gates
         float* top = (float*)lds + BN;                       // [2][BM]
         float most[RT];
+        if (cols != OUT) {                                   // channels that are not there (in eights: Cout is a multiple): 0, as is their bias
 #pragma unroll
-        for (int i = 0; i < RT; ++i) most[i] = 0.0f;
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const int c = wn * 64 + 32 * h + 16 * t;
-            // (Cout is a multiple of 8)
+                for (int v = 0; v < 16; v += 8)
+                    if (wn * 64 + 32 * h + 16 * t + v >= cols)
 #pragma unroll
-            for (int v = 0; v < 16; v += 8) {
-                const bool real = c + v < cols;
-                float bu[8], bg[8];
+                        for (int i = 0; i < RT; ++i)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) { bu[e] = bias[c + v + e]; bg[e] = bias[OUT + c + v + e]; }
-#pragma unroll
-                for (int i = 0; i < RT; ++i) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float f = real ? gate_value(acc[i][t][v + e] + bu[e], acc[i][t + CT / 2][v + e] + bg[e], a.gate) : 0.0f;
-                        acc[i][t][v + e] = f;
-                        most[i] = fmaxf(most[i], fabsf(f));
-                    }
-                }
-            }
+                            for (int e = 0; e < 8; ++e) acc[i][t][v + e] = acc[i][t + CT / 2][v + e] = 0.0f;
         }
+        if (a.gate == SIGE_GATE_GELU) gate_values<SIGE_GATE_GELU>(bias, acc, most, h, wn);
+        else gate_values<SIGE_GATE_SILU>(bias, acc, most, h, wn);
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
             if (most[i] == __uint_as_float(0x7f800000u)) {       // (a NaN is passed over by the maximum, an infinity has to be)
@@ -375,13 +391,15 @@ struct Tile8 {
     }
 };
 
-// Number `t` of tiles of my x nx: the tiles that are worked on at a time lie in strips of 8 tiles of rows, so that the workgroups of an XCD share
-// both operands in its L2.
+// Number t of the my x nx tiles, in strips of five tiles of rows: the workgroups of an XCD, 32 tiles at a time, share both operands in its L2.  (Not in
+// eights: rows whose distance is a power of two then ask the same channels of the memory at the same time; gated 4096 x 2560 -> 2 x 10240 by
+// tiles of 256 and of 64 rows 220 and 371 us in strips of eight, 211 and 308 in strips of five, 212 and 323 of three.)
 __device__ __forceinline__ void tile_place(int t, int nx, int my, int& row, int& col)
 {
-    const int g = t / (8 * nx), rem = t - g * 8 * nx, high = my - g * 8 < 8 ? my - g * 8 : 8;
+    constexpr int STRIP = 5;
+    const int g = t / (STRIP * nx), rem = t - g * STRIP * nx, high = my - g * STRIP < STRIP ? my - g * STRIP : STRIP;
     col = rem / high;
-    row = g * 8 + rem - col * high;
+    row = g * STRIP + rem - col * high;
 }
 
 // The workgroup's number among n, so that each XCD (workgroups go to the eight in turn) has a run of them.
