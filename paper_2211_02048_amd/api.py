@@ -819,8 +819,7 @@ def rows8_lds(C):
 
 def rows8(rows, C, device="cuda"):
     """Room for `rows` rows of C channels in 8 bits: codes and scales."""
-    ld, sld = rows8_lds(C)
-    return torch.empty((rows, ld), dtype=torch.uint8, device=device), torch.empty((rows, sld), dtype=torch.uint8, device=device)
+    return (torch.empty((rows, C + 127 & -128), dtype=_U8, device=device), torch.empty((rows, (C + 511 & -512) >> 7), dtype=_U8, device=device))
 
 
 _U8 = torch.uint8
@@ -828,7 +827,7 @@ _U8 = torch.uint8
 
 def _rows8(what, q, scales, rows, C):
     """Row strides of a matrix in 8 bits, [rows or more, codes] and [rows or more, scale bytes]."""
-    ld, sld = rows8_lds(C)
+    ld, sld = C + 127 & -128, (C + 511 & -512) >> 7
     if q.dtype is not _U8 or scales.dtype is not _U8:
         raise SigeError(1, f"{what}: codes and scales are {_U8}, not {q.dtype} and {scales.dtype}")
     (a, b), (c, d) = q.stride(), scales.stride()
@@ -844,10 +843,12 @@ def _rows8(what, q, scales, rows, C):
 
 def _row_count(x, n_rows, max_rows, count):
     """The most rows that a call may have, and those that it may touch."""
-    mr = x.numel() // max(x.shape[-1], 1) if max_rows is None else max_rows
+    if max_rows is None:
+        sh = x.shape
+        max_rows = sh[0] if len(sh) == 2 else x.numel() // max(sh[-1], 1)
     if count is not None:
         _table("count", count, _I32, 1)
-    return mr, mr if n_rows < 0 else n_rows
+    return max_rows, max_rows if n_rows < 0 else n_rows
 
 
 def sige_rows8_store(x, q, scales, C, *, n_rows=-1, count=None, rows_per_count=0, max_rows=None, x_ld=None):

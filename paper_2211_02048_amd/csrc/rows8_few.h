@@ -219,13 +219,8 @@ inline int launch_few(const char* who, const Linear8Args& a, int rows, int most_
     const dim3 grid((a.Cout + (GATED ? 127 : 16 * CT - 1)) / (GATED ? 128 : 16 * CT), (rows + 16 * RT - 1) / (16 * RT));
     SIGE_REQUIRE(grid.y < 65536, SIGE_ERR_UNSUPPORTED, "%s: too many rows", who);
     const auto kern = rows8_few_kernel<T, GATED, RT, CT, NBUF>;
-    static thread_local bool room = false;                    // (the attribute is a kernel's, the same whatever the call)
-    if (!room) {
-        hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-        SIGE_REQUIRE(e == hipSuccess, SIGE_ERR_HIP, "%s: %s", who, hipGetErrorString(e));
-        room = true;
-    }
     const int words = (a.blocks + 3) / 4, waves = GATED ? 8 : words < most_waves ? words : most_waves;
+    if (int rc = allow_lds(who, (const void*)kern, waves * S::WAVE)) return rc;
     hipLaunchKernelGGL(kern, grid, dim3(waves * 64), waves * S::WAVE, st, a);
     SIGE_LAUNCH_CHECK(who);
     return SIGE_OK;

@@ -27,8 +27,16 @@ struct Linear8Args {
     int blocks;                 // of 128 input channels
     int Cout, x_ld, xs_ld, w_ld, ws_ld, base_ld, y_ld, q_ld, s_ld;
     int gate;
-    int whole;                  // tiles that are not cut in half (tile kernel)
 };
+
+// Lets a kernel have more LDS than 48 KB (one limit whatever the call, so that calls from two threads do not undo each other's).
+inline int allow_lds(const char* who, const void* kern, int bytes)
+{
+    if (bytes <= 48 * 1024) return SIGE_OK;
+    const hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+    SIGE_REQUIRE(e == hipSuccess, SIGE_ERR_HIP, "%s: cannot reserve %d bytes of LDS: %s", who, bytes, hipGetErrorString(e));
+    return SIGE_OK;
+}
 
 __device__ __forceinline__ i32x8 both(i32x4 a, i32x4 b) { return i32x8{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}; }
 

@@ -6,9 +6,11 @@
 
 namespace sige {
 
-// What a form takes, in microseconds, by a model of measured calls (360 calls over the ranges 1 to 8192 rows and 16 to 8192 channels, replayed from a
-// graph with inputs that change: off by 6 to 14 %): start + rounds of workgroups over the chip * (tile + block * blocks of 128 channels that
-// a wave goes through).  The few-row kernel's workgroups are small and many: its time goes by blocks and tiles in all.
+// What a form takes, in microseconds, by a model fitted to measured calls (620 calls of 1 to 8192 rows and 16 to 8192 channels, drawn evenly over the
+// logarithms, every form of each replayed from a graph with inputs that change; off by 5 to 10 %): start + rounds of workgroups over the chip
+// * (tile + block * blocks of 128 channels that a wave goes through).  The few-row kernel's workgroups are small and many: its time goes by the blocks of
+// a wave, and by blocks and tiles in all.  The form that the model takes costs 0.8 % more than the fastest of the call in the mean (gated 0.2 %), one
+// call in sixteen over 5 %, 26 % at most.
 struct Linear8Cost {
     int rows, cols, slots, shares;
     float start, tile, block;
@@ -16,8 +18,8 @@ struct Linear8Cost {
 
 static float linear8_cost(const Linear8Cost& c, int rows, int cols, int blocks)
 {
-    const float tiles = (float)((rows + c.rows - 1) / c.rows) * (float)((cols + c.cols - 1) / c.cols), units = tiles / COMPUTE_UNITS;
-    float rounds = std::ceil(units / c.slots);
+    const float units = (float)((rows + c.rows - 1) / c.rows) * (float)((cols + c.cols - 1) / c.cols) / COMPUTE_UNITS;
+    float rounds = std::ceil(units);
     if (c.slots == 2) rounds = units <= 1.0f ? 0.62f : units <= 2.0f ? 1.0f : units / 2.0f;     // (one workgroup by itself has the compute unit's time)
     if (c.rows == 256) {
         const float whole = std::floor(units), over = units - whole;
@@ -28,21 +30,20 @@ static float linear8_cost(const Linear8Cost& c, int rows, int cols, int blocks)
 
 static float linear8_few_cost(bool exact, int rows, int cols, int blocks)
 {
-    const int words = (blocks + 3) / 4, waves = words < 8 ? words : 8, fit = 160 * 1024 / (waves * Few8<false, 1, 1, 2>::WAVE), slots = fit < 32 / waves ? fit : 32 / waves;
+    const int words = (blocks + 3) / 4, waves = words < 8 ? words : 8;
     const float units = (float)((rows + 15) / 16) * (float)((cols + 15) / 16) / COMPUTE_UNITS, steps = (float)(4 * ((words + waves - 1) / waves));
-    const float more = units / (float)slots > 1.0f ? units / (float)slots - 1.0f : 0.0f;
-    return exact ? 1.04f + 0.489f * steps + 0.057f * units * (float)blocks + 0.112f * units
-                 : 1.24f + 0.379f * steps + 0.053f * units * (float)blocks + 0.079f * units + 0.488f * more;
+    return exact ? 1.23f + 0.435f * steps + 0.064f * units * (float)blocks + 0.105f * units
+                 : 1.54f + 0.315f * steps + 0.066f * units * (float)blocks + 0.027f * units;
 }
 
 // The form with the smallest cost that can take the call: the kernels for tiles have 32-bit offsets into a tile's rows.
 static int linear8_form(const Linear8Args& a, int rows, bool exact)
 {
-    static const Linear8Cost half[LINEAR8_FORMS] = {{}, {32, 32, 1, 4, 1.32f, 1.38f, 0.352f}, {32, 64, 1, 4, 1.23f, 1.63f, 0.520f}, {64, 64, 1, 4, 0.84f, 2.41f, 0.679f},
-                                                   {128, 64, 2, 1, 0.92f, 2.97f, 0.512f}, {128, 128, 2, 1, 0.19f, 4.63f, 0.731f}, {128, 128, 1, 1, 0.0f, 3.50f, 0.402f},
-                                                   {256, 256, 1, 1, 0.0f, 6.44f, 0.973f}};
-    static const Linear8Cost single[LINEAR8_FORMS] = {{}, {32, 32, 1, 4, 1.27f, 1.58f, 0.525f}, {32, 64, 1, 4, 1.20f, 2.10f, 0.750f}, {64, 64, 1, 4, 0.32f, 3.22f, 1.024f},
-                                                     {128, 64, 2, 1, 0.0f, 4.96f, 0.858f}, {128, 128, 2, 1, 0.0f, 6.32f, 1.240f}, {128, 128, 1, 1, 0.0f, 4.25f, 0.776f}, {}};
+    static const Linear8Cost half[LINEAR8_FORMS] = {{}, {32, 32, 1, 4, 1.28f, 1.49f, 0.347f}, {32, 64, 1, 4, 0.99f, 1.87f, 0.523f}, {64, 64, 1, 4, 0.48f, 2.75f, 0.726f},
+                                                   {128, 64, 2, 1, 0.63f, 3.50f, 0.553f}, {128, 128, 2, 1, 0.0f, 5.17f, 0.838f}, {128, 128, 1, 1, 0.57f, 3.32f, 0.444f},
+                                                   {256, 256, 1, 1, 0.0f, 8.73f, 1.057f}};
+    static const Linear8Cost single[LINEAR8_FORMS] = {{}, {32, 32, 1, 4, 1.16f, 1.71f, 0.509f}, {32, 64, 1, 4, 0.93f, 2.10f, 0.737f}, {64, 64, 1, 4, 0.0f, 3.47f, 1.080f},
+                                                     {128, 64, 2, 1, 0.0f, 4.89f, 0.970f}, {128, 128, 2, 1, 0.0f, 6.13f, 1.397f}, {128, 128, 1, 1, 0.0f, 4.57f, 0.880f}, {}};
     const int set = knob(SIGE_KNOB_ROWS8_FORM);
     const bool offsets = a.x_ld < (1 << 22) && a.w_ld < (1 << 22);
     if (set >= 0 && (set < LINEAR8_TILE_128X64 || offsets)) return set;
@@ -58,8 +59,8 @@ static int linear8_form(const Linear8Args& a, int rows, bool exact)
 
 static int linear8_gated_form(const Linear8Args& a, int rows)
 {
-    static const Linear8Cost cost[GATED8_FORMS] = {{16, 128, 1, 1, 1.15f, 2.56f, 0.389f}, {64, 128, 1, 1, 0.70f, 5.32f, 0.468f}, {128, 128, 1, 1, 0.0f, 8.59f, 0.648f},
-                                                  {256, 128, 1, 1, 0.0f, 15.83f, 0.967f}};
+    static const Linear8Cost cost[GATED8_FORMS] = {{16, 128, 1, 1, 0.84f, 2.91f, 0.374f}, {64, 128, 1, 1, 1.68f, 3.61f, 0.457f}, {128, 128, 1, 1, 1.22f, 6.22f, 0.653f},
+                                                  {256, 128, 1, 1, 0.0f, 11.55f, 1.034f}};
     const int set = knob(SIGE_KNOB_ROWS8_FORM);
     const bool offsets = a.x_ld < (1 << 22) && 2L * a.Cout * a.w_ld < (1L << 31);
     if (set >= 0 && (set < GATED8_TILE_64 || offsets)) return set;
@@ -112,6 +113,7 @@ extern "C" int sige_rows8_linear(const void* x, int32_t x_ld, const void* x_scal
     if (rows == 0) return SIGE_OK;
     SIGE_REQUIRE(y, SIGE_ERR_INVALID_ARG, "%s: y is required", who);
     SIGE_REQUIRE(aligned16(y) && aligned16(base), SIGE_ERR_UNSUPPORTED, "%s: y and base must be 16-byte aligned", who);
+    SIGE_REQUIRE(y != x && y != w, SIGE_ERR_INVALID_ARG, "%s: y may be neither x nor w", who);
     a.base = base; a.base_ld = base_ld; a.y = y; a.y_ld = y_ld;
     hipStream_t st = (hipStream_t)stream;
     const int form = linear8_form(a, rows, dt == SIGE_F32);
@@ -132,7 +134,7 @@ extern "C" int sige_rows8_linear_gated(const void* x, int32_t x_ld, const void* 
         return rc;
     SIGE_REQUIRE(Cout % 8 == 0, SIGE_ERR_UNSUPPORTED, "%s: Cout must be a multiple of 8", who);
     if (int rc = rows8_check_matrix(who, "the output", q, q_ld, scales, s_ld, Cout, rows > 0)) return rc;
-    SIGE_REQUIRE(rows == 0 || (q != x && scales != x_scales), SIGE_ERR_INVALID_ARG, "%s: the output may not be x", who);
+    SIGE_REQUIRE(rows == 0 || (q != x && scales != x_scales && q != w && scales != w_scales), SIGE_ERR_INVALID_ARG, "%s: the output may be neither x nor w", who);
     if (rows == 0) return SIGE_OK;
     a.gate = gate; a.q = (unsigned char*)q; a.q_ld = q_ld; a.s = (unsigned char*)scales; a.s_ld = s_ld;
     return linear8_gated(who, a, rows, linear8_gated_form(a, rows), (hipStream_t)stream);

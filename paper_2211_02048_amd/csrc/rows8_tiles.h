@@ -453,12 +453,7 @@ inline int launch_tiles(const char* who, const Linear8Args& a, int rows, hipStre
     const long n = (long)((a.Cout + Tile::OUT - 1) / Tile::OUT) * ((rows + Tile::BM - 1) / Tile::BM);
     SIGE_REQUIRE(n < (1L << 23), SIGE_ERR_UNSUPPORTED, "%s: too many rows and channels", who);
     const auto kern = rows8_tile_kernel<T, GATED, RT, CT, NS, WGS, HALVES>;
-    static thread_local bool room = false;                    // (the attribute is a kernel's, the same whatever the call)
-    if (!room) {
-        hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-        SIGE_REQUIRE(e == hipSuccess, SIGE_ERR_HIP, "%s: %s", who, hipGetErrorString(e));
-        room = true;
-    }
+    if (int rc = allow_lds(who, (const void*)kern, Tile::LDS)) return rc;
     hipLaunchKernelGGL(kern, dim3((unsigned)(HALVES ? n + COMPUTE_UNITS / 2 : WGS > 1 || n < COMPUTE_UNITS ? n : COMPUTE_UNITS)), dim3(256), Tile::LDS, st, a);
     SIGE_LAUNCH_CHECK(who);
     return SIGE_OK;

@@ -153,12 +153,7 @@ inline int launch_waves(const char* who, const Linear8Args& a, int rows, hipStre
     const long n = (long)((a.Cout + 32 * CT - 1) / (32 * CT)) * ((rows + 32 * RT - 1) / (32 * RT));
     SIGE_REQUIRE(n < (1L << 22), SIGE_ERR_UNSUPPORTED, "%s: too many rows and channels", who);
     const auto kern = rows8_waves_kernel<T, RT, CT, NBUF, WAVES>;
-    static thread_local bool room = false;                    // (the attribute is a kernel's, the same whatever the call)
-    if (!room) {
-        hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-        SIGE_REQUIRE(e == hipSuccess, SIGE_ERR_HIP, "%s: %s", who, hipGetErrorString(e));
-        room = true;
-    }
+    if (int rc = allow_lds(who, (const void*)kern, LDS)) return rc;
     hipLaunchKernelGGL(kern, dim3((unsigned)n), dim3(64 * WAVES), LDS, st, a);
     SIGE_LAUNCH_CHECK(who);
     return SIGE_OK;
