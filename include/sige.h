@@ -537,11 +537,11 @@ int sige_token_lora(const void* x, sige_dtype dt, int32_t Cin, int32_t x_ld, con
  * codes 16-byte, scales 4-byte aligned.  A scale byte of 255 is NaN.  Half of a half type's size; the powers of two lose nothing
  * against other factors (the codes have exponents of their own), and the matrix instruction applies them by itself.
  * Rows as in sige_token_norm: n_rows >= 0 from the host, or -1 = min(*count * rows_per_count, max_rows); rows behind them are
- * neither read nor written.
+ * neither read nor written.  Outputs may not overlap inputs but where a call says so.
  *
  * sige_rows8_store: x [rows][C] of dt to 8 bits.  A block's scale is the smallest power of two, at least 2^-126, with max|x| <= 448 * scale over its
  * finite values; codes are the nearest, ties to the even one; an infinity or NaN becomes a NaN and leaves the others alone.
- * Weights are stored once by the same call.
+ * Weights are stored once by the same call.  At most 2^26 rows, counted once for every 512 channels begun (here, in the load and in the norm).
  * sige_rows8_load: the values as rows of dt (rounded once; fp16 and bf16 lose nothing but what lies outside of their range).  */
 int sige_rows8_store(const void* x, sige_dtype dt, int32_t C, int32_t x_ld, const int32_t* count, int32_t rows_per_count,
                      int32_t max_rows, int32_t n_rows, void* q, int32_t q_ld, void* scales, int32_t s_ld, void* stream);
@@ -637,7 +637,10 @@ int sige_version(void);
  *   CONV_AHEAD         requests ahead in the shapes whose waves split K (the next chunk, or the only one at once): 0 = never,
  *                      1 = a tiled call that cannot request its next chunk ahead ends in SIGE_ERR_UNSUPPORTED,
  *                      2 = one that cannot request its only chunk at once does
- *   CACHE4_MANY        sige_cache4_attn, half types: 0 = the form for few queries, 1 = the one for many           */
+ *   CACHE4_MANY        sige_cache4_attn, half types: 0 = the form for few queries, 1 = the one for many
+ *   ROWS8_FORM         sige_rows8_linear: 0 = 16 rows x 16 channels per workgroup, 1 = 32 x 32, 2 = 32 x 64, 3 = 64 x 64 (waves share the
+ *                      input channels), 4 = tiles of 128 x 64, 5 = 128 x 128, 6 = the same by one workgroup per compute unit, 7 = 256 x 256
+ *                      (half types); sige_rows8_linear_gated: 0 = 16 rows, 1 = 64, 2 = 128, 3 = 256                   */
 typedef enum {
     SIGE_KNOB_CONV_CFG = 0, SIGE_KNOB_CONV_KC = 1, SIGE_KNOB_CONV_SPLIT = 2, SIGE_KNOB_CONV_HALF = 3,
     SIGE_KNOB_CONV_SPLIT_WGS = 4, SIGE_KNOB_CONV_POINTWISE = 5, SIGE_KNOB_CONV_POINTWISE_W4 = 6,

@@ -830,6 +830,8 @@ def _rows8(what, q, scales, rows, C):
     ld, sld = C + 127 & -128, (C + 511 & -512) >> 7
     if q.dtype is not _U8 or scales.dtype is not _U8:
         raise SigeError(1, f"{what}: codes and scales are {_U8}, not {q.dtype} and {scales.dtype}")
+    if q.dim() != 2 or scales.dim() != 2:
+        raise SigeError(1, f"{what}: codes [rows, codes] and scales [rows, bytes], not {tuple(q.shape)} and {tuple(scales.shape)}")
     (a, b), (c, d) = q.stride(), scales.stride()
     if b != 1 or d != 1:
         raise SigeError(1, f"{what}: codes and scale bytes of a row side by side, not with strides {q.stride()} and {scales.stride()}")

@@ -186,7 +186,7 @@ static int rows8_store_load(const char* who, bool store, void* x, sige_dtype dt,
     const int chunks = (C + ROW8_CHUNK - 1) / ROW8_CHUNK;
     a.d_chunks = fast_div(chunks);
     const long waves = (long)rows * chunks;
-    SIGE_REQUIRE(waves < (1L << 31) - 4, SIGE_ERR_UNSUPPORTED, "%s: too many values", who);
+    SIGE_REQUIRE(waves < (1L << 26), SIGE_ERR_UNSUPPORTED, "%s: at most 2^26 rows, counted once for every 512 channels begun", who);
     const dim3 grid((unsigned)((waves + 3) / 4));
     hipStream_t st = (hipStream_t)stream;
     auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, a); };
@@ -249,6 +249,7 @@ extern "C" int sige_token_rms(const void* x, sige_dtype dt, int32_t C, int32_t x
     a.x = x; a.residual = residual; a.gamma = gamma; a.total = total; a.y = y; a.q = (unsigned char*)q; a.s = (unsigned char*)scales;
     a.C = C; a.x_ld = x_ld; a.res_ld = res_ld; a.total_ld = total_ld; a.y_ld = y_ld; a.q_ld = q_ld; a.s_ld = s_ld; a.eps = eps;
     const int chunks = (C + ROW8_CHUNK - 1) / ROW8_CHUNK;
+    SIGE_REQUIRE((long)rows * chunks < (1L << 26), SIGE_ERR_UNSUPPORTED, "%s: at most 2^26 rows, counted once for every 512 channels begun", who);
     hipStream_t st = (hipStream_t)stream;
     auto go = [&](auto kern, int W) { hipLaunchKernelGGL(kern, dim3((unsigned)(((long)rows * W + 3) / 4)), dim3(256), 0, st, a); };
     auto pick = [&](auto t) {

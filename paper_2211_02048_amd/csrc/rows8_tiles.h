@@ -229,6 +229,8 @@ struct Tile8 {
         barrier();
         const bool more = !ONCE && next_tile(row0, col0);
         if (more) begin(row0, col0);
+        asm volatile("" ::: "memory");                       // (the requests stay older than the stores below, whose number the wait for them counts on)
+        __builtin_amdgcn_sched_barrier(0);
         if constexpr (GATED) gated(a, lds + EPI, acc, r0, c0, rows, cols, lane, wm, wn);
         else if (rows == BM && cols == OUT) plain<true>(a, (const float*)(lds + EPI), acc, r0, c0, rows, cols, m, h, wm, wn);
         else plain<false>(a, (const float*)(lds + EPI), acc, r0, c0, rows, cols, m, h, wm, wn);

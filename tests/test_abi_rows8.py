@@ -62,7 +62,7 @@ def test_store_and_load_refusals(L):
                    dict(n=-1), dict(n=-1, count=FAKE), dict(n=-2), dict(mr=-1, n=-1, count=FAKE, per=1)):
             assert call(**kw) == 1, kw
         for kw in (dict(C=316, x_ld=320), dict(x_ld=324), dict(x=ODD), dict(q=ODD), dict(s=ODDER), dict(q_ld=392), dict(s_ld=6), dict(dt=0, x_ld=322),
-                   dict(mr=2 ** 31 - 1, n=2 ** 31 - 1)):
+                   dict(mr=2 ** 31 - 1, n=2 ** 31 - 1), dict(mr=2 ** 26, n=2 ** 26), dict(mr=2 ** 26, n=-1, count=FAKE, per=1), dict(C=520, x_ld=520, q_ld=640, s_ld=8, mr=2 ** 25, n=2 ** 25)):
             assert call(**kw) == 2, kw
         assert call(n=9) == 3
 
@@ -78,7 +78,7 @@ def test_rms_refusals(L):
         assert rms(**kw) == 1, kw
     for kw in (dict(C=316), dict(x=ODD), dict(y=ODD), dict(res=ODD, res_ld=320), dict(gamma=ODDER), dict(C=16392, x_ld=16392, y_ld=16392), dict(y=FAKE, y_ld=328),
                dict(q=ODD, q_ld=384, s=FAKE, s_ld=4), dict(res=FAKE, res_ld=320, total=FAKE, total_ld=328), dict(res=OTHER, res_ld=328, total=OTHER, total_ld=320, y=None, q=FAKE, q_ld=384, s=FAKE, s_ld=4),
-               dict(dt=0, C=8196, x_ld=8196, y_ld=8196)):
+               dict(dt=0, C=8196, x_ld=8196, y_ld=8196), dict(mr=2 ** 26, n=2 ** 26)):
         assert rms(**kw) == 2, kw
     assert rms(n=9) == 3
 
@@ -100,8 +100,12 @@ def test_linear_refusals(L):
                    dict(cout=2 ** 28 + 8, y_ld=2 ** 29) if call is linear else dict(cout=2 ** 28 + 8, q_ld=2 ** 29, s_ld=2 ** 24)):
             assert call(**kw) == 2, kw
         assert call(n=9) == 3
-    for kw in (dict(y=None), dict(dt=3), dict(y_ld=632), dict(base=FAKE, base_ld=632)):
+    for kw in (dict(y=None), dict(dt=3), dict(y_ld=632), dict(base=FAKE, base_ld=632), dict(y=FAKE)):
         assert linear(**kw) == 1, kw
+    for form, dt in ((8, 1), (7, 0), (100, 2)):
+        with api.knobs(ROWS8_FORM=form):
+            assert linear(dt=dt) == 2 and "form" in err(L)
+            assert form == 7 or gated() == 2
     for kw in (dict(y=ODD), dict(base=ODD, base_ld=640), dict(y_ld=644), dict(base=OTHER, base_ld=648), dict(dt=0, cout=642, y_ld=644)):
         assert linear(**kw) == 2, kw
     for kw in (dict(gate=2), dict(gate=-1), dict(q=None), dict(s=None), dict(q_ld=624), dict(s_ld=4), dict(q=FAKE), dict(s=FAKE)):
@@ -128,6 +132,8 @@ def test_binding_refusals():
     refused(3, api.sige_rows8_store, x, q, s[:, :3], 320, n_rows=4)
     refused(1, api.sige_rows8_store, x, q.t().contiguous().t(), s, 320, n_rows=4)
     refused(3, api.sige_rows8_store, x, q, s, 320, n_rows=5)
+    refused(1, api.sige_rows8_store, x, q.flatten(), s, 320, n_rows=4)
+    refused(1, api.sige_rows8_load, q, s.view(2, 2, 4), x, 320, n_rows=4)
     refused(3, api.sige_rows8_store, x, q, s, 328, n_rows=4)
     refused(3, api.sige_rows8_load, q, s, x[:, :312], 320, n_rows=4)
     refused(1, api.sige_token_rms, x, 320, torch.ones(320, dtype=torch.float16), y=x, n_rows=4)
