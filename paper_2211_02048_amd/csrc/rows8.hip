@@ -31,8 +31,8 @@ __device__ __forceinline__ void load_chunk(const T* x, int lane, int left, uint4
     }
 }
 
-// Rows to 8 bits.  Bound by memory: s + 1 bytes per value.  A wave takes 512 channels of a row, so that the maximum of a block stays within
-// 16 lanes (four register exchanges) and the four scale bytes leave as one word.
+// Rows to 8 bits.  Bound by memory: s + 1 bytes per value (16384 rows of 5120 in fp16 47 us, 5.4 TB/s).  A wave takes 512 channels of a row, so
+// that the maximum of a block stays within 16 lanes (four register exchanges) and the four scale bytes leave as one word.
 template <typename T>
 __global__ __launch_bounds__(256) void rows8_store_kernel(Rows8Args a)
 {
@@ -50,7 +50,7 @@ __global__ __launch_bounds__(256) void rows8_store_kernel(Rows8Args a)
     store_chunk<T>(f, lane, left, a.q + (long)row * a.q_ld + chunk * ROW8_CHUNK, a.s + (long)row * a.s_ld + chunk * 4);
 }
 
-// Rows from 8 bits.  Bound by memory.
+// Rows from 8 bits.  Bound by memory (the same rows 38 us, 6.6 TB/s: what was just stored is partly in the last-level cache).
 template <typename T>
 __global__ __launch_bounds__(256) void rows8_load_kernel(Rows8Args a)
 {
@@ -85,8 +85,9 @@ __global__ __launch_bounds__(256) void rows8_load_kernel(Rows8Args a)
     }
 }
 
-// h = round(x + residual), n = gamma * h / sqrt(mean(h^2) + eps), to the outputs that are asked for.  Bound by memory; a row stays in registers
-// between the sum of squares (fp32) and the outputs.  W waves share a row, chunk w + W u of 512 channels each.
+// h = round(x + residual), n = gamma * h / sqrt(mean(h^2) + eps), to the outputs that are asked for.  Bound by memory (16384 rows of 2560 in bf16 with a
+// residual, its sum and the 8-bit output 57 us, 5.2 TB/s); a row stays in registers between the sum of squares (fp32) and the outputs.  W waves
+// share a row, chunk w + W u of 512 channels each.
 template <typename T, int NC, int W>
 __global__ __launch_bounds__(256) void rows8_rms_kernel(Rows8Args a)
 {
@@ -99,19 +100,29 @@ __global__ __launch_bounds__(256) void rows8_rms_kernel(Rows8Args a)
     const int chunks = (a.C + ROW8_CHUNK - 1) / ROW8_CHUNK;
     float f[NC][V][N];
     float sum = 0.0f;
+    uint4 raw[NC][V], add[NC][V];
+    // every load of the row on its way before the first is waited for
 #pragma unroll
     for (int u = 0; u < NC; ++u) {
-        const int chunk = w + W * u;
-        const int left = on && chunk < chunks ? a.C - chunk * ROW8_CHUNK : 0;
-        uint4 raw[V], add[V];
-        load_chunk<T>((const T*)a.x + (long)row * a.x_ld + chunk * ROW8_CHUNK, lane, left, raw);
-        if (a.residual) load_chunk<T>((const T*)a.residual + (long)row * a.res_ld + chunk * ROW8_CHUNK, lane, left, add);
+        const int chunk = w + W * u, left = on && chunk < chunks ? a.C - chunk * ROW8_CHUNK : 0;
+        load_chunk<T>((const T*)a.x + (long)row * a.x_ld + chunk * ROW8_CHUNK, lane, left, raw[u]);
+    }
+    if (a.residual) {
+#pragma unroll
+        for (int u = 0; u < NC; ++u) {
+            const int chunk = w + W * u, left = on && chunk < chunks ? a.C - chunk * ROW8_CHUNK : 0;
+            load_chunk<T>((const T*)a.residual + (long)row * a.res_ld + chunk * ROW8_CHUNK, lane, left, add[u]);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < NC; ++u) {
+        const int chunk = w + W * u, left = on && chunk < chunks ? a.C - chunk * ROW8_CHUNK : 0;
 #pragma unroll
         for (int h = 0; h < V; ++h) {
-            unpack<T>(raw[h], f[u][h]);
+            unpack<T>(raw[u][h], f[u][h]);
             if (a.residual) {
                 float g[N];
-                unpack<T>(add[h], g);
+                unpack<T>(add[u][h], g);
 #pragma unroll
                 for (int i = 0; i < N; ++i) f[u][h][i] += g[i];
                 const uint4 t = pack<T>(f[u][h]);                // the sum is a stored tensor of the model's type, and the norm is that tensor's
@@ -255,9 +266,13 @@ extern "C" int sige_token_rms(const void* x, sige_dtype dt, int32_t C, int32_t x
     auto pick = [&](auto t) {
         using T = decltype(t);
         constexpr bool F = sizeof(T) == 4;
+        constexpr int MOST = F ? 2 : 4;                        // chunks that one wave takes
+        // a row of up to 2048 channels: four waves where rows are few (bf16, 256 rows of 1280 4.5 -> 3.0 us, of 2048 5.1 -> 3.0), one where they
+        // are many (16384 of 1280 23.8 -> 22.9) unless its values are wide (single precision, 16384 of 2048 59 -> 56 by four)
         if (chunks <= 1) go(rows8_rms_kernel<T, 1, 1>, 1);
+        else if (chunks <= 4 && (rows <= 2048 || (F && chunks > 2))) go(rows8_rms_kernel<T, 1, 4>, 4);
         else if (chunks <= 2) go(rows8_rms_kernel<T, 2, 1>, 1);
-        else if (chunks <= 4) go(rows8_rms_kernel<T, 4, 1>, 1);
+        else if (chunks <= MOST) go(rows8_rms_kernel<T, MOST, 1>, 1);
         else if (chunks <= 8) go(rows8_rms_kernel<T, 2, 4>, 4);
         else if (chunks <= 16) go(rows8_rms_kernel<T, 4, 4>, 4);
         else if constexpr (!F) go(rows8_rms_kernel<T, 8, 4>, 4);

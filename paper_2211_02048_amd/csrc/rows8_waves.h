@@ -1,6 +1,7 @@
 // The product of two matrices in 8 bits where tiles alone would leave compute units without work: the waves of a workgroup share the
 // input channels of one tile of 32 RT rows x 32 CT output channels, each by itself as in the kernel for few rows (blocks by direct loads into places of its own,
-// no barrier), and their sums meet in LDS in a fixed order.
+// no barrier), and their sums meet in LDS in a fixed order.  Bound by latency and by what a compute unit gets from L2.  Measured: 333 rows, 1288 -> 648
+// 3.9 us by 32 x 32 (by the kernel for few rows 5.3, by tiles of 128 x 64 6.1), 333 rows, 5120 -> 1280 9.8 by 32 x 64 (17.9, 17.8).
 #pragma once
 
 #include "rows8_tiles.h"

@@ -165,7 +165,7 @@ def close_codes(q, s, want, err, C, what=""):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
-@pytest.mark.parametrize("n,C", [(1, 8), (5, 128), (3, 136), (19, 320), (6, 512), (7, 640), (5, 1288), (9, 2048), (3, 2056), (1, 4096), (4, 5120), (2, 8192)])
+@pytest.mark.parametrize("n,C", [(1, 8), (5, 128), (3, 136), (19, 320), (6, 512), (7, 640), (5, 1288), (9, 2048), (3, 2056), (1, 4096), (4, 5120), (2, 8192), (2100, 640), (2060, 1032)])
 def test_rms(n, C, dtype):
     x, res = rows(C + n, n, C, dtype), rows(C + n + 1, n, C, dtype, 16)
     gamma = (torch.rand(C + 3, dtype=torch.float32) + 0.5).cuda()[3:] if C % 16 else (torch.rand(C) + 0.5).cuda()     # (also not 16-byte aligned)
