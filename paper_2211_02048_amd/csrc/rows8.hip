@@ -86,7 +86,7 @@ __global__ __launch_bounds__(256) void rows8_load_kernel(Rows8Args a)
 }
 
 // h = round(x + residual), n = gamma * h / sqrt(mean(h^2) + eps), to the outputs that are asked for.  Bound by memory (16384 rows of 2560 in bf16 with a
-// residual, its sum and the 8-bit output 57 us, 5.2 TB/s); a row stays in registers between the sum of squares (fp32) and the outputs.  W waves
+// residual, its sum and the 8-bit output 55 to 58 us, 5.1 to 5.3 TB/s); a row stays in registers between the sum of squares (fp32) and the outputs.  W waves
 // share a row, chunk w + W u of 512 channels each.
 template <typename T, int NC, int W>
 __global__ __launch_bounds__(256) void rows8_rms_kernel(Rows8Args a)

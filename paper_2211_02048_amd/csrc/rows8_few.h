@@ -7,7 +7,7 @@
 // compute units took 3.5 us, whole lines 2.1, of which a launch is 1.9.)  Plain: the waves of a workgroup share the input channels, 512 at a time (a
 // scale word), and their sums meet in LDS in a fixed order.  Gated: eight waves side by side have the 128 output channels of
 // a block, values and gates of 16 each, so that the row's scale is a maximum over the workgroup.  Measured: 16 rows, 5120 -> 1280 4.1 us, 1280 ->
-// 2 x 5120 gated 8.2 (40 workgroups of 330 KB each).
+// 2 x 5120 gated 8.0 (40 workgroups of 330 KB each).
 #pragma once
 
 #include "rows8_linear.h"

@@ -5,10 +5,10 @@
 // comes into LDS by direct loads, whole 128-byte lines (halves of lines took 1.4 times as long: twice the requests), NS blocks
 // deep; the 16-byte pieces of a row are permuted by the row's number, so that neither the loads nor the reads meet in a bank.  While the
 // pipe works on one half of a block, the next half's operands are read into registers, one read or request between two
-// matrix instructions: there is one wave per SIMD in the largest form, and whatever it waits for the pipe waits for too (requests in
-// one burst instead: 8192 x 8192 x 8192 2565 instead of 2750 TFLOP/s).  No branch in the loop: the compiler moves matrix instructions behind it (2040).
+// matrix instructions: there is one wave per SIMD in the largest form, and whatever it waits for the pipe waits for too (in a
+// prototype, 8192 x 8192 x 8192: requests in one burst 2565 TFLOP/s, spread 2750).  No branch in the loop: the compiler moves matrix instructions behind it (2040).
 // Measured, inputs changing: 8192 x 8192 -> 8192 420 us, 2620 TFLOP/s (inputs in the cache 402; all codes 0 347 and 296: the clock is at 1.9 GHz
-// of 2.4 for power); 8192 x 5120 -> 5120 182 us, 2360 TFLOP/s, matrix pipes busy 56 % of all cycles, LDS 18 %.
+// of 2.4 for power); 8192 x 5120 -> 5120 187 us, 2290 TFLOP/s, matrix pipes busy 57 % of all cycles, LDS 18 %.
 #pragma once
 
 #include "rows8_linear.h"
