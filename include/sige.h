@@ -554,7 +554,7 @@ int sige_rows8_load(const void* q, int32_t q_ld, const void* scales, int32_t s_l
  * the mean in fp32 (a sum of squares beyond its range gives a row of zeros), gamma fp32 [C] or NULL (1).  Outputs, each of its own: total = h [rows][C] (beside a
  * residual; may be NULL), y [rows][C] of dt, and q / scales: y in 8 bits, from the values before they are rounded to dt; y or
  * q may be NULL, not both.  total or y may be x or residual (same row stride).  C * size and the strides must be multiples of 16 bytes; at
- * most 32 KiB per token.                                                                */
+ * most 32 KiB per token; in single precision fewer than 2^24 rows of more than 1024 channels.                                                                */
 int sige_token_rms(const void* x, sige_dtype dt, int32_t C, int32_t x_ld, const void* residual, int32_t res_ld, const int32_t* count,
                    int32_t rows_per_count, int32_t max_rows, int32_t n_rows, const float* gamma, float eps, void* total,
                    int32_t total_ld, void* y, int32_t y_ld, void* q, int32_t q_ld, void* scales, int32_t s_ld, void* stream);

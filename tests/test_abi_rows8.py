@@ -83,6 +83,14 @@ def test_rms_refusals(L):
     assert rms(n=9) == 3
 
 
+def test_rms_more_workgroups_than_a_launch_has(L):
+    # single precision, three or four chunks of 512 channels: a workgroup of 256 threads per row, and a launch has fewer than 2^32 threads
+    n = 2 ** 24
+    for C in (1028, 2048):
+        assert L.sige_token_rms(FAKE, 0, C, C, None, 0, None, 0, n, n, None, ctypes.c_float(1e-6), None, 0, OTHER, C, None, 0, None, 0, None) == 2
+        assert "2^24" in err(L)
+
+
 def test_linear_refusals(L):
     def linear(x=FAKE, x_ld=384, xs=FAKE, xs_ld=4, cin=320, count=None, per=0, mr=8, n=8, w=FAKE, w_ld=384, ws=FAKE, ws_ld=4, cout=640, bias=None, base=None, base_ld=0,
                y=OTHER, dt=1, y_ld=640):
