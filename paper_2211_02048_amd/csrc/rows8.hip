@@ -198,6 +198,8 @@ static int rows8_store_load(const char* who, bool store, void* x, sige_dtype dt,
     a.d_chunks = fast_div(chunks);
     const long waves = (long)rows * chunks;
     SIGE_REQUIRE(waves < (1L << 26), SIGE_ERR_UNSUPPORTED, "%s: at most 2^26 rows, counted once for every 512 channels begun", who);
+    // (a wave writes a chunk while others still read the rows around it)
+    SIGE_REQUIRE(q != x && s != x && q != s, SIGE_ERR_INVALID_ARG, "%s: the 8-bit rows in the place of %s or of each other", who, store ? "x" : "y");
     const dim3 grid((unsigned)((waves + 3) / 4));
     hipStream_t st = (hipStream_t)stream;
     auto go = [&](auto kern) { hipLaunchKernelGGL(kern, grid, dim3(256), 0, st, a); };
@@ -261,7 +263,10 @@ extern "C" int sige_token_rms(const void* x, sige_dtype dt, int32_t C, int32_t x
     a.C = C; a.x_ld = x_ld; a.res_ld = res_ld; a.total_ld = total_ld; a.y_ld = y_ld; a.q_ld = q_ld; a.s_ld = s_ld; a.eps = eps;
     const int chunks = (C + ROW8_CHUNK - 1) / ROW8_CHUNK;
     SIGE_REQUIRE((long)rows * chunks < (1L << 26), SIGE_ERR_UNSUPPORTED, "%s: at most 2^26 rows, counted once for every 512 channels begun", who);
-    // (single precision, three or four chunks: a workgroup of 256 threads per row; every other form has fewer than 2^32 threads by the limit above)
+    for (const void* p : {(const void*)q, (const void*)scales})
+        SIGE_REQUIRE(!q || (p != x && p != residual && p != total && p != y && q != scales), SIGE_ERR_INVALID_ARG,
+                     "%s: the 8-bit rows in the place of another tensor or of each other", who);
+    // (single precision, three chunks: a workgroup of 256 threads per row; every other form has fewer than 2^32 threads by the limit above)
     SIGE_REQUIRE(dt != SIGE_F32 || chunks <= 2 || rows < (1 << 24), SIGE_ERR_UNSUPPORTED, "%s: fewer than 2^24 rows of more than 1024 channels in single precision", who);
     hipStream_t st = (hipStream_t)stream;
     auto go = [&](auto kern, int W) { hipLaunchKernelGGL(kern, dim3((unsigned)(((long)rows * W + 3) / 4)), dim3(256), 0, st, a); };

@@ -84,11 +84,28 @@ def test_rms_refusals(L):
 
 
 def test_rms_more_workgroups_than_a_launch_has(L):
-    # single precision, three or four chunks of 512 channels: a workgroup of 256 threads per row, and a launch has fewer than 2^32 threads
+    # single precision, three chunks of 512 channels: a workgroup of 256 threads per row, and a launch has fewer than 2^32 threads (four
+    # chunks: the limit of 2^26 rows times chunks comes first)
     n = 2 ** 24
-    for C in (1028, 2048):
+    for C in (1028, 1536):
         assert L.sige_token_rms(FAKE, 0, C, C, None, 0, None, 0, n, n, None, ctypes.c_float(1e-6), None, 0, OTHER, C, None, 0, None, 0, None) == 2
         assert "2^24" in err(L)
+
+
+def test_8_bit_rows_in_the_place_of_others_are_refused(L):
+    THIRD = ctypes.c_void_p(0x30000)
+    assert L.sige_rows8_store(FAKE, 1, 512, 512, None, 0, 8, 8, FAKE, 512, OTHER, 4, None) == 1 and "place" in err(L)
+    assert L.sige_rows8_store(FAKE, 1, 512, 512, None, 0, 8, 8, OTHER, 512, FAKE, 4, None) == 1
+    assert L.sige_rows8_store(FAKE, 1, 512, 512, None, 0, 8, 8, OTHER, 512, OTHER, 4, None) == 1
+    assert L.sige_rows8_load(FAKE, 512, OTHER, 4, 512, None, 0, 8, 8, FAKE, 1, 512, None) == 1 and "place" in err(L)
+    assert L.sige_rows8_load(FAKE, 512, OTHER, 4, 512, None, 0, 8, 8, OTHER, 1, 512, None) == 1
+
+    def rms(q, s, x=FAKE, res=None, total=None, y=None):
+        return L.sige_token_rms(x, 1, 512, 512, res, 512, None, 0, 8, 8, None, ctypes.c_float(1e-6), total, 512, y, 512, q, 512, s, 4, None)
+    FOURTH = ctypes.c_void_p(0x40000)
+    for kw in (dict(q=FAKE, s=FOURTH), dict(q=FOURTH, s=FAKE), dict(q=FOURTH, s=FOURTH), dict(q=OTHER, s=FOURTH, res=OTHER), dict(q=OTHER, s=FOURTH, y=OTHER),
+               dict(q=FOURTH, s=OTHER, y=OTHER), dict(q=THIRD, s=FOURTH, res=OTHER, total=THIRD), dict(q=FOURTH, s=THIRD, res=OTHER, total=THIRD)):
+        assert rms(**kw) == 1 and "place" in err(L), kw
 
 
 def test_linear_refusals(L):
