@@ -22,7 +22,7 @@ __device__ __forceinline__ int rows8_effective(const Rows8& r)
 {
     if (r.n_host >= 0) return r.n_host;
     const long n = (long)(*r.count) * r.rows_per_count;
-    return (int)(n < r.max_rows ? n : r.max_rows);
+    return (int)(n < 0 ? 0 : n < r.max_rows ? n : r.max_rows);       // (a count below zero is none: as 32 bits the product could be a large number)
 }
 
 // Checks of the rows; launch = the most rows there can be.

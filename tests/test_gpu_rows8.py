@@ -507,6 +507,31 @@ def test_product_rows_by_a_count_on_the_device():
         check_room(q, s, have, cout)
 
 
+def test_count_far_below_zero():
+    """-10^9 * 4 is 294967296 in 32 bits, and no rows all the same: nothing is written."""
+    n, C, cout = 200, 264, 136
+    kw = dict(count=torch.tensor([-10 ** 9], dtype=torch.int32, device="cuda"), rows_per_count=4, max_rows=n)
+    xq, xs, _ = matrix(1, n, C)
+    wq, ws, _ = matrix(2, 2 * cout, C)
+    x = rows(3, n, C, "bf16")
+    y, z = (torch.full((n, C), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    o = torch.full((n, cout), 7.0, dtype=torch.bfloat16, device="cuda")
+    (aq, as_), (bq, bs), (gq, gs) = room(n, C), room(n, C), room(n, cout)
+    api.sige_rows8_store(x, aq, as_, C, **kw)
+    api.sige_rows8_load(xq, xs, y, C, **kw)
+    api.sige_token_rms(x, C, y=z, q=bq, scales=bs, **kw)
+    for form in range(8):
+        with api.knobs(ROWS8_FORM=form):
+            api.sige_rows8_linear(xq, xs, wq, ws, o, C, cout, **kw)
+            if form < 4:
+                api.sige_rows8_linear_gated(xq, xs, wq, ws, gq, gs, C, cout, **kw)
+    torch.cuda.synchronize()
+    for t in (y, z, o):
+        assert (t == 7.0).all()
+    for q, s, c in ((aq, as_, C), (bq, bs, C), (gq, gs, cout)):
+        check_room(q, s, 0, c)
+
+
 @pytest.mark.parametrize("kind", ["store", "rms", "linear"])
 def test_offsets_beyond_32_bits(kind):
     """The last rows of tensors whose offsets do not fit 32 bits."""
