@@ -7,8 +7,8 @@
 // pipe works on one half of a block, the next half's operands are read into registers, one read or request between two
 // matrix instructions: there is one wave per SIMD in the largest form, and whatever it waits for the pipe waits for too (in a
 // prototype, 8192 x 8192 x 8192: requests in one burst 2565 TFLOP/s, spread 2750).  No branch in the loop: the compiler moves matrix instructions behind it (2040).
-// Measured, inputs changing: 8192 x 8192 -> 8192 420 us, 2620 TFLOP/s (inputs in the cache 402; all codes 0 347 and 296: the clock is at 1.9 GHz
-// of 2.4 for power); 8192 x 5120 -> 5120 187 us, 2290 TFLOP/s, matrix pipes busy 57 % of all cycles, LDS 18 %.
+// Measured, inputs changing: 8192 x 8192 -> 8192 409 us, 2690 TFLOP/s (inputs in the cache 390; all codes 0 331 and 289: the clock is at 1.9 GHz
+// of 2.4 for power); 8192 x 5120 -> 5120 184 us, 2340 TFLOP/s, with a base matrix pipes busy 58 % of all cycles, LDS 18 %.
 #pragma once
 
 #include "rows8_linear.h"
