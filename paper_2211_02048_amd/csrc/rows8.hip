@@ -194,7 +194,7 @@ static int rows8_store_load(const char* who, bool store, void* x, sige_dtype dt,
     if (int rc = rows8_check_matrix(who, "the 8-bit rows", q, q_ld, s, s_ld, C, rows > 0)) return rc;
     if (rows == 0) return SIGE_OK;
     a.x = x; a.y = x; a.x_ld = a.y_ld = x_ld; a.C = C; a.q = (unsigned char*)q; a.q_ld = q_ld; a.s = (unsigned char*)s; a.s_ld = s_ld;
-    const int chunks = (C + ROW8_CHUNK - 1) / ROW8_CHUNK;
+    const int chunks = (int)(((long)C + ROW8_CHUNK - 1) / ROW8_CHUNK);       // (C + 511 need not fit an int)
     a.d_chunks = fast_div(chunks);
     const long waves = (long)rows * chunks;
     SIGE_REQUIRE(waves < (1L << 26), SIGE_ERR_UNSUPPORTED, "%s: at most 2^26 rows, counted once for every 512 channels begun", who);

@@ -217,8 +217,9 @@ template <typename T, bool GATED, int RT, int CT, int NBUF>
 inline int launch_few(const char* who, const Linear8Args& a, int rows, int most_waves, hipStream_t st)
 {
     using S = Few8<GATED, RT, CT, NBUF>;
-    const dim3 grid((a.Cout + (GATED ? 127 : 16 * CT - 1)) / (GATED ? 128 : 16 * CT), (rows + 16 * RT - 1) / (16 * RT));
-    SIGE_REQUIRE(grid.y < 65536 && grid.x < (1u << 23), SIGE_ERR_UNSUPPORTED, "%s: too many rows or channels", who);
+    const long nx = parts_of(a.Cout, GATED ? 128 : 16 * CT), my = parts_of(rows, 16 * RT);
+    SIGE_REQUIRE(my < 65536 && nx < (1L << 23), SIGE_ERR_UNSUPPORTED, "%s: too many rows or channels", who);
+    const dim3 grid((unsigned)nx, (unsigned)my);
     const auto kern = rows8_few_kernel<T, GATED, RT, CT, NBUF>;
     const int words = (a.blocks + 3) / 4, waves = GATED ? 8 : words < most_waves ? words : most_waves;
     if (int rc = allow_lds(who, (const void*)kern, waves * S::WAVE)) return rc;

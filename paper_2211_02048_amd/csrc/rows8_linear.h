@@ -29,6 +29,9 @@ struct Linear8Args {
     int gate;
 };
 
+// n things in parts of `part`, the last one partly filled (in 64 bits: n + part - 1 need not fit an int).
+inline long parts_of(int n, int part) { return ((long)n + part - 1) / part; }
+
 // Lets a kernel have more LDS than 48 KB (one limit whatever the call, so that calls from two threads do not undo each other's).
 inline int allow_lds(const char* who, const void* kern, int bytes)
 {

@@ -18,7 +18,7 @@ struct Linear8Cost {
 
 static float linear8_cost(const Linear8Cost& c, int rows, int cols, int blocks)
 {
-    const float units = (float)((rows + c.rows - 1) / c.rows) * (float)((cols + c.cols - 1) / c.cols) / COMPUTE_UNITS;
+    const float units = (float)parts_of(rows, c.rows) * (float)parts_of(cols, c.cols) / COMPUTE_UNITS;
     float rounds = std::ceil(units);
     if (c.slots == 2) rounds = units <= 1.0f ? 0.62f : units <= 2.0f ? 1.0f : units / 2.0f;     // (one workgroup by itself has the compute unit's time)
     if (c.rows == 256) {
@@ -31,7 +31,7 @@ static float linear8_cost(const Linear8Cost& c, int rows, int cols, int blocks)
 static float linear8_few_cost(bool exact, int rows, int cols, int blocks)
 {
     const int words = (blocks + 3) / 4, waves = words < 8 ? words : 8;
-    const float units = (float)((rows + 15) / 16) * (float)((cols + 15) / 16) / COMPUTE_UNITS, steps = (float)(4 * ((words + waves - 1) / waves));
+    const float units = (float)parts_of(rows, 16) * (float)parts_of(cols, 16) / COMPUTE_UNITS, steps = (float)(4 * ((words + waves - 1) / waves));
     return exact ? 1.23f + 0.435f * steps + 0.064f * units * (float)blocks + 0.105f * units
                  : 1.54f + 0.315f * steps + 0.066f * units * (float)blocks + 0.027f * units;
 }

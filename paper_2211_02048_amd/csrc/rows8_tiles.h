@@ -458,7 +458,7 @@ template <typename T, bool GATED, int RT, int CT, int NS, int WGS, bool HALVES =
 inline int launch_tiles(const char* who, const Linear8Args& a, int rows, hipStream_t st)
 {
     using Tile = Tile8<T, GATED, RT, CT, NS>;
-    const long n = (long)((a.Cout + Tile::OUT - 1) / Tile::OUT) * ((rows + Tile::BM - 1) / Tile::BM);
+    const long n = parts_of(a.Cout, Tile::OUT) * parts_of(rows, Tile::BM);
     SIGE_REQUIRE(n < (1L << 23), SIGE_ERR_UNSUPPORTED, "%s: too many rows and channels", who);
     const auto kern = rows8_tile_kernel<T, GATED, RT, CT, NS, WGS, HALVES>;
     if (int rc = allow_lds(who, (const void*)kern, Tile::LDS)) return rc;

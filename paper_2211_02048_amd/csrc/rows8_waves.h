@@ -151,7 +151,7 @@ template <typename T, int RT, int CT, int NBUF, int WAVES>
 inline int launch_waves(const char* who, const Linear8Args& a, int rows, hipStream_t st)
 {
     constexpr int ROWS = 32 * (RT + CT), LDS = WAVES * (NBUF * ROWS * 128 + 2 * ((ROWS + 63) / 64) * 256);
-    const long n = (long)((a.Cout + 32 * CT - 1) / (32 * CT)) * ((rows + 32 * RT - 1) / (32 * RT));
+    const long n = parts_of(a.Cout, 32 * CT) * parts_of(rows, 32 * RT);
     SIGE_REQUIRE(n < (1L << 22), SIGE_ERR_UNSUPPORTED, "%s: too many rows and channels", who);
     const auto kern = rows8_waves_kernel<T, RT, CT, NBUF, WAVES>;
     if (int rc = allow_lds(who, (const void*)kern, LDS)) return rc;

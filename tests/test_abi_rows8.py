@@ -176,3 +176,23 @@ def test_binding_refusals():
     refused(3, api.sige_rows8_linear_gated, q, s, w, ws, o[:, :304], os_, 320, 320, n_rows=4)
     refused(1, api.sige_rows8_linear_gated, q, s, w, ws, o, os_, 320, 320, bias=torch.zeros(320), n_rows=4)
     refused(1, api.sige_rows8_linear_gated, q, s, w, ws, o, os_, 320, 320, n_rows=-1, count=torch.zeros(1), rows_per_count=1)
+
+
+def test_limits_at_the_end_of_32_bits(L):
+    """Rounding up to a tile's rows or a chunk's channels has to stay a positive number: no form's launch holds these calls."""
+    n = 2 ** 31 - 1
+    THIRD, FOURTH = ctypes.c_void_p(0x30000), ctypes.c_void_p(0x40000)
+    for rows in (n, n - 14, n - 127, n - 254):
+        for count, per, host in ((None, 0, rows), (FAKE, 1, -1)):
+            for form in range(-1, 8):
+                with api.knobs(ROWS8_FORM=form):
+                    for dt in (0, 1, 2) if form < 7 else (1, 2):
+                        assert L.sige_rows8_linear(FAKE, 384, FAKE, 4, 320, count, per, rows, host, FAKE, 384, FAKE, 4, 640, None, None, 0, OTHER, dt, 640, None) == 2, (rows, form, dt)
+                    if form < 4:
+                        assert L.sige_rows8_linear_gated(FAKE, 384, FAKE, 4, 320, count, per, rows, host, FAKE, 384, FAKE, 4, 640, None, 0, THIRD, 640, FOURTH, 8, None) == 2, (rows, form)
+            assert L.sige_token_rms(FAKE, 1, 320, 320, None, 0, count, per, rows, host, None, ctypes.c_float(1e-6), None, 0, OTHER, 320, None, 0, None, 0, None) == 2
+    # sixteen rows of 2^31 - 128 channels are 2^26 times 512 channels begun, and so many channels and 511 more do not fit an int
+    for C in (2 ** 31 - 128, 2 ** 31 - 504):
+        ld = -(-C // 128) * 128
+        assert L.sige_rows8_store(FAKE, 1, C, C, None, 0, 16, 16, THIRD, ld, FOURTH, 2 ** 24, None) == 2
+        assert L.sige_rows8_load(FAKE, ld, OTHER, 2 ** 24, C, None, 0, 16, 16, THIRD, 1, C, None) == 2

@@ -684,3 +684,23 @@ def test_recorded_calls():
     calls.run()
     torch.cuda.synchronize()
     assert len(calls) == 2 and torch.equal(y, want)
+
+
+def test_one_row_of_as_many_channels_as_an_int_counts():
+    """2^31 - 128 channels: chunks are counted without 2^31 - 128 + 511 becoming negative, and the row is what its blocks are as rows."""
+    C = 2 ** 31 - 128
+    n = C // 128
+    x = torch.empty(1, C, dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(31)
+    for i in range(0, C, 1 << 26):
+        x[0, i:i + (1 << 26)].normal_(generator=g)
+    q, s = api.rows8(1, C)
+    api.sige_rows8_store(x, q, s, C, n_rows=1)
+    bq, bs = api.rows8(n, 128)
+    api.sige_rows8_store(x.view(n, 128), bq, bs, 128, n_rows=n)
+    assert torch.equal(q.view(n, 128), bq) and torch.equal(s[0, :n], bs[:, 0]) and (s[0, n:] == 0).all()
+    y = torch.empty_like(x)
+    api.sige_rows8_load(q, s, y, C, n_rows=1)
+    by = torch.empty(n, 128, dtype=torch.bfloat16, device="cuda")
+    api.sige_rows8_load(bq, bs, by, 128, n_rows=n)
+    assert torch.equal(y.view(n, 128), by)
