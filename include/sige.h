@@ -541,7 +541,7 @@ int sige_token_lora(const void* x, sige_dtype dt, int32_t Cin, int32_t x_ld, con
  *
  * sige_rows8_store: x [rows][C] of dt to 8 bits.  A block's scale is the smallest power of two, at least 2^-126, with max|x| <= 448 * scale over its
  * finite values; codes are the nearest, ties to the even one; an infinity or NaN becomes a NaN and leaves the others alone.
- * Weights are stored once by the same call.  At most 2^26 rows, counted once for every 512 channels begun (here, in the load and in the norm).
+ * Weights are stored once by the same call.  At most 2^26 - 4 rows, counted once for every 512 channels begun (here, in the load and in the norm).
  * sige_rows8_load: the values as rows of dt (rounded once; fp16 and bf16 lose nothing but what lies outside of their range).  */
 int sige_rows8_store(const void* x, sige_dtype dt, int32_t C, int32_t x_ld, const int32_t* count, int32_t rows_per_count,
                      int32_t max_rows, int32_t n_rows, void* q, int32_t q_ld, void* scales, int32_t s_ld, void* stream);

@@ -9,6 +9,8 @@ namespace sige {
 constexpr int ROW8_BLOCK = 128;                     // channels of a scale
 constexpr int ROW8_CHUNK = 512;                     // channels of a scale word: what a wave of the row kernels takes at once
 
+constexpr long ROW8_MOST_WAVES = (1L << 26) - 4;    // four to a workgroup of 256 threads, of which a launch has fewer than 2^32
+
 inline long row8_ld(long C) { return (C + ROW8_BLOCK - 1) / ROW8_BLOCK * ROW8_BLOCK; }
 inline long row8_scale_ld(long C) { return (C + ROW8_CHUNK - 1) / ROW8_CHUNK * 4; }
 

@@ -197,7 +197,7 @@ static int rows8_store_load(const char* who, bool store, void* x, sige_dtype dt,
     const int chunks = (int)(((long)C + ROW8_CHUNK - 1) / ROW8_CHUNK);       // (C + 511 need not fit an int)
     a.d_chunks = fast_div(chunks);
     const long waves = (long)rows * chunks;
-    SIGE_REQUIRE(waves < (1L << 26), SIGE_ERR_UNSUPPORTED, "%s: at most 2^26 rows, counted once for every 512 channels begun", who);
+    SIGE_REQUIRE(waves <= ROW8_MOST_WAVES, SIGE_ERR_UNSUPPORTED, "%s: at most 2^26 - 4 rows, counted once for every 512 channels begun", who);
     // (a wave writes a chunk while others still read the rows around it)
     SIGE_REQUIRE(q != x && s != x && q != s, SIGE_ERR_INVALID_ARG, "%s: the 8-bit rows in the place of %s or of each other", who, store ? "x" : "y");
     const dim3 grid((unsigned)((waves + 3) / 4));
@@ -262,7 +262,7 @@ extern "C" int sige_token_rms(const void* x, sige_dtype dt, int32_t C, int32_t x
     a.x = x; a.residual = residual; a.gamma = gamma; a.total = total; a.y = y; a.q = (unsigned char*)q; a.s = (unsigned char*)scales;
     a.C = C; a.x_ld = x_ld; a.res_ld = res_ld; a.total_ld = total_ld; a.y_ld = y_ld; a.q_ld = q_ld; a.s_ld = s_ld; a.eps = eps;
     const int chunks = (C + ROW8_CHUNK - 1) / ROW8_CHUNK;
-    SIGE_REQUIRE((long)rows * chunks < (1L << 26), SIGE_ERR_UNSUPPORTED, "%s: at most 2^26 rows, counted once for every 512 channels begun", who);
+    SIGE_REQUIRE((long)rows * chunks <= ROW8_MOST_WAVES, SIGE_ERR_UNSUPPORTED, "%s: at most 2^26 - 4 rows, counted once for every 512 channels begun", who);
     for (const void* p : {(const void*)q, (const void*)scales})
         SIGE_REQUIRE(!q || (p != x && p != residual && p != total && p != y && q != scales), SIGE_ERR_INVALID_ARG,
                      "%s: the 8-bit rows in the place of another tensor or of each other", who);

@@ -196,3 +196,14 @@ def test_limits_at_the_end_of_32_bits(L):
         ld = -(-C // 128) * 128
         assert L.sige_rows8_store(FAKE, 1, C, C, None, 0, 16, 16, THIRD, ld, FOURTH, 2 ** 24, None) == 2
         assert L.sige_rows8_load(FAKE, ld, OTHER, 2 ** 24, C, None, 0, 16, 16, THIRD, 1, C, None) == 2
+
+
+def test_a_launch_has_fewer_than_2_32_threads(L):
+    """Four waves of 64 make a workgroup: from 2^26 - 3 waves on there would be 2^24 workgroups of 256 threads."""
+    THIRD, FOURTH = ctypes.c_void_p(0x30000), ctypes.c_void_p(0x40000)
+    for n in (2 ** 26 - 3, 2 ** 26 - 2, 2 ** 26 - 1):
+        for count, per, host in ((None, 0, n), (FAKE, 1, -1)):
+            for C in (8, 512):
+                assert L.sige_rows8_store(FAKE, 1, C, C, count, per, n, host, THIRD, 512, FOURTH, 4, None) == 2 and "2^26" in err(L)
+                assert L.sige_rows8_load(THIRD, 512, FOURTH, 4, C, count, per, n, host, FAKE, 1, C, None) == 2
+                assert L.sige_token_rms(FAKE, 1, C, C, None, 0, count, per, n, host, None, ctypes.c_float(1e-6), None, 0, OTHER, C, None, 0, None, 0, None) == 2

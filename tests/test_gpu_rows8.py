@@ -704,3 +704,20 @@ def test_one_row_of_as_many_channels_as_an_int_counts():
     by = torch.empty(n, 128, dtype=torch.bfloat16, device="cuda")
     api.sige_rows8_load(bq, bs, by, 128, n_rows=n)
     assert torch.equal(y.view(n, 128), by)
+
+
+def test_as_many_rows_as_a_launch_holds():
+    """2^26 - 4 rows, the most that the calls take: the last of them in the store, the load and the norm."""
+    C, n = 8, 2 ** 26 - 4
+    x = torch.zeros(n, C, dtype=torch.bfloat16, device="cuda")
+    x[-3:] = rows(26, 3, C, "bf16", 0)
+    q, s = api.rows8(n, C)
+    api.sige_rows8_store(x, q, s, C, n_rows=n)
+    y = torch.empty_like(x)
+    api.sige_rows8_load(q, s, y, C, n_rows=n)
+    same_codes(q[-3:], s[-3:], f64(x[-3:]), C)
+    np.testing.assert_array_equal(f64(y[-3:]), ref.values(q[-3:].cpu().numpy(), s[-3:].cpu().numpy(), C))
+    assert (y[:-3] == 0).all()
+    api.sige_token_rms(x, C, y=y, n_rows=n)
+    want = rms_expected(x[-3:], None, None, 1e-6, "bf16")[1]
+    assert (np.abs(f64(y[-3:]) - want) <= (2.0 ** -8 + 2.0 ** -10) * np.abs(want)).all() and (y[:-3] == 0).all()
