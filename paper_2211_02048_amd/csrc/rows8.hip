@@ -258,6 +258,8 @@ extern "C" int sige_token_rms(const void* x, sige_dtype dt, int32_t C, int32_t x
                      (!residual || y != residual || y_ld == res_ld),
                  SIGE_ERR_UNSUPPORTED, "%s: an output in the place of an input needs its row stride", who);
     SIGE_REQUIRE(!total || total != y, SIGE_ERR_INVALID_ARG, "%s: the sum and y are two outputs", who);
+    SIGE_REQUIRE(!gamma || rows == 0 || (total != gamma && y != gamma && q != gamma && scales != gamma), SIGE_ERR_INVALID_ARG,
+                 "%s: an output in the place of gamma", who);
     if (rows == 0) return SIGE_OK;
     a.x = x; a.residual = residual; a.gamma = gamma; a.total = total; a.y = y; a.q = (unsigned char*)q; a.s = (unsigned char*)scales;
     a.C = C; a.x_ld = x_ld; a.res_ld = res_ld; a.total_ld = total_ld; a.y_ld = y_ld; a.q_ld = q_ld; a.s_ld = s_ld; a.eps = eps;

@@ -113,7 +113,9 @@ extern "C" int sige_rows8_linear(const void* x, int32_t x_ld, const void* x_scal
     if (rows == 0) return SIGE_OK;
     SIGE_REQUIRE(y, SIGE_ERR_INVALID_ARG, "%s: y is required", who);
     SIGE_REQUIRE(aligned16(y) && aligned16(base), SIGE_ERR_UNSUPPORTED, "%s: y and base must be 16-byte aligned", who);
-    SIGE_REQUIRE(y != x && y != w, SIGE_ERR_INVALID_ARG, "%s: y may be neither x nor w", who);
+    // (workgroups write while others still read: the base is read by the lane that writes it)
+    for (const void* p : {x, x_scales, w, w_scales, (const void*)bias})
+        SIGE_REQUIRE(y != p, SIGE_ERR_INVALID_ARG, "%s: y in the place of x, w, their scales or the bias", who);
     a.base = base; a.base_ld = base_ld; a.y = y; a.y_ld = y_ld;
     hipStream_t st = (hipStream_t)stream;
     const int form = linear8_form(a, rows, dt == SIGE_F32);
@@ -134,8 +136,12 @@ extern "C" int sige_rows8_linear_gated(const void* x, int32_t x_ld, const void* 
         return rc;
     SIGE_REQUIRE(Cout % 8 == 0, SIGE_ERR_UNSUPPORTED, "%s: Cout must be a multiple of 8", who);
     if (int rc = rows8_check_matrix(who, "the output", q, q_ld, scales, s_ld, Cout, rows > 0)) return rc;
-    SIGE_REQUIRE(rows == 0 || (q != x && scales != x_scales && q != w && scales != w_scales), SIGE_ERR_INVALID_ARG, "%s: the output may be neither x nor w", who);
     if (rows == 0) return SIGE_OK;
+    const int form = linear8_gated_form(a, rows);
+    SIGE_REQUIRE(form < GATED8_FORMS, SIGE_ERR_UNSUPPORTED, "%s: the call has no form %d", who, form);
+    for (const void* p : {x, x_scales, w, w_scales, (const void*)bias})
+        SIGE_REQUIRE(q != p && scales != p, SIGE_ERR_INVALID_ARG, "%s: codes or scales in the place of x, w, their scales or the bias", who);
+    SIGE_REQUIRE(q != scales, SIGE_ERR_INVALID_ARG, "%s: codes and scales in one place", who);
     a.gate = gate; a.q = (unsigned char*)q; a.q_ld = q_ld; a.s = (unsigned char*)scales; a.s_ld = s_ld;
-    return linear8_gated(who, a, rows, linear8_gated_form(a, rows), (hipStream_t)stream);
+    return linear8_gated(who, a, rows, form, (hipStream_t)stream);
 }

@@ -207,3 +207,29 @@ def test_a_launch_has_fewer_than_2_32_threads(L):
                 assert L.sige_rows8_store(FAKE, 1, C, C, count, per, n, host, THIRD, 512, FOURTH, 4, None) == 2 and "2^26" in err(L)
                 assert L.sige_rows8_load(THIRD, 512, FOURTH, 4, C, count, per, n, host, FAKE, 1, C, None) == 2
                 assert L.sige_token_rms(FAKE, 1, C, C, None, 0, count, per, n, host, None, ctypes.c_float(1e-6), None, 0, OTHER, C, None, 0, None, 0, None) == 2
+
+
+def test_outputs_in_the_place_of_other_tensors_are_refused(L):
+    """Products: a tensor that another workgroup still reads, or that another output is written to."""
+    at = {name: ctypes.c_void_p(0x100000 * (i + 1)) for i, name in enumerate(("x", "xs", "w", "ws", "bias", "base", "y", "q", "s", "gamma"))}
+
+    def linear(**kw):
+        p = {**at, **kw}
+        return L.sige_rows8_linear(p["x"], 512, p["xs"], 4, 512, None, 0, 8, 8, p["w"], 512, p["ws"], 4, 512, p["bias"], p["base"], 512, p["y"], 1, 512, None)
+
+    def gated(**kw):
+        p = {**at, **kw}
+        return L.sige_rows8_linear_gated(p["x"], 512, p["xs"], 4, 512, None, 0, 8, 8, p["w"], 512, p["ws"], 4, 512, p["bias"], 0, p["q"], 512, p["s"], 4, None)
+
+    def rms(**kw):
+        p = {**at, **kw}
+        return L.sige_token_rms(p["x"], 1, 512, 512, p["base"], 512, None, 0, 8, 8, p["gamma"], ctypes.c_float(1e-6), p["w"], 512, p["y"], 512, p["q"], 512, p["s"], 4, None)
+    for name in ("x", "xs", "w", "ws", "bias"):
+        assert linear(y=at[name]) == 1 and "place" in err(L), name
+        assert gated(q=at[name]) == 1 and "place" in err(L), name
+        assert gated(s=at[name]) == 1 and "place" in err(L), name
+    assert gated(s=at["q"]) == 1 and "place" in err(L)
+    for out in ("w", "y", "q", "s"):                            # (w: the sum)
+        assert rms(**{out: at["gamma"]}) == 1 and "place" in err(L), out
+    # calls without rows touch nothing
+    assert L.sige_rows8_linear_gated(at["x"], 512, at["xs"], 4, 512, None, 0, 8, 0, at["w"], 512, at["ws"], 4, 512, None, 0, at["q"], 512, at["q"], 4, None) == 0
