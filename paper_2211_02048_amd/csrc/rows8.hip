@@ -240,8 +240,9 @@ extern "C" int sige_token_rms(const void* x, sige_dtype dt, int32_t C, int32_t x
     Rows8Args a = {};
     int rows;
     if (int rc = rows8_check(who, count, rows_per_count, max_rows, n_rows, &a.rows, &rows)) return rc;
-    SIGE_REQUIRE(y || q, SIGE_ERR_INVALID_ARG, "%s: y or the 8-bit rows are required", who);
-    SIGE_REQUIRE(residual || !total, SIGE_ERR_INVALID_ARG, "%s: the sum is an output beside a residual only", who);
+    // (without rows a tensor's address may be null: which tensors there are says nothing)
+    SIGE_REQUIRE(y || q || rows == 0, SIGE_ERR_INVALID_ARG, "%s: y or the 8-bit rows are required", who);
+    SIGE_REQUIRE(residual || !total || rows == 0, SIGE_ERR_INVALID_ARG, "%s: the sum is an output beside a residual only", who);
     if (int rc = check_tensor(who, "x", x, dt, C, x_ld, rows > 0)) return rc;
     if (residual)
         if (int rc = check_tensor(who, "residual", residual, dt, C, res_ld, rows > 0)) return rc;
@@ -253,14 +254,14 @@ extern "C" int sige_token_rms(const void* x, sige_dtype dt, int32_t C, int32_t x
         if (int rc = rows8_check_matrix(who, "the 8-bit rows", q, q_ld, scales, s_ld, C, rows > 0)) return rc;
     SIGE_REQUIRE(C * dtype_size(dt) <= 32768, SIGE_ERR_UNSUPPORTED, "%s: at most 32 KiB per token", who);
     SIGE_REQUIRE((reinterpret_cast<uintptr_t>(gamma) & 3u) == 0, SIGE_ERR_UNSUPPORTED, "%s: gamma must be 4-byte aligned", who);
+    if (rows == 0) return SIGE_OK;
     // (a wave writes a row's sums where it has read that row, and only that row's)
     SIGE_REQUIRE((total != x || total_ld == x_ld) && (total != residual || !total || total_ld == res_ld) && (y != x || y_ld == x_ld) &&
                      (!residual || y != residual || y_ld == res_ld),
                  SIGE_ERR_UNSUPPORTED, "%s: an output in the place of an input needs its row stride", who);
     SIGE_REQUIRE(!total || total != y, SIGE_ERR_INVALID_ARG, "%s: the sum and y are two outputs", who);
-    SIGE_REQUIRE(!gamma || rows == 0 || (total != gamma && y != gamma && q != gamma && scales != gamma), SIGE_ERR_INVALID_ARG,
+    SIGE_REQUIRE(!gamma || (total != gamma && y != gamma && q != gamma && scales != gamma), SIGE_ERR_INVALID_ARG,
                  "%s: an output in the place of gamma", who);
-    if (rows == 0) return SIGE_OK;
     a.x = x; a.residual = residual; a.gamma = gamma; a.total = total; a.y = y; a.q = (unsigned char*)q; a.s = (unsigned char*)scales;
     a.C = C; a.x_ld = x_ld; a.res_ld = res_ld; a.total_ld = total_ld; a.y_ld = y_ld; a.q_ld = q_ld; a.s_ld = s_ld; a.eps = eps;
     const int chunks = (C + ROW8_CHUNK - 1) / ROW8_CHUNK;

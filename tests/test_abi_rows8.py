@@ -233,3 +233,17 @@ def test_outputs_in_the_place_of_other_tensors_are_refused(L):
         assert rms(**{out: at["gamma"]}) == 1 and "place" in err(L), out
     # calls without rows touch nothing
     assert L.sige_rows8_linear_gated(at["x"], 512, at["xs"], 4, 512, None, 0, 8, 0, at["w"], 512, at["ws"], 4, 512, None, 0, at["q"], 512, at["q"], 4, None) == 0
+
+
+def test_calls_without_rows_take_tensors_without_memory(L):
+    """An edit that touches nothing: tensors of no rows, whose addresses are null."""
+    eps = ctypes.c_float(1e-6)
+    for count, per, mr, host in ((None, 0, 0, 0), (FAKE, 16, 0, -1), (None, 0, 8, 0)):
+        rows = (count, per, mr, host)
+        assert L.sige_rows8_store(None, 1, 320, 320, *rows, None, 384, None, 4, None) == 0
+        assert L.sige_rows8_load(None, 384, None, 4, 320, *rows, None, 1, 320, None) == 0
+        assert L.sige_rows8_linear(None, 384, None, 4, 320, *rows, FAKE, 384, FAKE, 4, 640, None, None, 0, None, 1, 640, None) == 0
+        assert L.sige_rows8_linear_gated(None, 384, None, 4, 320, *rows, FAKE, 384, FAKE, 4, 640, None, 0, None, 640, None, 8, None) == 0
+        for res_ld, total_ld, y_ld, q_ld, s_ld in ((0, 0, 320, 0, 0), (0, 0, 0, 384, 4), (320, 320, 328, 0, 0), (328, 320, 0, 384, 4), (320, 0, 336, 384, 4)):
+            assert L.sige_token_rms(None, 1, 320, 320, None, res_ld, *rows, None, eps, None, total_ld, None, y_ld, None, q_ld, None, s_ld, None) == 0, (rows, y_ld, err(L))
+            assert L.sige_token_rms(FAKE, 1, 320, 320, None, res_ld, *rows, None, eps, None, total_ld, None, y_ld, None, q_ld, None, s_ld, None) == 0

@@ -721,3 +721,23 @@ def test_as_many_rows_as_a_launch_holds():
     api.sige_token_rms(x, C, y=y, n_rows=n)
     want = rms_expected(x[-3:], None, None, 1e-6, "bf16")[1]
     assert (np.abs(f64(y[-3:]) - want) <= (2.0 ** -8 + 2.0 ** -10) * np.abs(want)).all() and (y[:-3] == 0).all()
+
+
+@pytest.mark.parametrize("counted", [False, True])
+def test_an_edit_without_blocks(counted):
+    """Every call on tensors of no rows, also by a count on the device that such a program keeps."""
+    C, cout = 320, 640
+    kw = dict(n_rows=-1, count=torch.tensor([3], dtype=torch.int32, device="cuda"), rows_per_count=16) if counted else dict(n_rows=0)
+    x, y, t = (torch.empty(0, C, dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    z = torch.empty(0, cout, dtype=torch.bfloat16, device="cuda")
+    (q, s), (o, os_) = api.rows8(0, C), api.rows8(0, cout)
+    w, ws = api.rows8(2 * cout, C)
+    w.zero_(), ws.zero_()
+    api.sige_rows8_store(x, q, s, C, **kw)
+    api.sige_rows8_load(q, s, y, C, **kw)
+    api.sige_token_rms(x, C, y=y, **kw)
+    api.sige_token_rms(x, C, q=q, scales=s, **kw)
+    api.sige_token_rms(x, C, residual=y, total=t, y=torch.empty(0, C + 8, dtype=torch.bfloat16, device="cuda"), q=q, scales=s, **kw)
+    api.sige_rows8_linear(q, s, w, ws, z, C, cout, base=torch.empty(0, cout + 8, dtype=torch.bfloat16, device="cuda"), **kw)
+    api.sige_rows8_linear_gated(q, s, w, ws, o, os_, C, cout, **kw)
+    torch.cuda.synchronize()
