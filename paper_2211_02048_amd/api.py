@@ -843,11 +843,19 @@ def _rows8(what, q, scales, rows, C):
     return a if n > 1 else max(ld, a), c if m > 1 else max(sld, c)
 
 
+def _int32(who, *sizes):
+    """Sizes that reach the library as 32-bit integers (of a larger one their lower 32 bits would)."""
+    if max(sizes) > 0x7fffffff:
+        raise SigeError(2, f"{who}: sizes and strides below 2^31, not {max(sizes)}")
+
+
 def _row_count(x, n_rows, max_rows, count):
     """The most rows that a call may have, and those that it may touch."""
     if max_rows is None:
         sh = x.shape
         max_rows = sh[0] if len(sh) == 2 else x.numel() // max(sh[-1], 1)
+        if n_rows >= 0 and max_rows > n_rows:
+            max_rows = n_rows                                          # (room for more is nothing the call has to know)
     if count is not None:
         _table("count", count, _I32, 1)
     return max_rows, max_rows if n_rows < 0 else n_rows
@@ -858,6 +866,7 @@ def sige_rows8_store(x, q, scales, C, *, n_rows=-1, count=None, rows_per_count=0
     mr, rows = _row_count(x, n_rows, max_rows, count)
     x_ld = _lines(x, rows, C, x_ld)
     q_ld, s_ld = _rows8("q", q, scales, rows, C)
+    _int32("sige_rows8_store", C, x_ld, rows_per_count, mr, n_rows, q_ld, s_ld)
     stream = _stream_of(x, q, scales, count)
     rc = lib().sige_rows8_store(x.data_ptr(), _DT[x.dtype], C, x_ld, _at(count), rows_per_count, mr, n_rows, q.data_ptr(), q_ld,
                                 scales.data_ptr(), s_ld, stream)
@@ -870,6 +879,7 @@ def sige_rows8_load(q, scales, y, C, *, n_rows=-1, count=None, rows_per_count=0,
     mr, rows = _row_count(y, n_rows, max_rows, count)
     y_ld = _lines(y, rows, C, y_ld)
     q_ld, s_ld = _rows8("q", q, scales, rows, C)
+    _int32("sige_rows8_load", C, y_ld, rows_per_count, mr, n_rows, q_ld, s_ld)
     stream = _stream_of(y, q, scales, count)
     rc = lib().sige_rows8_load(q.data_ptr(), q_ld, scales.data_ptr(), s_ld, C, _at(count), rows_per_count, mr, n_rows, y.data_ptr(),
                                _DT[y.dtype], y_ld, stream)
@@ -891,6 +901,7 @@ def sige_token_rms(x, C, gamma=None, eps=1e-6, *, residual=None, total=None, y=N
     total_ld = 0 if total is None else _lines(total, rows, C, total_ld)
     y_ld = 0 if y is None else _lines(y, rows, C, y_ld)
     q_ld, s_ld = (0, 0) if q is None else _rows8("q", q, scales, rows, C)
+    _int32("sige_token_rms", C, x_ld, res_ld, total_ld, y_ld, rows_per_count, mr, n_rows, q_ld, s_ld)
     stream = _stream_of(x, residual, total, y, q, scales, gamma, count)
     rc = lib().sige_token_rms(x.data_ptr(), _DT[x.dtype], C, x_ld, _at(residual), res_ld, _at(count), rows_per_count, mr, n_rows, _at(gamma),
                               eps, _at(total), total_ld, _at(y), y_ld, _at(q), q_ld, _at(scales), s_ld, stream)
@@ -908,6 +919,7 @@ def sige_rows8_linear(x, x_scales, w, w_scales, y, Cin, Cout, *, bias=None, base
     y_ld = _lines(y, rows, Cout, y_ld)
     base_ld = 0 if base is None else _lines(base, rows, Cout, base_ld)
     (q_ld, s_ld), (w_ld, ws_ld) = _rows8("x", x, x_scales, rows, Cin), _rows8("w", w, w_scales, Cout, Cin)
+    _int32("sige_rows8_linear", Cin, Cout, y_ld, base_ld, rows_per_count, mr, n_rows, q_ld, s_ld, w_ld, ws_ld)
     stream = _stream_of(y, x, x_scales, w, w_scales, bias, base, count)
     rc = lib().sige_rows8_linear(x.data_ptr(), q_ld, x_scales.data_ptr(), s_ld, Cin, _at(count), rows_per_count, mr, n_rows, w.data_ptr(),
                                  w_ld, w_scales.data_ptr(), ws_ld, Cout, _at(bias), _at(base), base_ld, y.data_ptr(), _DT[y.dtype], y_ld,
@@ -924,6 +936,7 @@ def sige_rows8_linear_gated(x, x_scales, w, w_scales, q, scales, Cin, Cout, *, g
         _table("bias", bias, torch.float32, 2 * Cout)
     (x_ld, xs_ld), (w_ld, ws_ld) = _rows8("x", x, x_scales, rows, Cin), _rows8("w", w, w_scales, 2 * Cout, Cin)
     q_ld, s_ld = _rows8("q", q, scales, rows, Cout)
+    _int32("sige_rows8_linear_gated", Cin, Cout, rows_per_count, mr, n_rows, x_ld, xs_ld, w_ld, ws_ld, q_ld, s_ld)
     stream = _stream_of(q, scales, x, x_scales, w, w_scales, bias, count)
     rc = lib().sige_rows8_linear_gated(x.data_ptr(), x_ld, x_scales.data_ptr(), xs_ld, Cin, _at(count), rows_per_count, mr, n_rows,
                                        w.data_ptr(), w_ld, w_scales.data_ptr(), ws_ld, Cout, _at(bias), gate, q.data_ptr(), q_ld,

@@ -247,3 +247,41 @@ def test_calls_without_rows_take_tensors_without_memory(L):
         for res_ld, total_ld, y_ld, q_ld, s_ld in ((0, 0, 320, 0, 0), (0, 0, 0, 384, 4), (320, 320, 328, 0, 0), (328, 320, 0, 384, 4), (320, 0, 336, 384, 4)):
             assert L.sige_token_rms(None, 1, 320, 320, None, res_ld, *rows, None, eps, None, total_ld, None, y_ld, None, q_ld, None, s_ld, None) == 0, (rows, y_ld, err(L))
             assert L.sige_token_rms(FAKE, 1, 320, 320, None, res_ld, *rows, None, eps, None, total_ld, None, y_ld, None, q_ld, None, s_ld, None) == 0
+
+
+def test_binding_refuses_what_an_int_does_not_hold():
+    """Sizes of 2^31 and more would reach the library as their lower 32 bits, and 2^32 + 5 rows be 5 (tensors without memory: nothing is read)."""
+    big = 2 ** 32 + 5
+
+    def tensor(*shape, dtype=torch.float16, strides=None):
+        return torch.empty_strided(shape, strides or (shape[1], 1), dtype=dtype, device="meta")
+    u8 = torch.uint8
+    q, s = tensor(8, 128, dtype=u8), tensor(8, 4, dtype=u8)
+    w, ws = tensor(64, 128, dtype=u8), tensor(64, 4, dtype=u8)
+    x, y = tensor(8, 64), tensor(8, 32)
+    count = torch.empty(1, dtype=torch.int32, device="meta")
+    far = tensor(8, 64, strides=(2 ** 32 + 64, 1))
+    qb, sb, xb, yb = tensor(big, 128, dtype=u8), tensor(big, 4, dtype=u8), tensor(big, 64), tensor(big, 32)
+    wide, qw, sw = tensor(8, 2 ** 32 + 64), tensor(8, 2 ** 32 + 128, dtype=u8), tensor(8, 2 ** 25 + 4, dtype=u8)
+    hw, hws = tensor(2 ** 33 + 64, 128, dtype=u8), tensor(2 ** 33 + 64, 4, dtype=u8)
+    calls = [(api.sige_token_rms, (xb, 64), dict(y=xb, n_rows=big)), (api.sige_token_rms, (xb, 64), dict(y=xb, count=count, rows_per_count=16)),
+             (api.sige_token_rms, (xb, 64), dict(y=xb, count=count, rows_per_count=16, max_rows=big)), (api.sige_token_rms, (x, 64), dict(y=far, n_rows=8)),
+             (api.sige_token_rms, (x, 64), dict(y=x, residual=far, n_rows=8)), (api.sige_token_rms, (x, 64), dict(y=x, residual=x, total=far, n_rows=8)),
+             (api.sige_token_rms, (wide, 2 ** 32 + 64), dict(y=wide, n_rows=8)), (api.sige_token_rms, (x, 64), dict(y=x, count=count, rows_per_count=2 ** 32 + 1)),
+             (api.sige_rows8_store, (xb, qb, sb, 64), dict(n_rows=big)), (api.sige_rows8_store, (far, q, s, 64), dict(n_rows=8)),
+             (api.sige_rows8_store, (wide, qw, sw, 2 ** 32 + 64), dict(n_rows=8)),
+             (api.sige_rows8_load, (qb, sb, xb, 64), dict(n_rows=big)), (api.sige_rows8_load, (q, s, far, 64), dict(n_rows=8)),
+             (api.sige_rows8_load, (tensor(8, 128, dtype=u8, strides=(2 ** 32 + 128, 1)), s, x, 64), dict(n_rows=8)),
+             (api.sige_rows8_load, (q, tensor(8, 4, dtype=u8, strides=(2 ** 32 + 4, 1)), x, 64), dict(n_rows=8)),
+             (api.sige_rows8_linear, (qb, sb, w, ws, yb, 64, 32), dict(n_rows=big)), (api.sige_rows8_linear, (q, s, w, ws, far, 64, 32), dict(n_rows=8)),
+             (api.sige_rows8_linear, (q, s, w, ws, y, 64, 32), dict(n_rows=8, base=tensor(8, 32, strides=(2 ** 32 + 32, 1)))),
+             (api.sige_rows8_linear, (q, s, hw, hws, tensor(8, 2 ** 32 + 32), 64, 2 ** 32 + 32), dict(n_rows=8)),
+             (api.sige_rows8_linear_gated, (qb, sb, w, ws, qb, sb, 64, 32), dict(n_rows=big)),
+             (api.sige_rows8_linear_gated, (q, s, hw, hws, qw, sw, 64, 2 ** 32 + 32), dict(n_rows=8)),
+             (api.sige_rows8_linear_gated, (q, s, tensor(64, 128, dtype=u8, strides=(2 ** 32 + 128, 1)), ws, q, s, 64, 32), dict(n_rows=8))]
+    for fn, a, kw in calls:
+        with pytest.raises(api.SigeError) as e:
+            fn(*a, **kw)
+        assert e.value.code == 2 and "2^31" in str(e.value), (fn.__name__, e.value)
+    with pytest.raises(api.SigeError, match="another device"):      # eight rows of a tensor of more than a call may have: nothing to refuse but the device
+        api.sige_token_rms(xb, 64, y=xb, n_rows=8)
