@@ -551,7 +551,8 @@ int sige_rows8_load(const void* q, int32_t q_ld, const void* scales, int32_t s_l
 /* The root-mean-square norm, beside sige_token_norm for models that have it, with the residual's addition before it:
  *   h[r][c] = x[r][c] + residual[r][c], rounded to dt (residual NULL: h = x),
  *   y[r][c] = h[r][c] / sqrt(mean_c(h[r][c]^2) + eps) * gamma[c],
- * the mean in fp32 (a sum of squares beyond its range gives a row of zeros), gamma fp32 [C] or NULL (1).  Outputs, each of its own: total = h [rows][C] (beside a
+ * the mean in fp32 (rows whose squares leave its range are scaled by a power of two first; an infinity makes the rest of its row 0 and itself NaN),
+ * gamma fp32 [C] or NULL (1).  Outputs, each of its own: total = h [rows][C] (beside a
  * residual; may be NULL), y [rows][C] of dt, and q / scales: y in 8 bits, from the values before they are rounded to dt; y or
  * q may be NULL, not both.  total or y may be x or residual (same row stride).  C * size and the strides must be multiples of 16 bytes; at
  * most 32 KiB per token; in single precision fewer than 2^24 rows of more than 1024 channels.                                                                */

@@ -134,17 +134,39 @@ __global__ __launch_bounds__(256) void rows8_rms_kernel(Rows8Args a)
             for (int i = 0; i < N; ++i) sum = fmaf(f[u][h][i], f[u][h][i], sum);
         }
     }
+    const auto over_row = [&] {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
-    if constexpr (W > 1) {
-        if (lane == 0) part[wave] = sum;
-        __syncthreads();
-        sum = part[0];
+        for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
+        if constexpr (W > 1) {
+            if (lane == 0) part[wave] = sum;
+            __syncthreads();
+            sum = part[0];
 #pragma unroll
-        for (int i = 1; i < W; ++i) sum += part[i];
-        if (!on) return;
+            for (int i = 1; i < W; ++i) sum += part[i];
+        }
+    };
+    over_row();
+    if (W > 1 && !on) return;                                // (four waves: the workgroup's one row)
+    // Squares below fp32's normal numbers lose bits, or all of them, where eps does not hide them; above them the sum is infinite.  Such a row
+    // is taken times a power of two, and eps with it: the quotient is the same, and what falls below the range now is 2^-100 of the largest.
+    float eps = a.eps;
+    const float by = sum < 0x1p-110f && eps < 0x1p-80f ? 0x1p100f : sum == __uint_as_float(0x7f800000u) ? 0x1p-80f : 1.0f;
+    if (by != 1.0f) {
+        eps = eps * by * by;
+        sum = 0.0f;
+#pragma unroll
+        for (int u = 0; u < NC; ++u)
+#pragma unroll
+            for (int h = 0; h < V; ++h)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    f[u][h][i] *= by;
+                    sum = fmaf(f[u][h][i], f[u][h][i], sum);
+                }
+        if constexpr (W > 1) __syncthreads();                // (every wave has read the parts)
+        over_row();
     }
-    const float r = 1.0f / sqrtf(sum / (float)a.C + a.eps);
+    const float r = 1.0f / sqrtf(sum / (float)a.C + eps);
 #pragma unroll
     for (int u = 0; u < NC; ++u) {
         const int chunk = w + W * u;

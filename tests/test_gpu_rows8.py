@@ -741,3 +741,49 @@ def test_an_edit_without_blocks(counted):
     api.sige_rows8_linear(q, s, w, ws, z, C, cout, base=torch.empty(0, cout + 8, dtype=torch.bfloat16, device="cuda"), **kw)
     api.sige_rows8_linear_gated(q, s, w, ws, o, os_, C, cout, **kw)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,C", [(8, 40), (8, 320), (9, 640), (8, 1288), (8, 4096), (8, 8192), (2060, 1032), (2060, 2048)])
+def test_rms_rows_of_any_size(n, C, dtype):
+    """Rows whose squares lie below or above what single precision holds, between others."""
+    x = rows(C + n, n, C, dtype).clone()
+    size = [0, -80, -120, -138 if dtype == "f32" else -130, 90, 118, -56, 0]
+    for i, e in enumerate(size):
+        x[i] = torch.ldexp(x[i].float(), torch.tensor(e, device="cuda")).to(DT[dtype])
+    assert torch.isfinite(x).all()
+    gamma = (torch.rand(C, generator=torch.Generator().manual_seed(C)) + 0.5).cuda()
+    for gm, eps in ((None, 0.0), (gamma, 2.0 ** -160), (gamma, 2.0 ** -120), (None, 2.0 ** -81), (None, 2.0 ** -79), (gamma, 1e-6)):
+        want = rms_expected(x, None, gm, float(np.float32(eps)), dtype)[1]
+        rel = (C / 2 + 16) * 2.0 ** -24         # as in test_rms: powers of two add nothing
+        y, (q, s) = torch.empty_like(x), room(n, C)
+        api.sige_token_rms(x, C, gm, eps, y=y, q=q, scales=s, n_rows=n)
+        torch.cuda.synchronize()
+        # (where eps leaves values among single precision's smallest, both products round to its steps there, the first times gamma <= 1.5)
+        tiny = 2.5 * 2.0 ** -150
+        bound = (rel + torch.finfo(DT[dtype]).eps / 2 * (1 + rel)) * np.abs(want) + tiny + TINY[dtype]
+        off = np.abs(f64(y) - want)
+        assert (off <= bound).all(), (eps, np.argwhere(~(off <= bound))[:4].tolist())
+        close_codes(q, s, want, rel * np.abs(want) + tiny, C, "norm")
+        check_room(q, s, n, C)
+    # in place behind a residual; the sum is the tensor that is normed
+    z, res = x.clone(), torch.zeros_like(x)
+    res[:, :8] = x[:, :8]
+    h, want = rms_expected(x, res, None, 0.0, dtype)
+    api.sige_token_rms(z, C, None, 0.0, residual=res, total=res, y=z, n_rows=n)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(f64(res), h)
+    assert (np.abs(f64(z) - want) <= (rel + torch.finfo(DT[dtype]).eps / 2 * (1 + rel)) * np.abs(want) + TINY[dtype]).all()
+
+
+def test_rms_rows_of_any_size_that_are_not_finite():
+    """A row of zeros without eps is 0 / 0; NaN and infinity beside numbers that overflow."""
+    for C in (320, 640, 4096):
+        x = torch.zeros(5, C, dtype=torch.float32, device="cuda")
+        x[1], x[2], x[3], x[4] = 2.0 ** 120, 2.0 ** -100, 2.0 ** 100, 1.0
+        x[1, 3], x[3, 5], x[2, 0] = float("inf"), float("nan"), 2.0 ** -101
+        y = torch.empty_like(x)
+        api.sige_token_rms(x, C, None, 0.0, y=y, n_rows=5)
+        assert torch.isnan(y[0]).all() and torch.isnan(y[3]).all() and torch.isnan(y[1, 3])
+        assert (torch.cat([y[1, :3], y[1, 4:]]) == 0).all()
+        assert (y[4] == 1).all() and abs(y[2, 1].item() / y[2, 0].item() - 2) < 2.0 ** -22 and abs(y[2, 1].item() - 1) < 2.0 / C
