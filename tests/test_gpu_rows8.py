@@ -787,3 +787,35 @@ def test_rms_rows_of_any_size_that_are_not_finite():
         assert torch.isnan(y[0]).all() and torch.isnan(y[3]).all() and torch.isnan(y[1, 3])
         assert (torch.cat([y[1, :3], y[1, 4:]]) == 0).all()
         assert (y[4] == 1).all() and abs(y[2, 1].item() / y[2, 0].item() - 2) < 2.0 ** -22 and abs(y[2, 1].item() - 1) < 2.0 / C
+
+
+@pytest.mark.parametrize("gate", [api.GATE_GELU, api.GATE_SILU])
+@pytest.mark.parametrize("form", range(4))
+def test_gates_far_below_zero(form, gate):
+    """The activation relative to its own value, to the ends where that is nearly nothing: gates and values that come from the biases alone, every
+    block of 128 channels with gates of one size, so that its scale is that of their values."""
+    n, cin, cout = 3, 16, 128 * 192
+    rng = np.random.default_rng(form + 8 * gate)
+    lo, hi = (-12.9, 9.0) if gate == api.GATE_GELU else (-80.0, 40.0)
+    g = (np.repeat(rng.uniform(lo, hi, cout // 128), 128) + rng.uniform(-0.05, 0.05, cout)).astype(np.float32)
+    u = (rng.uniform(0.5, 2.0, cout) * rng.choice([-1.0, 1.0], cout)).astype(np.float32)
+    x, xs, _ = matrix(3, n, cin)
+    w, ws = torch.zeros(2 * cout, 128, dtype=torch.uint8, device="cuda"), torch.zeros(2 * cout, 4, dtype=torch.uint8, device="cuda")
+    ws[:, 0] = 127
+    q, s = room(n, cout)
+    with api.knobs(ROWS8_FORM=form):
+        api.sige_rows8_linear_gated(x, xs, w, ws, q, s, cin, cout, gate=gate, bias=torch.from_numpy(np.concatenate([u, g])).cuda(), n_rows=n)
+    torch.cuda.synchronize()
+    check_room(q, s, n, cout)
+    d, z = g.astype(float), np.abs(g.astype(float))
+    want = u * ref.gate(d, gate)
+    # gelu: 1.7e-6 of the fit and its arithmetic (below 32 steps of 2^-24), and the exponent z * (z * c), |c| = 0.72, rounded twice: 2^-23 of itself, in powers of e
+    # z^2 / 2 * 2^-23; silu: the exponent is rounded once, as its factor is: 2^-23 z; exp2 and reciprocal of the instruction set one step of 2^-23 each, four roundings
+    rel = 2.0 ** -24 * (z * z + 40 if gate == api.GATE_GELU else 2 * z + 10)
+    low, high = np.abs(want) * (1 - rel), np.abs(want) * (1 + rel)
+    got, bytes_ = q.cpu().numpy()[:n, :cout], s.cpu().numpy()[:n, :cout // 128].astype(int)
+    e = np.vectorize(ref.scale_exponent)
+    assert (bytes_ - 127 >= e(low.reshape(-1, 128).max(1))).all() and (bytes_ - 127 <= e(high.reshape(-1, 128).max(1))).all()
+    scale = 2.0 ** (np.repeat(bytes_, 128, 1) - 127.0)
+    assert (got & 0x7f >= ref.nearest_code(low / scale)).all() and (got & 0x7f <= ref.nearest_code(high / scale)).all()
+    assert ((got > 127) == (want < 0))[got & 0x7f != 0].all() and (got & 0x7f != 0).mean() > 0.95
