@@ -62,7 +62,7 @@ static int linear8_gated_form(const Linear8Args& a, int rows)
     static const Linear8Cost cost[GATED8_FORMS] = {{16, 128, 1, 1, 0.84f, 2.91f, 0.374f}, {64, 128, 1, 1, 1.68f, 3.61f, 0.457f}, {128, 128, 1, 1, 1.22f, 6.22f, 0.653f},
                                                   {256, 128, 1, 1, 0.0f, 11.55f, 1.034f}};
     const int set = knob(SIGE_KNOB_ROWS8_FORM);
-    const bool offsets = a.x_ld < (1 << 22) && 2L * a.Cout * a.w_ld < (1L << 31);
+    const bool offsets = a.x_ld < (1 << 22) && a.w_ld < (1 << 22);
     if (set >= 0 && (set < GATED8_TILE_64 || offsets)) return set;
     int best = GATED8_FEW;
     float least = INFINITY;

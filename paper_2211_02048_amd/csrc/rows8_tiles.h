@@ -35,6 +35,10 @@ struct Tile8 {
     static constexpr int BM = 64 * RT, BN = 64 * CT, OUT = GATED ? BN / 2 : BN;          // rows, weight rows and output channels of a tile
     static constexpr int XB = BM * 128, STAGE = XB + BN * 128, SC = NS * STAGE;          // bytes in LDS; where the scale words are
     static constexpr int XI = BM / 32, WI = BN / 32, REQ = XI + WI;                      // direct loads of a wave per block
+    // (gated: requests i and i ^ 2 are for values and gates of the same channels; each kind's rows are counted from its own first one, so that
+    // the offsets do not have to hold the way from one to the other)
+    static constexpr int WO = GATED ? WI / 2 : WI;
+    static constexpr int wo_of(int i) { return GATED ? (i & 1) | i >> 2 << 1 : i; }
     static constexpr int N = RT * CT;                                                    // matrix instructions of a wave per half block
     // a block's 2 N matrix instructions are its time: operands of its second half are read beside the first of them, READS at a time; behind
     // number FREE its place is requested into again, PER requests at a time, and at number COME the next block has to have come
@@ -60,7 +64,7 @@ struct Tile8 {
     // Where a tile's operands come from.
     struct Source {
         int row0, col0, rows, cols;                          // of the tile (rows and output channels that are there)
-        int xo[XI], wo[WI];                                  // a lane's places in the tile's rows, for each of its requests per block
+        int xo[XI], wo[WO];                                  // a lane's places in the tile's rows, for each of its requests per block
         const unsigned char* sp[2];                          // its scale words
         float bias;                                          // thread t's: that of the t-th row of weights of the tile, in the order of the channels
     };
@@ -77,9 +81,11 @@ struct Tile8 {
         typedef __attribute__((address_space(3))) void* lds_ptr;
         typedef const __attribute__((address_space(1))) void* global_ptr;
         const auto request = [&](int b, int place, int i) {
+            // (gated: the tokens' rows first; the weights' first 4096 x 2560 -> 2 x 10240 with the load behind it takes 224 us instead of 215)
+            if constexpr (GATED) i = i < XI ? i + WI : i - XI;
             if (i < WI) {
-                const auto wr = __builtin_amdgcn_make_buffer_rsrc((void*)(a.w + (long)t.col0 * a.w_ld), 0, ((GATED ? a.Cout : 0) + t.cols) * a.w_ld, 0x00027000);
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_ptr)(lds + place + XB + (wave + 4 * i) * 1024), 16, t.wo[i], 128 * b, 0, 0);
+                const auto wr = __builtin_amdgcn_make_buffer_rsrc((void*)(a.w + ((GATED && (i >> 1 & 1) ? (long)a.Cout : 0L) + t.col0) * a.w_ld), 0, t.cols * a.w_ld, 0x00027000);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_ptr)(lds + place + XB + (wave + 4 * i) * 1024), 16, t.wo[wo_of(i)], 128 * b, 0, 0);
             } else {
                 const auto xr = __builtin_amdgcn_make_buffer_rsrc((void*)(a.x + (long)t.row0 * a.x_ld), 0, t.rows * a.x_ld, 0x00027000);
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(xr, (lds_ptr)(lds + place + (wave + 4 * (i - WI)) * 1024), 16, t.xo[i - WI], 128 * b, 0, 0);
@@ -98,9 +104,9 @@ struct Tile8 {
             t.cols = a.Cout - col0 < OUT ? a.Cout - col0 : OUT;
             // what a wave requests: 8 rows of 128 bytes at a time, lane l piece (l % 8) ^ (row / 2 % 8) of row l / 8 (rows that are not there: the last one)
             const int piece = ((lane & 7) ^ ((4 * (wave & 1) + (lane >> 4)) & 7)) * 16;
-            const auto weight_row = [&](int p) {
+            const auto channel = [&](int p) {
                 const int c = tile_channel<GATED>(p);
-                return (GATED && (p >> 6 & 1) ? a.Cout : 0) + (c < t.cols ? c : t.cols - 1);
+                return c < t.cols ? c : t.cols - 1;
             };
 #pragma unroll
             for (int i = 0; i < XI; ++i) {
@@ -108,13 +114,14 @@ struct Tile8 {
                 t.xo[i] = (p < t.rows ? p : t.rows - 1) * a.x_ld + piece;
             }
 #pragma unroll
-            for (int i = 0; i < WI; ++i) t.wo[i] = weight_row(8 * (wave + 4 * i) + (lane >> 3)) * a.w_ld + piece;
+            for (int i = 0; i < WI; ++i)
+                if (!GATED || !(i >> 1 & 1)) t.wo[wo_of(i)] = channel(8 * (wave + 4 * i) + (lane >> 3)) * a.w_ld + piece;
 #pragma unroll
             for (int i = 0; i < REQ; ++i) request(0, 0, i);
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int p = ((2 * wave + e) % GROUPS) * 64 + lane;
-                t.sp[e] = p < BM ? a.xs + (long)(row0 + (p < t.rows ? p : t.rows - 1)) * a.xs_ld : a.ws + (long)(col0 + weight_row(p - BM)) * a.ws_ld;
+                t.sp[e] = p < BM ? a.xs + (long)(row0 + (p < t.rows ? p : t.rows - 1)) * a.xs_ld : a.ws + (long)((GATED && ((p - BM) >> 6 & 1) ? a.Cout : 0) + col0 + channel(p - BM)) * a.ws_ld;
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) request_word(e >> 1, e & 1);

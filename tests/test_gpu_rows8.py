@@ -819,3 +819,36 @@ def test_gates_far_below_zero(form, gate):
     scale = 2.0 ** (np.repeat(bytes_, 128, 1) - 127.0)
     assert (got & 0x7f >= ref.nearest_code(low / scale)).all() and (got & 0x7f <= ref.nearest_code(high / scale)).all()
     assert ((got > 127) == (want < 0))[got & 0x7f != 0].all() and (got & 0x7f != 0).mean() > 0.95
+
+
+def test_gated_product_with_weights_of_more_than_2_gib():
+    """Gates that begin more than 2^31 bytes behind their values: every form, and more rows than the form for few of them takes."""
+    cin, cout, wide = 640, 264, 2 ** 22 - 128
+    x, xs, _ = matrix(41, 200, cin)
+    w, ws, _ = matrix(42, 2 * cout, cin, cin ** -0.5)
+    bias = torch.randn(2 * cout, generator=torch.Generator().manual_seed(43)).cuda()
+    far = torch.empty(2 * cout, wide, dtype=torch.uint8, device="cuda")[:, :w.shape[1]]
+    far.copy_(w)
+    assert cout * wide + (cout - 1) * wide >= 2 ** 31
+    for form in [-1] + list(range(4)):
+        got = []
+        for weights in (w, far):
+            q, s = room(200, cout)
+            with api.knobs(ROWS8_FORM=form):
+                api.sige_rows8_linear_gated(x, xs, weights, ws, q, s, cin, cout, bias=bias, n_rows=200)
+            check_room(q, s, 200, cout)
+            got.append((q, s))
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1]), form
+    # 2^20 rows: as the same rows 2^19 at a time by weights without gaps
+    n, cin = 2 ** 20, 128
+    g = torch.Generator(device="cuda").manual_seed(44)
+    t = torch.randn(n, cin, generator=g, device="cuda", dtype=torch.float32).bfloat16()
+    x, xs = api.rows8(n, cin)
+    api.sige_rows8_store(t, x, xs, cin, n_rows=n)
+    near = far[:, :cin].contiguous()
+    q, s = api.rows8(n, cout)
+    api.sige_rows8_linear_gated(x, xs, far, ws, q, s, cin, cout, bias=bias, n_rows=n)
+    for i in (0, n // 2):
+        q2, s2 = api.rows8(n // 2, cout)
+        api.sige_rows8_linear_gated(x[i:i + n // 2], xs[i:i + n // 2], near, ws, q2, s2, cin, cout, bias=bias, n_rows=n // 2)
+        assert torch.equal(q[i:i + n // 2], q2) and torch.equal(s[i:i + n // 2], s2)
