@@ -70,7 +70,8 @@ struct Tile8 {
     };
 
     // Tiles from next(row0, col0), one after the other: a tile's first blocks are requested before the results of the one before are worked on
-    // (4096 x 2560 -> 2 x 10240 gated by tiles of 128 rows 267 -> 254 us; tiles of 256 x 256 have no registers for it: ONCE, one tile).
+    // (4096 x 2560 -> 2 x 10240 gated by tiles of 128 rows 267 -> 254 us; tiles of 256 x 256 have no registers for it, and plain calls
+    // of more tiles than compute units take other forms: ONCE, one tile).
     template <bool ONCE, typename Next>
     static __device__ __forceinline__ void run(const Linear8Args& a, unsigned char* lds, int all_rows, Next&& next_tile)
     {
@@ -243,8 +244,9 @@ struct Tile8 {
         else if (rows == BM && cols == OUT) plain<true>(a, (const float*)(lds + EPI), acc, r0, c0, rows, cols, m, h, wm, wn);
         else plain<false>(a, (const float*)(lds + EPI), acc, r0, c0, rows, cols, m, h, wm, wn);
         if (!more) return;
-        // (the stores above are newer than the next tile's requests: all of a whole tile's may be on their way)
-        constexpr int stores = GATED ? 2 * RT : 2 * RT * CT * (8 / Vec16<T>::N), most = (NS - 1) * REQ + stores < 63 ? (NS - 1) * REQ + stores : 63;
+        // (the stores above are newer than the next tile's requests: all of a whole tile's, two per 32 rows, may be on their way)
+        static_assert(ONCE || GATED, "the stores that the wait counts on");
+        constexpr int most = (NS - 1) * REQ + 2 * RT < 63 ? (NS - 1) * REQ + 2 * RT : 63;
         if (a.blocks >= NS && rows == BM && cols == OUT) __builtin_amdgcn_s_waitcnt(wait(most, 0));
         else __builtin_amdgcn_s_waitcnt(wait(0, 0));
         }
@@ -433,7 +435,7 @@ __global__ __launch_bounds__(256, WGS) void rows8_tile_kernel(Linear8Args a)
     const int rows = rows8_effective(a.rows), id = blockIdx.x;
     const int nx = (a.Cout + Tile::OUT - 1) / Tile::OUT, my = (rows + Tile::BM - 1) / Tile::BM, n = nx * my;
     const int over = n % COMPUTE_UNITS, whole = HALVES && n > COMPUTE_UNITS && over <= COMPUTE_UNITS / 2 ? n - over : n;
-    constexpr bool ONCE = HALVES || WGS > 1;                  // (else the grid is the chip at most, and a workgroup goes from tile to tile)
+    constexpr bool ONCE = HALVES || !GATED;                   // (else the grid is the chip at most, and a workgroup goes from tile to tile)
     if (id < whole) {
         int turn = 0;
         Tile::template run<ONCE>(a, tile_lds, rows, [&](int& row0, int& col0) {
@@ -469,7 +471,7 @@ inline int launch_tiles(const char* who, const Linear8Args& a, int rows, hipStre
     SIGE_REQUIRE(n < (1L << 23), SIGE_ERR_UNSUPPORTED, "%s: too many rows and channels", who);
     const auto kern = rows8_tile_kernel<T, GATED, RT, CT, NS, WGS, HALVES>;
     if (int rc = allow_lds(who, (const void*)kern, Tile::LDS)) return rc;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(HALVES ? n + COMPUTE_UNITS / 2 : WGS > 1 || n < COMPUTE_UNITS ? n : COMPUTE_UNITS)), dim3(256), Tile::LDS, st, a);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(HALVES ? n + COMPUTE_UNITS / 2 : !GATED || n < COMPUTE_UNITS ? n : COMPUTE_UNITS)), dim3(256), Tile::LDS, st, a);
     SIGE_LAUNCH_CHECK(who);
     return SIGE_OK;
 }

@@ -852,3 +852,22 @@ def test_gated_product_with_weights_of_more_than_2_gib():
         q2, s2 = api.rows8(n // 2, cout)
         api.sige_rows8_linear_gated(x[i:i + n // 2], xs[i:i + n // 2], near, ws, q2, s2, cin, cout, bias=bias, n_rows=n // 2)
         assert torch.equal(q[i:i + n // 2], q2) and torch.equal(s[i:i + n // 2], s2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_more_tiles_of_128_than_compute_units(dtype):
+    """The form with four blocks on their way, on more tiles than compute units with more blocks than that: the bits of the form with two."""
+    for n, cin, cout in ((2100, 520, 2200), (2176, 1160, 2304)):
+        x, w = drawn(n, n, cin), drawn(cout, cout, cin, cin ** -0.5)
+        bias, base = torch.randn(cout, device="cuda"), torch.randn(n, cout, device="cuda").to(DT[dtype])
+        y = []
+        for form in (5, 6):
+            y.append(torch.full((n + 1, cout + 8), 7.0, dtype=DT[dtype], device="cuda"))
+            with api.knobs(ROWS8_FORM=form):
+                api.sige_rows8_linear(*x, *w, y[-1][:n, :cout], cin, cout, bias=bias, base=base, n_rows=n)
+        assert torch.equal(y[0], y[1]) and (y[1][n] == 7.0).all() and (y[1][:, cout:] == 7.0).all()
+        xv, wv = on_gpu(*x, cin), on_gpu(*w, cin)
+        want = xv @ wv.t() + bias.double() + base.double()
+        bound = (cin + 4) * 2.0 ** -24 * (xv.abs() @ wv.abs().t() + bias.double().abs() + base.double().abs()) + (0 if dtype == "f32" else cut_of(xv, wv))
+        bound = bound + torch.finfo(DT[dtype]).eps / 2 * (want.abs() + bound) + TINY[dtype]
+        assert ((y[1][:n, :cout].double() - want).abs() <= bound).all()
