@@ -537,7 +537,9 @@ int sige_token_lora(const void* x, sige_dtype dt, int32_t Cin, int32_t x_ld, con
  * codes 16-byte, scales 4-byte aligned.  A scale byte of 255 is NaN.  Half of a half type's size; the powers of two lose nothing
  * against other factors (the codes have exponents of their own), and the matrix instruction applies them by itself.
  * Rows as in sige_token_norm: n_rows >= 0 from the host, or -1 = min(*count * rows_per_count, max_rows); rows behind them are
- * neither read nor written.  Outputs may not overlap inputs but where a call says so.
+ * neither read nor written.  With a count on the device the products' kernel is chosen for max_rows (15 % of them take up to 2.4 times
+ * what the same rows take from the host), so max_rows is worth being no more than there can be.
+ * Outputs may not overlap inputs or each other but where a call says so.
  *
  * sige_rows8_store: x [rows][C] of dt to 8 bits.  A block's scale is the smallest power of two, at least 2^-126, with max|x| <= 448 * scale over its
  * finite values; codes are the nearest, ties to the even one; an infinity or NaN becomes a NaN and leaves the others alone.
@@ -565,9 +567,12 @@ int sige_token_rms(const void* x, sige_dtype dt, int32_t C, int32_t x_ld, const 
  * x (codes and scales) [rows][Cin], w [Cout][Cin], bias fp32 [Cout] or NULL, base [rows][Cout] of dt or NULL (a residual, or what another layer
  * left), y [rows][Cout] of dt, rounded once; y == base is allowed (same row stride).  Sums in fp32.  Half types: the matrix instruction for 8 bits, which cuts off
  * of a product what lies 13 places and more below the largest one that it adds in the same step (within a block of 128 channels; 1.5e-5 of
- * the result in the mean over normal numbers, the codes' own rounding is 1000 times as much).  Single precision cuts off nothing:
- * the codes are multiplied as bf16 numbers, which they are (scales of 2^-110 to 2^110; below 2^-126 values become 0).
- * Cout must be a multiple of 16 bytes' worth of dt, Cin may be anything.                       */
+ * the result in the mean over normal numbers, the codes' own rounding is 1000 times as much; never more than 2^-6 of a block's largest
+ * product).  Single precision cuts off nothing:
+ * the codes are multiplied as bf16 numbers, which they are (scales of 2^-110 to 2^110; below 2^-126 values become 0): results in fp32
+ * are the choice of a program that wants the sums whole, at half the rate or less.
+ * Cout must be a multiple of 16 bytes' worth of dt, Cin may be anything.  A launch holds fewer than
+ * 2^30 rows and 2^37 results for sure; calls that it does not hold are refused.                 */
 int sige_rows8_linear(const void* x, int32_t x_ld, const void* x_scales, int32_t xs_ld, int32_t Cin, const int32_t* count,
                       int32_t rows_per_count, int32_t max_rows, int32_t n_rows, const void* w, int32_t w_ld, const void* w_scales,
                       int32_t ws_ld, int32_t Cout, const float* bias, const void* base, int32_t base_ld, void* y, sige_dtype dt,
@@ -576,8 +581,10 @@ int sige_rows8_linear(const void* x, int32_t x_ld, const void* x_scales, int32_t
 /* The first feed-forward layer: the same product with 2 * Cout output channels, the values in rows 0..Cout-1 of w, their gates in the
  * rows Cout..2*Cout-1 (bias likewise, fp32 [2 * Cout]), and the gated activation behind it, to 8 bits:
  *   v[r][o] = u[r][o] * act(g[r][o]),  act = gelu(g) = g/2 * (1 + erf(g / sqrt 2)) or silu(g) = g / (1 + exp(-g)),
- * from the fp32 sums (with the matrix instruction for 8 bits) to codes and scales [rows][Cout] as sige_rows8_store makes them, so that the
- * next layer takes them as they are.  Cout must be a multiple of 8.                           */
+ * from the fp32 sums (with the matrix instruction for 8 bits: two codes in a thousand are not the nearest; fp32 results of
+ * sige_rows8_linear, their gate and sige_rows8_store are the way to those that are) to codes and scales [rows][Cout] as sige_rows8_store makes
+ * them, so that the next layer takes them as they are.  act within 1e-5 of its own value to gelu(-13) and silu(-87), 0 below.
+ * Cout must be a multiple of 8.                                                              */
 typedef enum { SIGE_GATE_GELU = 0, SIGE_GATE_SILU = 1 } sige_gate;
 int sige_rows8_linear_gated(const void* x, int32_t x_ld, const void* x_scales, int32_t xs_ld, int32_t Cin, const int32_t* count,
                             int32_t rows_per_count, int32_t max_rows, int32_t n_rows, const void* w, int32_t w_ld,
